@@ -259,7 +259,8 @@ lar_status_t lar_cache_get_state(lar_cache_t* c, int layer, int32_t* lens, int32
  * the last poll (bits in *bits_out, may be NULL: 1 capacity, 2 line-end off boundary, 4 wait limit,
  * 8 decode on an empty cache, 16 the length the host passed to a decode kernel differs from
  * the device's, e.g. a captured graph replayed out of order, 32 a line end met a score that is not finite -- a NaN
- * or Inf in a key or query; such entries rank lowest, exactly n are still evicted); clears the word. */
+ * or Inf in a key or query; such entries rank lowest, exactly n are still evicted, 64 a page or slot outside the
+ * cache, see lar_paged_kv_t); clears the word. */
 lar_status_t lar_cache_poll_device_status(lar_cache_t* c, uint32_t* bits_out, void* stream);
 
 /* Enable (1) / disable (0) the host-side call-order checks at run time (see LAR_FLAG_NO_HOST_CHECKS). */
@@ -293,6 +294,120 @@ lar_status_t lar_cache_get_plan(const lar_cache_t* c, lar_plan_t* plan_out);
  * (different streams, no dependency) race on it -- order them. */
 lar_status_t lar_attend_dense_noalloc(const void* q, const void* k, const void* v, void* out, int n_units, int group,
                                       int head_dim, int len, float softmax_scale, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Rotary positions with several axes, paged caches of the caller's, attention of chunks of new tokens.
+ *
+ * The calls below serve what surrounds the decode step: rotating q and k by time / row / column positions, filling a
+ * paged cache with a ragged batch of chunks (prompts, candidate tokens, single tokens), and the attention of those chunks
+ * over the cache.  They keep no state: the caller describes its cache in a lar_paged_kv_t (lar_cache_paged_view describes
+ * a layer of the library's own cache the same way).  Device pointers belong to the device that is current at the call;
+ * work is only enqueued on `stream`, nothing is allocated, and every call may be captured into a CUDA graph (launch
+ * shapes depend on the host arguments alone; lengths, positions and page tables are read on the device at replay).
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* Rotary position embedding with 1 to 4 position axes.  Pair i of a row of head_dim elements is turned by the angle
+ * pos[axis(i)] * theta^(-e_i): the first axis_pairs[0] pairs follow axis 0, the next axis_pairs[1] axis 1, and so on (they sum
+ * to head_dim / 2; an axis whose position is 0 leaves its pairs unturned).  restart = 0: e_i = i / (head_dim / 2) runs on over
+ * the axes (one frequency ladder cut into sections); restart != 0: e_i = (i - first pair of the axis) / axis_pairs[axis] (each
+ * axis has the whole ladder).  interleaved = 0 turns the pairs (i, i + head_dim / 2), interleaved != 0 the pairs (2 i, 2 i + 1):
+ *     x' = x cos - y sin,  y' = y cos + x sin     (fp32, every product and sum rounded, result rounded to the storage type)
+ * as lar_decode_step_rope does.  Angles are formed in fp64 from int32 positions (negative ones included). */
+typedef struct lar_rope {
+    uint32_t struct_size;   /* = sizeof(lar_rope_t) */
+    int32_t head_dim;       /* 64 or 128 */
+    int32_t n_axes;         /* 1..4 */
+    int32_t axis_pairs[4];  /* >= 1 each, summing to head_dim / 2 */
+    int32_t interleaved;
+    int32_t restart;
+    double theta;           /* > 0 */
+} lar_rope_t;
+
+/* Rows [token][head][head_dim] in device memory, innermost dimension dense: element (t, h, i) lies at data[t * token_stride
+ * + h * head_stride + i] (strides in elements).  data is 16-byte aligned and strides are multiples of 16 bytes, at least
+ * head_dim (a stride of an extent of one is ignored); the rows of an output do not overlap. */
+typedef struct lar_rows {
+    void* data;
+    int64_t token_stride, head_stride;
+} lar_rows_t;
+
+/* A paged K/V cache.  Slot j of sequence s and KV head h is row (j % page_tokens) of page
+ *     page_table[s * table_seq_stride + h * table_head_stride + j / page_tokens],
+ * and row r of page p and head h starts at element p * page_stride + r * row_stride + h * head_stride of each pool.
+ * One table shared by the heads has table_head_stride = 0; heads with pages of their own have head_stride = 0.
+ * lens[s * lens_stride] entries of sequence s are live.  A page number outside 0 .. n_pages - 1, or a token whose slot the
+ * table does not hold, is never followed: its rows are not written, read as zeros, and status bit 64 is recorded in *status
+ * (if given; lar_cache_poll_device_status reports it for the library's own caches). */
+typedef struct lar_paged_kv {
+    uint32_t struct_size;      /* = sizeof(lar_paged_kv_t) */
+    int32_t dtype;             /* lar_dtype_t */
+    int32_t n_seqs, n_kv_heads;
+    int32_t head_dim;          /* 64 or 128 */
+    int32_t page_tokens;       /* 16, 32, 64 or 128 */
+    int32_t n_pages;           /* pages of each pool */
+    int32_t table_cols;        /* table entries per sequence (and head); table_cols * page_tokens <= 2^30 */
+    int64_t page_stride, row_stride, head_stride; /* elements, multiples of 16 bytes, the same for both pools */
+    void* k_pool;              /* device, 16-byte aligned */
+    void* v_pool;
+    const int32_t* page_table; /* device */
+    int64_t table_seq_stride, table_head_stride;  /* entries */
+    const int32_t* lens;       /* device: live entries of each sequence, the tokens of the current chunks included */
+    int64_t lens_stride;       /* entries */
+    uint32_t* status;          /* device word, or NULL */
+} lar_paged_kv_t;
+
+/* cos and sin of every pair for n_rows positions: cos_sin (device, fp32) [n_rows, head_dim], the head_dim / 2 cosines of a
+ * row, then the sines -- what lar_decode_step_rope takes.  pos: device, int32, axis a of row r at pos[a * pos_axis_stride + r]
+ * (pos_axis_stride >= n_rows where there are several axes). */
+lar_status_t lar_rope_table(const lar_rope_t* rope, const int32_t* pos, int64_t pos_axis_stride, int n_rows, float* cos_sin,
+                            void* stream);
+
+/* Rotates the rows of q and of k (k, k_out NULL and n_kv_heads 0: q alone) by their tokens' positions, or back with inverse
+ * != 0 (the gradient of the rotation is the rotation back).  An output may be its own input (same data and strides); outputs
+ * overlap nothing else. */
+lar_status_t lar_rope_rotate(const lar_rope_t* rope, int dtype, const int32_t* pos, int64_t pos_axis_stride, int64_t n_tokens,
+                             const lar_rows_t* q, const lar_rows_t* q_out, int n_q_heads, const lar_rows_t* k,
+                             const lar_rows_t* k_out, int n_kv_heads, int inverse, void* stream);
+
+/* Appends the keys (rotated by their positions) and values of a packed batch of chunks to a paged cache, in one launch.
+ * Sequence s owns the tokens cu_tokens[s] .. cu_tokens[s + 1] - 1 (device, int32, [n_seqs + 1], ascending; NULL: n_tokens /
+ * n_seqs each); its i-th of T tokens goes to slot lens[s] - T + i, so lens already counts them.  Tokens before
+ * cu_tokens[0] or from cu_tokens[n_seqs] on belong to nobody and are left alone (n_tokens may be a padded batch size).
+ * rope and pos NULL: keys are stored as they are.  q (or NULL with n_q_heads 0) is rotated to q_out in the same launch. */
+lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* rope, const int32_t* pos, int64_t pos_axis_stride,
+                                   const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q, const lar_rows_t* q_out,
+                                   int n_q_heads, int64_t n_tokens, const int32_t* cu_tokens, void* stream);
+
+/* Attention of the newest tokens of every sequence (the packed chunks of lar_paged_append_rope) over its paged cache:
+ *   out[t, h] = softmax(q[t, h] K^T scale) V    over the slots kv_start[s] .. slot of t   (causal != 0)
+ *                                               or            kv_start[s] .. lens[s] - 1  (causal = 0)
+ * kv_start (device, int32, [n_seqs], or NULL: 0) masks left padding.  A row that sees no slot is zero; memory of slots that
+ * no row of a sequence sees (behind lens, before kv_start) may hold anything.  Tokens that belong to no sequence are left alone.  A
+ * non-finite key or value in a slot that some row of the chunk sees may reach every row of the chunk.
+ * Query head hq uses KV head hq / (n_q_heads / n_kv_heads); their ratio is 1..16.  softmax_scale 0 selects 1/sqrt(head_dim).
+ * max_chunk and max_len bound the tokens of a chunk and the entries of a cache (0: not known); they only choose the launch
+ * shape, never the result's correctness.
+ * workspace (device, 16-byte aligned, lar_paged_attn_workspace_bytes of the same arguments, contents irrelevant) lets the
+ * kernel spread the slots of a unit over several CTAs; NULL: it does not.  LAR_ERR_NOMEM: workspace_bytes is too small.
+ * Calls that may overlap on the GPU need workspaces of their own (two graphs that share one are ordered by the caller). */
+lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads, int64_t n_tokens,
+                            const int32_t* cu_tokens, const int32_t* kv_start, int causal, float softmax_scale, int max_chunk,
+                            int max_len, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace lar_paged_attn wants for these arguments (0: none, or the arguments are invalid).  No CUDA call. */
+size_t lar_paged_attn_workspace_bytes(const lar_paged_kv_t* kv, int n_q_heads, int64_t n_tokens, int max_chunk, int max_len);
+
+/* Describes a layer of the library's own cache for lar_paged_attn (heads have pages of their own).  The pointers lie in the
+ * slab and hold as long as it does; after lar_append_kv / lar_append_kv_rope of the prefix its chunk is the prefix.
+ * Read-only use: what is appended past the library goes unnoticed by its bookkeeping. */
+lar_status_t lar_cache_paged_view(lar_cache_t* c, int layer, lar_paged_kv_t* out);
+
+/* The prefill of lar_append_kv with the rotary embedding on the way: k, v (and q -> q_out, or NULL both) are rows of batch *
+ * n_tokens tokens, sequence by sequence, at positions pos; n_tokens = C.  rope and pos NULL: stored as they are.
+ * LAR_ERR_BAD_STATE unless the layer is empty and C > 0. */
+lar_status_t lar_append_kv_rope(lar_cache_t* c, int layer, const lar_rope_t* rope, const int32_t* pos, int64_t pos_axis_stride,
+                                const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q, const lar_rows_t* q_out,
+                                int n_tokens, void* stream);
 
 const char* lar_status_str(lar_status_t s);
 int lar_last_cuda_error(void); /* cudaError_t of the last failed runtime call in this thread, 0 if none */

@@ -9,14 +9,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "liblar.so")
-SOURCES = [os.path.join(CSRC, "lar_api.cu")]
-DEPS = SOURCES + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")] + \
+SOURCES = [os.path.join(CSRC, f) for f in ("lar_api.cu", "paged_api.cu")]
+DEPS = SOURCES + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))] + \
     [os.path.join(ROOT, "include", "lar.h")]
 
 
 def nvcc_cmd(verbose: bool = False):
     cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared",
+           "-Xcompiler", "-fPIC", "-shared", "--threads", "0",
            "-I", os.path.join(ROOT, "include"), "-o", OUT] + SOURCES
     if verbose:
         cmd[1:1] = ["-Xptxas", "-v"]

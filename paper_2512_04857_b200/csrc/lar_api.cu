@@ -16,22 +16,18 @@
 #include "decode_stream.cuh"
 #include "line_end.cuh"
 #include "attend_noalloc.cuh"
+#include "host_util.h"
+#include "paged_host.h"
 
 namespace {
 
 thread_local int g_last_cuda_error = 0;
 
-#define LAR_CUDA(call)                                   \
-    do {                                                 \
-        cudaError_t e__ = (call);                        \
-        if (e__ != cudaSuccess) {                        \
-            g_last_cuda_error = (int)e__;                \
-            (void)cudaGetLastError();                    \
-            if (getenv("LAR_DEBUG"))                     \
-                fprintf(stderr, "lar: line %d: %s -> %s\n", __LINE__, #call, cudaGetErrorString(e__)); \
-            return LAR_ERR_CUDA;                         \
-        }                                                \
-    } while (0)
+}  // namespace
+
+int& lar::last_cuda_error() { return g_last_cuda_error; }
+
+namespace {
 
 constexpr int kHostSlots = 4;  // staging slots of the host-buffer entry point (calls in flight)
 
@@ -799,6 +795,58 @@ lar_status_t lar_append_kv(lar_cache_t* c, int layer, const void* k, const void*
         sh.v += 1;
         sh.n_tok += 1;
     }
+    return LAR_OK;
+}
+
+lar_status_t lar_cache_paged_view(lar_cache_t* c, int layer, lar_paged_kv_t* out) {
+    if (bad_layer(c, layer) || !out) return LAR_ERR_INVALID_ARG;
+    const lar::LayerView lv = view_of(c, layer);
+    memset(out, 0, sizeof(*out));
+    out->struct_size = sizeof(*out);
+    out->dtype = c->cfg.dtype;
+    out->n_seqs = c->cfg.batch;
+    out->n_kv_heads = c->cfg.n_kv_heads;
+    out->head_dim = c->cfg.head_dim;
+    out->page_tokens = c->d.P;
+    out->n_pages = c->d.units * c->d.ppu;
+    out->table_cols = c->d.ppu;
+    out->page_stride = (int64_t)c->d.P * c->cfg.head_dim;
+    out->row_stride = c->cfg.head_dim;
+    out->head_stride = 0;  // every head has pages of its own
+    out->k_pool = lv.k_pool;
+    out->v_pool = lv.v_pool;
+    out->page_table = lv.page_table;
+    out->table_head_stride = c->d.ppu;
+    out->table_seq_stride = (int64_t)c->d.ppu * c->cfg.n_kv_heads;
+    out->lens = reinterpret_cast<const int32_t*>(lv.state);  // UnitState::len of the sequence's first head (all heads alike)
+    out->lens_stride = (int64_t)(sizeof(lar::UnitState) / sizeof(int32_t)) * c->cfg.n_kv_heads;
+    out->status = lv.status;
+    return LAR_OK;
+}
+
+lar_status_t lar_append_kv_rope(lar_cache_t* c, int layer, const lar_rope_t* rope, const int32_t* pos, int64_t pos_axis_stride,
+                                const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q, const lar_rows_t* q_out,
+                                int n_tokens, void* stream) {
+    if (bad_layer(c, layer) || n_tokens < 1) return LAR_ERR_INVALID_ARG;
+    LayerShadow& sh = c->sh[layer];
+    // the prefill only: a visual token's key is rotated by lar_decode_step_rope
+    if (c->cfg.cond_len < 1 || sh.prefilled) return LAR_ERR_BAD_STATE;
+    if (n_tokens != c->cfg.cond_len) return LAR_ERR_INVALID_ARG;
+    lar_paged_kv_t kv;
+    lar_status_t st = lar_cache_paged_view(c, layer, &kv);
+    if (st != LAR_OK) return st;
+    const lar::LayerView lv = view_of(c, layer);
+    lar::OwnCache oc;
+    oc.index_map = lv.index_map;
+    oc.state = lv.state;
+    oc.cap_pad = c->d.cap_pad;
+    st = lar::paged_append(kv, rope, pos, pos_axis_stride, k, v, q, q_out, q ? c->cfg.n_q_heads : 0,
+                           (int64_t)c->cfg.batch * n_tokens, nullptr, &oc, stream);
+    if (st != LAR_OK) return st;
+    c->launches++;
+    c->last_layer = layer;
+    c->last_writer[layer] = ++c->seq;  // (the kernel does not release its dependents early: a full barrier in the numbering)
+    sh.prefilled = true;
     return LAR_OK;
 }
 

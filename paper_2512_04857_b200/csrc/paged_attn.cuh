@@ -1,0 +1,33 @@
+// Attention of a chunk of new tokens over a paged K/V cache: what the two kernels share.
+//
+//   out[t, h] = sum_j p_j V_j,  p = softmax_j(scale q[t, h] . K_j),  j over the slots start[s] .. last(t)
+//
+// last(t) is the token's own slot (causal) or lens[s] - 1; a row that sees no slot is zero.  The G query heads of a KV head
+// share its rows: the rows of a tile are (token, head of the group) pairs, TQ = BM / G tokens by G heads, so that K and V are read
+// once per tile and not once per head.  A unit is one (sequence, KV head, row tile).
+#pragma once
+#include "paged.cuh"
+#include "rope_rows.cuh"  // RowsView, PackRow
+
+namespace lar {
+
+struct PagedAttnArgs {
+    PagedView kv;
+    RowsView q, out;
+    const int* start;  // [n_seqs] first slot that is seen, or null
+    int group, causal;
+    int tq;            // tokens of a row tile
+    float scale_log2;  // softmax scale * log2(e)
+    float* part_o;     // partial results of units whose slots are spread over several CTAs
+    float* part_ml;
+    int n_splits;
+};
+
+// Row tiles of a sequence / slots [lo, hi) that any row of a tile of it may see.
+__device__ __forceinline__ int tiles_of(const PagedAttnArgs& a, int s) {
+    int t0, t1;
+    chunk_of(a.kv, s, t0, t1);
+    return (t1 - t0 + a.tq - 1) / a.tq;
+}
+
+}  // namespace lar

@@ -1,0 +1,544 @@
+"""Rotary positions with several axes, the append to a paged cache and the chunk attention over it, against plain 64-bit
+forms on the sizes and masks where they can go wrong; refusals run without a GPU."""
+import ctypes as C
+import random
+
+import pytest
+import torch
+
+import _paged_reference as R
+from paper_2512_04857_b200 import lar
+
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+# ------------------------------------------------------------------------------------------------- refusals (no GPU)
+def _kv(**kw):
+    base = dict(struct_size=C.sizeof(lar.lar_paged_kv_t), dtype=lar.LAR_BF16, n_seqs=2, n_kv_heads=2, head_dim=64,
+                page_tokens=32, n_pages=8, table_cols=4, page_stride=2 * 32 * 64, row_stride=2 * 64, head_stride=64,
+                k_pool=4096, v_pool=8192, page_table=256, table_seq_stride=4, table_head_stride=0, lens=512, lens_stride=1,
+                status=None)
+    base.update(kw)
+    return lar.lar_paged_kv_t(**base)
+
+
+def _r(data=4096, token_stride=256, head_stride=64):
+    return lar.lar_rows_t(data, token_stride, head_stride)
+
+
+def _attn(kv, q=None, out=None, hq=4, n=6, cu=None, start=None, causal=1, scale=0.0, mc=0, ml=0, ws=None, nb=0):
+    return lar.lib().lar_paged_attn(kv, q or _r(), out or _r(1 << 20), hq, n, cu, start, causal, scale, mc, ml, ws, nb, None)
+
+
+INVALID = lar.LAR_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bad", [
+    dict(struct_size=8), dict(dtype=2), dict(n_seqs=0), dict(n_kv_heads=0), dict(head_dim=96), dict(page_tokens=48),
+    dict(page_tokens=8), dict(page_tokens=256), dict(n_pages=0), dict(table_cols=0), dict(table_cols=1 << 26),
+    dict(page_stride=2 * 32 * 64 + 4), dict(row_stride=32), dict(row_stride=-128), dict(head_stride=0), dict(head_stride=4),
+    dict(k_pool=4098), dict(v_pool=None), dict(k_pool=None), dict(page_table=None), dict(page_table=258), dict(lens=None),
+    dict(lens=514), dict(lens_stride=-1), dict(table_seq_stride=-1), dict(status=6),
+])
+def test_paged_cache_refusals(bad):
+    assert _attn(_kv(**bad)) == INVALID
+    rows = _r(4096, 128, 64)
+    assert lar.lib().lar_paged_append_rope(_kv(**bad), None, None, 0, rows, rows, None, None, 0, 6, None, None) == INVALID
+    assert lar.lib().lar_paged_attn_workspace_bytes(_kv(**bad), 4, 6, 3, 128) == 0
+
+
+def test_attention_refusals():
+    kv = _kv()
+    assert _attn(kv, hq=3) == INVALID                       # not a multiple of the KV heads
+    assert _attn(kv, hq=34) == INVALID                      # 17 heads per KV head
+    assert _attn(kv, n=5) == INVALID                        # equal chunks: not divisible
+    assert _attn(kv, n=-1) == INVALID
+    assert _attn(kv, scale=-1.0) == INVALID and _attn(kv, scale=float("nan")) == INVALID
+    assert _attn(kv, scale=float("inf")) == INVALID
+    assert _attn(kv, mc=-1) == INVALID and _attn(kv, ml=-1) == INVALID
+    assert _attn(kv, cu=258) == INVALID and _attn(kv, start=258) == INVALID
+    assert _attn(kv, q=_r(4104)) == INVALID and _attn(kv, q=_r(None)) == INVALID
+    assert _attn(kv, q=_r(4096, 260)) == INVALID and _attn(kv, q=_r(4096, 256, 32)) == INVALID
+    assert _attn(kv, out=_r(1 << 20, 64, 64)) == INVALID    # output rows on top of one another
+    assert _attn(kv, n=0) == lar.LAR_OK                     # nothing to do
+    assert lar.lib().lar_paged_attn(None, _r(), _r(), 4, 6, None, None, 1, 0.0, 0, 0, None, 0, None) == INVALID
+    big = _kv(n_seqs=1, n_pages=4096, table_cols=4096)      # one token over 131072 slots: the workspace is wanted
+    need = lar.lib().lar_paged_attn_workspace_bytes(big, 4, 1, 1, 0)
+    assert need > 0
+    assert _attn(big, n=1, ws=4096, nb=need - 1) == lar.LAR_ERR_NOMEM
+    assert _attn(big, n=1, ws=4100, nb=need) == INVALID
+
+
+def test_append_refusals():
+    L, kv, rows = lar.lib(), _kv(), _r(4096, 128, 64)
+    rope = lar.make_rope(64, (8, 12, 12))
+
+    def call(kv=kv, rope=rope, pos=256, ps=6, k=rows, v=rows, q=None, qo=None, hq=0, n=6, cu=None):
+        return L.lar_paged_append_rope(kv, rope, pos, ps, k, v, q, qo, hq, n, cu, None)
+    assert call(pos=None) == INVALID and call(rope=None) == INVALID and call(ps=5) == INVALID and call(pos=258) == INVALID
+    assert call(k=None) == INVALID and call(v=_r(None)) == INVALID and call(k=_r(4097, 128, 64)) == INVALID
+    assert call(q=rows) == INVALID and call(q=rows, qo=rows) == INVALID and call(hq=2) == INVALID and call(hq=-1) == INVALID
+    assert call(rope=lar.make_rope(128, (64,))) == INVALID  # another head_dim
+    assert call(n=7) == INVALID and call(cu=255) == INVALID and call(n=0) == lar.LAR_OK
+
+
+def test_rope_refusals():
+    L, rows = lar.lib(), _r(4096, 128, 64)
+
+    def rot(rope, dtype=lar.LAR_BF16, pos=256, ps=6, n=6, q=rows, qo=rows, hq=2, k=None, ko=None, hk=0):
+        return L.lar_rope_rotate(rope, dtype, pos, ps, n, q, qo, hq, k, ko, hk, 0, None)
+    good = lar.make_rope(64, (8, 12, 12))
+    for bad in (lar.make_rope(64, (8, 12)), lar.make_rope(64, (8, 12, 13)), lar.make_rope(64, (32, 0)), lar.make_rope(96, (48,)),
+                lar.make_rope(64, (33, -1)), lar.make_rope(64, (32,), theta=0.0), lar.make_rope(64, (32,), theta=float("nan")),
+                lar.make_rope(64, (1 << 30, 1 << 30, 32))):
+        assert rot(bad) == INVALID
+        assert L.lar_rope_table(bad, 256, 6, 6, 4096, None) == INVALID
+    with pytest.raises(lar.LarError):
+        lar.make_rope(64, (8, 8, 8, 4, 4))
+    assert rot(good, dtype=3) == INVALID and rot(good, pos=None) == INVALID and rot(good, ps=5) == INVALID
+    assert rot(good, hq=0) == INVALID and rot(good, k=rows) == INVALID and rot(good, hk=1) == INVALID
+    assert rot(good, n=-1) == INVALID and rot(good, n=0) == lar.LAR_OK and rot(None) == INVALID
+    assert rot(good, qo=_r(4096, 64, 64)) == INVALID and rot(good, q=_r(4100, 128, 64)) == INVALID
+    assert L.lar_rope_table(good, 256, 6, -1, 4096, None) == INVALID and L.lar_rope_table(good, 256, 6, 0, 4096, None) == lar.LAR_OK
+    assert L.lar_rope_table(good, 256, 5, 6, 4096, None) == INVALID and L.lar_rope_table(good, 256, 6, 6, 4098, None) == INVALID
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    x, pos = torch.zeros(4, 2, 64), torch.zeros(1, 4, dtype=torch.int32)
+    rope = lar.make_rope(64, (32,))
+    with pytest.raises(lar.LarError):
+        lar.rope_rotate(rope, pos, x, x)                                       # not on a GPU
+    with pytest.raises(lar.LarError):
+        lar.rope_rotate(rope, pos, x.double(), x.double())
+    with pytest.raises(lar.LarError):
+        lar.rope_rotate(rope, pos.long(), x, x)
+    with pytest.raises(lar.LarError):
+        lar.rope_rotate(rope, pos[:, :3], x, x)
+    pool, table, lens = torch.zeros(4, 32, 2, 64), torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    lar.PagedKV(pool, pool, table, lens, 2)
+    for a in ((pool, pool.bfloat16(), table, lens, 2), (pool, pool, table.long(), lens, 2), (pool, pool, table, lens, 4),
+              (pool, pool, table[:, None], lens, 2), (pool, pool, table, lens[:0], 2)):
+        with pytest.raises(lar.LarError):
+            lar.PagedKV(*a)
+
+
+# ---------------------------------------------------------------------------------------------------------- rotary
+def _randn(shape, dtype, seed, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float32) * scale).to(dtype)
+
+
+def _pos(axes, n, seed, far=100000):
+    g = torch.Generator().manual_seed(seed)
+    p = torch.randint(-20, far, (axes, n), generator=g, dtype=torch.int32)
+    if axes > 1:
+        p[1:] %= 128
+    return p
+
+
+def _assert_close(got, ref, tol, what=""):
+    err = (got.double().cpu() - ref).abs()
+    bad = ~(err <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {float((err / tol).nan_to_num(9e9).max()):.3g} x the bound"
+
+
+ROPES = [((32,), 64), ((16, 16), 64), ((8, 12, 12), 64), ((11, 5, 9, 7), 64), ((64,), 128), ((16, 24, 24), 128), ((1, 62, 1), 128)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("restart", [False, True])
+@pytest.mark.parametrize("axes,d", ROPES)
+def test_rotary_rows(dtype, interleaved, restart, axes, d):
+    for n, hq, hk in ((1, 1, 0), (5, 3, 1), (130, 20, 20), (2400, 5, 2)):
+        x = _randn((n, hq + hk + 1, d), dtype, n + d)                    # views of one projection's output
+        pos = _pos(len(axes), n, n)
+        rope = lar.make_rope(d, axes, theta=10000.0, interleaved=interleaved, restart=restart)
+        xd, pd = x.to(DEV), pos.to(DEV)
+        q, k = xd[:, :hq], xd[:, hq:hq + hk] if hk else None
+        qo = torch.full((hq, n, d), 7.0, dtype=dtype, device=DEV).transpose(0, 1)    # head-major output
+        ko = torch.empty(n, hk, d, dtype=dtype, device=DEV) if hk else None
+        lar.rope_rotate(rope, pd, q, qo, k, ko)
+        ref = R.rotate(x, pos, axes, 10000.0, interleaved, restart)
+        tol = R.rotation_tolerance(dtype, ref, x, interleaved)
+        _assert_close(qo, ref[:, :hq], tol[:, :hq], "q")
+        if hk:
+            _assert_close(ko, ref[:, hq:hq + hk], tol[:, hq:hq + hk], "k")
+        # in place and back: two rotations' roundings, the first's scaled by |cos| + |sin| <= sqrt 2
+        lar.rope_rotate(rope, pd, q, q)
+        assert torch.equal(q, qo)
+        assert torch.equal(xd[:, hq + hk:].cpu(), x[:, hq + hk:])        # neighbours untouched
+        lar.rope_rotate(rope, pd, q, q, inverse=True)
+        xq = x[:, :hq]
+        first = R.rotation_tolerance(dtype, ref[:, :hq], xq, interleaved)
+        back = R.partner_sum(first, interleaved) + R.rotation_tolerance(dtype, xq.double(), ref[:, :hq].abs() + first, interleaved)
+        _assert_close(q, xq.double(), back, "back")
+
+
+@pytest.mark.gpu
+def test_rotary_gradient_is_the_inverse_rotation():
+    """d/dx of <g, rotate(x)> against differences of the 64-bit form, and against the kernel's inverse rotation of g."""
+    axes, d, n, h = (8, 12, 12), 64, 3, 2
+    x, g, pos = _randn((n, h, d), F32, 1), _randn((n, h, d), F32, 2), _pos(3, n, 3)
+    rope = lar.make_rope(d, axes)
+    gx = torch.empty(n, h, d, device=DEV)
+    lar.rope_rotate(rope, pos.to(DEV), g.to(DEV), gx, inverse=True)
+    f = lambda y: (g.double() * R.rotate(y, pos, axes, 10000.0, False, False)).sum()
+    ref = torch.zeros(n, h, d, dtype=torch.float64)
+    for i in range(n * h * d):
+        e = torch.zeros(n * h * d, dtype=torch.float64)
+        e[i] = 0.5                                             # the form is linear: any step gives the exact quotient
+        e = e.view(n, h, d)
+        ref.view(-1)[i] = f(x.double() + e) - f(x.double() - e)
+    _assert_close(gx, ref, R.rotation_tolerance(F32, ref, g, False) + 1e-12, "gradient")
+
+
+@pytest.mark.gpu
+def test_table_feeds_the_decode_step():
+    """lar_rope_table -> lar_decode_step_rope equals lar_rope_rotate -> lar_decode_step, bit for bit."""
+    for interleaved in (False, True):
+        w = dict(n_layers=1, batch=3, n_q_heads=4, n_kv_heads=2, head_dim=64, dtype="bf16", cond_len=5, line_width=8, n_lines=4,
+                 anchor_len=8, recent_lines=1, budget_lines=4)
+        caches = [lar.Cache(lar.make_config(**w)) for _ in range(2)]
+        rope = lar.make_rope(64, (10, 11, 11), interleaved=interleaved)
+        kc, vc = _randn((3, 2, 5, 64), BF, 1).to(DEV), _randn((3, 2, 5, 64), BF, 2).to(DEV)
+        for c in caches:
+            c.append_kv(0, kc, vc, 5)
+        for step in range(4):
+            q, k, v = (_randn((3, h, 64), BF, 10 * step + i).to(DEV) for i, h in enumerate((4, 2, 2)))
+            pos = _pos(3, 3, step).to(DEV)
+            cs = torch.empty(3, 64, device=DEV)
+            lar.rope_table(rope, pos, cs)
+            outs = [torch.empty_like(q) for _ in range(2)]
+            caches[0].decode_step_rope(0, q, k, v, outs[0], 256, 128, 128, 256, cs, interleaved)
+            qr, kr = torch.empty_like(q), torch.empty_like(k)
+            lar.rope_rotate(rope, pos, q, qr, k, kr)
+            caches[1].decode_step(0, qr, kr, v, outs[1])
+            assert torch.equal(outs[0], outs[1])
+        for c in caches:
+            assert c.poll_device_status() == 0
+            c.close()
+
+
+# ------------------------------------------------------------------------------------------------- a cache for the tests
+class PagedCase:
+    """Pools with shuffled pages, NaN wherever no live row lies, and a table whose unused entries are out of range."""
+
+    def __init__(self, dtype, d, hkv, page, layout, n, lens, seed=0, extra_cols=1):
+        rng = random.Random(seed)
+        self.dtype, self.d, self.hkv, self.page, self.layout, self.n, self.lens = dtype, d, hkv, page, layout, n, lens
+        S, per_head = len(n), layout == "heads"
+        tables = hkv if per_head else 1
+        cols = -(-max(max(lens), 1) // page) + extra_cols
+        need = [-(-x // page) for x in lens]
+        n_pages = sum(need) * tables + 3
+        ids = rng.sample(range(n_pages), sum(need) * tables)
+        self.table = torch.full((S, tables, cols), 1 << 30, dtype=torch.int32)
+        for s in range(S):
+            for h in range(tables):
+                for c in range(need[s]):
+                    self.table[s, h, c] = ids.pop()
+                if cols - need[s] > 1:
+                    self.table[s, h, need[s] + 1:] = -7
+        heads = 1 if per_head else hkv
+        shape = (n_pages, heads, page, d) if layout == "hnd" else (n_pages, page, heads, d)
+        self.pools = [torch.full(shape, float("nan"), dtype=dtype) for _ in range(2)]
+        if layout == "hnd":
+            self.pools = [p.transpose(1, 2) for p in self.pools]
+        self.dev = [self._to_dev(p) for p in self.pools]
+        tab = (self.table if per_head else self.table[:, 0]).contiguous().to(DEV)
+        self.status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        self.lens_dev = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        self.kv = lar.PagedKV(self.dev[0], self.dev[1], tab, self.lens_dev, hkv, status=self.status)
+        self.cu = torch.tensor([0] + list(torch.tensor(n).cumsum(0)), dtype=torch.int32, device=DEV)
+
+    def _to_dev(self, p):
+        return p.transpose(1, 2).contiguous().to(DEV).transpose(1, 2) if self.layout == "hnd" else p.to(DEV)
+
+    def place(self, s, h, j):
+        per_head = self.layout == "heads"
+        return int(self.table[s, h if per_head else 0, j // self.page]), j % self.page, 0 if per_head else h
+
+    def fill(self, start, seed):
+        """Random live rows (slots before start stay NaN)."""
+        for i, p in enumerate(self.pools):
+            for s, L in enumerate(self.lens):
+                x = _randn((self.hkv, L, self.d), self.dtype, seed * 1000 + 2 * s + i)
+                for h in range(self.hkv):
+                    for j in range(start[s] if start else 0, L):
+                        a, b, c = self.place(s, h, j)
+                        p[a, b, c] = x[h, j]
+            self.dev[i].copy_(p.to(DEV))
+
+    def rows(self, which):
+        def get(s, h, j0, j1):
+            return torch.stack([self.pools[which][self.place(s, h, j)] for j in range(j0, j1)])
+        return get
+
+
+# ---------------------------------------------------------------------------------------------------------- append
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout,page,d,hkv,hq", [("heads", 32, 128, 3, 6), ("nhd", 16, 64, 5, 0), ("hnd", 64, 128, 2, 8),
+                                                  ("nhd", 128, 64, 1, 4), ("heads", 16, 64, 20, 20)])
+@pytest.mark.parametrize("n,lens", [([1], [1]), ([1, 0, 1, 1], [64, 9, 65, 1]), ([0, 33, 7, 0, 130], [3, 33, 70, 0, 257])])
+def test_append(dtype, layout, page, d, hkv, hq, n, lens):
+    for rotated in (True, False):
+        c = PagedCase(dtype, d, hkv, page, layout, n, lens, seed=page + d)
+        T = sum(n)
+        pad = 2                                                # a padded batch: tokens that belong to no sequence
+        x = _randn((T + pad, hq + 2 * hkv, d), dtype, 5)
+        xd = x.to(DEV)
+        axes = (8, 12, 12) if d == 64 else (16, 24, 24)
+        pos = _pos(3, T + pad, 6)
+        rope = lar.make_rope(d, axes, interleaved=page == 16)
+        qo = torch.full((T + pad, hq, d), 7.0, dtype=dtype, device=DEV) if hq else None
+        c.kv.append_rope(xd[:, hq:hq + hkv], xd[:, hq + hkv:], c.cu, rope if rotated else None, pos.to(DEV) if rotated else None,
+                         xd[:, :hq] if hq else None, qo)
+        ref = R.rotate(x, pos, axes, 10000.0, page == 16, False) if rotated else x.double()
+        tol = R.rotation_tolerance(dtype, ref, x, page == 16) if rotated else torch.zeros_like(ref)
+        want = [p.double().clone() for p in c.pools]
+        tols = torch.zeros_like(want[0])
+        t = 0
+        for s, a in enumerate(n):
+            for i in range(a):
+                for h in range(hkv):
+                    at = c.place(s, h, lens[s] - a + i)
+                    want[0][at], want[1][at] = ref[t, hq + h], x[t, hq + hkv + h].double()
+                    tols[at] = tol[t, hq + h]
+                t += 1
+        for i in range(2):
+            got, nan = c.dev[i].double().cpu(), want[i].isnan()
+            assert torch.equal(got.isnan(), nan)               # every other row as it was
+            _assert_close(got[~nan], want[i][~nan], (tols if i == 0 else tols * 0)[~nan], f"pool {i}")
+        if hq:
+            _assert_close(qo[:T], ref[:T, :hq], tol[:T, :hq], "q")
+            assert (qo[T:] == 7.0).all()
+        assert int(c.status) == 0
+
+
+@pytest.mark.gpu
+def test_append_follows_no_bad_page_or_slot():
+    c = PagedCase(BF, 64, 2, 32, "nhd", [40, 3], [40, 10])
+    table = c.kv._keep[2]
+    table[0, 1] = 10 ** 6                                     # the second page of sequence 0
+    c.lens_dev[1] = 2                                          # fewer entries than the chunk has tokens
+    before = [x.clone() for x in c.dev]
+    x = _randn((43, 4, 64), BF, 1).to(DEV)
+    c.kv.append_rope(x[:, :2], x[:, 2:], c.cu)
+    assert int(c.status) == 64
+    for which, pool in enumerate(c.dev):
+        want = before[which].clone()
+        want[int(c.table[0, 0, 0])] = x[:32, 2 * which:2 * which + 2]
+        page = int(c.table[1, 0, 0])
+        want[page, 0:2] = x[41:43, 2 * which:2 * which + 2]    # tokens 1 and 2 of the chunk have slots 0 and 1
+        assert torch.equal(pool.nan_to_num(9.0), want.nan_to_num(9.0))
+
+
+# ------------------------------------------------------------------------------------------------------- attention
+LENGTHS = [
+    ([1], [1]),
+    ([1, 1, 0, 1], [63, 64, 9, 65]),
+    ([1, 1], [700, 129]),
+    ([3, 0, 17, 2], [3, 0, 130, 257]),
+    ([40, 1, 130], [40, 300, 200]),
+    ([300, 5], [310, 5]),
+]
+SHAPES = [("heads", 32, 128, 2, 4), ("nhd", 64, 64, 2, 2), ("hnd", 16, 128, 1, 8), ("nhd", 128, 128, 3, 3), ("heads", 64, 64, 1, 3),
+          ("hnd", 32, 64, 1, 16)]
+
+
+def _check_attention(c, hq, causal, start, workspace, seed, out_pad=2, hints=True, q=None, scale=0.0):
+    T, d, dtype = sum(c.n), c.d, c.dtype
+    q = _randn((T + out_pad, hq, d), dtype, seed) if q is None else q
+    buf = torch.full((T + out_pad, hq + 1, d), 5.0, dtype=dtype, device=DEV)     # out is a view with a gap behind each token
+    out = buf[:, :hq]
+    mc, ml = (max(c.n), max(c.lens)) if hints else (0, 0)
+    ws = c.kv.attn_workspace(hq, T + out_pad, mc, ml) if workspace else None
+    if ws is not None:
+        ws.fill_(255)
+    sd = torch.tensor(start, dtype=torch.int32, device=DEV) if start is not None else None
+    c.kv.attn(q.to(DEV), out, c.cu, causal=causal, kv_start=sd, softmax_scale=scale, max_chunk=mc, max_len=ml, workspace=ws)
+    ref, mag, big = R.attention(q[:T], c.rows(0), c.rows(1), c.n, c.lens, start, causal, hq // c.hkv, scale or d ** -0.5)
+    tol = R.attention_tolerance(dtype, ref, mag, big, d, max(c.lens))
+    _assert_close(out[:T], ref, tol, f"causal {causal} start {start} workspace {ws is not None}")
+    assert (out[T:] == 5.0).all() and (buf[:, hq:] == 5.0).all()
+    assert int(c.status) == 0
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout,page,d,hkv,hq", SHAPES)
+@pytest.mark.parametrize("n,lens", LENGTHS)
+def test_attention(dtype, layout, page, d, hkv, hq, n, lens):
+    c = PagedCase(dtype, d, hkv, page, layout, n, lens, seed=d + page)
+    c.fill(None, 3)
+    for causal in (True, False):
+        for workspace in (False, True):
+            _check_attention(c, hq, causal, None, workspace, 11)
+    _check_attention(c, hq, True, None, True, 12, hints=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,lens,start", [
+    ([20, 5, 1], [20, 70, 66], [7, 69, 65]),          # the first tokens of a chunk are padding: they see nothing
+    ([40, 1, 9], [40, 64, 9], [200, 64, 9]),          # nothing is live: every row is zero
+    ([150, 3], [400, 140], [129, 128]),               # the padding ends inside, and at the end of, a step of slots
+    ([2, 2], [90, 90], [-5, 33]),                     # negative: no padding
+])
+def test_attention_with_left_padding(dtype, n, lens, start):
+    c = PagedCase(dtype, 64, 2, 32, "heads", n, lens)
+    c.fill([max(s, 0) for s in start], 4)
+    for causal in (True, False):
+        for workspace in (False, True):
+            out = _check_attention(c, 4, causal, start, workspace, 21)
+            if start[0] == 200:
+                assert (out[:sum(n)] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_extreme_logits(dtype):
+    """Logits of several hundred either way: the running maximum has to be taken off, and to grow along the cache."""
+    c = PagedCase(dtype, 64, 1, 32, "nhd", [70, 1], [300, 513])
+    c.fill(None, 5)
+    for i, s in enumerate(c.lens):                    # keys that grow with the slot
+        for j in range(s):
+            c.pools[0][c.place(i, 0, j)] *= 1.0 + j / 16
+    c.dev[0].copy_(c.pools[0].to(DEV))
+    for workspace in (False, True):
+        _check_attention(c, 2, True, None, workspace, 31)
+        _check_attention(c, 2, True, None, workspace, 32, scale=2.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_reads_a_bad_page_as_zeros(dtype):
+    c = PagedCase(dtype, 128, 2, 32, "nhd", [3, 2], [100, 40])
+    c.fill(None, 6)
+    table = c.kv._keep[2]
+    for bad in (10 ** 6, -1, -2 ** 31, 2 ** 31 - 1):
+        table[0, 1] = bad
+        q = _randn((5, 4, 128), dtype, 7)
+        out = torch.empty(5, 4, 128, dtype=dtype, device=DEV)
+        c.kv.attn(q.to(DEV), out, c.cu)
+        assert int(c.status) == 64
+        c.status.zero_()
+        zeroed = lambda which: (lambda s, h, j0, j1: torch.stack([
+            torch.zeros(128, dtype=dtype) if s == 0 and 32 <= j < 64 else c.pools[which][c.place(s, h, j)] for j in range(j0, j1)]))
+        ref, mag, big = R.attention(q, zeroed(0), zeroed(1), c.n, c.lens, None, True, 2, 128 ** -0.5)
+        _assert_close(out, ref, R.attention_tolerance(dtype, ref, mag, big, 128, 100))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_lengths_the_table_cannot_hold(dtype):
+    """A length beyond the table is cut to what the table holds; a chunk longer than its cache sees what there is."""
+    c = PagedCase(dtype, 64, 1, 32, "heads", [2, 9], [64, 4], extra_cols=0)
+    c.fill(None, 8)
+    q = _randn((11, 1, 64), dtype, 9)
+    out = torch.empty(11, 1, 64, dtype=dtype, device=DEV)
+    c.lens_dev[0] = 10 ** 6
+    c.kv.attn(q.to(DEV), out, c.cu)
+    ref, mag, big = R.attention(q[:2], c.rows(0), c.rows(1), [2, 0], [64, 4], None, True, 1, 0.125)
+    _assert_close(out[:2], ref, R.attention_tolerance(dtype, ref, mag, big, 64, 64))
+    assert (out[2:7] == 0).all()                       # slots before the cache's first
+    ref, mag, big = R.attention(q[7:], c.rows(0), c.rows(1), [0, 4], [64, 4], None, True, 1, 0.125)
+    _assert_close(out[7:], ref, R.attention_tolerance(dtype, ref, mag, big, 64, 64))
+
+
+# ------------------------------------------------------------------------------------------------- used together
+@pytest.mark.gpu
+def test_prefill_of_the_librarys_cache_then_decode_steps():
+    """A conditional prefix enters the cache with rotated keys, its attention runs over the cache, and decode steps with
+    the table of the same rotary embedding follow: everything against the 64-bit forms."""
+    S, Hq, Hkv, d, Cn = 3, 4, 2, 128, 37
+    for flags, dtype in ((0, "bf16"), (lar.LAR_FLAG_SHUFFLE_PAGES | lar.LAR_FLAG_PDL, "bf16"), (lar.LAR_FLAG_SHUFFLE_PAGES, "fp32")):
+        td = BF if dtype == "bf16" else F32
+        cfg = lar.make_config(n_layers=2, batch=S, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, dtype=dtype, cond_len=Cn,
+                              line_width=8, n_lines=4, anchor_len=8, recent_lines=1, budget_lines=4, flags=flags, page_seed=3)
+        cache = lar.Cache(cfg)
+        axes = (16, 24, 24)
+        rope = lar.make_rope(d, axes)
+        start = [0, 5, 36]
+        sd = torch.tensor(start, dtype=torch.int32, device=DEV)
+        for layer in range(2):
+            x = _randn((S * Cn, Hq + 2 * Hkv, d), td, layer)
+            pos = _pos(3, S * Cn, layer)
+            xd, qo = x.to(DEV), torch.empty(S * Cn, Hq, d, dtype=td, device=DEV)
+            cache.append_kv_rope(layer, xd[:, Hq:Hq + Hkv], xd[:, Hq + Hkv:], Cn, rope, pos.to(DEV), xd[:, :Hq], qo)
+            with pytest.raises(lar.LarError) as e:
+                cache.append_kv_rope(layer, xd[:, Hq:Hq + Hkv], xd[:, Hq + Hkv:], Cn)
+            assert e.value.status == lar.LAR_ERR_BAD_STATE
+            out = torch.empty_like(qo)
+            view = cache.paged_view(layer)
+            view.attn(qo, out, kv_start=sd, max_chunk=Cn, max_len=Cn, workspace=view.attn_workspace(Hq, S * Cn, Cn, Cn))
+            turned = R.rotate(x[:, :Hq + Hkv], pos, axes, 10000.0, False, False).to(td)
+            k, v = turned[:, Hq:].view(S, Cn, Hkv, d), x[:, Hq + Hkv:].view(S, Cn, Hkv, d)
+            ref, mag, big = R.attention(qo.cpu(), lambda s, h, a, b: k[s, a:b, h], lambda s, h, a, b: v[s, a:b, h], [Cn] * S, [Cn] * S,
+                                        start, True, Hq // Hkv, d ** -0.5)
+            # the reference's keys may round to the other neighbour: one step of bf16 (2^-7) or fp32 (2^-23) of each product
+            step = (2.0 ** -7 if td == BF else 2.0 ** -23) * 2 * big[..., None] * mag
+            _assert_close(out, ref, R.attention_tolerance(td, ref, mag, big, d, Cn) + step, f"{dtype} layer {layer}")
+            lens, imap = cache.get_state(layer)
+            assert (lens == Cn).all() and (imap[:, :Cn] == torch.arange(Cn).numpy()).all()
+            # a decode step behind it: compared with the plain attention over the same rows (no padding mask there)
+            q1, k1, v1 = (_randn((S, h, d), td, 50 + layer + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+            o1 = torch.empty(S, Hq, d, dtype=td, device=DEV)
+            cache.decode_step(layer, q1.to(DEV), k1.to(DEV), v1.to(DEV), o1)
+            view.attn(q1.to(DEV), out[:S], max_chunk=1, max_len=Cn + 1)       # the same token as a chunk of one
+            ka, va = torch.cat([k, k1[:, None]], 1), torch.cat([v, v1[:, None]], 1)
+            ref, mag, big = R.attention(q1, lambda s, h, a, b: ka[s, a:b, h], lambda s, h, a, b: va[s, a:b, h], [1] * S, [Cn + 1] * S,
+                                        None, True, Hq // Hkv, d ** -0.5)
+            step = (2.0 ** -7 if td == BF else 2.0 ** -23) * 2 * big[..., None] * mag
+            for o in (o1, out[:S]):
+                _assert_close(o, ref, R.attention_tolerance(td, ref, mag, big, d, Cn + 1) + step, f"{dtype} step {layer}")
+        assert cache.poll_device_status() == 0
+        cache.close()
+
+
+@pytest.mark.gpu
+def test_chunks_of_a_growing_cache_in_a_graph():
+    """Append and attention of chunks captured once and replayed with other lengths, positions and pages: the graph reads
+    them on the device.  Two replays share the workspace, one behind the other; they run on a side stream."""
+    hq, hkv, d, page, S = 4, 2, 64, 32, 3
+    n, T = [4, 1, 7], 12
+    c = PagedCase(BF, d, hkv, page, "nhd", n, [300, 290, 310], extra_cols=0)
+    c.fill(None, 1)
+    rope, axes = lar.make_rope(d, (32,)), (32,)
+    x, pos = torch.empty(T, hq + 2 * hkv, d, dtype=BF, device=DEV), torch.zeros(1, T, dtype=torch.int32, device=DEV)
+    qo, out = torch.empty(T, hq, d, dtype=BF, device=DEV), torch.empty(T, hq, d, dtype=BF, device=DEV)
+    ws = c.kv.attn_workspace(hq, T, 7, 310)
+    side = torch.cuda.Stream()
+
+    def step():
+        c.kv.append_rope(x[:, hq:hq + hkv], x[:, hq + hkv:], c.cu, rope, pos, x[:, :hq], qo)
+        c.kv.attn(qo, out, c.cu, max_chunk=7, max_len=310, workspace=ws)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    c.fill(None, 1)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step()
+    for rep, lens in enumerate(([300, 290, 310], [4, 1, 30], [257, 64, 128])):
+        xs, ps = _randn((T, hq + 2 * hkv, d), BF, 60 + rep), _pos(1, T, rep)
+        x.copy_(xs.to(DEV))
+        pos.copy_(ps.to(DEV))
+        c.lens_dev.copy_(torch.tensor(lens, dtype=torch.int32))
+        c.lens = lens
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):                              # the rows the append has just written
+            c.pools[i].copy_(c.dev[i].cpu())
+        ref, mag, big = R.attention(qo.cpu(), c.rows(0), c.rows(1), n, lens, None, True, hq // hkv, d ** -0.5)
+        _assert_close(out, ref, R.attention_tolerance(BF, ref, mag, big, d, 310), f"replay {rep}")
+        turned = R.rotate(xs[:, :hq], ps, axes, 10000.0, False, False)
+        _assert_close(qo, turned, R.rotation_tolerance(BF, turned, xs[:, :hq], False), "q")
+    assert int(c.status) == 0
