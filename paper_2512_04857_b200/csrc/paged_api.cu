@@ -8,6 +8,7 @@
 
 #include "host_util.h"
 #include "paged_attn_simt.cuh"
+#include "paged_attn_tc.cuh"
 #include "paged_host.h"
 #include "rope_rows.cuh"
 
@@ -128,19 +129,54 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
 
 // ------------------------------------------------------------------------------------------ chunk attention
 struct AttnPlan {
-    int bm, splits, tiles;  // fp32: rows of a tile, CTAs along a unit's slots, bound on the row tiles of all sequences
-    size_t bytes;           // workspace
+    int tq;        // tokens of a row tile
+    int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows)
+    int stages, grid, rows_cap;  // bf16: K/V ring, persistent CTAs, rows of a row tile
+    int bm, splits, tiles;       // fp32: rows of a tile, CTAs along a unit's slots, bound on the row tiles of all sequences
+    size_t bytes;  // workspace
+    size_t smem;
 };
+
+template <int NT>
+size_t tc_smem(int d, int rows_cap, int stages, int n_seqs) {
+    return d == 64 ? lar::TcSmem<64, NT>::bytes(rows_cap, stages, n_seqs) : lar::TcSmem<128, NT>::bytes(rows_cap, stages, n_seqs);
+}
 
 AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, bool split) {
     AttnPlan p;
+    memset(&p, 0, sizeof(p));
     const int64_t chunk = max_chunk > 0 ? max_chunk : (n_tokens + k.n_seqs - 1) / k.n_seqs;
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
-    p.bm = chunk * group <= 16 ? 16 : 64;
-    const int tq = p.bm / group;
     const int64_t with_tokens = n_tokens < k.n_seqs ? n_tokens : k.n_seqs;
-    p.tiles = (int)(n_tokens / tq + with_tokens);
+    const int d = k.head_dim;
+    if (k.dtype == LAR_BF16) {
+        constexpr size_t kSmem = 227 * 1024;
+        p.nt = chunk * group > 128 ? 2 : 1;
+        p.tq = 128 / group;
+        if (p.nt == 1 && chunk < p.tq) p.tq = (int)chunk;
+        p.rows_cap = (p.tq * group + 7) / 8 * 8;
+        int per_sm = 1;
+        if (p.nt == 2) {
+            p.stages = lar::kTcMaxStages;
+            while (p.stages > 1 && tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs) > kSmem) --p.stages;
+            p.smem = tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs);
+        } else {
+            // two CTAs per SM, unless the lengths of very many sequences leave no room for two stages each
+            constexpr size_t kHalf = 233472 / 2 - 1024;
+            p.stages = lar::kTcMaxStages;
+            while (p.stages > 2 && tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs) > kHalf) --p.stages;
+            per_sm = tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs) <= kHalf ? 2 : 1;
+            p.smem = tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs);
+        }
+        p.grid = per_sm * kSms;
+        p.splits = split && p.nt == 1 ? 2 : 1;
+        if (p.splits > 1) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
+        return p;
+    }
+    p.bm = chunk * group <= 16 ? 16 : 64;
+    p.tq = p.bm / group;
+    p.tiles = (int)(n_tokens / p.tq + with_tokens);
     p.splits = 1;
     if (split) {
         const int64_t units = (int64_t)p.tiles * k.n_kv_heads;
@@ -149,28 +185,108 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         if (s > 64) s = 64;
         p.splits = s < 1 ? 1 : (int)s;
     }
-    p.bytes = p.splits > 1 ? (size_t)p.splits * n_tokens * k.n_kv_heads * group * (k.head_dim + 2) * sizeof(float) : 0;
+    p.bytes = p.splits > 1 ? (size_t)p.splits * n_tokens * k.n_kv_heads * group * (d + 2) * sizeof(float) : 0;
     return p;
 }
 
 using SimtFn = void (*)(const lar::PagedAttnArgs);
-template <typename T, int D, int BM>
+template <int D, int BM>
 lar_status_t launch_simt(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    SimtFn fn = lar::paged_attn_simt_kernel<T, D, BM>;
+    SimtFn fn = lar::paged_attn_simt_kernel<float, D, BM>;
     constexpr int smem = lar::SimtShape<D, BM>::SMEM;
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), lar::SimtShape<D, BM>::THREADS, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     if (p.splits > 1) {
         const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.n_kv_heads * a.group;
-        lar::combine_splits_kernel<T, D><<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);
+        lar::combine_splits_kernel<float, D><<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);
         LAR_CUDA(cudaGetLastError());
     }
     return LAR_OK;
 }
-template <typename T, int D>
-lar_status_t launch_simt_bm(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    return p.bm == 16 ? launch_simt<T, D, 16>(a, p, s) : launch_simt<T, D, 64>(a, p, s);
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+lar_status_t encode_4d(EncodeTiledFn encode, CUtensorMap* m, void* p, const cuuint64_t (&dim)[4], const int64_t (&stride)[3],
+                       const cuuint32_t (&box)[4]) {
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    const cuuint64_t st[3] = {(cuuint64_t)stride[0] * 2, (cuuint64_t)stride[1] * 2, (cuuint64_t)stride[2] * 2};
+    if (encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, p, dim, st, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+        lar::last_cuda_error() = (int)cudaErrorInvalidValue;
+        return LAR_ERR_CUDA;
+    }
+    return LAR_OK;
+}
+
+lar_status_t make_maps(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, int box_rows, lar::TcMaps& m) {
+    static const EncodeTiledFn encode = [] {
+        void* fp = nullptr;
+        cudaDriverEntryPointQueryResult res;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fp, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            fp = nullptr;
+        }
+        return reinterpret_cast<EncodeTiledFn>(fp);
+    }();
+    if (!encode) {
+        lar::last_cuda_error() = (int)cudaErrorNotSupported;
+        return LAR_ERR_CUDA;
+    }
+    const cuuint64_t d = (cuuint64_t)k.head_dim;
+    const cuuint64_t qdim[4] = {d, (cuuint64_t)a.group, (cuuint64_t)k.n_kv_heads, (cuuint64_t)a.kv.n_tokens};
+    const int64_t qst[3] = {a.q.head_stride, a.q.head_stride * a.group, a.q.token_stride};
+    const cuuint32_t qbox[4] = {64, (cuuint32_t)a.group, 1, (cuuint32_t)a.tq};
+    lar_status_t st = encode_4d(encode, &m.q, a.q.p, qdim, qst, qbox);
+    const int heads = k.head_stride > 0 ? k.n_kv_heads : 1;  // heads with pages of their own: every page is one head's
+    const int64_t page_stride = k.n_pages > 1 ? k.page_stride : k.row_stride * k.page_tokens * heads;
+    const cuuint64_t kdim[4] = {d, (cuuint64_t)k.page_tokens, (cuuint64_t)heads, (cuuint64_t)k.n_pages};
+    const int64_t kst[3] = {k.row_stride, heads > 1 ? k.head_stride : page_stride, page_stride};
+    const cuuint32_t kbox[4] = {64, (cuuint32_t)box_rows, 1, 1};
+    if (st == LAR_OK) st = encode_4d(encode, &m.k, k.k_pool, kdim, kst, kbox);
+    if (st == LAR_OK) st = encode_4d(encode, &m.v, k.v_pool, kdim, kst, kbox);
+    return st;
+}
+
+template <int D, int NT>
+lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
+    using S = lar::TcShape<D, NT>;
+    lar::TcArgs t;
+    memset(&t, 0, sizeof(t));
+    lar::TcMaps m;
+    t.a = a;
+    t.stages = p.stages;
+    t.rows_cap = p.rows_cap;
+    t.box_rows = k.page_tokens < S::BN ? k.page_tokens : S::BN;
+    t.split = p.splits > 1;
+    t.min_items = 4;
+    if (t.split) {  // records, then (m, l), then O of every CTA's two parts
+        t.records = reinterpret_cast<int4*>(a.part_o);
+        t.a.part_ml = reinterpret_cast<float*>(t.records + p.grid);
+        t.a.part_o = t.a.part_ml + (size_t)p.grid * 2 * p.rows_cap * 2;
+    }
+    lar_status_t st = make_maps(k, a, t.box_rows, m);
+    if (st != LAR_OK) return st;
+    const void* fn = (const void*)lar::paged_attn_tc_kernel<D, NT>;
+    LAR_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
+    lar::paged_attn_tc_kernel<D, NT><<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
+    LAR_CUDA(cudaGetLastError());
+    if (t.split) {
+        cudaLaunchConfig_t lc;
+        memset(&lc, 0, sizeof(lc));
+        lc.gridDim = dim3((unsigned)p.grid, (unsigned)((p.rows_cap * (D / 4) + 511) / 512), 1);
+        lc.blockDim = dim3(128, 1, 1);
+        lc.stream = s;
+        cudaLaunchAttribute at;
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        lc.attrs = &at;
+        lc.numAttrs = 1;
+        LAR_CUDA(cudaLaunchKernelEx(&lc, lar::join_ranges_kernel<D>, (const lar::TcArgs)t));
+    }
+    return LAR_OK;
 }
 
 }  // namespace
@@ -279,20 +395,25 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     if (n_tokens == 0) return LAR_OK;
     const int elt = elt_of(kv->dtype), d = kv->head_dim;
     if (!rows_view(q, n_tokens, n_q_heads, d, elt, false, a.q) || !rows_view(out, n_tokens, n_q_heads, d, elt, true, a.out)) return LAR_ERR_INVALID_ARG;
+    if (kv->dtype == LAR_BF16 && kv->n_seqs > lar::kTcMaxSeqs) return LAR_ERR_CAPACITY;
     const AttnPlan p = attn_plan(*kv, group, n_tokens, max_chunk, max_len, workspace != nullptr);
     if (workspace && !aligned(workspace, 16)) return LAR_ERR_INVALID_ARG;
     if (p.bytes > workspace_bytes) return LAR_ERR_NOMEM;
     a.start = kv_start;
     a.group = group;
     a.causal = causal != 0;
-    a.tq = p.bm / group;
+    a.tq = p.tq;
     a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d)) * 1.4426950408889634f;
     a.n_splits = p.splits;
     a.part_o = static_cast<float*>(workspace);
-    a.part_ml = p.splits > 1 ? a.part_o + (size_t)p.splits * n_tokens * n_q_heads * d : nullptr;
+    a.part_ml = p.splits > 1 ? a.part_o + (size_t)p.splits * n_tokens * n_q_heads * d : nullptr;  // (fp32; launch_tc lays its own out)
     cudaStream_t s = (cudaStream_t)stream;
-    if (kv->dtype == LAR_BF16) return d == 64 ? launch_simt_bm<__nv_bfloat16, 64>(a, p, s) : launch_simt_bm<__nv_bfloat16, 128>(a, p, s);
-    return d == 64 ? launch_simt_bm<float, 64>(a, p, s) : launch_simt_bm<float, 128>(a, p, s);
+    if (kv->dtype == LAR_BF16) {
+        if (p.nt == 2) return d == 64 ? launch_tc<64, 2>(*kv, a, p, s) : launch_tc<128, 2>(*kv, a, p, s);
+        return d == 64 ? launch_tc<64, 1>(*kv, a, p, s) : launch_tc<128, 1>(*kv, a, p, s);
+    }
+    if (p.bm == 16) return d == 64 ? launch_simt<64, 16>(a, p, s) : launch_simt<128, 16>(a, p, s);
+    return d == 64 ? launch_simt<64, 64>(a, p, s) : launch_simt<128, 64>(a, p, s);
 }
 
 }  // extern "C"

@@ -1,0 +1,722 @@
+// Chunk attention for bf16 storage on the 5th-generation tensor cores (tcgen05, accumulators in TMEM), one persistent kernel
+// for single tokens over long caches (bound by the cache's bytes) and for prompts (bound by the tensor cores and the
+// exponentials).
+//
+// A row tile is up to 128 (token, head of the group) rows of one KV head.  A CTA works on NT of them at a time:
+//   NT = 2  chunks of more than 128 rows: 256 rows share every K/V tile; while the softmax of one row tile runs on its warps, the tensor core
+//           works on the other.
+//   NT = 1  few rows: K/V tiles of 64 slots, two logit buffers (the logits of the next tile are formed while the softmax of this
+//           one runs) and two CTAs per SM, since what counts is that the cache streams without a pause.
+// Roles (coupled by mbarriers only, every wait bounded):
+//   NT * 4 softmax warps  one thread per row: logits from TMEM, mask, running maximum and sum (fp32), P (bf16) back into
+//                         TMEM over the logits it came from; output rows at the end.
+//   one MMA warp          S = Q K^T (both from shared memory), O += P V (P from TMEM, V from shared memory with the slots
+//                         as its K dimension).
+//   one producer warp     a ring of K/V stages: one TMA box per page (or part of one) and 64 columns, the lanes issuing them side by side.
+// The output accumulator is rescaled only where a row's maximum has grown by more than 2^8 since its last rescaling (P then
+// reaches 2^8 at most, far inside the range of bf16 and fp32; the factor cancels in the final division), so the
+// accumulator hardly ever leaves TMEM.
+//
+// Slots outside [start, len) of a tile hold memory that may be anything: keys are masked by selection, and the value rows
+// are cleared in shared memory before the product (0 * NaN would reach the output).
+//
+// Work is dealt in one of two ways.  NT = 2: units (sequence, KV head, row tiles) round-robin, the longest tiles of a sequence
+// first, heads outermost, so that the CTAs of a moment share K/V in L2.  NT = 1: all units' slot tiles form one list that
+// is cut into equal ranges, one per CTA; a unit cut by a range boundary leaves (O, m, l) per CTA in the workspace and
+// join_ranges_kernel adds them up in the order of the CTAs.
+#pragma once
+#include <cuda.h>
+
+#include "decode_stream.cuh"  // wait_or_abort, mbar_arrive, ex2_approx, proxy fences
+#include "paged_attn.cuh"
+
+namespace lar {
+
+constexpr int kTcMaxSeqs = 1024;  // sequences of a call (their lengths are kept in shared memory)
+constexpr int kTcMaxStages = 4;
+
+template <int D, int NT>
+struct TcShape {
+    static constexpr int BN = NT == 2 ? 128 : 64;            // slots of a K/V tile
+    static constexpr int HALVES = D / 64;                    // 128-byte column blocks
+    static constexpr int TILE_BYTES = BN * D * 2;            // K or V tile
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
+    static constexpr int SM_WARPS = NT * 4;
+    static constexpr int THREADS = SM_WARPS * 32 + 64;
+    static constexpr int S_COLS = BN, O_COL = 2 * BN;        // TMEM: two logit buffers, then NT accumulators of D columns
+    static constexpr int TMEM_COLS = NT == 2 ? 512 : 256;
+    static_assert(O_COL + NT * D <= TMEM_COLS, "TMEM");
+};
+
+struct TcMaps {
+    CUtensorMap q;     // {d, heads of a group, KV heads, tokens}, box 64 x group x 1 x tq
+    CUtensorMap k, v;  // {d, rows of a page, heads, pages}, box 64 x min(page, BN) x 1 x 1
+};
+
+struct TcArgs {
+    PagedAttnArgs a;
+    int stages;
+    int rows_cap;      // rows of a row tile in shared memory: tq * group rounded up to 8
+    int box_rows;      // slots of one K/V box
+    int split;         // NT = 1: ranges may cut units
+    int min_items;     // NT = 1: slot tiles a CTA gets at least
+    int4* records;     // NT = 1, split: per CTA the unit that begins there and goes on in the next CTAs
+};
+
+// per sequence, in shared memory
+struct SeqInfo {
+    int t0, n, len, lo;
+};
+
+// ---------------------------------------------------------------------------------- tcgen05
+__device__ __forceinline__ void tc_alloc(uint32_t smem_dst, int cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_dealloc(uint32_t tmem, int cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
+}
+#define LAR_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define LAR_I4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
+// 32 columns of the warp's 32 lanes, one lane per thread
+__device__ __forceinline__ void tc_ld32(uint32_t tmem, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : LAR_R4(r, 0), LAR_R4(r, 4), LAR_R4(r, 8), LAR_R4(r, 12), LAR_R4(r, 16), LAR_R4(r, 20), LAR_R4(r, 24), LAR_R4(r, 28)
+        : "r"(tmem));
+}
+__device__ __forceinline__ void tc_st32(uint32_t tmem, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(tmem), LAR_I4(r, 0), LAR_I4(r, 4),
+        LAR_I4(r, 8), LAR_I4(r, 12), LAR_I4(r, 16), LAR_I4(r, 20), LAR_I4(r, 24), LAR_I4(r, 28)
+        : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t tmem, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(tmem),
+        LAR_I4(r, 0), LAR_I4(r, 4), LAR_I4(r, 8), LAR_I4(r, 12)
+        : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory matrix descriptors, 128-byte swizzle.  K-major rows of 128 bytes (64 elements of the contracted dimension): groups of 8 rows
+// lie 1024 bytes apart.  Slots-as-K (V): 64 columns per 128-byte row, column blocks lead_bytes apart, groups of 8 slots 1024 apart.
+__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead_bytes) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lead_bytes >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// fp32 accumulator, bf16 operands, M = 128
+__host__ __device__ constexpr uint32_t tc_idesc(int n, bool b_transposed) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_transposed ? 1u : 0u) << 16) | ((uint32_t)(n / 8) << 17) | ((128u / 16u) << 24);
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
+}
+
+// ---------------------------------------------------------------------------------- shared memory
+template <int D, int NT>
+struct TcSmem {
+    using S = TcShape<D, NT>;
+    static __host__ __device__ int q_bytes(int rows_cap) { return NT * S::HALVES * ((rows_cap * 128 + 1023) / 1024 * 1024); }
+    // the MMA reads 128 rows whatever rows_cap is: behind the last Q tile there is always a K/V stage or more
+    static __host__ __device__ int tail(int n_seqs) { return 32 * 8 + 16 + n_seqs * 16 + (n_seqs + 1) * 8 + 64 * 8; }
+    static __host__ __device__ int bytes(int rows_cap, int stages, int n_seqs) {
+        return 1024 + q_bytes(rows_cap) + stages * S::STAGE_BYTES + tail(n_seqs);
+    }
+};
+
+// ---------------------------------------------------------------------------------- work list
+// One step of a CTA's work: some slot tiles of one unit.
+struct TcSeg {
+    int seq, head, tok0, n_tok;  // tokens of the unit
+    int slot0;                   // slot of its first token
+    int lo, len;                 // live slots of the sequence
+    int jb;                      // first slot tile
+    int nb[2];                   // slot tiles of each row tile
+    int nmax;
+    int whole;                   // nothing of the unit lies in other CTAs
+    int b0;                      // tiles of the unit before this step's
+    long long unit_end;          // end of the unit in the list of items
+};
+
+template <int NT, int BN>
+struct TcWork {
+    const SeqInfo* info;
+    const long long* pre;  // items before each sequence
+    int n_seqs, heads, tq, causal, units;  // units: an item is a whole unit (else a slot tile)
+    long long x, end, step;
+
+    __device__ __forceinline__ bool next(TcSeg& g) {
+        if (x >= end) return false;
+        int a = 0, b = n_seqs;  // pre[a] <= x < pre[b]
+        while (b - a > 1) {
+            const int m = (a + b) >> 1;
+            if (pre[m] <= x) a = m; else b = m;
+        }
+        const SeqInfo s = info[a];
+        const int ut = NT * tq, tiles = (s.n + ut - 1) / ut;
+        const int first = s.lo / BN, full = s.len > s.lo ? (s.len + BN - 1) / BN - first : 0;
+        const int w = units ? 1 : full > 0 ? full : 1;
+        const long long r = x - pre[a];
+        const long long unit = r / w;
+        g.b0 = (int)(r - unit * w);
+        g.head = (int)(unit / tiles);
+        int tile = (int)(unit - (long long)g.head * tiles);
+        if (units) tile = tiles - 1 - tile;  // the tiles that see most first
+        int take = w - g.b0;
+        if ((long long)take > end - x) take = (int)(end - x);
+        if (units) {
+            x += step;
+            g.whole = 1;
+        } else {
+            g.whole = g.b0 == 0 && take == w;
+            g.unit_end = x + (w - g.b0);
+            x += take;
+        }
+        g.seq = a;
+        g.tok0 = s.t0 + tile * ut;
+        g.n_tok = min(ut, s.n - tile * ut);
+        g.slot0 = s.len - s.n + tile * ut;
+        g.lo = s.lo;
+        g.len = s.len;
+        g.jb = first + (units ? 0 : g.b0);
+        g.nmax = 0;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int nt = min(tq, g.n_tok - i * tq);
+            const int hi = nt <= 0 ? 0 : causal ? min(s.len, g.slot0 + i * tq + nt) : s.len;
+            int n = hi > s.lo ? (hi + BN - 1) / BN - g.jb : 0;
+            if (!units && n > take) n = take;
+            g.nb[i] = n > 0 ? n : 0;
+            g.nmax = max(g.nmax, g.nb[i]);
+        }
+        return true;
+    }
+};
+
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// The whole warp waits, and gives up together (what follows are warp-wide instructions).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
+    using S = TcShape<D, NT>;
+    constexpr int BN = S::BN, HALVES = S::HALVES;
+    const PagedAttnArgs& a = ta.a;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char* gbase = smem_raw + (base - smem_u32(smem_raw));
+    const int NS = ta.stages;
+    const uint32_t q_half = (uint32_t)((ta.rows_cap * 128 + 1023) / 1024 * 1024);  // bytes of 64 columns of a Q tile
+    const uint32_t q_tile = q_half * HALVES;
+    const uint32_t ring = base + NT * q_tile;
+    unsigned char* tail = gbase + NT * q_tile + NS * S::STAGE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(tail);
+    const uint32_t bar0 = smem_u32(bars);
+    auto q_full = [&](int i) { return bar0 + 8u * i; };
+    auto q_empty = [&](int i) { return bar0 + 8u * (2 + i); };
+    auto s_full = [&](int i) { return bar0 + 8u * (4 + i); };
+    auto p_full = [&](int i) { return bar0 + 8u * (6 + i); };
+    auto pv_done = [&](int i) { return bar0 + 8u * (8 + i); };
+    auto o_free = [&](int i) { return bar0 + 8u * (10 + i); };
+    const uint32_t bar_drain = bar0 + 8u * 12;
+    auto k_full = [&](int st) { return bar0 + 8u * (13 + st); };
+    auto v_full = [&](int st) { return bar0 + 8u * (17 + st); };
+    auto kv_empty = [&](int st) { return bar0 + 8u * (21 + st); };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 32);
+    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(bars + 32) + 1;
+    SeqInfo* info = reinterpret_cast<SeqInfo*>(bars + 34);
+    long long* pre = reinterpret_cast<long long*>(info + a.kv.n_seqs);
+    long long* wsum = pre + a.kv.n_seqs + 1;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool units = NT == 2 || !ta.split;
+
+    if (warp == S::SM_WARPS) {
+        if (lane == 0) {
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(q_full(i), 1);
+                mbar_init(q_empty(i), 1);
+                mbar_init(s_full(i), 1);
+                mbar_init(p_full(i), 4);
+                mbar_init(pv_done(i), 1);
+                mbar_init(o_free(i), 4);
+            }
+            mbar_init(bar_drain, 1);
+            for (int i = 0; i < kTcMaxStages; ++i) {
+                mbar_init(k_full(i), 1);
+                mbar_init(v_full(i), 1);
+                mbar_init(kv_empty(i), 1);
+            }
+            mbar_fence_init_smem();
+            *abort_flag = 0;
+        }
+        __syncwarp();
+        tc_alloc(smem_u32(tmem_ptr), S::TMEM_COLS);
+    }
+    // items before each sequence: every thread takes a run of sequences
+    {
+        const int per = (a.kv.n_seqs + S::THREADS - 1) / S::THREADS, s0 = tid * per;
+        long long sum = 0;
+        for (int s = s0; s < min(s0 + per, a.kv.n_seqs); ++s) {
+            SeqInfo v;
+            int t1;
+            chunk_of(a.kv, s, v.t0, t1);
+            v.n = t1 - v.t0;
+            v.len = live_len(a.kv, s);
+            v.lo = a.start ? max(a.start[s], 0) : 0;
+            info[s] = v;
+            const int ut = NT * a.tq, tiles = (v.n + ut - 1) / ut;
+            const int full = v.len > v.lo ? (v.len + BN - 1) / BN - v.lo / BN : 0;
+            sum += (long long)tiles * a.kv.n_kv_heads * (units ? 1 : full > 0 ? full : 1);
+            pre[s + 1] = sum;
+        }
+        long long inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long up = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += up;
+        }
+        if (lane == 31) wsum[warp] = inc;
+        __syncthreads();
+        long long before = inc - sum;
+        for (int w = 0; w < warp; ++w) before += wsum[w];
+        for (int s = s0; s < min(s0 + per, a.kv.n_seqs); ++s) pre[s + 1] += before;
+        if (tid == 0) pre[0] = 0;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_ptr;
+
+    TcWork<NT, BN> work;
+    work.info = info;
+    work.pre = pre;
+    work.n_seqs = a.kv.n_seqs;
+    work.heads = a.kv.n_kv_heads;
+    work.tq = a.tq;
+    work.causal = a.causal;
+    work.units = units ? 1 : 0;
+    const long long total = pre[a.kv.n_seqs];
+    // ranges: as many CTAs as get min_items each
+    long long n_ranges = (total + ta.min_items - 1) / ta.min_items;
+    if (n_ranges > gridDim.x) n_ranges = gridDim.x;
+    if (units) {
+        work.x = blockIdx.x;
+        work.step = gridDim.x;
+        work.end = total;
+    } else {
+        work.x = blockIdx.x < n_ranges ? total * blockIdx.x / n_ranges : 0;
+        work.end = blockIdx.x < n_ranges ? total * (blockIdx.x + 1) / n_ranges : 0;
+        work.step = 0;
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
+    }
+
+    if (warp < S::SM_WARPS) {
+        // ------------------------------------------------------------------ softmax: one thread per row
+        const int tile = warp >> 2, w4 = warp & 3;
+        const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
+        const uint32_t tm_o = tmem + lane_base + S::O_COL + tile * D;
+        const int row = w4 * 32 + lane;
+        const int G = a.group;
+        const float sc = a.scale_log2;
+        int steps = 0;     // softmax steps of this row tile so far
+        int kv_count = 0;  // slot tiles of the CTA so far
+        bool ok = true, recorded = false;
+        TcSeg g;
+        while (ok && work.next(g)) {
+            const int n = g.nb[tile];
+            const int nt = min(a.tq, g.n_tok - tile * a.tq);  // tokens of this row tile
+            const int rows = nt > 0 ? nt * G : 0;
+            const int t = row / G, head_g = row - t * G;
+            const int slot_first = g.slot0 + tile * a.tq;
+            const int last = row >= rows ? -1 : a.causal ? min(slot_first + t, g.len - 1) : g.len - 1;
+            const int min_last = a.causal ? min(slot_first, g.len - 1) : g.len - 1;
+            const bool active = w4 * 32 < rows;
+            float m_used = -INFINITY, l = 0.f;
+            for (int j = 0; j < n; ++j) {
+                const int buf = NT == 2 ? tile : (steps & 1);
+                const int sp = NT == 2 ? (steps & 1) : ((steps >> 1) & 1);
+                if (!(ok = warp_wait(s_full(buf), sp, abort_flag))) break;
+                tc_fence_after();
+                const int base_slot = (g.jb + j) * BN;
+                if (base_slot < g.lo || base_slot + BN > g.len) {
+                    // value rows of slots that are not live: cleared, by the first row tile that uses the slot tile
+                    if (tile == 0 || j >= g.nb[0]) {
+                        const int st = (kv_count + j) % NS;
+                        if (!(ok = warp_wait(v_full(st), ((kv_count + j) / NS) & 1, abort_flag))) break;
+                        const int slot = base_slot + row;
+                        if (row < BN && (slot < g.lo || slot >= g.len)) {
+                            const uint32_t at = ring + st * S::STAGE_BYTES + S::TILE_BYTES + row * 128;
+#pragma unroll
+                            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                                for (int c = 0; c < 8; ++c)
+                                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + h * BN * 128 + c * 16), "r"(0) : "memory");
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                }
+                if (active) {
+                    const uint32_t tm_s = tmem + lane_base + buf * S::S_COLS;
+                    uint32_t s[BN];
+#pragma unroll
+                    for (int c = 0; c < BN; c += 32) tc_ld32(tm_s + c, s + c);
+                    tc_wait_ld();
+                    if (base_slot < g.lo || base_slot + BN - 1 > min_last) {
+                        const int c_lo = g.lo - base_slot, c_hi = last - base_slot;
+#pragma unroll
+                        for (int c = 0; c < BN; ++c)
+                            if (c < c_lo || c > c_hi) s[c] = 0xff800000u;
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < BN; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
+                    const float m_new = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(fmaxf(mx[2], mx[3]), m_used));
+                    const bool grow = row < rows && m_new > m_used && (m_new - m_used) * sc > 8.f;
+                    if (j == 0) {
+                        m_used = m_new;
+                    } else if (__any_sync(0xffffffffu, grow)) {
+                        if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
+                        tc_fence_after();
+                        const float f = grow ? ex2_approx((m_used - m_new) * sc) : 1.f;
+                        l *= f;
+                        if (grow) m_used = m_new;
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            tc_ld32(tm_o + c, o);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tc_st32(tm_o + c, o);
+                        }
+                    }
+                    const float mref = m_used == -INFINITY ? 0.f : m_used * sc;
+                    const uint64_t sc2 = pack_f32x2(sc, sc), mr2 = pack_f32x2(-mref, -mref);
+                    uint64_t sum2[2] = {0, 0};
+#pragma unroll
+                    for (int c = 0; c < BN; c += 64) {
+                        uint32_t p[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            float x, y;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1])), sc2, mr2), x, y);
+                            x = ex2_approx(x);
+                            y = ex2_approx(y);
+                            sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(x, y));
+                            p[i] = pack_bf16(x, y);
+                        }
+                        tc_st32(tm_s + c / 2, p);
+                    }
+                    float s0, s1, s2, s3;
+                    unpack_f32x2(sum2[0], s0, s1);
+                    unpack_f32x2(sum2[1], s2, s3);
+                    l += (s0 + s1) + (s2 + s3);
+                    tc_wait_st();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full(buf));
+                ++steps;
+            }
+            if (!ok) break;
+            // the output rows, or this CTA's part of them
+            if (n > 0) {
+                // (a parity wait is safe only for the phase behind the last one known to be over.  The last logits show that the
+                // product two steps back is done, or with NT = 2 the one just before)
+                if (NT == 1 && n > 1 && !(ok = warp_wait(pv_done(tile), (steps - 2) & 1, abort_flag))) break;
+                if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
+                tc_fence_after();
+            }
+            const bool mine = row < rows;
+            const long long tok = g.tok0 + tile * a.tq + t;
+            const int slotp = blockIdx.x * 2 + (g.b0 > 0 ? 0 : 1);
+            if (active) {
+                const float inv = g.whole ? (l > 0.f ? 1.0f / l : l) : 1.f;  // nothing seen: 0; NaN stays NaN
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    if (n > 0) {
+                        tc_ld32(tm_o + c, o);
+                        tc_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0;
+                    }
+                    if (mine && g.whole) {
+                        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + tok * a.out.token_stride + (long long)(g.head * G + head_g) * a.out.head_stride + c;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint4 u;
+                            u.x = pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                            u.y = pack_bf16(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+                            u.z = pack_bf16(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+                            u.w = pack_bf16(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+                            *reinterpret_cast<uint4*>(dst + i) = u;
+                        }
+                    } else if (mine) {
+                        float* dst = a.part_o + ((size_t)slotp * ta.rows_cap + row) * D + c;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    }
+                    __syncwarp();  // (tcgen05.ld is a warp-wide instruction: all lanes together again)
+                }
+                if (mine && !g.whole) {
+                    float* ml = a.part_ml + ((size_t)slotp * ta.rows_cap + row) * 2;
+                    ml[0] = m_used;
+                    ml[1] = l;
+                }
+            }
+            if (!g.whole && g.b0 == 0) {
+                // the unit goes on in the next CTAs: up to the one that holds its last item
+                if (tid == 0) ta.records[blockIdx.x] = make_int4(g.tok0, rows, g.head, (int)((g.unit_end * n_ranges + total - 1) / total - 1));
+                recorded = true;
+            }
+            if (n > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(o_free(tile));
+            }
+            kv_count += g.nmax;
+        }
+        if (!units && !recorded && tid == 0) ta.records[blockIdx.x] = make_int4(0, 0, 0, 0);
+    } else if (warp == S::SM_WARPS) {
+        // ------------------------------------------------------------------ MMA: one thread
+        if (lane == 0) {
+            constexpr uint32_t id_s = tc_idesc(BN, false), id_o = tc_idesc(D, true);
+            int kv_count = 0, steps[2] = {0, 0}, segs[2] = {0, 0};
+            int s_steps = 0;  // NT = 1: logit tiles formed so far
+            bool ok = true;
+            auto form_logits = [&](int i, int buf, int kv) {  // S_buf = Q_i K^T
+                const int st = kv % NS;
+                const uint32_t qa = base + i * q_tile, ka = ring + st * S::STAGE_BYTES;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    tc_mma_ss(tmem + buf * S::S_COLS, tc_desc(qa + (k >> 2) * q_half + (k & 3) * 32, 16),
+                              tc_desc(ka + (k >> 2) * (BN * 128) + (k & 3) * 32, 16), id_s, k > 0);
+                tc_commit(s_full(buf));
+            };
+            auto add_values = [&](int i, int buf, int kv, bool acc) {  // O_i += P_buf V
+                const int st = kv % NS;
+                const uint32_t va = ring + st * S::STAGE_BYTES + S::TILE_BYTES;
+#pragma unroll
+                for (int k = 0; k < BN / 16; ++k)
+                    tc_mma_ts(tmem + S::O_COL + i * D, tmem + buf * S::S_COLS + k * 8, tc_desc(va + k * 2048, BN * 128), id_o, acc || k > 0);
+            };
+            TcSeg g;
+            while (ok && work.next(g)) {
+                for (int i = 0; ok && i < NT; ++i) {
+                    if (g.nb[i] == 0) continue;
+                    ok = wait_or_abort(q_full(i), segs[i] & 1, abort_flag);
+                }
+                // (steps[] counts the PV products of a row tile, segs[] its segments)
+                auto wait_k = [&](int j) { return wait_or_abort(k_full((kv_count + j) % NS), ((kv_count + j) / NS) & 1, abort_flag); };
+                auto wait_v = [&](int j) { return wait_or_abort(v_full((kv_count + j) % NS), ((kv_count + j) / NS) & 1, abort_flag); };
+                if (ok && g.nmax > 0) {
+                    ok = wait_k(0);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+                        if (g.nb[i] > 0) {
+                            form_logits(i, NT == 2 ? i : (s_steps & 1), kv_count);
+                            ++s_steps;
+                            if (g.nb[i] == 1) tc_commit(q_empty(i));
+                        }
+                }
+                for (int j = 0; ok && j < g.nmax; ++j) {
+                    bool k_ready = false, v_ready = false;
+                    if (NT == 1 && j + 1 < g.nmax) {
+                        if (!(ok = wait_k(j + 1))) break;
+                        tc_fence_after();
+                        form_logits(0, s_steps & 1, kv_count + j + 1);
+                        ++s_steps;
+                        if (j + 1 == g.nb[0] - 1) tc_commit(q_empty(0));
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        if (!ok || j >= g.nb[i]) continue;
+                        if (!v_ready) {
+                            if (!(ok = wait_v(j))) break;
+                            v_ready = true;
+                        }
+                        if (j == 0 && segs[i] > 0 && !(ok = wait_or_abort(o_free(i), (segs[i] - 1) & 1, abort_flag))) break;
+                        const int buf = NT == 2 ? i : (steps[0] & 1);
+                        const int pp = NT == 2 ? (steps[i] & 1) : ((steps[0] >> 1) & 1);
+                        if (!(ok = wait_or_abort(p_full(buf), pp, abort_flag))) break;
+                        tc_fence_after();
+                        add_values(i, buf, kv_count + j, j > 0);
+                        tc_commit(pv_done(i));
+                        ++steps[i];
+                        if (NT == 2 && j + 1 < g.nb[i]) {
+                            if (!k_ready) {
+                                if (!(ok = wait_k(j + 1))) break;
+                                tc_fence_after();
+                                k_ready = true;
+                            }
+                            form_logits(i, i, kv_count + j + 1);
+                            if (j + 1 == g.nb[i] - 1) tc_commit(q_empty(i));
+                        }
+                    }
+                    if (ok) tc_commit(kv_empty((kv_count + j) % NS));
+                }
+                for (int i = 0; i < NT; ++i)
+                    if (g.nb[i] > 0) ++segs[i];
+                kv_count += g.nmax;
+            }
+            // everything issued has completed before TMEM is given back
+            tc_commit(bar_drain);
+            mbar_wait_bounded(bar_drain, 0);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ producer
+        int kv_count = 0, issued = 0, segs[2] = {0, 0};
+        bool ok = true;
+        const int nbox = BN / ta.box_rows;  // boxes of 64 columns of a tile (at most 8)
+        const int is_v = lane >> 4, idx = lane & 15, box = idx & (nbox - 1), half = idx / nbox;
+        const bool boxes = half < HALVES;
+        const int row_mask = a.kv.page_tokens - 1;
+        const long long cap = (long long)a.kv.table_cols << a.kv.page_shift;
+        TcSeg g;
+        while (ok && work.next(g)) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                if (g.nb[i] == 0) continue;
+                if (segs[i] > 0 && !(ok = warp_wait(q_empty(i), (segs[i] - 1) & 1, abort_flag))) break;
+                ++segs[i];
+                if (lane == 0) {
+                    mbar_expect_tx(q_full(i), (uint32_t)(a.tq * a.group * 128 * HALVES));
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) tma_load_4d(base + i * q_tile + h * q_half, &maps.q, h * 64, 0, g.head, g.tok0 + i * a.tq, q_full(i));
+                }
+            }
+            if (!ok) break;
+            const int* table = a.kv.table + g.seq * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
+            const int head_c = a.kv.head_stride > 0 ? g.head : 0;
+            auto page_of = [&](int j) {
+                const int slot = (g.jb + j) * BN + box * ta.box_rows;
+                int page = a.kv.n_pages;  // outside the tensor: the box is filled with zeros
+                if (boxes && j < g.nmax && slot < g.len && slot + ta.box_rows > g.lo && slot < cap) {
+                    const int p = table[slot >> a.kv.page_shift];
+                    if (p >= 0 && p < a.kv.n_pages) page = p;
+                    else paged_report(a.kv, kStPage);
+                }
+                return page;
+            };
+            int page = page_of(0);
+            for (int j = 0; j < g.nmax; ++j) {
+                const int st = (kv_count + j) % NS, turn = (kv_count + j) / NS;
+                const int page_next = page_of(j + 1);
+                if (turn > 0 && !(ok = warp_wait(kv_empty(st), (turn - 1) & 1, abort_flag))) break;
+                if (lane == 0) {
+                    mbar_expect_tx(k_full(st), S::TILE_BYTES);
+                    mbar_expect_tx(v_full(st), S::TILE_BYTES);
+                }
+                __syncwarp();
+                if (boxes) {
+                    const uint32_t dst = ring + st * S::STAGE_BYTES + is_v * S::TILE_BYTES + half * (BN * 128) + box * ta.box_rows * 128;
+                    tma_load_4d(dst, is_v ? &maps.v : &maps.k, half * 64, ((g.jb + j) * BN + box * ta.box_rows) & row_mask, head_c, page,
+                                is_v ? v_full(st) : k_full(st));
+                }
+                ++issued;
+                page = page_next;
+            }
+            if (!ok) break;
+            kv_count += g.nmax;
+        }
+        if (!ok && lane == 0) {
+            // given up: the copies in flight land before the CTA's shared memory goes to somebody else
+            for (int i = 0; i < NT; ++i)
+                if (segs[i] > 0) mbar_wait_bounded(q_full(i), (segs[i] - 1) & 1);
+            for (int n = issued > NS ? issued - NS : 0; n < issued; ++n) {
+                mbar_wait_bounded(k_full(n % NS), (n / NS) & 1);
+                mbar_wait_bounded(v_full(n % NS), (n / NS) & 1);
+            }
+        }
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == S::SM_WARPS) tc_dealloc(tmem, S::TMEM_COLS);
+    if (tid == 0 && *abort_flag) paged_report(a.kv, kStWaitLimit);
+}
+
+// Adds up the parts of the units that range boundaries cut, in the order of the CTAs that left them.
+template <int D>
+__global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant__ TcArgs ta) {
+    grid_dep_wait();
+    const PagedAttnArgs& a = ta.a;
+    const int4 rec = ta.records[blockIdx.x];  // first token, rows, head, last CTA
+    const int c0 = blockIdx.x, c1 = min(rec.w, (int)gridDim.x - 1);
+    // four columns of a row per thread
+    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rec.y * (D / 4); i += gridDim.y * blockDim.x) {
+        const int row = i / (D / 4), e = (i - row * (D / 4)) * 4;
+        auto at = [&](int c) { return (size_t)(c * 2 + (c == c0 ? 1 : 0)) * ta.rows_cap + row; };
+        float M = -INFINITY;
+        for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.part_ml[at(c) * 2]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float L = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) {
+            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at(c) * 2);
+            const float4 p = *reinterpret_cast<const float4*>(a.part_o + at(c) * D + e);
+            const float f = ex2_approx((ml.x - ref) * a.scale_log2);
+            L = fmaf(ml.y, f, L);
+            o.x = fmaf(p.x, f, o.x);
+            o.y = fmaf(p.y, f, o.y);
+            o.z = fmaf(p.z, f, o.z);
+            o.w = fmaf(p.w, f, o.w);
+        }
+        const float inv = L > 0.f ? 1.0f / L : L;
+        const int t = row / a.group, h = rec.z * a.group + row - t * a.group;
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + (long long)(rec.x + t) * a.out.token_stride + (long long)h * a.out.head_stride + e;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    }
+}
+
+}  // namespace lar
