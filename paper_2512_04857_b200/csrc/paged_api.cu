@@ -26,13 +26,14 @@ bool rope_freqs(const lar_rope_t* r, int inverse, lar::RopeFreqs& f) {
     if (!(r->head_dim == 64 || r->head_dim == 128) || r->n_axes < 1 || r->n_axes > lar::kRopeMaxAxes) return false;
     if (!(r->theta > 0.0) || !isfinite(r->theta)) return false;
     const int half = r->head_dim / 2;
+    const double ln = log(r->theta);
     int first = 0;
     for (int a = 0; a < r->n_axes; ++a) {
         const int n = r->axis_pairs[a];
         if (n < 1 || n > half - first) return false;
         for (int i = 0; i < n; ++i) {
             const double e = r->restart ? (double)i / n : (double)(first + i) / half;
-            const double t = pow(r->theta, -e) / 6.283185307179586476925286766559;
+            const double t = exp(-e * ln) * 0.15915494309189533576888;  // 1 / (2 pi)
             f.turns[first + i] = inverse ? -t : t;
             f.axis[first + i] = (unsigned char)a;
         }

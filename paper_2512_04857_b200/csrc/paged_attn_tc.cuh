@@ -10,9 +10,9 @@
 // Roles (coupled by mbarriers only, every wait bounded):
 //   NT * 4 softmax warps  one thread per row: logits from TMEM, mask, running maximum and sum (fp32), P (bf16) back into
 //                         TMEM over the logits it came from; output rows at the end.
-//   one MMA warp          S = Q K^T (both from shared memory), O += P V (P from TMEM, V from shared memory with the slots
+//   NT MMA warps          S = Q K^T (both from shared memory), O += P V (P from TMEM, V from shared memory with the slots
 //                         as its K dimension).
-//   one producer warp     a ring of K/V stages: one TMA box per page (or part of one) and 64 columns, the lanes issuing them side by side.
+//   NT producer warps     a ring of K/V stages: one TMA box per page (or part of one) and 64 columns, the lanes issuing them side by side.
 // The output accumulator is rescaled only where a row's maximum has grown by more than 2^8 since its last rescaling (P then
 // reaches 2^8 at most, far inside the range of bf16 and fp32; the factor cancels in the final division), so the
 // accumulator hardly ever leaves TMEM.
@@ -32,6 +32,9 @@
 
 namespace lar {
 
+#ifndef LAR_SMR
+#define LAR_SMR 216
+#endif
 constexpr int kTcMaxSeqs = 1024;  // sequences of a call (their lengths are kept in shared memory)
 constexpr int kTcMaxStages = 4;
 
@@ -42,10 +45,19 @@ struct TcShape {
     static constexpr int TILE_BYTES = BN * D * 2;            // K or V tile
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
     static constexpr int SM_WARPS = NT * 4;
-    static constexpr int THREADS = SM_WARPS * 32 + 64;
-    static constexpr int S_COLS = BN, O_COL = 2 * BN;        // TMEM: two logit buffers, then NT accumulators of D columns
+    // NT = 2: three warpgroups, the third (two MMA warps, two producers) gives registers to the softmax warps: 2 * 224 + 56 =
+    // 3 * 168, what the block was launched with
+    static constexpr int THREADS = NT == 2 ? 384 : SM_WARPS * 32 + 64;
+    static constexpr int SM_REGS = LAR_SMR, OTHER_REGS = 504 - 2 * LAR_SMR;
+    static constexpr int P_PARTS = NT == 2 ? 2 : 1;          // P is handed over in parts of 64 slots: the product starts on the first
+    // TMEM columns.  NT = 2: one logit buffer for both row tiles (a softmax warp takes its logits into registers at once, so the buffer is
+    // free for the other row tile's), P of each row tile (64 columns), two accumulators.  NT = 1: two logit buffers that P overlays,
+    // one accumulator.
+    static constexpr int P_COL = NT == 2 ? BN : 0, P_COLS = BN / (NT == 2 ? 2 : 1), O_COL = 2 * BN;
     static constexpr int TMEM_COLS = NT == 2 ? 512 : 256;
     static_assert(O_COL + NT * D <= TMEM_COLS, "TMEM");
+    static __host__ __device__ constexpr int s_col(int buf) { return NT == 2 ? 0 : buf * BN; }
+    static __host__ __device__ constexpr int p_col(int buf) { return P_COL + buf * P_COLS; }
 };
 
 struct TcMaps {
@@ -81,16 +93,23 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+// D += A B over 16 elements of the contracted dimension.  a_lo, b_lo: low words of the descriptors, to which the immediate offsets are
+// added here, so that a loop keeps two registers and not one descriptor per step.
+template <uint32_t HIGH, uint32_t A_OFF, uint32_t B_OFF>
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool acc) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        "{\n .reg .pred p;\n .reg .b32 x, y;\n .reg .b64 a, b;\n setp.ne.u32 p, %4, 0;\n add.u32 x, %1, %5;\n add.u32 y, %2, %6;\n"
+        " mov.b64 a, {x, %7};\n mov.b64 b, {y, %7};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)acc), "n"(A_OFF), "n"(B_OFF), "r"(HIGH)
         : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+// the same with A in TMEM
+template <uint32_t HIGH, uint32_t A_OFF, uint32_t B_OFF>
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, bool acc) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        "{\n .reg .pred p;\n .reg .b32 x, y;\n .reg .b64 b;\n setp.ne.u32 p, %4, 0;\n add.u32 x, %1, %5;\n add.u32 y, %2, %6;\n"
+        " mov.b64 b, {y, %7};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, p;\n}\n" ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"((uint32_t)acc), "n"(A_OFF), "n"(B_OFF), "r"(HIGH)
         : "memory");
 }
 #define LAR_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
@@ -121,9 +140,23 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 
 // Shared-memory matrix descriptors, 128-byte swizzle.  K-major rows of 128 bytes (64 elements of the contracted dimension): groups of 8 rows
 // lie 1024 bytes apart.  Slots-as-K (V): 64 columns per 128-byte row, column blocks lead_bytes apart, groups of 8 slots 1024 apart.
-__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead_bytes) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lead_bytes >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+// low word: address / 16 | column-block distance / 16 << 16; high word: group distance / 16 | version 1 << 14 | 128-byte swizzle << 29
+// Position in the ring of stages: which stage, and the parity of this use of it.
+struct RingPos {
+    int st = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next(int n) {
+        if (++st == n) {
+            st = 0;
+            ph ^= 1;
+        }
+    }
+    __device__ __forceinline__ void skip(int k, int n) {
+        const int to = st + k, turns = to / n;
+        st = to - turns * n;
+        ph ^= turns & 1;
+    }
+};
 // fp32 accumulator, bf16 operands, M = 128
 __host__ __device__ constexpr uint32_t tc_idesc(int n, bool b_transposed) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((b_transposed ? 1u : 0u) << 16) | ((uint32_t)(n / 8) << 17) | ((128u / 16u) << 24);
@@ -141,7 +174,7 @@ struct TcSmem {
     using S = TcShape<D, NT>;
     static __host__ __device__ int q_bytes(int rows_cap) { return NT * S::HALVES * ((rows_cap * 128 + 1023) / 1024 * 1024); }
     // the MMA reads 128 rows whatever rows_cap is: behind the last Q tile there is always a K/V stage or more
-    static __host__ __device__ int tail(int n_seqs) { return 32 * 8 + 16 + n_seqs * 16 + (n_seqs + 1) * 8 + 64 * 8; }
+    static __host__ __device__ int tail(int n_seqs) { return 36 * 8 + n_seqs * 16 + (n_seqs + 1) * 8 + 64 * 8; }
     static __host__ __device__ int bytes(int rows_cap, int stages, int n_seqs) {
         return 1024 + q_bytes(rows_cap) + stages * S::STAGE_BYTES + tail(n_seqs);
     }
@@ -154,8 +187,7 @@ struct TcSeg {
     int slot0;                   // slot of its first token
     int lo, len;                 // live slots of the sequence
     int jb;                      // first slot tile
-    int nb[2];                   // slot tiles of each row tile
-    int nmax;
+    int nb;                      // slot tiles
     int whole;                   // nothing of the unit lies in other CTAs
     int b0;                      // tiles of the unit before this step's
     long long unit_end;          // end of the unit in the list of items
@@ -202,16 +234,11 @@ struct TcWork {
         g.lo = s.lo;
         g.len = s.len;
         g.jb = first + (units ? 0 : g.b0);
-        g.nmax = 0;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const int nt = min(tq, g.n_tok - i * tq);
-            const int hi = nt <= 0 ? 0 : causal ? min(s.len, g.slot0 + i * tq + nt) : s.len;
-            int n = hi > s.lo ? (hi + BN - 1) / BN - g.jb : 0;
-            if (!units && n > take) n = take;
-            g.nb[i] = n > 0 ? n : 0;
-            g.nmax = max(g.nmax, g.nb[i]);
-        }
+        // (NT = 2: both row tiles take the same steps, the first one's last may be masked whole)
+        const int hi = causal ? min(s.len, g.slot0 + g.n_tok) : s.len;
+        int n = hi > s.lo ? (hi + BN - 1) / BN - g.jb : 0;
+        if (!units && n > take) n = take;
+        g.nb = max(n, 0);
         return true;
     }
 };
@@ -231,6 +258,31 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+
+#ifndef LAR_POLY_OF_
+#endif
+#ifndef LAR_POLY_OF
+#define LAR_POLY_OF 99
+#endif
+// 2^x of two numbers on the multiply-add pipe: x = n + f, |f| <= 1/2; 2^f by the cubic of least largest relative error
+// (2^-13.7, found with the Remez exchange; a rounding to bf16 follows), n added to its exponent.  x <= 127; below -126 the result
+// is some number under 2^-125.
+__device__ __forceinline__ void ex2_poly_x2(uint64_t v, float& a, float& b) {
+    float x, y;
+    unpack_f32x2(v, x, y);
+    v = pack_f32x2(fmaxf(x, -126.f), fmaxf(y, -126.f));
+    const uint64_t magic = pack_f32x2(12582912.f, 12582912.f), neg = pack_f32x2(-12582912.f, -12582912.f);
+    const uint64_t t = add_f32x2(v, magic);  // n in the low bits
+    const uint64_t f = fma_f32x2(add_f32x2(t, neg), pack_f32x2(-1.f, -1.f), v);
+    uint64_t p = fma_f32x2(f, pack_f32x2(0.05517167f, 0.05517167f), pack_f32x2(0.24261113f, 0.24261113f));
+    p = fma_f32x2(p, f, pack_f32x2(0.69326097f, 0.69326097f));
+    p = fma_f32x2(p, f, pack_f32x2(0.99992806f, 0.99992806f));
+    float n0, n1;
+    unpack_f32x2(t, n0, n1);
+    unpack_f32x2(p, a, b);
+    a = __int_as_float(__float_as_int(a) + (__float_as_int(n0) << 23));
+    b = __int_as_float(__float_as_int(b) + (__float_as_int(n1) << 23));
 }
 
 // The whole warp waits, and gives up together (what follows are warp-wide instructions).
@@ -262,10 +314,13 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
     const uint32_t bar_drain = bar0 + 8u * 12;
     auto k_full = [&](int st) { return bar0 + 8u * (13 + st); };
     auto v_full = [&](int st) { return bar0 + 8u * (17 + st); };
-    auto kv_empty = [&](int st) { return bar0 + 8u * (21 + st); };
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 32);
-    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(bars + 32) + 1;
-    SeqInfo* info = reinterpret_cast<SeqInfo*>(bars + 34);
+    auto k_empty = [&](int st) { return bar0 + 8u * (21 + st); };
+    auto v_empty = [&](int st) { return bar0 + 8u * (25 + st); };  // NT = 1: not used, k_empty is both
+    auto p2_full = [&](int i) { return bar0 + 8u * (29 + i); };
+    auto s_free = [&](int i) { return bar0 + 8u * (31 + i); };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 34);
+    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(bars + 34) + 1;
+    SeqInfo* info = reinterpret_cast<SeqInfo*>(bars + 36);
     long long* pre = reinterpret_cast<long long*>(info + a.kv.n_seqs);
     long long* wsum = pre + a.kv.n_seqs + 1;
 
@@ -279,14 +334,17 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 mbar_init(q_empty(i), 1);
                 mbar_init(s_full(i), 1);
                 mbar_init(p_full(i), 4);
+                mbar_init(p2_full(i), 4);
                 mbar_init(pv_done(i), 1);
                 mbar_init(o_free(i), 4);
+                mbar_init(s_free(i), 4);
             }
-            mbar_init(bar_drain, 1);
+            mbar_init(bar_drain, NT);
             for (int i = 0; i < kTcMaxStages; ++i) {
                 mbar_init(k_full(i), 1);
                 mbar_init(v_full(i), 1);
-                mbar_init(kv_empty(i), 1);
+                mbar_init(k_empty(i), NT);  // (each row tile's MMA warp)
+                mbar_init(v_empty(i), NT);
             }
             mbar_fence_init_smem();
             *abort_flag = 0;
@@ -352,6 +410,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
     }
 
+    if (NT == 2) {
+        if (warp < S::SM_WARPS)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SM_REGS));
+        else
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
+    }
     if (warp < S::SM_WARPS) {
         // ------------------------------------------------------------------ softmax: one thread per row
         const int tile = warp >> 2, w4 = warp & 3;
@@ -361,11 +425,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         const int G = a.group;
         const float sc = a.scale_log2;
         int steps = 0;     // softmax steps of this row tile so far
-        int kv_count = 0;  // slot tiles of the CTA so far
+        RingPos ring0;     // stage of the segment's first slot tile
         bool ok = true, recorded = false;
         TcSeg g;
         while (ok && work.next(g)) {
-            const int n = g.nb[tile];
+            const int n = g.nb;
             const int nt = min(a.tq, g.n_tok - tile * a.tq);  // tokens of this row tile
             const int rows = nt > 0 ? nt * G : 0;
             const int t = row / G, head_g = row - t * G;
@@ -381,45 +445,58 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 tc_fence_after();
                 const int base_slot = (g.jb + j) * BN;
                 if (base_slot < g.lo || base_slot + BN > g.len) {
-                    // value rows of slots that are not live: cleared, by the first row tile that uses the slot tile
-                    if (tile == 0 || j >= g.nb[0]) {
-                        const int st = (kv_count + j) % NS;
-                        if (!(ok = warp_wait(v_full(st), ((kv_count + j) / NS) & 1, abort_flag))) break;
-                        const int slot = base_slot + row;
-                        if (row < BN && (slot < g.lo || slot >= g.len)) {
-                            const uint32_t at = ring + st * S::STAGE_BYTES + S::TILE_BYTES + row * 128;
+                    // value rows of slots that are not live: cleared (by each row tile's warps for their own product: both write zeros)
+                    RingPos rp = ring0;
+                    rp.skip(j, NS);
+                    if (!(ok = warp_wait(v_full(rp.st), rp.ph, abort_flag))) break;
+                    const int slot = base_slot + row;
+                    if (row < BN && (slot < g.lo || slot >= g.len)) {
+                        const uint32_t at = ring + rp.st * S::STAGE_BYTES + S::TILE_BYTES + row * 128;
 #pragma unroll
-                            for (int h = 0; h < HALVES; ++h)
+                        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                                for (int c = 0; c < 8; ++c)
-                                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + h * BN * 128 + c * 16), "r"(0) : "memory");
-                        }
-                        fence_proxy_async_smem();
-                        __syncwarp();
+                            for (int c = 0; c < 8; ++c)
+                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + h * BN * 128 + c * 16), "r"(0) : "memory");
                     }
+                    fence_proxy_async_smem();
+                    __syncwarp();
                 }
+                uint32_t s[BN];
                 if (active) {
-                    const uint32_t tm_s = tmem + lane_base + buf * S::S_COLS;
-                    uint32_t s[BN];
+                    const uint32_t tm_s = tmem + lane_base + S::s_col(buf);
 #pragma unroll
                     for (int c = 0; c < BN; c += 32) tc_ld32(tm_s + c, s + c);
                     tc_wait_ld();
+                }
+                if (NT == 2) {  // the logit buffer goes to the other row tile
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_free(tile));
+                }
+                // NT = 2: before P is stored, P of the step before has been read (NT = 1 has two buffers); before the accumulator is
+                // rescaled, the products of all steps before are in it
+                bool product_over = j == 0;
+                if (active) {
+                    const uint32_t tm_p = tmem + lane_base + S::p_col(buf);
                     if (base_slot < g.lo || base_slot + BN - 1 > min_last) {
                         const int c_lo = g.lo - base_slot, c_hi = last - base_slot;
 #pragma unroll
                         for (int c = 0; c < BN; ++c)
                             if (c < c_lo || c > c_hi) s[c] = 0xff800000u;
                     }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float mx[4] = {m_used, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < BN; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
-                    const float m_new = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(fmaxf(mx[2], mx[3]), m_used));
+                    for (int c = 0; c < BN; c += 8)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mx[i] = fmaxf(fmaxf(mx[i], __uint_as_float(s[c + i])), __uint_as_float(s[c + 4 + i]));
+                    const float m_new = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     const bool grow = row < rows && m_new > m_used && (m_new - m_used) * sc > 8.f;
                     if (j == 0) {
                         m_used = m_new;
                     } else if (__any_sync(0xffffffffu, grow)) {
                         if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
                         tc_fence_after();
+                        product_over = true;
                         const float f = grow ? ex2_approx((m_used - m_new) * sc) : 1.f;
                         l *= f;
                         if (grow) m_used = m_new;
@@ -442,23 +519,43 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             float x, y;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1])), sc2, mr2), x, y);
-                            x = ex2_approx(x);
-                            y = ex2_approx(y);
+                            const uint64_t v = fma_f32x2(pack_f32x2(__uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1])), sc2, mr2);
+                            if (NT == 2 && i % LAR_POLY_OF == LAR_POLY_OF - 1) {
+                                ex2_poly_x2(v, x, y);
+                            } else {
+                                unpack_f32x2(v, x, y);
+                                x = ex2_approx(x);
+                                y = ex2_approx(y);
+                            }
                             sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(x, y));
                             p[i] = pack_bf16(x, y);
                         }
-                        tc_st32(tm_s + c / 2, p);
+                        if (NT == 2 && c == 0 && !product_over) {
+                            if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
+                            tc_fence_after();
+                        }
+                        tc_st32(tm_p + c / 2, p);
+                        if (c + 64 < BN) {  // the first part goes ahead
+                            tc_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(p_full(buf));
+                        }
                     }
+                    if (!ok) break;
                     float s0, s1, s2, s3;
                     unpack_f32x2(sum2[0], s0, s1);
                     unpack_f32x2(sum2[1], s2, s3);
                     l += (s0 + s1) + (s2 + s3);
                     tc_wait_st();
+                } else if (NT == 2) {
+                    // (a warp without rows keeps step with the products too: it waits for every phase in turn)
+                    if (!product_over && !(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
+                    if (lane == 0) mbar_arrive(p_full(buf));
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(buf));
+                if (lane == 0) mbar_arrive(S::P_PARTS == 2 ? p2_full(buf) : p_full(buf));
                 ++steps;
             }
             if (!ok) break;
@@ -519,112 +616,113 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 __syncwarp();
                 if (lane == 0) mbar_arrive(o_free(tile));
             }
-            kv_count += g.nmax;
+            ring0.skip(n, NS);
         }
         if (!units && !recorded && tid == 0) ta.records[blockIdx.x] = make_int4(0, 0, 0, 0);
-    } else if (warp == S::SM_WARPS) {
-        // ------------------------------------------------------------------ MMA: one thread
+    } else if (warp == S::SM_WARPS || (NT == 2 && warp == S::SM_WARPS + 3)) {
+        // ------------------------------------------------------------------ MMA: one thread per row tile, so that a wait for one row tile
+        // holds up nothing of the other
         if (lane == 0) {
             constexpr uint32_t id_s = tc_idesc(BN, false), id_o = tc_idesc(D, true);
-            int kv_count = 0, steps[2] = {0, 0}, segs[2] = {0, 0};
-            int s_steps = 0;  // NT = 1: logit tiles formed so far
+            constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+            constexpr uint32_t kStage = S::STAGE_BYTES >> 4;
+            const int tile = warp == S::SM_WARPS ? 0 : 1;
+            const uint32_t qa = ((base + tile * q_tile) >> 4) | (1u << 16), qb = qa + (q_half >> 4), k_lo = (ring >> 4) | (1u << 16);
+            const uint32_t v_lo = ((ring + S::TILE_BYTES) >> 4) | ((uint32_t)(BN * 128 >> 4) << 16);
+            const uint32_t tm_o = tmem + S::O_COL + tile * D;
+            RingPos kp, vp;     // next K tile to form logits with, V tile of the current step
+            int formed = 0;     // logit tiles formed so far
+            int steps = 0;      // products issued so far
+            int segs = 0;       // segments with steps so far
             bool ok = true;
-            auto form_logits = [&](int i, int buf, int kv) {  // S_buf = Q_i K^T
-                const int st = kv % NS;
-                const uint32_t qa = base + i * q_tile, ka = ring + st * S::STAGE_BYTES;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    tc_mma_ss(tmem + buf * S::S_COLS, tc_desc(qa + (k >> 2) * q_half + (k & 3) * 32, 16),
-                              tc_desc(ka + (k >> 2) * (BN * 128) + (k & 3) * 32, 16), id_s, k > 0);
+            // S = Q K^T with the K tile at kp.  NT = 2: the two row tiles use the logit buffer in turn, and each use waits until
+            // the one before it has been taken into registers.
+            auto form_logits = [&](bool last) {
+                if (!wait_or_abort(k_full(kp.st), kp.ph, abort_flag)) return false;
+                if (NT == 2 && tile + formed > 0 && !wait_or_abort(s_free(1 - tile), (formed - 1 + tile) & 1, abort_flag)) return false;
+                tc_fence_after();
+                const int buf = NT == 2 ? tile : formed & 1;
+                const uint32_t ka = k_lo + kp.st * kStage, d = tmem + S::s_col(buf);
+                tc_mma_ss<kDescHigh, 0, 0>(d, qa, ka, id_s, false);
+                tc_mma_ss<kDescHigh, 2, 2>(d, qa, ka, id_s, true);
+                tc_mma_ss<kDescHigh, 4, 4>(d, qa, ka, id_s, true);
+                tc_mma_ss<kDescHigh, 6, 6>(d, qa, ka, id_s, true);
+                if (HALVES == 2) {
+                    const uint32_t kb = ka + BN * 128 / 16;
+                    tc_mma_ss<kDescHigh, 0, 0>(d, qb, kb, id_s, true);
+                    tc_mma_ss<kDescHigh, 2, 2>(d, qb, kb, id_s, true);
+                    tc_mma_ss<kDescHigh, 4, 4>(d, qb, kb, id_s, true);
+                    tc_mma_ss<kDescHigh, 6, 6>(d, qb, kb, id_s, true);
+                }
                 tc_commit(s_full(buf));
+                if (NT == 2) tc_commit(k_empty(kp.st));
+                if (last) tc_commit(q_empty(tile));
+                kp.next(NS);
+                ++formed;
+                return true;
             };
-            auto add_values = [&](int i, int buf, int kv, bool acc) {  // O_i += P_buf V
-                const int st = kv % NS;
-                const uint32_t va = ring + st * S::STAGE_BYTES + S::TILE_BYTES;
-#pragma unroll
-                for (int k = 0; k < BN / 16; ++k)
-                    tc_mma_ts(tmem + S::O_COL + i * D, tmem + buf * S::S_COLS + k * 8, tc_desc(va + k * 2048, BN * 128), id_o, acc || k > 0);
+            auto add_values = [&](int buf, bool acc, int k0) {  // O += P V, slots k0 * 16 .. + 63 of the V tile at vp
+                const uint32_t va = v_lo + vp.st * kStage + k0 * 128, pa = tmem + S::p_col(buf) + k0 * 8;
+                tc_mma_ts<kDescHigh, 0, 0>(tm_o, pa, va, id_o, acc);
+                tc_mma_ts<kDescHigh, 8, 128>(tm_o, pa, va, id_o, true);
+                tc_mma_ts<kDescHigh, 16, 256>(tm_o, pa, va, id_o, true);
+                tc_mma_ts<kDescHigh, 24, 384>(tm_o, pa, va, id_o, true);
             };
             TcSeg g;
             while (ok && work.next(g)) {
-                for (int i = 0; ok && i < NT; ++i) {
-                    if (g.nb[i] == 0) continue;
-                    ok = wait_or_abort(q_full(i), segs[i] & 1, abort_flag);
-                }
-                // (steps[] counts the PV products of a row tile, segs[] its segments)
-                auto wait_k = [&](int j) { return wait_or_abort(k_full((kv_count + j) % NS), ((kv_count + j) / NS) & 1, abort_flag); };
-                auto wait_v = [&](int j) { return wait_or_abort(v_full((kv_count + j) % NS), ((kv_count + j) / NS) & 1, abort_flag); };
-                if (ok && g.nmax > 0) {
-                    ok = wait_k(0);
-                    if (!ok) break;
+                const int n = g.nb;
+                if (n == 0) continue;
+                if (!(ok = wait_or_abort(q_full(tile), segs & 1, abort_flag))) break;
+                ok = form_logits(n == 1);
+                for (int j = 0; ok && j < n; ++j) {
+                    // the logits of the next step come first, so that they are there when the softmax of this step is done
+                    if (j + 1 < n) {
+                        ok = form_logits(j + 2 == n);
+                        if (!ok) break;
+                    }
+                    const int buf = NT == 2 ? tile : steps & 1, pp = NT == 2 ? steps & 1 : (steps >> 1) & 1;
+                    if (!(ok = wait_or_abort(v_full(vp.st), vp.ph, abort_flag))) break;
+                    if (j == 0 && segs > 0 && !(ok = wait_or_abort(o_free(tile), (segs - 1) & 1, abort_flag))) break;
+                    if (!(ok = wait_or_abort(p_full(buf), pp, abort_flag))) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < NT; ++i)
-                        if (g.nb[i] > 0) {
-                            form_logits(i, NT == 2 ? i : (s_steps & 1), kv_count);
-                            ++s_steps;
-                            if (g.nb[i] == 1) tc_commit(q_empty(i));
-                        }
-                }
-                for (int j = 0; ok && j < g.nmax; ++j) {
-                    bool k_ready = false, v_ready = false;
-                    if (NT == 1 && j + 1 < g.nmax) {
-                        if (!(ok = wait_k(j + 1))) break;
+                    add_values(buf, j > 0, 0);
+                    if (S::P_PARTS == 2) {
+                        if (!(ok = wait_or_abort(p2_full(buf), pp, abort_flag))) break;
                         tc_fence_after();
-                        form_logits(0, s_steps & 1, kv_count + j + 1);
-                        ++s_steps;
-                        if (j + 1 == g.nb[0] - 1) tc_commit(q_empty(0));
+                        add_values(buf, true, 4);
                     }
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        if (!ok || j >= g.nb[i]) continue;
-                        if (!v_ready) {
-                            if (!(ok = wait_v(j))) break;
-                            v_ready = true;
-                        }
-                        if (j == 0 && segs[i] > 0 && !(ok = wait_or_abort(o_free(i), (segs[i] - 1) & 1, abort_flag))) break;
-                        const int buf = NT == 2 ? i : (steps[0] & 1);
-                        const int pp = NT == 2 ? (steps[i] & 1) : ((steps[0] >> 1) & 1);
-                        if (!(ok = wait_or_abort(p_full(buf), pp, abort_flag))) break;
-                        tc_fence_after();
-                        add_values(i, buf, kv_count + j, j > 0);
-                        tc_commit(pv_done(i));
-                        ++steps[i];
-                        if (NT == 2 && j + 1 < g.nb[i]) {
-                            if (!k_ready) {
-                                if (!(ok = wait_k(j + 1))) break;
-                                tc_fence_after();
-                                k_ready = true;
-                            }
-                            form_logits(i, i, kv_count + j + 1);
-                            if (j + 1 == g.nb[i] - 1) tc_commit(q_empty(i));
-                        }
-                    }
-                    if (ok) tc_commit(kv_empty((kv_count + j) % NS));
+                    tc_commit(pv_done(tile));
+                    tc_commit(NT == 2 ? v_empty(vp.st) : k_empty(vp.st));
+                    ++steps;
+                    vp.next(NS);
                 }
-                for (int i = 0; i < NT; ++i)
-                    if (g.nb[i] > 0) ++segs[i];
-                kv_count += g.nmax;
+                ++segs;
             }
             // everything issued has completed before TMEM is given back
             tc_commit(bar_drain);
             mbar_wait_bounded(bar_drain, 0);
         }
         __syncwarp();
-    } else {
-        // ------------------------------------------------------------------ producer
-        int kv_count = 0, issued = 0, segs[2] = {0, 0};
+    } else if (warp <= S::SM_WARPS + NT) {
+        // ------------------------------------------------------------------ producers: NT = 2 one warp for Q and K and one for V (a K tile's
+        // place is free as soon as its logits are formed, a V tile's a step later); NT = 1 one warp, lanes 0-15 K and 16-31 V
+        const bool k_warp = warp == S::SM_WARPS + 1;
+        int issued = 0, segs[2] = {0, 0};
+        RingPos kv;
         bool ok = true;
         const int nbox = BN / ta.box_rows;  // boxes of 64 columns of a tile (at most 8)
-        const int is_v = lane >> 4, idx = lane & 15, box = idx & (nbox - 1), half = idx / nbox;
+        const int is_v = NT == 2 ? !k_warp : lane >> 4, idx = NT == 2 ? lane : lane & 15, box = idx & (nbox - 1), half = idx / nbox;
         const bool boxes = half < HALVES;
-        const int row_mask = a.kv.page_tokens - 1;
-        const long long cap = (long long)a.kv.table_cols << a.kv.page_shift;
+        const int box_slot = box * ta.box_rows, row_mask = a.kv.page_tokens - 1;
+        const int cap = a.kv.table_cols << a.kv.page_shift;
+        const uint32_t dst0 = ring + is_v * S::TILE_BYTES + half * (BN * 128) + box_slot * 128;
+        const CUtensorMap* map = is_v ? &maps.v : &maps.k;
+        const uint32_t full0 = is_v ? v_full(0) : k_full(0), empty0 = NT == 2 && is_v ? v_empty(0) : k_empty(0);
         TcSeg g;
         while (ok && work.next(g)) {
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                if (g.nb[i] == 0) continue;
+                if (g.nb == 0 || !k_warp) continue;
                 if (segs[i] > 0 && !(ok = warp_wait(q_empty(i), (segs[i] - 1) & 1, abort_flag))) break;
                 ++segs[i];
                 if (lane == 0) {
@@ -636,45 +734,35 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             if (!ok) break;
             const int* table = a.kv.table + g.seq * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
             const int head_c = a.kv.head_stride > 0 ? g.head : 0;
-            auto page_of = [&](int j) {
-                const int slot = (g.jb + j) * BN + box * ta.box_rows;
+            const int nmax = g.nb, len = min(g.len, cap), lo = g.lo;
+            int slot = g.jb * BN + box_slot;  // first slot of this lane's box
+            auto page_of = [&](int slot) {
                 int page = a.kv.n_pages;  // outside the tensor: the box is filled with zeros
-                if (boxes && j < g.nmax && slot < g.len && slot + ta.box_rows > g.lo && slot < cap) {
+                if (boxes && slot < len && slot + ta.box_rows > lo) {
                     const int p = table[slot >> a.kv.page_shift];
                     if (p >= 0 && p < a.kv.n_pages) page = p;
                     else paged_report(a.kv, kStPage);
                 }
                 return page;
             };
-            int page = page_of(0);
-            for (int j = 0; j < g.nmax; ++j) {
-                const int st = (kv_count + j) % NS, turn = (kv_count + j) / NS;
-                const int page_next = page_of(j + 1);
-                if (turn > 0 && !(ok = warp_wait(kv_empty(st), (turn - 1) & 1, abort_flag))) break;
-                if (lane == 0) {
-                    mbar_expect_tx(k_full(st), S::TILE_BYTES);
-                    mbar_expect_tx(v_full(st), S::TILE_BYTES);
-                }
+            int page = nmax > 0 ? page_of(slot) : 0;
+            for (int j = 0; j < nmax; ++j) {
+                const int page_next = j + 1 < nmax ? page_of(slot + BN) : 0;
+                if (issued >= NS && !(ok = warp_wait(empty0 + 8u * kv.st, kv.ph ^ 1, abort_flag))) break;
+                if (NT == 2 ? lane == 0 : idx == 0) mbar_expect_tx(full0 + 8u * kv.st, S::TILE_BYTES);
                 __syncwarp();
-                if (boxes) {
-                    const uint32_t dst = ring + st * S::STAGE_BYTES + is_v * S::TILE_BYTES + half * (BN * 128) + box * ta.box_rows * 128;
-                    tma_load_4d(dst, is_v ? &maps.v : &maps.k, half * 64, ((g.jb + j) * BN + box * ta.box_rows) & row_mask, head_c, page,
-                                is_v ? v_full(st) : k_full(st));
-                }
+                if (boxes) tma_load_4d(dst0 + kv.st * S::STAGE_BYTES, map, half * 64, slot & row_mask, head_c, page, full0 + 8u * kv.st);
                 ++issued;
+                kv.next(NS);
+                slot += BN;
                 page = page_next;
             }
-            if (!ok) break;
-            kv_count += g.nmax;
         }
-        if (!ok && lane == 0) {
+        if (!ok && (NT == 2 ? lane == 0 : idx == 0)) {
             // given up: the copies in flight land before the CTA's shared memory goes to somebody else
             for (int i = 0; i < NT; ++i)
                 if (segs[i] > 0) mbar_wait_bounded(q_full(i), (segs[i] - 1) & 1);
-            for (int n = issued > NS ? issued - NS : 0; n < issued; ++n) {
-                mbar_wait_bounded(k_full(n % NS), (n / NS) & 1);
-                mbar_wait_bounded(v_full(n % NS), (n / NS) & 1);
-            }
+            for (int n = issued > NS ? issued - NS : 0; n < issued; ++n) mbar_wait_bounded(full0 + 8u * (n % NS), (n / NS) & 1);
         }
         __syncwarp();
     }

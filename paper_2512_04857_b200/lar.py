@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -70,6 +71,7 @@ class LarError(RuntimeError):
 
 
 _LIB = None
+_torch = None   # the module, once a call that takes tensors has been made
 
 
 def lib():
@@ -273,22 +275,26 @@ def make_rope(head_dim, axis_pairs, *, theta=10000.0, interleaved=False, restart
                       int(restart), float(theta))
 
 
-def _rows(x):
-    """lar_rows_t of a [tokens, heads, head_dim] tensor (any token and head stride), or None."""
-    if x is None:
-        return None
-    t, h, e = x.stride()
-    if e != 1 and x.shape[2] > 1:
-        raise LarError(LAR_ERR_INVALID_ARG, "rows: the innermost dimension is not dense")
-    return lar_rows_t(x.data_ptr(), t, h)
+# One step of a model makes a call per layer and operator, so the marshalling below is written for host time: the row
+# views are packed as bytes, and the calls go through function objects of their own that take them as plain pointers.
+_pack_rows = struct.Struct("=Qqq").pack      # lar_rows_t
+_FAST = None
 
 
-def _dtype_of(x) -> int:
-    import torch
-    try:
-        return {torch.bfloat16: LAR_BF16, torch.float32: LAR_FP32}[x.dtype]
-    except KeyError:
-        raise LarError(LAR_ERR_INVALID_ARG, f"dtype {x.dtype}") from None
+def _fast():
+    """The entry points of this section with every pointer argument untyped."""
+    global _FAST, _torch
+    if _FAST is None:
+        import torch
+        typed, raw = lib(), C.CDLL(LIB_PATH)
+        names = ("lar_rope_table", "lar_rope_rotate", "lar_paged_append_rope", "lar_paged_attn", "lar_append_kv_rope")
+        plain = {C.POINTER(t): C.c_void_p for t in (lar_rope_t, lar_rows_t, lar_paged_kv_t)}
+        for name in names:
+            fn = getattr(raw, name)
+            fn.restype, fn.argtypes = C.c_int, [plain.get(a, a) for a in getattr(typed, name).argtypes]
+        _torch = torch
+        _FAST = raw
+    return _FAST
 
 
 def _require(ok, what):
@@ -296,74 +302,83 @@ def _require(ok, what):
         raise LarError(LAR_ERR_INVALID_ARG, what)
 
 
-def _same(x, like, what):
-    _require(x is None or (x.dtype == like.dtype and x.device == like.device), f"{what}: dtype or device")
+def _rows(x, n, heads, d, dtype, dev, what):
+    """lar_rows_t of a [n, heads, d] tensor with any token and head stride."""
+    st = x.stride()
+    if x.shape != (n, heads, d) or st[2] != 1 or x.dtype != dtype or x.get_device() != dev:
+        raise LarError(LAR_ERR_INVALID_ARG, f"{what}: a {dtype} tensor [{n}, {heads}, {d}] with a dense innermost dimension "
+                       f"on the same GPU is expected, not {x.dtype} {list(x.shape)} on {x.device}")
+    return _pack_rows(x.data_ptr(), st[0], st[1])
 
 
-def _ints(x, shape, like, what):
-    """A dense int32 tensor of this shape on the device of `like` (or None)."""
+def _dtype_of(x) -> int:
+    import torch
+    if x.dtype == torch.bfloat16:
+        return LAR_BF16
+    if x.dtype == torch.float32:
+        return LAR_FP32
+    raise LarError(LAR_ERR_INVALID_ARG, f"dtype {x.dtype}")
+
+
+def _ints(x, n, dev, what):
+    """Address of a dense int32 tensor [n] on the GPU dev, or None."""
     if x is None:
-        return
-    import torch
-    _require(x.dtype == torch.int32 and x.device == like.device and tuple(x.shape) == shape and x.is_contiguous(),
-             f"{what}: an int32 tensor {shape} on {like.device} is expected")
+        return None
+    if x.dtype != _torch.int32 or x.get_device() != dev or x.shape != (n,) or (n > 1 and x.stride(0) != 1):
+        raise LarError(LAR_ERR_INVALID_ARG, f"{what}: a dense int32 tensor [{n}] on the same GPU is expected")
+    return x.data_ptr()
 
 
-def _pos_stride(pos, rope, n_tokens, like, what):
-    """pos: int32 [axes, tokens] (or [tokens] for one axis), dense along the tokens; returns the axes' stride."""
-    import torch
-    _require(pos.dtype == torch.int32 and pos.device == like.device, f"{what}: pos is an int32 tensor on {like.device}")
-    shape = tuple(pos.shape) if pos.dim() == 2 else (1,) + tuple(pos.shape)
-    _require(shape == (rope.n_axes, n_tokens) and (n_tokens <= 1 or pos.stride(-1) == 1), f"{what}: pos is [axes, tokens]")
-    return pos.stride(0) if pos.dim() == 2 and rope.n_axes > 1 else n_tokens
+def _positions(pos, rope, n, dev, what):
+    """Address and axis stride of pos, int32 [axes, tokens] (or [tokens] for one axis), dense along the tokens."""
+    axes = rope.n_axes
+    if pos.dtype != _torch.int32 or pos.get_device() != dev or pos.shape != ((axes, n) if pos.dim() == 2 else (n,)) or \
+            (pos.dim() == 1 and axes != 1) or (n > 1 and pos.stride(-1) != 1):
+        raise LarError(LAR_ERR_INVALID_ARG, f"{what}: pos is an int32 tensor [{axes}, {n}] on the same GPU")
+    return pos.data_ptr(), pos.stride(0) if axes > 1 else n
 
 
-class _on:
-    """Makes a tensor's device current for a call and gives the handle of torch's current stream on it."""
-    __slots__ = ("dev", "guard")
+def _device_of(x) -> int:
+    dev = x.get_device()
+    if dev < 0:
+        raise LarError(LAR_ERR_INVALID_ARG, f"a CUDA tensor is expected, not one on {x.device}")
+    return dev
 
-    def __init__(self, x):
-        self.dev = x.device
-        self.guard = None
 
-    def __enter__(self):
-        import torch
-        if self.dev.type != "cuda":
-            raise LarError(LAR_ERR_INVALID_ARG, f"a CUDA tensor is expected, not one on {self.dev}")
-        if torch.cuda.current_device() != self.dev.index:
-            self.guard = torch.cuda.device(self.dev)
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.dev).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(name, dev, *args):
+    """The entry point on the GPU dev and torch's current stream there."""
+    fn = getattr(_FAST, name)
+    if _torch._C._cuda_getDevice() == dev:
+        status = fn(*args, _torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with _torch.cuda.device(dev):
+            status = fn(*args, _torch._C._cuda_getCurrentRawStream(dev))
+    if status != LAR_OK:
+        raise LarError(status, name)
 
 
 def rope_table(rope, pos, cos_sin):
     """cos_sin [rows, head_dim] fp32: what decode_step_rope takes, for the positions pos [axes, rows]."""
-    import torch
-    rows = cos_sin.shape[0]
-    _require(cos_sin.dtype == torch.float32 and tuple(cos_sin.shape) == (rows, rope.head_dim) and cos_sin.is_contiguous(),
+    _fast()
+    dev, rows = _device_of(cos_sin), cos_sin.shape[0]
+    _require(cos_sin.dtype == _torch.float32 and cos_sin.shape == (rows, rope.head_dim) and cos_sin.is_contiguous(),
              "rope_table: cos_sin")
-    stride = _pos_stride(pos, rope, rows, cos_sin, "rope_table")
-    with _on(cos_sin) as stream:
-        _chk(lib().lar_rope_table(rope, pos.data_ptr(), stride, rows, cos_sin.data_ptr(), stream), "lar_rope_table")
+    at, stride = _positions(pos, rope, rows, dev, "rope_table")
+    _call("lar_rope_table", dev, C.addressof(rope), at, stride, rows, cos_sin.data_ptr())
 
 
 def rope_rotate(rope, pos, q, q_out, k=None, k_out=None, inverse=False):
     """Rotates q (and k), [tokens, heads, head_dim] with any token and head strides, by pos [axes, tokens]."""
+    _fast()
+    code, dt, dev = _dtype_of(q), q.dtype, _device_of(q)
     n, hq, d = q.shape
-    dt = _dtype_of(q)
-    for x in (q_out, k, k_out):
-        _same(x, q, "rope_rotate")
-    _require(q_out.shape == q.shape and d == rope.head_dim and (k is None) == (k_out is None), "rope_rotate: shapes")
-    if k is not None:
-        _require(k.shape == k_out.shape and k.shape[0] == n and k.shape[2] == d, "rope_rotate: shapes")
-    stride = _pos_stride(pos, rope, n, q, "rope_rotate")
-    with _on(q) as stream:
-        _chk(lib().lar_rope_rotate(rope, dt, pos.data_ptr(), stride, n, _rows(q), _rows(q_out), hq, _rows(k), _rows(k_out),
-                                   0 if k is None else k.shape[1], int(inverse), stream), "lar_rope_rotate")
+    _require(d == rope.head_dim and (k is None) == (k_out is None), "rope_rotate: shapes")
+    at, stride = _positions(pos, rope, n, dev, "rope_rotate")
+    hk = 0 if k is None else k.shape[1]
+    _call("lar_rope_rotate", dev, C.addressof(rope), code, at, stride, n, _rows(q, n, hq, d, dt, dev, "rope_rotate: q"),
+          _rows(q_out, n, hq, d, dt, dev, "rope_rotate: q_out"), hq,
+          None if k is None else _rows(k, n, hk, d, dt, dev, "rope_rotate: k"),
+          None if k is None else _rows(k_out, n, hk, d, dt, dev, "rope_rotate: k_out"), hk, int(inverse))
 
 
 class PagedKV:
@@ -374,14 +389,14 @@ class PagedKV:
     page_table      int32 [seqs, columns], or [seqs, kv_heads, columns] where every head has pages of its own (the pools
                     then have one head)
     lens            int32 [seqs]: live entries, the tokens of the current chunks included
+    status          int32 [1] (or None): takes the status bits of pages and slots outside the cache
     """
 
     def __init__(self, k_pool, v_pool, page_table, lens, n_kv_heads, status=None):
         import torch
         per_head = page_table.dim() == 3
-        _same(v_pool, k_pool, "PagedKV")
         _require(k_pool.dim() == 4 and k_pool.shape == v_pool.shape and k_pool.stride() == v_pool.stride() and
-                 k_pool.stride(3) == 1, "PagedKV: pools")
+                 k_pool.stride(3) == 1 and k_pool.dtype == v_pool.dtype and k_pool.device == v_pool.device, "PagedKV: pools")
         pages, page_tokens, heads, d = k_pool.shape
         _require(heads == (1 if per_head else n_kv_heads), "PagedKV: heads of the pools")
         _require(page_table.dtype == torch.int32 and page_table.device == k_pool.device and page_table.dim() in (2, 3) and
@@ -391,66 +406,58 @@ class PagedKV:
         _require(status is None or (status.dtype in (torch.int32, torch.uint32) and status.device == k_pool.device and
                                     status.numel() == 1), "PagedKV: status")
         self._keep = (k_pool, v_pool, page_table, lens, status)
-        self.k_pool = k_pool
-        self.n_seqs, self.n_kv_heads, self.head_dim = seqs, n_kv_heads, d
-        self.desc = lar_paged_kv_t(
+        self._set(lar_paged_kv_t(
             C.sizeof(lar_paged_kv_t), _dtype_of(k_pool), seqs, n_kv_heads, d, page_tokens, pages, page_table.shape[-1],
             k_pool.stride(0), k_pool.stride(1), 0 if per_head else k_pool.stride(2), k_pool.data_ptr(), v_pool.data_ptr(),
             page_table.data_ptr(), page_table.stride(0), page_table.stride(1) if per_head else 0, lens.data_ptr(),
-            lens.stride(0), _ptr(status))
+            lens.stride(0), _ptr(status)), k_pool.dtype, k_pool.device)
+
+    def _set(self, desc, dtype, device):
+        self.desc, self._at, self.dtype, self.device = desc, C.addressof(desc), dtype, device
+        self.n_seqs, self.n_kv_heads, self.head_dim = desc.n_seqs, desc.n_kv_heads, desc.head_dim
 
     @classmethod
     def of_cache(cls, cache: "Cache", layer: int) -> "PagedKV":
         """A layer of the library's own cache (its slab must outlive the object)."""
-        self = cls.__new__(cls)
-        self.desc = lar_paged_kv_t()
-        _chk(lib().lar_cache_paged_view(cache.handle, layer, self.desc), "lar_cache_paged_view")
         import torch
-        dt = torch.bfloat16 if cache.cfg.dtype == LAR_BF16 else torch.float32
+        self, desc = cls.__new__(cls), lar_paged_kv_t()
+        _chk(lib().lar_cache_paged_view(cache.handle, layer, desc), "lar_cache_paged_view")
         self._keep = (cache,)
-        self.k_pool = torch.empty(0, dtype=dt, device=cache.slab.device)   # dtype and device of the rows
-        self.n_seqs, self.n_kv_heads, self.head_dim = cache.cfg.batch, cache.cfg.n_kv_heads, cache.cfg.head_dim
+        self._set(desc, torch.bfloat16 if cache.cfg.dtype == LAR_BF16 else torch.float32, cache.slab.device)
         return self
-
-    def _check_rows(self, what, *xs):
-        for x, heads, n in xs:
-            if x is not None:
-                _same(x, self.k_pool, what)
-                _require(tuple(x.shape) == (n, heads, self.head_dim), f"{what}: shapes")
 
     def append_rope(self, k, v, cu_tokens=None, rope=None, pos=None, q=None, q_out=None):
         """Stores the chunks' keys (rotated by rope at pos [axes, tokens]) and values; q is rotated into q_out."""
-        n = k.shape[0]
+        _fast()
+        n, hkv, d, dt, dev = k.shape[0], self.n_kv_heads, self.head_dim, self.dtype, _device_of(k)
+        _require((rope is None) == (pos is None) and (q is None) == (q_out is None) and dev == self.device.index, "append_rope")
+        at, stride = (None, 0) if pos is None else _positions(pos, rope, n, dev, "append_rope")
         hq = 0 if q is None else q.shape[1]
-        self._check_rows("append_rope", (k, self.n_kv_heads, n), (v, self.n_kv_heads, n), (q, hq, n), (q_out, hq, n))
-        _require((rope is None) == (pos is None) and (q is None) == (q_out is None), "append_rope")
-        _ints(cu_tokens, (self.n_seqs + 1,), k, "append_rope: cu_tokens")
-        stride = 0 if pos is None else _pos_stride(pos, rope, n, k, "append_rope")
-        with _on(k) as stream:
-            _chk(lib().lar_paged_append_rope(self.desc, rope, _ptr(pos), stride, _rows(k), _rows(v), _rows(q), _rows(q_out),
-                                             hq, n, _ptr(cu_tokens), stream), "lar_paged_append_rope")
+        _call("lar_paged_append_rope", dev, self._at, None if rope is None else C.addressof(rope), at, stride,
+              _rows(k, n, hkv, d, dt, dev, "append_rope: k"), _rows(v, n, hkv, d, dt, dev, "append_rope: v"),
+              None if q is None else _rows(q, n, hq, d, dt, dev, "append_rope: q"),
+              None if q is None else _rows(q_out, n, hq, d, dt, dev, "append_rope: q_out"), hq, n,
+              _ints(cu_tokens, self.n_seqs + 1, dev, "append_rope: cu_tokens"))
 
     def attn_workspace(self, n_q_heads, n_tokens, max_chunk=0, max_len=0):
         """A workspace tensor for attn calls of these sizes (None where none is used)."""
         import torch
         n = lib().lar_paged_attn_workspace_bytes(self.desc, n_q_heads, n_tokens, max_chunk, max_len)
-        return torch.empty(n, dtype=torch.uint8, device=self.k_pool.device) if n else None
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
 
     def attn(self, q, out, cu_tokens=None, causal=True, kv_start=None, softmax_scale=0.0, max_chunk=0, max_len=0,
              workspace=None):
         """Attention of the chunks' queries [tokens, heads, head_dim] over the cache; see lar_paged_attn."""
-        n, hq = q.shape[0], q.shape[1]
-        self._check_rows("attn", (q, hq, n), (out, hq, n))
-        _ints(cu_tokens, (self.n_seqs + 1,), q, "attn: cu_tokens")
-        _ints(kv_start, (self.n_seqs,), q, "attn: kv_start")
-        ws = 0
+        _fast()
+        n, hq, d, dt, dev = q.shape[0], q.shape[1], self.head_dim, self.dtype, _device_of(q)
+        _require(dev == self.device.index, "attn: the cache lies on another GPU")
+        ws_at, ws = None, 0
         if workspace is not None:
-            _require(workspace.device == q.device and workspace.is_contiguous(), "attn: workspace")
-            ws = workspace.numel() * workspace.element_size()
-        with _on(q) as stream:
-            _chk(lib().lar_paged_attn(self.desc, _rows(q), _rows(out), hq, n, _ptr(cu_tokens), _ptr(kv_start), int(causal),
-                                      float(softmax_scale), max_chunk, max_len, _ptr(workspace), ws, stream),
-                 "lar_paged_attn")
+            _require(workspace.get_device() == dev and workspace.is_contiguous(), "attn: workspace")
+            ws_at, ws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _call("lar_paged_attn", dev, self._at, _rows(q, n, hq, d, dt, dev, "attn: q"), _rows(out, n, hq, d, dt, dev, "attn: out"),
+              hq, n, _ints(cu_tokens, self.n_seqs + 1, dev, "attn: cu_tokens"), _ints(kv_start, self.n_seqs, dev, "attn: kv_start"),
+              int(causal), softmax_scale, max_chunk, max_len, ws_at, ws)
 
 
 class Cache:
@@ -497,16 +504,16 @@ class Cache:
 
     def append_kv_rope(self, layer, k, v, n_tokens, rope=None, pos=None, q=None, q_out=None):
         """The prefill with rotated keys: k, v, q are [batch * n_tokens, heads, head_dim], sequence by sequence."""
-        n, hq = self.cfg.batch * n_tokens, self.cfg.n_q_heads
-        for x, heads in ((k, self.cfg.n_kv_heads), (v, self.cfg.n_kv_heads), (q, hq), (q_out, hq)):
-            if x is not None:
-                _require(tuple(x.shape) == (n, heads, self.cfg.head_dim) and _dtype_of(x) == self.cfg.dtype and
-                         x.device == k.device, "append_kv_rope: shapes")
-        _require((rope is None) == (pos is None) and (q is None) == (q_out is None), "append_kv_rope")
-        stride = 0 if pos is None else _pos_stride(pos, rope, n, k, "append_kv_rope")
-        with _on(k) as stream:
-            _chk(lib().lar_append_kv_rope(self.handle, layer, rope, _ptr(pos), stride, _rows(k), _rows(v), _rows(q),
-                                          _rows(q_out), n_tokens, stream), "lar_append_kv_rope")
+        _fast()
+        n, hq, hkv, d, dt, dev = (self.cfg.batch * n_tokens, self.cfg.n_q_heads, self.cfg.n_kv_heads, self.cfg.head_dim,
+                                  k.dtype, _device_of(k))
+        _require((rope is None) == (pos is None) and (q is None) == (q_out is None) and _dtype_of(k) == self.cfg.dtype and
+                 dev == self.slab.get_device(), "append_kv_rope")
+        at, stride = (None, 0) if pos is None else _positions(pos, rope, n, dev, "append_kv_rope")
+        _call("lar_append_kv_rope", dev, self.handle, layer, None if rope is None else C.addressof(rope), at, stride,
+              _rows(k, n, hkv, d, dt, dev, "append_kv_rope: k"), _rows(v, n, hkv, d, dt, dev, "append_kv_rope: v"),
+              None if q is None else _rows(q, n, hq, d, dt, dev, "append_kv_rope: q"),
+              None if q is None else _rows(q_out, n, hq, d, dt, dev, "append_kv_rope: q_out"), n_tokens)
 
     def paged_view(self, layer) -> "PagedKV":
         """The layer as a PagedKV: attention of a chunk (the prefix) over it."""
