@@ -171,8 +171,10 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
             p.smem = tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs);
         }
         p.grid = per_sm * kSms;
-        p.splits = split && p.nt == 1 ? 2 : 1;
-        if (p.splits > 1) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
+        // Units may be cut, except where there are so many or so short ones that whole units fill the CTAs evenly enough.
+        const int64_t units = (n_tokens / (p.tq * p.nt) + with_tokens) * k.n_kv_heads;
+        p.splits = split && (p.nt == 1 || (units < 16 * p.grid && len >= 2048)) ? 2 : 1;
+        if (p.splits > 1) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         return p;
     }
     p.bm = chunk * group <= 16 ? 16 : 64;
@@ -262,11 +264,11 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     t.rows_cap = p.rows_cap;
     t.box_rows = k.page_tokens < S::BN ? k.page_tokens : S::BN;
     t.split = p.splits > 1;
-    t.min_items = 4;
+    t.min_items = 6;
     if (t.split) {  // records, then (m, l), then O of every CTA's two parts
         t.records = reinterpret_cast<int4*>(a.part_o);
         t.a.part_ml = reinterpret_cast<float*>(t.records + p.grid);
-        t.a.part_o = t.a.part_ml + (size_t)p.grid * 2 * p.rows_cap * 2;
+        t.a.part_o = t.a.part_ml + (size_t)p.grid * 2 * NT * p.rows_cap * 2;
     }
     lar_status_t st = make_maps(k, a, t.box_rows, m);
     if (st != LAR_OK) return st;
@@ -277,7 +279,7 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     if (t.split) {
         cudaLaunchConfig_t lc;
         memset(&lc, 0, sizeof(lc));
-        lc.gridDim = dim3((unsigned)p.grid, (unsigned)((p.rows_cap * (D / 4) + 511) / 512), 1);
+        lc.gridDim = dim3((unsigned)p.grid, (unsigned)((NT * p.rows_cap * (D / 4) + 511) / 512), 1);
         lc.blockDim = dim3(128, 1, 1);
         lc.stream = s;
         cudaLaunchAttribute at;
@@ -285,7 +287,7 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
         at.val.programmaticStreamSerializationAllowed = 1;
         lc.attrs = &at;
         lc.numAttrs = 1;
-        LAR_CUDA(cudaLaunchKernelEx(&lc, lar::join_ranges_kernel<D>, (const lar::TcArgs)t));
+        LAR_CUDA(cudaLaunchKernelEx(&lc, lar::join_ranges_kernel<D, NT>, (const lar::TcArgs)t));
     }
     return LAR_OK;
 }
@@ -400,6 +402,11 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     const AttnPlan p = attn_plan(*kv, group, n_tokens, max_chunk, max_len, workspace != nullptr);
     if (workspace && !aligned(workspace, 16)) return LAR_ERR_INVALID_ARG;
     if (p.bytes > workspace_bytes) return LAR_ERR_NOMEM;
+    if (kv->dtype == LAR_BF16) {  // the kernel counts units and slot tiles in 31 bits
+        const int64_t units = (n_tokens / p.tq + (n_tokens < kv->n_seqs ? n_tokens : kv->n_seqs)) * kv->n_kv_heads;
+        const int64_t tiles = ((int64_t)kv->table_cols * kv->page_tokens + 63) / 64 + 4;
+        if (units > (1ll << 30) / tiles) return LAR_ERR_CAPACITY;
+    }
     a.start = kv_start;
     a.group = group;
     a.causal = causal != 0;

@@ -20,10 +20,10 @@
 // Slots outside [start, len) of a tile hold memory that may be anything: keys are masked by selection, and the value rows
 // are cleared in shared memory before the product (0 * NaN would reach the output).
 //
-// Work is dealt in one of two ways.  NT = 2: units (sequence, KV head, row tiles) round-robin, the longest tiles of a sequence
-// first, heads outermost, so that the CTAs of a moment share K/V in L2.  NT = 1: all units' slot tiles form one list that
-// is cut into equal ranges, one per CTA; a unit cut by a range boundary leaves (O, m, l) per CTA in the workspace and
-// join_ranges_kernel adds them up in the order of the CTAs.
+// Work.  A unit is one (sequence, KV head, NT row tiles).  NT = 2: whole units round-robin, as many full rounds as there are, heads
+// outermost (the CTAs of a moment share K/V in L2) and the longest tiles of a sequence first.  What is left of them, and with NT = 1 all
+// units, is one list of slot tiles that is cut into equal ranges, one per CTA; a unit cut by a range boundary leaves (O, m, l) per
+// CTA in the workspace and join_ranges_kernel adds them up in the order of the CTAs.  Without a workspace every unit stays whole.
 #pragma once
 #include <cuda.h>
 
@@ -70,9 +70,9 @@ struct TcArgs {
     int stages;
     int rows_cap;      // rows of a row tile in shared memory: tq * group rounded up to 8
     int box_rows;      // slots of one K/V box
-    int split;         // NT = 1: ranges may cut units
-    int min_items;     // NT = 1: slot tiles a CTA gets at least
-    int4* records;     // NT = 1, split: per CTA the unit that begins there and goes on in the next CTAs
+    int split;         // ranges may cut units
+    int min_items;     // slot tiles that a range has at least
+    int4* records;     // split: per CTA the unit that begins in its range and goes on in the next CTAs
 };
 
 // per sequence, in shared memory
@@ -174,7 +174,7 @@ struct TcSmem {
     using S = TcShape<D, NT>;
     static __host__ __device__ int q_bytes(int rows_cap) { return NT * S::HALVES * ((rows_cap * 128 + 1023) / 1024 * 1024); }
     // the MMA reads 128 rows whatever rows_cap is: behind the last Q tile there is always a K/V stage or more
-    static __host__ __device__ int tail(int n_seqs) { return 36 * 8 + n_seqs * 16 + (n_seqs + 1) * 8 + 64 * 8; }
+    static __host__ __device__ int tail(int n_seqs) { return 36 * 8 + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
     static __host__ __device__ int bytes(int rows_cap, int stages, int n_seqs) {
         return 1024 + q_bytes(rows_cap) + stages * S::STAGE_BYTES + tail(n_seqs);
     }
@@ -190,56 +190,70 @@ struct TcSeg {
     int nb;                      // slot tiles
     int whole;                   // nothing of the unit lies in other CTAs
     int b0;                      // tiles of the unit before this step's
-    long long unit_end;          // end of the unit in the list of items
+    int unit_end;                // end of the unit in the list of slot tiles
 };
 
-template <int NT, int BN>
+// A CTA's work: first whole units, every step-th one, then an equal range of the slot tiles of the units that are left.
+template <int NT, int BN, int D>
 struct TcWork {
+    static constexpr int kUnitCost = NT == 1 && D == 64 ? 3 : 2;
     const SeqInfo* info;
-    const long long* pre;  // items before each sequence
-    int n_seqs, heads, tq, causal, units;  // units: an item is a whole unit (else a slot tile)
-    long long x, end, step;
+    const int* pre;    // units before each sequence
+    const int* items;  // slot tiles before each sequence, of the units from first_cut on
+    int n_seqs, tq, causal;
+    int x, end, step;  // whole units
+    int y, y_end;      // range of slot tiles
+    int first_cut;     // the first unit that may be cut
+
+    // Items of a unit in the list that is cut into ranges: its slot tiles, and kUnitCost more for taking up and finishing a
+    // unit (queries, last product, output rows: measured 2.3 us against 0.75 us for a tile with D = 64).
+    static __device__ __forceinline__ int tiles_of_unit(const SeqInfo& s) { return s.len > s.lo ? (s.len + BN - 1) / BN - s.lo / BN : 0; }
+    static __device__ __forceinline__ int items_of_unit(const SeqInfo& s) { return tiles_of_unit(s) + kUnitCost; }
 
     __device__ __forceinline__ bool next(TcSeg& g) {
-        if (x >= end) return false;
-        int a = 0, b = n_seqs;  // pre[a] <= x < pre[b]
-        while (b - a > 1) {
-            const int m = (a + b) >> 1;
-            if (pre[m] <= x) a = m; else b = m;
-        }
-        const SeqInfo s = info[a];
-        const int ut = NT * tq, tiles = (s.n + ut - 1) / ut;
-        const int first = s.lo / BN, full = s.len > s.lo ? (s.len + BN - 1) / BN - first : 0;
-        const int w = units ? 1 : full > 0 ? full : 1;
-        const long long r = x - pre[a];
-        const long long unit = r / w;
-        g.b0 = (int)(r - unit * w);
-        g.head = (int)(unit / tiles);
-        int tile = (int)(unit - (long long)g.head * tiles);
-        if (units) tile = tiles - 1 - tile;  // the tiles that see most first
-        int take = w - g.b0;
-        if ((long long)take > end - x) take = (int)(end - x);
-        if (units) {
-            x += step;
+        for (;;) {
+            const bool cut = x >= end;
+            if (cut && y >= y_end) return false;
+            const int at = cut ? y : x;
+            const int* before = cut ? items : pre;
+            int a = 0, b = n_seqs;  // before[a] <= at < before[b]
+            while (b - a > 1) {
+                const int m = (a + b) >> 1;
+                if (before[m] <= at) a = m; else b = m;
+            }
+            const SeqInfo s = info[a];
+            const int ut = NT * tq, tiles = (s.n + ut - 1) / ut;
+            const int r = at - before[a];
+            int unit = r, take = 1 << 30;
+            g.b0 = 0;
             g.whole = 1;
-        } else {
-            g.whole = g.b0 == 0 && take == w;
-            g.unit_end = x + (w - g.b0);
-            x += take;
+            if (cut) {
+                const int full = tiles_of_unit(s), w = full + kUnitCost;
+                const int q = r / w;
+                unit = NT == 2 ? q + max(first_cut - pre[a], 0) : q;
+                g.b0 = r - q * w;
+                g.unit_end = y - g.b0 + max(full, 1);  // (the items behind the slot tiles belong to the range with the last tile)
+                take = min(w - g.b0, y_end - y);
+                y += take;
+                if (g.b0 > 0 && g.b0 >= full) continue;
+                g.whole = g.b0 == 0 && take >= full;
+            } else {
+                x += step;
+            }
+            g.head = unit / tiles;
+            const int tile = tiles - 1 - (unit - g.head * tiles);  // the tiles that see most first
+            g.seq = a;
+            g.tok0 = s.t0 + tile * ut;
+            g.n_tok = min(ut, s.n - tile * ut);
+            g.slot0 = s.len - s.n + tile * ut;
+            g.lo = s.lo;
+            g.len = s.len;
+            g.jb = s.lo / BN + g.b0;
+            // (NT = 2: both row tiles take the same steps, the first one's last may be masked whole)
+            const int hi = causal ? min(s.len, g.slot0 + g.n_tok) : s.len;
+            g.nb = hi > s.lo ? max(min((hi + BN - 1) / BN - g.jb, take), 0) : 0;
+            return true;
         }
-        g.seq = a;
-        g.tok0 = s.t0 + tile * ut;
-        g.n_tok = min(ut, s.n - tile * ut);
-        g.slot0 = s.len - s.n + tile * ut;
-        g.lo = s.lo;
-        g.len = s.len;
-        g.jb = first + (units ? 0 : g.b0);
-        // (NT = 2: both row tiles take the same steps, the first one's last may be masked whole)
-        const int hi = causal ? min(s.len, g.slot0 + g.n_tok) : s.len;
-        int n = hi > s.lo ? (hi + BN - 1) / BN - g.jb : 0;
-        if (!units && n > take) n = take;
-        g.nb = max(n, 0);
-        return true;
     }
 };
 
@@ -294,6 +308,7 @@ template <int D, int NT>
 __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
     using S = TcShape<D, NT>;
     constexpr int BN = S::BN, HALVES = S::HALVES;
+    using Work = TcWork<NT, BN, D>;
     const PagedAttnArgs& a = ta.a;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -321,11 +336,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 34);
     uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(bars + 34) + 1;
     SeqInfo* info = reinterpret_cast<SeqInfo*>(bars + 36);
-    long long* pre = reinterpret_cast<long long*>(info + a.kv.n_seqs);
-    long long* wsum = pre + a.kv.n_seqs + 1;
+    int* pre = reinterpret_cast<int*>(info + a.kv.n_seqs);
+    int* items = pre + a.kv.n_seqs + 1;
+    int* wsum = items + a.kv.n_seqs + 1;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const bool units = NT == 2 || !ta.split;
 
     if (warp == S::SM_WARPS) {
         if (lane == 0) {
@@ -352,11 +367,29 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         __syncwarp();
         tc_alloc(smem_u32(tmem_ptr), S::TMEM_COLS);
     }
-    // items before each sequence: every thread takes a run of sequences
+    // units and slot tiles before each sequence: every thread takes a run of sequences.  (The host makes sure that the sums fit
+    // 31 bits.)
+    const int per = (a.kv.n_seqs + S::THREADS - 1) / S::THREADS, s0 = tid * per, s1 = min(s0 + per, a.kv.n_seqs);
+    auto scan = [&](int sum, int* out) {  // out[s + 1] holds the sums within this thread's run
+        int inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += up;
+        }
+        if (lane == 31) wsum[warp] = inc;
+        __syncthreads();
+        int before = inc - sum;
+        for (int w = 0; w < warp; ++w) before += wsum[w];
+        for (int s = s0; s < s1; ++s) out[s + 1] += before;
+        if (tid == 0) out[0] = 0;
+        __syncthreads();
+    };
+    if (ta.split) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
+    const bool by_tiles = NT == 1 && ta.split;  // every unit may be cut: its slot tiles are all that is counted
     {
-        const int per = (a.kv.n_seqs + S::THREADS - 1) / S::THREADS, s0 = tid * per;
-        long long sum = 0;
-        for (int s = s0; s < min(s0 + per, a.kv.n_seqs); ++s) {
+        int sum = 0;
+        for (int s = s0; s < s1; ++s) {
             SeqInfo v;
             int t1;
             chunk_of(a.kv, s, v.t0, t1);
@@ -364,51 +397,51 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             v.len = live_len(a.kv, s);
             v.lo = a.start ? max(a.start[s], 0) : 0;
             info[s] = v;
-            const int ut = NT * a.tq, tiles = (v.n + ut - 1) / ut;
-            const int full = v.len > v.lo ? (v.len + BN - 1) / BN - v.lo / BN : 0;
-            sum += (long long)tiles * a.kv.n_kv_heads * (units ? 1 : full > 0 ? full : 1);
-            pre[s + 1] = sum;
+            sum += (v.n + NT * a.tq - 1) / (NT * a.tq) * a.kv.n_kv_heads * (by_tiles ? Work::items_of_unit(v) : 1);
+            (by_tiles ? items : pre)[s + 1] = sum;
         }
-        long long inc = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long up = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += up;
+        scan(sum, by_tiles ? items : pre);
+    }
+    Work work;
+    work.info = info;
+    work.pre = pre;
+    work.items = items;
+    work.n_seqs = a.kv.n_seqs;
+    work.tq = a.tq;
+    work.causal = a.causal;
+    work.x = blockIdx.x;
+    work.step = gridDim.x;
+    work.end = by_tiles ? 0 : pre[a.kv.n_seqs];
+    work.y = work.y_end = 0;
+    work.first_cut = work.end;
+    int total = 0, n_ranges = 0;  // slot tiles that are dealt out in ranges, and the CTAs that get one
+    if (ta.split) {
+        if (NT == 2) {
+            const int first = work.end / gridDim.x * gridDim.x, left = work.end - first;
+            int sum = 0;
+            for (int s = s0; s < s1; ++s) {
+                const int n = pre[s + 1] - max(first, pre[s]);
+                if (n > 0) sum += n * Work::items_of_unit(info[s]);
+                items[s + 1] = sum;
+            }
+            scan(sum, items);
+            total = items[a.kv.n_seqs];
+            // a last round that fills most of the CTAs, or whose idle ones would wait for a few slot tiles only, stays whole
+            if ((long long)total * (gridDim.x - left) >= 8ll * left * gridDim.x) work.end = work.first_cut = first;
+            else total = 0;
+        } else {
+            total = items[a.kv.n_seqs];
         }
-        if (lane == 31) wsum[warp] = inc;
-        __syncthreads();
-        long long before = inc - sum;
-        for (int w = 0; w < warp; ++w) before += wsum[w];
-        for (int s = s0; s < min(s0 + per, a.kv.n_seqs); ++s) pre[s + 1] += before;
-        if (tid == 0) pre[0] = 0;
+        n_ranges = min((total + ta.min_items - 1) / ta.min_items, (int)gridDim.x);
+        if ((int)blockIdx.x < n_ranges) {
+            work.y = (int)((long long)total * blockIdx.x / n_ranges);
+            work.y_end = (int)((long long)total * (blockIdx.x + 1) / n_ranges);
+        }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_ptr;
-
-    TcWork<NT, BN> work;
-    work.info = info;
-    work.pre = pre;
-    work.n_seqs = a.kv.n_seqs;
-    work.heads = a.kv.n_kv_heads;
-    work.tq = a.tq;
-    work.causal = a.causal;
-    work.units = units ? 1 : 0;
-    const long long total = pre[a.kv.n_seqs];
-    // ranges: as many CTAs as get min_items each
-    long long n_ranges = (total + ta.min_items - 1) / ta.min_items;
-    if (n_ranges > gridDim.x) n_ranges = gridDim.x;
-    if (units) {
-        work.x = blockIdx.x;
-        work.step = gridDim.x;
-        work.end = total;
-    } else {
-        work.x = blockIdx.x < n_ranges ? total * blockIdx.x / n_ranges : 0;
-        work.end = blockIdx.x < n_ranges ? total * (blockIdx.x + 1) / n_ranges : 0;
-        work.step = 0;
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
-    }
 
     if (NT == 2) {
         if (warp < S::SM_WARPS)
@@ -427,6 +460,15 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         int steps = 0;     // softmax steps of this row tile so far
         RingPos ring0;     // stage of the segment's first slot tile
         bool ok = true, recorded = false;
+        // The product of a step is over.  A parity wait is safe only for the newest phase a barrier can be in, with the phase before it known
+        // to be over.  NT = 2: every step waits for the one before.  NT = 1 waits now and then, so each logit buffer has a
+        // barrier of its own: the logits of step s show that the product of s - 2 (same buffer) is over, and that of s + 1 needs P
+        // which has not been handed over yet.
+        auto product_wait = [&](int s) {
+            const bool done = NT == 2 ? warp_wait(pv_done(tile), s & 1, abort_flag) : warp_wait(pv_done(s & 1), (s >> 1) & 1, abort_flag);
+            tc_fence_after();
+            return done;
+        };
         TcSeg g;
         while (ok && work.next(g)) {
             const int n = g.nb;
@@ -494,13 +536,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                     if (j == 0) {
                         m_used = m_new;
                     } else if (__any_sync(0xffffffffu, grow)) {
-                        if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
-                        tc_fence_after();
+                        if (!(ok = product_wait(steps - 1))) break;
                         product_over = true;
                         const float f = grow ? ex2_approx((m_used - m_new) * sc) : 1.f;
                         l *= f;
                         if (grow) m_used = m_new;
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
                             uint32_t o[32];
                             tc_ld32(tm_o + c, o);
@@ -531,8 +572,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                             p[i] = pack_bf16(x, y);
                         }
                         if (NT == 2 && c == 0 && !product_over) {
-                            if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
-                            tc_fence_after();
+                            if (!(ok = product_wait(steps - 1))) break;
                         }
                         tc_st32(tm_p + c / 2, p);
                         if (c + 64 < BN) {  // the first part goes ahead
@@ -550,7 +590,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                     tc_wait_st();
                 } else if (NT == 2) {
                     // (a warp without rows keeps step with the products too: it waits for every phase in turn)
-                    if (!product_over && !(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
+                    if (!product_over && !(ok = product_wait(steps - 1))) break;
                     if (lane == 0) mbar_arrive(p_full(buf));
                 }
                 tc_fence_before();
@@ -560,19 +600,13 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             }
             if (!ok) break;
             // the output rows, or this CTA's part of them
-            if (n > 0) {
-                // (a parity wait is safe only for the phase behind the last one known to be over.  The last logits show that the
-                // product two steps back is done, or with NT = 2 the one just before)
-                if (NT == 1 && n > 1 && !(ok = warp_wait(pv_done(tile), (steps - 2) & 1, abort_flag))) break;
-                if (!(ok = warp_wait(pv_done(tile), (steps - 1) & 1, abort_flag))) break;
-                tc_fence_after();
-            }
+            if (n > 0 && !(ok = product_wait(steps - 1))) break;
             const bool mine = row < rows;
             const long long tok = g.tok0 + tile * a.tq + t;
             const int slotp = blockIdx.x * 2 + (g.b0 > 0 ? 0 : 1);
             if (active) {
                 const float inv = g.whole ? (l > 0.f ? 1.0f / l : l) : 1.f;  // nothing seen: 0; NaN stays NaN
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     if (n > 0) {
@@ -594,21 +628,21 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                             *reinterpret_cast<uint4*>(dst + i) = u;
                         }
                     } else if (mine) {
-                        float* dst = a.part_o + ((size_t)slotp * ta.rows_cap + row) * D + c;
+                        float* dst = a.part_o + (((size_t)slotp * NT + tile) * ta.rows_cap + row) * D + c;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                     }
                     __syncwarp();  // (tcgen05.ld is a warp-wide instruction: all lanes together again)
                 }
                 if (mine && !g.whole) {
-                    float* ml = a.part_ml + ((size_t)slotp * ta.rows_cap + row) * 2;
+                    float* ml = a.part_ml + (((size_t)slotp * NT + tile) * ta.rows_cap + row) * 2;
                     ml[0] = m_used;
                     ml[1] = l;
                 }
             }
             if (!g.whole && g.b0 == 0) {
                 // the unit goes on in the next CTAs: up to the one that holds its last item
-                if (tid == 0) ta.records[blockIdx.x] = make_int4(g.tok0, rows, g.head, (int)((g.unit_end * n_ranges + total - 1) / total - 1));
+                if (tid == 0) ta.records[blockIdx.x] = make_int4(g.tok0, g.n_tok, g.head, (int)(((long long)g.unit_end * n_ranges + total - 1) / total - 1));
                 recorded = true;
             }
             if (n > 0) {
@@ -618,7 +652,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             }
             ring0.skip(n, NS);
         }
-        if (!units && !recorded && tid == 0) ta.records[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (ta.split && !recorded && tid == 0) ta.records[blockIdx.x] = make_int4(0, 0, 0, 0);
     } else if (warp == S::SM_WARPS || (NT == 2 && warp == S::SM_WARPS + 3)) {
         // ------------------------------------------------------------------ MMA: one thread per row tile, so that a wait for one row tile
         // holds up nothing of the other
@@ -691,7 +725,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                         tc_fence_after();
                         add_values(buf, true, 4);
                     }
-                    tc_commit(pv_done(tile));
+                    tc_commit(pv_done(buf));
                     tc_commit(NT == 2 ? v_empty(vp.st) : k_empty(vp.st));
                     ++steps;
                     vp.next(NS);
@@ -774,17 +808,19 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
 }
 
 // Adds up the parts of the units that range boundaries cut, in the order of the CTAs that left them.
-template <int D>
+template <int D, int NT>
 __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant__ TcArgs ta) {
     grid_dep_wait();
     const PagedAttnArgs& a = ta.a;
-    const int4 rec = ta.records[blockIdx.x];  // first token, rows, head, last CTA
+    const int4 rec = ta.records[blockIdx.x];  // first token, tokens, head, last CTA
     const int c0 = blockIdx.x, c1 = min(rec.w, (int)gridDim.x - 1);
     // four columns of a row per thread
-    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rec.y * (D / 4); i += gridDim.y * blockDim.x) {
-        const int row = i / (D / 4), e = (i - row * (D / 4)) * 4;
-        auto at = [&](int c) { return (size_t)(c * 2 + (c == c0 ? 1 : 0)) * ta.rows_cap + row; };
+    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rec.y * a.group * (D / 4); i += gridDim.y * blockDim.x) {
+        const int unit_row = i / (D / 4), e = (i - unit_row * (D / 4)) * 4;  // (token, head of the group) of the unit
+        const int t = unit_row / a.group, tile = NT == 2 && t >= a.tq ? 1 : 0, row = unit_row - tile * a.tq * a.group;
+        auto at = [&](int c) { return ((size_t)(c * 2 + (c == c0 ? 1 : 0)) * NT + tile) * ta.rows_cap + row; };
         float M = -INFINITY;
+#pragma unroll 4
         for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.part_ml[at(c) * 2]);
         const float ref = M == -INFINITY ? 0.f : M;
         float L = 0.f;
@@ -801,7 +837,7 @@ __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant_
             o.w = fmaf(p.w, f, o.w);
         }
         const float inv = L > 0.f ? 1.0f / L : L;
-        const int t = row / a.group, h = rec.z * a.group + row - t * a.group;
+        const int h = rec.z * a.group + unit_row - t * a.group;
         __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + (long long)(rec.x + t) * a.out.token_stride + (long long)h * a.out.head_stride + e;
         *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
     }

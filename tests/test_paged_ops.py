@@ -401,9 +401,10 @@ def test_attention_with_left_padding(dtype, n, lens, start):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_attention_of_extreme_logits(dtype):
+@pytest.mark.parametrize("n,d", [([70, 1], 64), ([3, 1], 64), ([2, 9], 128)])
+def test_attention_of_extreme_logits(dtype, n, d):
     """Logits of several hundred either way: the running maximum has to be taken off, and to grow along the cache."""
-    c = PagedCase(dtype, 64, 1, 32, "nhd", [70, 1], [300, 513])
+    c = PagedCase(dtype, d, 1, 32, "nhd", n, [300, 513])
     c.fill(None, 5)
     for i, s in enumerate(c.lens):                    # keys that grow with the slot
         for j in range(s):
@@ -412,6 +413,31 @@ def test_attention_of_extreme_logits(dtype):
     for workspace in (False, True):
         _check_attention(c, 2, True, None, workspace, 31)
         _check_attention(c, 2, True, None, workspace, 32, scale=2.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,lens", [([1] * 40, [700] * 40), ([1, 1, 1], [5000, 70, 3000]), ([90] * 6, [1200] * 6), ([300], [4000])])
+def test_attention_repeats_itself(n, lens):
+    """Many runs of the same call, next to work on another stream, give the same bits and never run into a wait limit."""
+    c = PagedCase(BF, 128, 2, 64, "nhd", [0] * len(n), lens)
+    c.n = n
+    c.cu = torch.tensor([0] + list(torch.tensor(n).cumsum(0)), dtype=torch.int32, device=DEV)
+    for p in c.dev:
+        p.normal_()
+    T = sum(n)
+    q = _randn((T, 8, 128), BF, 1).to(DEV) * 3
+    outs = [torch.empty_like(q) for _ in range(2)]
+    ws = c.kv.attn_workspace(8, T, max(n), max(lens))
+    side, big = torch.cuda.Stream(), torch.randn(1 << 24, device=DEV)
+    for rep in range(60):
+        out = outs[min(rep, 1)]
+        out.fill_(7.0)
+        with torch.cuda.stream(side):
+            big.mul_(1.0001)
+        c.kv.attn(q, out, c.cu, max_chunk=max(n), max_len=max(lens), workspace=ws)
+        if rep:
+            assert torch.equal(outs[0], outs[1]), rep
+    assert int(c.status) == 0
 
 
 @pytest.mark.gpu
