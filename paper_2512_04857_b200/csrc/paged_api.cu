@@ -183,7 +183,7 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     p.splits = 1;
     if (split) {
         const int64_t units = (int64_t)p.tiles * k.n_kv_heads;
-        int64_t s = (4 * kSms + units - 1) / units;
+        int64_t s = (12 * kSms + units - 1) / units;  // four rounds of three CTAs per SM: the last one costs little
         if (s > (len + 255) / 256) s = (len + 255) / 256;  // at least 256 slots each
         if (s > 64) s = 64;
         p.splits = s < 1 ? 1 : (int)s;
@@ -195,14 +195,14 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
 using SimtFn = void (*)(const lar::PagedAttnArgs);
 template <int D, int BM>
 lar_status_t launch_simt(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    SimtFn fn = lar::paged_attn_simt_kernel<float, D, BM>;
+    SimtFn fn = lar::paged_attn_simt_kernel<D, BM>;
     constexpr int smem = lar::SimtShape<D, BM>::SMEM;
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), lar::SimtShape<D, BM>::THREADS, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     if (p.splits > 1) {
         const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.n_kv_heads * a.group;
-        lar::combine_splits_kernel<float, D><<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);
+        lar::combine_splits_kernel<D><<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);
         LAR_CUDA(cudaGetLastError());
     }
     return LAR_OK;

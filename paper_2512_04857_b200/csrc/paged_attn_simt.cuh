@@ -1,11 +1,13 @@
 // Chunk attention for fp32 storage, on the CUDA cores: the tensor cores take no fp32 operands, and rounding q, K and V
 // to tf32 would lose what fp32 storage is chosen for.
 //
-// A CTA holds BM query rows and walks the unit's slots 64 at a time: S = Q K^T and O += P V as register tiles of 4 rows,
-// operands in shared memory (Q and K transposed, so that a thread's 4 rows and its keys are vector loads), softmax with the
-// running maximum and sum in fp32.  Bound: fp32 multiply-adds (64 rows), or, with BM = 16 for a few rows per
-// sequence (a decode step), the cache bytes.  Slots of a unit may be split over gridDim.z CTAs (few rows, long cache): they
-// leave (O, m, l) in the workspace and combine_splits_kernel joins them.
+// A CTA holds BM query rows and walks the unit's slots 64 at a time: S = Q K^T and O += P V as register tiles of RT rows by KC keys
+// (columns), operands row by row in shared memory, softmax with the running maximum and sum in fp32.  Rows of Q and K are padded
+// by 16 bytes, so that the 16-byte loads of the lanes of a quarter warp (8 keys) fall into different banks.  Bound: fp32 multiply-adds
+// and the shared-memory loads that feed them (64 rows; 8 rows a thread where registers and shared memory allow three CTAs per SM), or, with BM = 16
+// for a few rows per sequence (a decode step), the cache bytes.  K of the next step is copied (cp.async) while this step's P V
+// runs, V while the next step's S is formed.  Slots of a unit may be split over gridDim.z CTAs (few rows, long cache): they leave
+// (O, m, l) in the workspace and combine_splits_kernel joins them.
 #pragma once
 #include "paged_attn.cuh"
 
@@ -15,14 +17,16 @@ constexpr int kSimtKeys = 64;
 
 template <int D, int BM>
 struct SimtShape {
+    // rows of a thread: rg, rg + RG, ... (two neighbours in a warp, so that their loads fall into different banks)
+    static constexpr int RT = BM == 64 && D == 64 ? 8 : 4;
     static constexpr int KG = BM == 64 ? 16 : 32;    // threads along the keys
-    static constexpr int RG = BM / 4;                // threads along the rows, 4 rows each
+    static constexpr int RG = BM / RT;               // threads along the rows
     static constexpr int THREADS = KG * RG;
-    static constexpr int KC = kSimtKeys / KG;        // keys of a thread
+    static constexpr int KC = kSimtKeys / KG;        // keys of a thread: kg, kg + KG, ...
     static constexpr int OC = D / KG;                // output columns of a thread
     static constexpr int VC = OC < 4 ? OC : 4;       // ... in vectors of VC
-    static constexpr int QS = BM + 4, KS = kSimtKeys + 4, PS = BM + 4;
-    static constexpr int SMEM = (D * QS + D * KS + kSimtKeys * D + kSimtKeys * PS) * 4;
+    static constexpr int QS = D + 4, KS = D + 4, PS = BM + 4;
+    static constexpr int SMEM = (BM * QS + kSimtKeys * KS + kSimtKeys * D + kSimtKeys * PS) * 4;
 };
 
 template <int N>
@@ -31,18 +35,25 @@ template <> struct FVec<2> { using type = float2; };
 template <> struct FVec<4> { using type = float4; };
 
 template <int N>
-__device__ __forceinline__ void load_vec(const float* p, float (&v)[N]) {
+__device__ __forceinline__ void load_vec(const float* p, float* v) {
     *reinterpret_cast<typename FVec<N>::type*>(v) = *reinterpret_cast<const typename FVec<N>::type*>(p);
 }
+// 16 bytes to shared memory, or zeros
+__device__ __forceinline__ void copy16_async(float* dst, const float* src, bool live) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <typename T, int D, int BM>
-__global__ void __launch_bounds__(SimtShape<D, BM>::THREADS) paged_attn_simt_kernel(const PagedAttnArgs a) {
+template <int D, int BM>
+__global__ void __launch_bounds__(SimtShape<D, BM>::THREADS, SimtShape<D, BM>::RT == 8 ? 3 : 1) paged_attn_simt_kernel(const PagedAttnArgs a) {
     using S = SimtShape<D, BM>;
-    constexpr int E = Elt<T>::kPerChunk, CH = D / E;  // 16-byte chunks of a row
+    constexpr int CH = D / 4, RT = S::RT;  // 16-byte chunks of a row
     extern __shared__ __align__(16) float sm[];
-    float* qt = sm;                      // [D][QS]
-    float* kt = qt + D * S::QS;          // [D][KS]
-    float* vs = kt + D * S::KS;          // [64][D]
+    float* qs = sm;                      // [BM][QS]
+    float* ks = qs + BM * S::QS;         // [64][KS]
+    float* vs = ks + kSimtKeys * S::KS;  // [64][D]
     float* pt = vs + kSimtKeys * D;      // [64][PS]
 
     const int tid = threadIdx.x, lane = tid & 31;
@@ -76,6 +87,7 @@ __global__ void __launch_bounds__(SimtShape<D, BM>::THREADS) paged_attn_simt_ker
     if (seq < 0) return;
     int t0, t1;
     chunk_of(a.kv, seq, t0, t1);
+    tile = (t1 - t0 + a.tq - 1) / a.tq - 1 - tile;     // the tiles that see most first
     const int len = live_len(a.kv, seq);
     const int tok0 = t0 + tile * a.tq;                 // first token of the tile
     const int n_tok = min(a.tq, t1 - tok0);
@@ -88,81 +100,90 @@ __global__ void __launch_bounds__(SimtShape<D, BM>::THREADS) paged_attn_simt_ker
     const int per = (b_hi - b_lo + a.n_splits - 1) / a.n_splits;
     const int b0 = min(b_hi, b_lo + (int)blockIdx.z * per), b1 = min(b_hi, b0 + per);
 
-    // Q transposed; rows behind the tile's last are zero
-    for (int i = tid; i < BM * CH; i += S::THREADS) {
-        const int r = i % BM, c = i / BM;
-        float f[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = 0.f;
-        if (r < rows) {
-            const int t = r / G, g = r - t * G;
-            const T* p = reinterpret_cast<const T*>(a.q.p) + (long long)(tok0 + t) * a.q.token_stride + (head * G + g) * a.q.head_stride;
-            Elt<T>::unpack(*reinterpret_cast<const uint4*>(p + c * E), f);
+    const int* table = a.kv.table + seq * a.kv.table_seq_stride + head * a.kv.table_head_stride;
+    // the K or V rows of a step; slots outside [lo, hi) are zero whatever their memory holds
+    auto fetch = [&](float* dst, int stride, const char* pool, int j0, bool report) {
+        for (int i = tid; i < kSimtKeys * CH; i += S::THREADS) {
+            const int j = i / CH, c = i % CH, slot = j0 + j;
+            const float* src = reinterpret_cast<const float*>(pool);
+            bool live = slot >= lo && slot < hi;
+            if (live) {
+                const int page = table[slot >> a.kv.page_shift];
+                live = page >= 0 && page < a.kv.n_pages;
+                if (live) src += page * a.kv.page_stride + (slot & (a.kv.page_tokens - 1)) * a.kv.row_stride + head * a.kv.head_stride + c * 4;
+                else if (report && c == 0) paged_report(a.kv, kStPage);
+            }
+            copy16_async(dst + j * stride + c * 4, src, live);
         }
-#pragma unroll
-        for (int e = 0; e < E; ++e) qt[(c * E + e) * S::QS + r] = f[e];
+        copy_commit();
+    };
+    // Q; rows behind the tile's last are zero
+    for (int i = tid; i < BM * CH; i += S::THREADS) {
+        const int r = i / CH, c = i % CH, t = r / G, g = r - t * G;
+        const float* p = reinterpret_cast<const float*>(a.q.p);
+        const bool live = r < rows;
+        if (live) p += (long long)(tok0 + t) * a.q.token_stride + (head * G + g) * a.q.head_stride + c * 4;
+        copy16_async(qs + r * S::QS + c * 4, p, live);
+    }
+    if (b0 < b1) {
+        fetch(ks, S::KS, a.kv.k_pool, b0 * kSimtKeys, true);   // (with Q: one group)
+        fetch(vs, D, a.kv.v_pool, b0 * kSimtKeys, false);
     }
 
-    float o[4][S::OC], m[4], l[4];
-    int last[4];  // last slot each row sees
+    uint64_t o[RT][S::OC / 2];  // pairs of columns
+    float m[RT], l[RT];
+    int last[RT];  // last slot each row sees
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY;
         l[r] = 0.f;
-        const int row = rg * 4 + r;
+        const int row = rg + S::RG * r;
         last[r] = row >= rows ? -1 : a.causal ? min(slot0 + row / G, len - 1) : len - 1;
 #pragma unroll
-        for (int i = 0; i < S::OC; ++i) o[r][i] = 0.f;
+        for (int i = 0; i < S::OC / 2; ++i) o[r][i] = 0;
     }
 
     for (int b = b0; b < b1; ++b) {
         const int j0 = b * kSimtKeys;
-        __syncthreads();  // the previous step's tiles have been read
-        // K and V rows of the step; slots outside [lo, hi) are zero whatever their memory holds
-        for (int i = tid; i < kSimtKeys * CH; i += S::THREADS) {
-            const int j = i % kSimtKeys, c = i / kSimtKeys, slot = j0 + j;
-            float fk[E], fv[E];
+        copy_wait<1>();   // K of this step (V may be on its way)
+        __syncthreads();
+        float s[RT][S::KC];
+        {
+            uint64_t acc[RT][S::KC];  // sums over the even and the odd elements of a row
 #pragma unroll
-            for (int e = 0; e < E; ++e) fk[e] = fv[e] = 0.f;
-            if (slot >= lo && slot < hi) {
-                const int page = a.kv.table[seq * a.kv.table_seq_stride + head * a.kv.table_head_stride + (slot >> a.kv.page_shift)];
-                if (page >= 0 && page < a.kv.n_pages) {
-                    const long long off = page * a.kv.page_stride + (slot & (a.kv.page_tokens - 1)) * a.kv.row_stride + head * a.kv.head_stride + c * E;
-                    Elt<T>::unpack(*reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.kv.k_pool) + off), fk);
-                    Elt<T>::unpack(*reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.kv.v_pool) + off), fv);
-                } else if (c == 0) {
-                    paged_report(a.kv, kStPage);
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int k = 0; k < S::KC; ++k) acc[r][k] = 0;
+#pragma unroll 2
+            for (int d = 0; d < D; d += 4) {
+                ulonglong2 kv[S::KC];
+#pragma unroll
+                for (int k = 0; k < S::KC; ++k) kv[k] = *reinterpret_cast<const ulonglong2*>(ks + (kg + k * S::KG) * S::KS + d);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const ulonglong2 qv = *reinterpret_cast<const ulonglong2*>(qs + (rg + S::RG * r) * S::QS + d);
+#pragma unroll
+                    for (int k = 0; k < S::KC; ++k) acc[r][k] = fma_f32x2(qv.y, kv[k].y, fma_f32x2(qv.x, kv[k].x, acc[r][k]));
                 }
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                kt[(c * E + e) * S::KS + j] = fk[e];
-                vs[j * D + c * E + e] = fv[e];
-            }
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int k = 0; k < S::KC; ++k) {
+                    float even, odd;
+                    unpack_f32x2(acc[r][k], even, odd);
+                    s[r][k] = even + odd;
+                }
         }
-        __syncthreads();
-        float s[4][S::KC];
+        __syncthreads();  // K has been read
+        if (b + 1 < b1) fetch(ks, S::KS, a.kv.k_pool, j0 + kSimtKeys, true);
+        else copy_commit();
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int k = 0; k < S::KC; ++k) s[r][k] = 0.f;
-#pragma unroll 8
-        for (int d = 0; d < D; ++d) {
-            float qv[4], kv[S::KC];
-            load_vec(qt + d * S::QS + rg * 4, qv);
-            load_vec(kt + d * S::KS + kg * S::KC, kv);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int k = 0; k < S::KC; ++k) s[r][k] = fmaf(qv[r], kv[k], s[r][k]);
-        }
-        float p[S::KC][4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < RT; ++r) {
             float mx = -INFINITY;
 #pragma unroll
             for (int k = 0; k < S::KC; ++k) {
-                const int slot = j0 + kg * S::KC + k;
+                const int slot = j0 + kg + k * S::KG;
                 s[r][k] = slot >= lo && slot <= last[r] ? s[r][k] * a.scale_log2 : -INFINITY;
                 mx = fmaxf(mx, s[r][k]);
             }
@@ -174,59 +195,74 @@ __global__ void __launch_bounds__(SimtShape<D, BM>::THREADS) paged_attn_simt_ker
             float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < S::KC; ++k) {
-                p[k][r] = exp2f(s[r][k] - ref);
-                sum += p[k][r];
+                s[r][k] = exp2f(s[r][k] - ref);
+                sum += s[r][k];
             }
             l[r] = l[r] * corr + sum;  // (this thread's keys only: joined over the threads of the row at the end)
 #pragma unroll
-            for (int i = 0; i < S::OC; ++i) o[r][i] *= corr;
+            for (int i = 0; i < S::OC / 2; ++i) o[r][i] = mul_f32x2(o[r][i], pack_f32x2(corr, corr));
         }
 #pragma unroll
         for (int k = 0; k < S::KC; ++k)
-            *reinterpret_cast<float4*>(pt + (kg * S::KC + k) * S::PS + rg * 4) = make_float4(p[k][0], p[k][1], p[k][2], p[k][3]);
-        // the threads that share these rows lie in one warp: their part of P is visible after a warp barrier
-        __syncwarp();
+#pragma unroll
+            for (int r = 0; r < RT; r += 4)
+                *reinterpret_cast<float4*>(pt + (kg + k * S::KG) * S::PS + rg * RT + r) = make_float4(s[r][k], s[r + 1][k], s[r + 2][k], s[r + 3][k]);
+        copy_wait<1>();   // V of this step
+        __syncthreads();
 #pragma unroll 4
         for (int j = 0; j < kSimtKeys; ++j) {
-            float pv[4];
-            load_vec(pt + j * S::PS + rg * 4, pv);
+            float pv[RT];
+#pragma unroll
+            for (int r = 0; r < RT; r += 4) load_vec<4>(pt + j * S::PS + rg * RT + r, pv + r);
 #pragma unroll
             for (int i = 0; i < S::OC / S::VC; ++i) {
-                float vv[S::VC];
-                load_vec(vs + j * D + i * (S::KG * S::VC) + kg * S::VC, vv);
+                uint64_t vv[S::VC / 2];
+                load_vec<S::VC>(vs + j * D + i * (S::KG * S::VC) + kg * S::VC, reinterpret_cast<float*>(vv));
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int e = 0; e < S::VC; ++e) o[r][i * S::VC + e] = fmaf(pv[r], vv[e], o[r][i * S::VC + e]);
+                    for (int e = 0; e < S::VC / 2; ++e)
+                        o[r][i * (S::VC / 2) + e] = fma_f32x2(pack_f32x2(pv[r], pv[r]), vv[e], o[r][i * (S::VC / 2) + e]);
             }
         }
+        __syncthreads();  // V and P have been read
+        if (b + 1 < b1) fetch(vs, D, a.kv.v_pool, j0 + kSimtKeys, false);
+        else copy_commit();
     }
+    copy_commit();
+    copy_wait<0>();  // (nothing is in flight when the CTA ends)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RT; ++r) {
 #pragma unroll
         for (int w = S::KG / 2; w >= 1; w >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
-        const int row = rg * 4 + r;
+        const int row = rg + S::RG * r;
         if (row >= rows) continue;
         const int t = row / G, g = row - t * G;
-        if (a.n_splits > 1) {
-            const size_t at = (size_t)blockIdx.z * a.kv.n_tokens * a.kv.n_kv_heads * G + (size_t)(tok0 + t) * a.kv.n_kv_heads * G + head * G + g;
+        const size_t at = (size_t)blockIdx.z * a.kv.n_tokens * a.kv.n_kv_heads * G + (size_t)(tok0 + t) * a.kv.n_kv_heads * G + head * G + g;
+        float* dst = a.n_splits > 1 ? a.part_o + at * D
+                                    : reinterpret_cast<float*>(a.out.p) + (long long)(tok0 + t) * a.out.token_stride + (head * G + g) * a.out.head_stride;
+        const float inv = a.n_splits > 1 ? 1.f : l[r] > 0.f ? 1.0f / l[r] : l[r];  // nothing seen: 0; NaN stays NaN
 #pragma unroll
-            for (int i = 0; i < S::OC; ++i) a.part_o[at * D + (i / S::VC) * (S::KG * S::VC) + kg * S::VC + i % S::VC] = o[r][i];
-            if (kg == 0) {
-                a.part_ml[at * 2] = m[r];
-                a.part_ml[at * 2 + 1] = l[r];
+        for (int i = 0; i < S::OC / S::VC; ++i) {
+            typename FVec<S::VC>::type v;
+#pragma unroll
+            for (int e = 0; e < S::VC / 2; ++e) {
+                float x, y;
+                unpack_f32x2(o[r][i * (S::VC / 2) + e], x, y);
+                reinterpret_cast<float*>(&v)[2 * e] = x * inv;
+                reinterpret_cast<float*>(&v)[2 * e + 1] = y * inv;
             }
-        } else {
-            const float inv = l[r] > 0.f ? 1.0f / l[r] : l[r];  // nothing seen: 0; NaN stays NaN
-            T* dst = reinterpret_cast<T*>(a.out.p) + (long long)(tok0 + t) * a.out.token_stride + (head * G + g) * a.out.head_stride;
-#pragma unroll
-            for (int i = 0; i < S::OC; ++i) dst[(i / S::VC) * (S::KG * S::VC) + kg * S::VC + i % S::VC] = Elt<T>::from_float(o[r][i] * inv);
+            *reinterpret_cast<typename FVec<S::VC>::type*>(dst + i * (S::KG * S::VC) + kg * S::VC) = v;
+        }
+        if (a.n_splits > 1 && kg == 0) {
+            a.part_ml[at * 2] = m[r];
+            a.part_ml[at * 2 + 1] = l[r];
         }
     }
 }
 
 // Joins the splits of every row, in the order of the splits: one warp per (token, head).
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(128) combine_splits_kernel(const PagedAttnArgs a) {
     constexpr int PER = D / 32;
     const int hq = a.kv.n_kv_heads * a.group, lane = threadIdx.x & 31;
@@ -248,9 +284,9 @@ __global__ void __launch_bounds__(128) combine_splits_kernel(const PagedAttnArgs
         for (int i = 0; i < PER; ++i) o[i] = fmaf(a.part_o[at * D + i * 32 + lane], f, o[i]);
     }
     const float inv = L > 0.f ? 1.0f / L : L;
-    T* dst = reinterpret_cast<T*>(a.out.p) + (long long)t * a.out.token_stride + h * a.out.head_stride;
+    float* dst = reinterpret_cast<float*>(a.out.p) + (long long)t * a.out.token_stride + h * a.out.head_stride;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) dst[i * 32 + lane] = Elt<T>::from_float(o[i] * inv);
+    for (int i = 0; i < PER; ++i) dst[i * 32 + lane] = o[i] * inv;
 }
 
 }  // namespace lar
