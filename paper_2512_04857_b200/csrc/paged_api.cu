@@ -8,6 +8,7 @@
 
 #include "host_util.h"
 #include "paged_attn_simt.cuh"
+#include "paged_attn_few.cuh"
 #include "paged_attn_tc.cuh"
 #include "paged_host.h"
 #include "rope_rows.cuh"
@@ -131,7 +132,8 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
 // ------------------------------------------------------------------------------------------ chunk attention
 struct AttnPlan {
     int tq;        // tokens of a row tile
-    int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows)
+    int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows; 0: at most 16 rows, the kernel for few rows)
+    int nr;        // bf16, few rows: blocks of 8 rows
     int stages, grid, rows_cap;  // bf16: K/V ring, persistent CTAs, rows of a row tile
     int bm, splits, tiles;       // fp32: rows of a tile, CTAs along a unit's slots, bound on the row tiles of all sequences
     size_t bytes;  // workspace
@@ -153,7 +155,18 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     const int d = k.head_dim;
     if (k.dtype == LAR_BF16) {
         constexpr size_t kSmem = 227 * 1024;
-        p.nt = chunk * group > 128 ? 2 : 1;
+        p.nt = chunk * group > 128 ? 2 : chunk * group > lar::kFewRows ? 1 : 0;
+        if (p.nt == 0) {
+            p.tq = (int)chunk;
+            p.rows_cap = p.tq * group;
+            p.nr = p.rows_cap > 8 ? 2 : 1;
+            p.smem = d == 64 ? (p.nr == 1 ? lar::FewShape<64, 1>::bytes(k.n_seqs) : lar::FewShape<64, 2>::bytes(k.n_seqs))
+                             : (p.nr == 1 ? lar::FewShape<128, 1>::bytes(k.n_seqs) : lar::FewShape<128, 2>::bytes(k.n_seqs));
+            p.grid = (p.smem <= 233472 / 2 - 1024 ? 2 : 1) * kSms;
+            p.splits = split ? 2 : 1;
+            if (split) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
+            return p;
+        }
         p.tq = 128 / group;
         if (p.nt == 1 && chunk < p.tq) p.tq = (int)chunk;
         p.rows_cap = (p.tq * group + 7) / 8 * 8;
@@ -253,9 +266,22 @@ lar_status_t make_maps(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, int
     return st;
 }
 
-template <int D, int NT>
+// The bf16 kernels: NT row tiles of 128 rows, or (NT = 0) few rows in NR blocks of 8.
+template <int D, int NT, int NR = 0>
+struct TcKernel {
+    static constexpr int BN = lar::TcShape<D, NT>::BN, THREADS = lar::TcShape<D, NT>::THREADS;
+    static constexpr auto fn = lar::paged_attn_tc_kernel<D, NT>;
+};
+template <int D, int NR>
+struct TcKernel<D, 0, NR> {
+    static constexpr int BN = lar::FewShape<D, NR>::KT, THREADS = lar::FewShape<D, NR>::THREADS;
+    static constexpr auto fn = lar::paged_attn_few_kernel<D, NR>;
+};
+
+template <int D, int NT_, int NR = 0>
 lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    using S = lar::TcShape<D, NT>;
+    using S = TcKernel<D, NT_, NR>;
+    constexpr int NT = NT_ == 0 ? 1 : NT_;
     lar::TcArgs t;
     memset(&t, 0, sizeof(t));
     lar::TcMaps m;
@@ -272,9 +298,9 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     }
     lar_status_t st = make_maps(k, a, t.box_rows, m);
     if (st != LAR_OK) return st;
-    const void* fn = (const void*)lar::paged_attn_tc_kernel<D, NT>;
-    LAR_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
-    lar::paged_attn_tc_kernel<D, NT><<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
+    constexpr auto fn = S::fn;
+    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
+    fn<<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
     LAR_CUDA(cudaGetLastError());
     if (t.split) {
         cudaLaunchConfig_t lc;
@@ -404,7 +430,7 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     if (p.bytes > workspace_bytes) return LAR_ERR_NOMEM;
     if (kv->dtype == LAR_BF16) {  // the kernel counts units and slot tiles in 31 bits
         const int64_t units = (n_tokens / p.tq + (n_tokens < kv->n_seqs ? n_tokens : kv->n_seqs)) * kv->n_kv_heads;
-        const int64_t tiles = ((int64_t)kv->table_cols * kv->page_tokens + 63) / 64 + 4;
+        const int64_t tiles = ((int64_t)kv->table_cols * kv->page_tokens + 31) / 32 + 4;
         if (units > (1ll << 30) / tiles) return LAR_ERR_CAPACITY;
     }
     a.start = kv_start;
@@ -418,7 +444,9 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     cudaStream_t s = (cudaStream_t)stream;
     if (kv->dtype == LAR_BF16) {
         if (p.nt == 2) return d == 64 ? launch_tc<64, 2>(*kv, a, p, s) : launch_tc<128, 2>(*kv, a, p, s);
-        return d == 64 ? launch_tc<64, 1>(*kv, a, p, s) : launch_tc<128, 1>(*kv, a, p, s);
+        if (p.nt == 1) return d == 64 ? launch_tc<64, 1>(*kv, a, p, s) : launch_tc<128, 1>(*kv, a, p, s);
+        if (p.nr == 2) return d == 64 ? launch_tc<64, 0, 2>(*kv, a, p, s) : launch_tc<128, 0, 2>(*kv, a, p, s);
+        return d == 64 ? launch_tc<64, 0, 1>(*kv, a, p, s) : launch_tc<128, 0, 1>(*kv, a, p, s);
     }
     if (p.bm == 16) return d == 64 ? launch_simt<64, 16>(a, p, s) : launch_simt<128, 16>(a, p, s);
     return d == 64 ? launch_simt<64, 64>(a, p, s) : launch_simt<128, 64>(a, p, s);

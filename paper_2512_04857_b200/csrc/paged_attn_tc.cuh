@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 }
                 if (mine && !g.whole) {
                     float* ml = a.part_ml + (((size_t)slotp * NT + tile) * ta.rows_cap + row) * 2;
-                    ml[0] = m_used;
+                    ml[0] = m_used * sc;  // (-inf: nothing seen)
                     ml[1] = l;
                 }
             }
@@ -802,22 +802,20 @@ __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant_
         const int unit_row = i / (D / 4), e = (i - unit_row * (D / 4)) * 4;  // (token, head of the group) of the unit
         const int t = unit_row / a.group, tile = NT == 2 && t >= a.tq ? 1 : 0, row = unit_row - tile * a.tq * a.group;
         auto at = [&](int c) { return ((size_t)(c * 2 + (c == c0 ? 1 : 0)) * NT + tile) * ta.rows_cap + row; };
-        float M = -INFINITY;
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) M = fmaxf(M, a.part_ml[at(c) * 2]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f;
+        float M = -INFINITY, L = 0.f;  // (one pass with a running maximum: the loads of all parts are under way at once)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int c = c0; c <= c1; ++c) {
             const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at(c) * 2);
             const float4 p = *reinterpret_cast<const float4*>(a.part_o + at(c) * D + e);
-            const float f = ex2_approx((ml.x - ref) * a.scale_log2);
-            L = fmaf(ml.y, f, L);
-            o.x = fmaf(p.x, f, o.x);
-            o.y = fmaf(p.y, f, o.y);
-            o.z = fmaf(p.z, f, o.z);
-            o.w = fmaf(p.w, f, o.w);
+            const float mn = fmaxf(M, ml.x), ref = mn == -INFINITY ? 0.f : mn;
+            const float f0 = ex2_approx(M - ref), f = ex2_approx(ml.x - ref);
+            M = mn;
+            L = fmaf(ml.y, f, L * f0);
+            o.x = fmaf(p.x, f, o.x * f0);
+            o.y = fmaf(p.y, f, o.y * f0);
+            o.z = fmaf(p.z, f, o.z * f0);
+            o.w = fmaf(p.w, f, o.w * f0);
         }
         const float inv = L > 0.f ? 1.0f / L : L;
         const int h = rec.z * a.group + unit_row - t * a.group;

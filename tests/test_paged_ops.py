@@ -401,7 +401,7 @@ def test_attention_with_left_padding(dtype, n, lens, start):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("n,d", [([70, 1], 64), ([3, 1], 64), ([2, 9], 128)])
+@pytest.mark.parametrize("n,d", [([70, 1], 64), ([40, 9], 64), ([33, 1], 128), ([3, 1], 64), ([2, 8], 128)])
 def test_attention_of_extreme_logits(dtype, n, d):
     """Logits of several hundred either way: the running maximum has to be taken off, and to grow along the cache."""
     c = PagedCase(dtype, d, 1, 32, "nhd", n, [300, 513])
@@ -416,7 +416,7 @@ def test_attention_of_extreme_logits(dtype, n, d):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,lens", [([1] * 40, [700] * 40), ([1, 1, 1], [5000, 70, 3000]), ([90] * 6, [1200] * 6), ([300], [4000])])
+@pytest.mark.parametrize("n,lens", [([1] * 40, [700] * 40), ([1, 1, 1], [5000, 70, 3000]), ([20] * 6, [1200] * 6), ([90] * 6, [1200] * 6), ([300], [4000])])
 def test_attention_repeats_itself(n, lens):
     """Many runs of the same call, next to work on another stream, give the same bits and never run into a wait limit."""
     c = PagedCase(BF, 128, 2, 64, "nhd", [0] * len(n), lens)
