@@ -135,7 +135,8 @@ struct AttnPlan {
     int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows; 0: at most 16 rows, the kernel for few rows)
     int nr;        // bf16, few rows: blocks of 8 rows
     int stages, grid, rows_cap;  // bf16: K/V ring, persistent CTAs, rows of a row tile
-    int bm, splits, tiles;       // fp32: rows of a tile, CTAs along a unit's slots, bound on the row tiles of all sequences
+    int splits;    // bf16: 1 units stay whole, 2 they may be cut, 3 they are handed out on demand; fp32: CTAs along a unit's slots
+    int bm, tiles; // fp32: rows of a tile, bound on the row tiles of all sequences
     size_t bytes;  // workspace
     size_t smem;
 };
@@ -162,7 +163,8 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
             p.nr = p.rows_cap > 8 ? 2 : 1;
             p.smem = d == 64 ? (p.nr == 1 ? lar::FewShape<64, 1>::bytes(k.n_seqs) : lar::FewShape<64, 2>::bytes(k.n_seqs))
                              : (p.nr == 1 ? lar::FewShape<128, 1>::bytes(k.n_seqs) : lar::FewShape<128, 2>::bytes(k.n_seqs));
-            p.grid = (p.smem <= 233472 / 2 - 1024 ? 2 : 1) * kSms;
+            const int fit = (int)(233472 / (p.smem + 1024)), want = d == 64 ? lar::FewShape<64, 1>::PER_SM : lar::FewShape<128, 1>::PER_SM;
+            p.grid = (fit < want ? fit : want) * kSms;
             p.splits = split ? 2 : 1;
             if (split) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
             return p;
@@ -184,10 +186,14 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
             p.smem = tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs);
         }
         p.grid = per_sm * kSms;
-        // Units may be cut, except where there are so many or so short ones that whole units fill the CTAs evenly enough.
+        // One row tile: units are cut.  Two: whole units on demand where there are many, or where their lengths differ much (chunks
+        // that make up much of their cache); long units are cut where a few rounds of whole ones would leave CTAs idle.
         const int64_t units = (n_tokens / (p.tq * p.nt) + with_tokens) * k.n_kv_heads;
-        p.splits = split && (p.nt == 1 || (units < 16 * p.grid && len >= 2048)) ? 2 : 1;
-        if (p.splits > 1) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
+        p.splits = 1;
+        if (split && (p.nt == 1 || (units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid)))) p.splits = 2;
+        else if (split && units > p.grid) p.splits = 3;
+        if (p.splits == 2) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
+        if (p.splits == 3) p.bytes = sizeof(int4);
         return p;
     }
     p.bm = chunk * group <= 16 ? 16 : 64;
@@ -289,8 +295,12 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     t.stages = p.stages;
     t.rows_cap = p.rows_cap;
     t.box_rows = k.page_tokens < S::BN ? k.page_tokens : S::BN;
-    t.split = p.splits > 1;
+    t.split = p.splits == 2;
     t.min_items = 6;
+    if (p.splits == 3) {
+        t.counter = reinterpret_cast<int*>(a.part_o);
+        LAR_CUDA(cudaMemsetAsync(t.counter, 0, sizeof(int), s));
+    }
     if (t.split) {  // records, then (m, l), then O of every CTA's two parts
         t.records = reinterpret_cast<int4*>(a.part_o);
         t.a.part_ml = reinterpret_cast<float*>(t.records + p.grid);

@@ -20,24 +20,25 @@ constexpr int kFewRows = 16;
 
 template <int D, int NR>
 struct FewShape {
-    static constexpr int KT = D == 64 ? 64 : 32;  // slots of a tile
+    static constexpr int KT = 32;                 // slots of a tile
     static constexpr int HALVES = D / 64;
     static constexpr int MT = KT / 16;            // 16-slot blocks
     static constexpr int KS = D / 16;
     static constexpr int TILE_BYTES = KT * D * 2, STAGE_BYTES = 2 * TILE_BYTES;
-    static constexpr int W = 4, THREADS = (W + 2) * 32;  // producer, consumers, epilogue
+    static constexpr int W = 2, THREADS = (W + 2) * 32;  // producer, consumers, epilogue
+    static constexpr int PER_SM = D == 64 ? 4 : 2;  // CTAs per SM: 64 KB of cache on the way in each
     static constexpr int NS = 4;                  // stages: a multiple of W, a stage is always read by the same consumer
     static constexpr int ROWS = 8 * NR;
     static constexpr int Q_HALF = ROWS * 128, Q_SLOT = Q_HALF * HALVES;
     static constexpr int PS = D + 4;              // floats of a partial row: O, m, l, padding
-    static constexpr int PBUFS = D == 128 && NR == 2 ? 1 : 2;
+    static constexpr int PBUFS = 2;
     static constexpr int PBUF_FLOATS = W * ROWS * PS;
     static constexpr int FIXED = 1024 + NS * STAGE_BYTES + 2 * Q_SLOT + PBUFS * PBUF_FLOATS * 4 + 32 * 8;
     static __host__ __device__ int bytes(int n_seqs) { return FIXED + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
 };
 
 template <int D, int NR>
-__global__ void __launch_bounds__(FewShape<D, NR>::THREADS, 2) paged_attn_few_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
+__global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER_SM) paged_attn_few_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
     using S = FewShape<D, NR>;
     using Work = TcWork<1, S::KT, D>;
     constexpr int KT = S::KT, W = S::W, NS = S::NS, HALVES = S::HALVES;

@@ -20,10 +20,13 @@
 // Slots outside [start, len) of a tile hold memory that may be anything: keys are masked by selection, and the value rows
 // are cleared in shared memory before the product (0 * NaN would reach the output).
 //
-// Work.  A unit is one (sequence, KV head, NT row tiles).  NT = 2: whole units round-robin, as many full rounds as there are, heads
-// outermost (the CTAs of a moment share K/V in L2) and the longest tiles of a sequence first.  What is left of them, and with NT = 1 all
-// units, is one list of slot tiles that is cut into equal ranges, one per CTA; a unit cut by a range boundary leaves (O, m, l) per
-// CTA in the workspace and join_ranges_kernel adds them up in the order of the CTAs.  Without a workspace every unit stays whole.
+// Work.  A unit is one (sequence, KV head, NT row tiles), heads outermost (the CTAs of a moment share K/V in L2), the longest tiles of
+// a sequence first.
+//   Many units, or units of unlike length (prompts): whole units, each CTA takes the next one when it is free (a counter in the workspace).
+//   Fewer, long units: NT = 2 whole units round-robin, as many full rounds as there are; what is left, and with NT = 1 all units,
+//   is one list of slot tiles that is cut into equal ranges, one per CTA; a unit cut by a range boundary leaves (O, m, l) per
+//   CTA in the workspace and join_ranges_kernel adds them up in the order of the CTAs.
+//   Without a workspace: whole units round-robin.
 #pragma once
 #include <cuda.h>
 
@@ -72,6 +75,7 @@ struct TcArgs {
     int box_rows;      // slots of one K/V box
     int split;         // ranges may cut units
     int min_items;     // slot tiles that a range has at least
+    int* counter;      // whole units are handed out as CTAs ask for them (zero before the launch); null: round-robin
     int4* records;     // split: per CTA the unit that begins in its range and goes on in the next CTAs
 };
 
@@ -168,35 +172,36 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
         : "memory");
 }
 
+// ---------------------------------------------------------------------------------- work list
+// One step of a CTA's work: some slot tiles of one unit.
+struct alignas(16) TcSeg {
+    int seq, head, tok0, n_tok;  // tokens of the unit
+    int slot0;                   // slot of its first token
+    int lo, len;                 // live slots of the sequence
+    int jb;                      // first slot tile
+    int nb;                      // slot tiles (-1: no more work)
+    int whole;                   // nothing of the unit lies in other CTAs
+    int b0;                      // tiles of the unit before this step's
+    int unit_end;                // end of the unit in the list of slot tiles; in the ring, the CTA that holds its last one
+};
+constexpr int kTcSegs = 4;  // steps that are known ahead of the warps that work on them
+
 // ---------------------------------------------------------------------------------- shared memory
 template <int D, int NT>
 struct TcSmem {
     using S = TcShape<D, NT>;
     static __host__ __device__ int q_bytes(int rows_cap) { return NT * S::HALVES * ((rows_cap * 128 + 1023) / 1024 * 1024); }
     // the MMA reads 128 rows whatever rows_cap is: behind the last Q tile there is always a K/V stage or more
-    static __host__ __device__ int tail(int n_seqs) { return 36 * 8 + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
+    static __host__ __device__ int tail(int n_seqs) { return 44 * 8 + kTcSegs * (int)sizeof(TcSeg) + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
     static __host__ __device__ int bytes(int rows_cap, int stages, int n_seqs) {
         return 1024 + q_bytes(rows_cap) + stages * S::STAGE_BYTES + tail(n_seqs);
     }
 };
 
-// ---------------------------------------------------------------------------------- work list
-// One step of a CTA's work: some slot tiles of one unit.
-struct TcSeg {
-    int seq, head, tok0, n_tok;  // tokens of the unit
-    int slot0;                   // slot of its first token
-    int lo, len;                 // live slots of the sequence
-    int jb;                      // first slot tile
-    int nb;                      // slot tiles
-    int whole;                   // nothing of the unit lies in other CTAs
-    int b0;                      // tiles of the unit before this step's
-    int unit_end;                // end of the unit in the list of slot tiles
-};
-
 // A CTA's work: first whole units, every step-th one, then an equal range of the slot tiles of the units that are left.
 template <int NT, int BN, int D>
 struct TcWork {
-    static constexpr int kUnitCost = NT == 1 && D == 64 ? 3 : 2;
+    static constexpr int kUnitCost = NT == 2 ? 2 : BN == 64 ? (D == 64 ? 3 : 2) : (D == 64 ? 8 : 4);
     const SeqInfo* info;
     const int* pre;    // units before each sequence
     const int* items;  // slot tiles before each sequence, of the units from first_cut on
@@ -316,9 +321,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
     auto v_empty = [&](int st) { return bar0 + 8u * (25 + st); };  // NT = 1: not used, k_empty is both
     auto p2_full = [&](int i) { return bar0 + 8u * (29 + i); };
     auto s_free = [&](int i) { return bar0 + 8u * (31 + i); };
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 34);
-    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(bars + 34) + 1;
-    SeqInfo* info = reinterpret_cast<SeqInfo*>(bars + 36);
+    auto seg_full = [&](int i) { return bar0 + 8u * (34 + i); };
+    auto seg_empty = [&](int i) { return bar0 + 8u * (38 + i); };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 42);
+    uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(bars + 42) + 1;
+    TcSeg* seg_ring = reinterpret_cast<TcSeg*>(bars + 44);
+    SeqInfo* info = reinterpret_cast<SeqInfo*>(seg_ring + kTcSegs);
     int* pre = reinterpret_cast<int*>(info + a.kv.n_seqs);
     int* items = pre + a.kv.n_seqs + 1;
     int* wsum = items + a.kv.n_seqs + 1;
@@ -343,6 +351,10 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 mbar_init(v_full(i), 1);
                 mbar_init(k_empty(i), NT);  // (each row tile's MMA warp)
                 mbar_init(v_empty(i), NT);
+            }
+            for (int i = 0; i < kTcSegs; ++i) {
+                mbar_init(seg_full(i), 1);
+                mbar_init(seg_empty(i), S::SM_WARPS + 2 * NT - 1);  // softmax, MMA and (NT = 2) V warps
             }
             mbar_fence_init_smem();
             *abort_flag = 0;
@@ -426,6 +438,18 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
     tc_fence_after();
     const uint32_t tmem = *tmem_ptr;
 
+    // The K producer works out the steps and leaves them in a ring; the other warps (MMA: one thread) read them from there.
+    int seg_no = 0;
+    auto next_seg = [&](TcSeg& g, bool one_thread) {
+        const int r = seg_no % kTcSegs;
+        const uint32_t turn = (seg_no / kTcSegs) & 1;
+        ++seg_no;
+        if (!(one_thread ? wait_or_abort(seg_full(r), turn, abort_flag) : warp_wait(seg_full(r), turn, abort_flag))) return false;
+        g = seg_ring[r];
+        if (!one_thread) __syncwarp();
+        if (one_thread || lane == 0) mbar_arrive(seg_empty(r));
+        return g.nb >= 0;
+    };
     if (NT == 2) {
         if (warp < S::SM_WARPS)
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SM_REGS));
@@ -453,7 +477,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             return done;
         };
         TcSeg g;
-        while (ok && work.next(g)) {
+        while (ok && next_seg(g, false)) {
             const int n = g.nb;
             const int nt = min(a.tq, g.n_tok - tile * a.tq);  // tokens of this row tile
             const int rows = nt > 0 ? nt * G : 0;
@@ -625,7 +649,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             }
             if (!g.whole && g.b0 == 0) {
                 // the unit goes on in the next CTAs: up to the one that holds its last item
-                if (tid == 0) ta.records[blockIdx.x] = make_int4(g.tok0, g.n_tok, g.head, (int)(((long long)g.unit_end * n_ranges + total - 1) / total - 1));
+                if (tid == 0) ta.records[blockIdx.x] = make_int4(g.tok0, g.n_tok, g.head, g.unit_end);
                 recorded = true;
             }
             if (n > 0) {
@@ -686,7 +710,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 tc_mma_ts<kDescHigh, 24, 384>(tm_o, pa, va, id_o, true);
             };
             TcSeg g;
-            while (ok && work.next(g)) {
+            while (ok && next_seg(g, true)) {
                 const int n = g.nb;
                 if (n == 0) continue;
                 if (!(ok = wait_or_abort(q_full(tile), segs & 1, abort_flag))) break;
@@ -736,7 +760,29 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         const CUtensorMap* map = is_v ? &maps.v : &maps.k;
         const uint32_t full0 = is_v ? v_full(0) : k_full(0), empty0 = NT == 2 && is_v ? v_empty(0) : k_empty(0);
         TcSeg g;
-        while (ok && work.next(g)) {
+        int unit = blockIdx.x, asked = 0;  // whole units handed out on demand: this one, and what the counter gave for the next
+        for (;;) {
+            if (k_warp) {
+                bool more = true;
+                if (ta.counter) {
+                    if (seg_no > 0) unit = gridDim.x + __shfl_sync(0xffffffffu, asked, 0);
+                    work.x = unit;
+                    if (lane == 0 && unit < work.end) asked = atomicAdd(ta.counter, 1);  // (used a unit later)
+                }
+                more = work.next(g);
+                if (!more) g.nb = -1;
+                else if (!g.whole) g.unit_end = (int)(((long long)g.unit_end * n_ranges + total - 1) / total - 1);  // the CTA with its last item
+                const int r = seg_no % kTcSegs;
+                if (seg_no >= kTcSegs && !(ok = warp_wait(seg_empty(r), (seg_no / kTcSegs - 1) & 1, abort_flag))) break;
+                ++seg_no;
+                if (lane == 0) {
+                    seg_ring[r] = g;
+                    mbar_arrive(seg_full(r));
+                }
+                if (!more) break;
+            } else if (!next_seg(g, false)) {
+                break;
+            }
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 if (g.nb == 0 || !k_warp) continue;
@@ -774,6 +820,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 slot += BN;
                 page = page_next;
             }
+            if (!ok) break;
         }
         if (!ok && (NT == 2 ? lane == 0 : idx == 0)) {
             // given up: the copies in flight land before the CTA's shared memory goes to somebody else

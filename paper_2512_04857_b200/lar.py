@@ -312,10 +312,10 @@ def _rows(x, n, heads, d, dtype, dev, what):
 
 
 def _dtype_of(x) -> int:
-    import torch
-    if x.dtype == torch.bfloat16:
+    _fast()
+    if x.dtype == _torch.bfloat16:
         return LAR_BF16
-    if x.dtype == torch.float32:
+    if x.dtype == _torch.float32:
         return LAR_FP32
     raise LarError(LAR_ERR_INVALID_ARG, f"dtype {x.dtype}")
 
@@ -331,11 +331,11 @@ def _ints(x, n, dev, what):
 
 def _positions(pos, rope, n, dev, what):
     """Address and axis stride of pos, int32 [axes, tokens] (or [tokens] for one axis), dense along the tokens."""
-    axes = rope.n_axes
-    if pos.dtype != _torch.int32 or pos.get_device() != dev or pos.shape != ((axes, n) if pos.dim() == 2 else (n,)) or \
-            (pos.dim() == 1 and axes != 1) or (n > 1 and pos.stride(-1) != 1):
+    axes, st = rope.n_axes, pos.stride()
+    if pos.dtype != _torch.int32 or pos.get_device() != dev or (n > 1 and st[-1] != 1) or \
+            (pos.shape != (axes, n) and (axes != 1 or pos.shape != (n,))):
         raise LarError(LAR_ERR_INVALID_ARG, f"{what}: pos is an int32 tensor [{axes}, {n}] on the same GPU")
-    return pos.data_ptr(), pos.stride(0) if axes > 1 else n
+    return pos.data_ptr(), st[0] if axes > 1 else n
 
 
 def _device_of(x) -> int:
@@ -369,7 +369,6 @@ def rope_table(rope, pos, cos_sin):
 
 def rope_rotate(rope, pos, q, q_out, k=None, k_out=None, inverse=False):
     """Rotates q (and k), [tokens, heads, head_dim] with any token and head strides, by pos [axes, tokens]."""
-    _fast()
     code, dt, dev = _dtype_of(q), q.dtype, _device_of(q)
     n, hq, d = q.shape
     _require(d == rope.head_dim and (k is None) == (k_out is None), "rope_rotate: shapes")

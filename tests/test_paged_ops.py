@@ -416,7 +416,33 @@ def test_attention_of_extreme_logits(dtype, n, d):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,lens", [([1] * 40, [700] * 40), ([1, 1, 1], [5000, 70, 3000]), ([20] * 6, [1200] * 6), ([90] * 6, [1200] * 6), ([300], [4000])])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_many_ragged_prompts(d, causal):
+    """More row tiles than SMs, of very different lengths: CTAs take them on demand."""
+    rng = random.Random(d)
+    n = [rng.choice([1, 33, 64, 65, 90]) for _ in range(48)]
+    lens = [a + rng.choice([0, 0, 100]) for a in n]
+    c = PagedCase(BF, d, 2, 32, "nhd", n, lens, seed=d)
+    start = [rng.choice([0, 0, 7, 40]) for _ in n]
+    c.fill(start, 3)
+    _check_attention(c, 8, causal, start, True, 5)
+    _check_attention(c, 8, causal, start, False, 6)
+
+
+@pytest.mark.gpu
+def test_attention_of_long_chunks_in_whole_and_cut_rounds():
+    """One full round of row tiles over the SMs, and a rest whose slots are cut into equal ranges."""
+    c = PagedCase(BF, 64, 4, 64, "hnd", [1280, 1216], [2900, 2850])
+    for p, x in zip(c.pools, c.dev):
+        x.normal_()
+        p.copy_(x.cpu())
+    _check_attention(c, 16, True, None, True, 7)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,lens", [([1] * 40, [700] * 40), ([1, 1, 1], [5000, 70, 3000]), ([20] * 6, [1200] * 6), ([90] * 6, [1200] * 6), ([100] * 40, [150] * 40),
+                                    ([300], [4000])])
 def test_attention_repeats_itself(n, lens):
     """Many runs of the same call, next to work on another stream, give the same bits and never run into a wait limit."""
     c = PagedCase(BF, 128, 2, 64, "nhd", [0] * len(n), lens)
