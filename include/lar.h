@@ -370,6 +370,7 @@ lar_status_t lar_rope_rotate(const lar_rope_t* rope, int dtype, const int32_t* p
                              const lar_rows_t* k_out, int n_kv_heads, int inverse, void* stream);
 
 /* Appends the keys (rotated by their positions) and values of a packed batch of chunks to a paged cache, in one launch.
+ * Sequences may share pages that are only read (a common prefix); no two tokens of a call may have the same row.
  * Sequence s owns the tokens cu_tokens[s] .. cu_tokens[s + 1] - 1 (device, int32, [n_seqs + 1], ascending; NULL: n_tokens /
  * n_seqs each); its i-th of T tokens goes to slot lens[s] - T + i, so lens already counts them.  Tokens before
  * cu_tokens[0] or from cu_tokens[n_seqs] on belong to nobody and are left alone (n_tokens may be a padded batch size).
@@ -383,7 +384,8 @@ lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* r
  *                                               or            kv_start[s] .. lens[s] - 1  (causal = 0)
  * kv_start (device, int32, [n_seqs], or NULL: 0) masks left padding.  A row that sees no slot is zero; memory of slots that
  * no row of a sequence sees (behind lens, before kv_start) may hold anything.  Tokens that belong to no sequence are left alone.  A
- * non-finite key or value in a slot that some row of the chunk sees may reach every row of the chunk.
+ * non-finite value in a slot that some row of the chunk sees may reach every row of the chunk.  out overlaps nothing else.
+ * LAR_ERR_CAPACITY: bf16 with more than 1024 sequences, or 2^30 (query tile, cache tile) pairs or more.
  * Query head hq uses KV head hq / (n_q_heads / n_kv_heads); their ratio is 1..16.  softmax_scale 0 selects 1/sqrt(head_dim).
  * max_chunk and max_len bound the tokens of a chunk and the entries of a cache (0: not known); they only choose the launch
  * shape, never the result's correctness.

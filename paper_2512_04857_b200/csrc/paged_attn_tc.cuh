@@ -35,9 +35,6 @@
 
 namespace lar {
 
-#ifndef LAR_SMR
-#define LAR_SMR 216
-#endif
 constexpr int kTcMaxSeqs = 1024;  // sequences of a call (their lengths are kept in shared memory)
 constexpr int kTcMaxStages = 4;
 
@@ -48,10 +45,10 @@ struct TcShape {
     static constexpr int TILE_BYTES = BN * D * 2;            // K or V tile
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
     static constexpr int SM_WARPS = NT * 4;
-    // NT = 2: three warpgroups, the third (two MMA warps, two producers) gives registers to the softmax warps: 2 * 224 + 56 =
+    // NT = 2: three warpgroups, the third (two MMA warps, two producers) gives registers to the softmax warps: 2 * 216 + 72 =
     // 3 * 168, what the block was launched with
     static constexpr int THREADS = NT == 2 ? 384 : SM_WARPS * 32 + 64;
-    static constexpr int SM_REGS = LAR_SMR, OTHER_REGS = 504 - 2 * LAR_SMR;
+    static constexpr int SM_REGS = 216, OTHER_REGS = 504 - 2 * SM_REGS;
     static constexpr int P_PARTS = NT == 2 ? 2 : 1;          // P is handed over in parts of 64 slots: the product starts on the first
     // TMEM columns.  NT = 2: one logit buffer for both row tiles (a softmax warp takes its logits into registers at once, so the buffer is
     // free for the other row tile's), P of each row tile (64 columns), two accumulators.  NT = 1: two logit buffers that P overlays,
@@ -131,12 +128,6 @@ __device__ __forceinline__ void tc_st32(uint32_t tmem, const uint32_t* r) {
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
         "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(tmem), LAR_I4(r, 0), LAR_I4(r, 4),
         LAR_I4(r, 8), LAR_I4(r, 12), LAR_I4(r, 16), LAR_I4(r, 20), LAR_I4(r, 24), LAR_I4(r, 28)
-        : "memory");
-}
-__device__ __forceinline__ void tc_st16(uint32_t tmem, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(tmem),
-        LAR_I4(r, 0), LAR_I4(r, 4), LAR_I4(r, 8), LAR_I4(r, 12)
         : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -261,31 +252,6 @@ struct TcWork {
         }
     }
 };
-
-#ifndef LAR_POLY_OF_
-#endif
-#ifndef LAR_POLY_OF
-#define LAR_POLY_OF 99
-#endif
-// 2^x of two numbers on the multiply-add pipe: x = n + f, |f| <= 1/2; 2^f by the cubic of least largest relative error
-// (2^-13.7, found with the Remez exchange; a rounding to bf16 follows), n added to its exponent.  x <= 127; below -126 the result
-// is some number under 2^-125.
-__device__ __forceinline__ void ex2_poly_x2(uint64_t v, float& a, float& b) {
-    float x, y;
-    unpack_f32x2(v, x, y);
-    v = pack_f32x2(fmaxf(x, -126.f), fmaxf(y, -126.f));
-    const uint64_t magic = pack_f32x2(12582912.f, 12582912.f), neg = pack_f32x2(-12582912.f, -12582912.f);
-    const uint64_t t = add_f32x2(v, magic);  // n in the low bits
-    const uint64_t f = fma_f32x2(add_f32x2(t, neg), pack_f32x2(-1.f, -1.f), v);
-    uint64_t p = fma_f32x2(f, pack_f32x2(0.05517167f, 0.05517167f), pack_f32x2(0.24261113f, 0.24261113f));
-    p = fma_f32x2(p, f, pack_f32x2(0.69326097f, 0.69326097f));
-    p = fma_f32x2(p, f, pack_f32x2(0.99992806f, 0.99992806f));
-    float n0, n1;
-    unpack_f32x2(t, n0, n1);
-    unpack_f32x2(p, a, b);
-    a = __int_as_float(__float_as_int(a) + (__float_as_int(n0) << 23));
-    b = __int_as_float(__float_as_int(b) + (__float_as_int(n1) << 23));
-}
 
 // The whole warp waits, and gives up together (what follows are warp-wide instructions).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -568,13 +534,9 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                         for (int i = 0; i < 32; ++i) {
                             float x, y;
                             const uint64_t v = fma_f32x2(pack_f32x2(__uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1])), sc2, mr2);
-                            if (NT == 2 && i % LAR_POLY_OF == LAR_POLY_OF - 1) {
-                                ex2_poly_x2(v, x, y);
-                            } else {
-                                unpack_f32x2(v, x, y);
-                                x = ex2_approx(x);
-                                y = ex2_approx(y);
-                            }
+                            unpack_f32x2(v, x, y);
+                            x = ex2_approx(x);
+                            y = ex2_approx(y);
                             sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(x, y));
                             p[i] = pack_bf16(x, y);
                         }

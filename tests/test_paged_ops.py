@@ -68,6 +68,10 @@ def test_attention_refusals():
     assert need > 0
     assert _attn(big, n=1, ws=4096, nb=need - 1) == lar.LAR_ERR_NOMEM
     assert _attn(big, n=1, ws=4100, nb=need) == INVALID
+    many = _kv(n_seqs=1025, dtype=lar.LAR_BF16)             # bf16: the lengths of at most 1024 sequences are kept on chip
+    assert _attn(many, n=1025) == lar.LAR_ERR_CAPACITY
+    huge = _kv(n_seqs=1024, n_pages=1 << 30, table_cols=1 << 23, page_tokens=128)
+    assert _attn(huge, hq=2, n=1 << 20, q=_r(4096, 128), out=_r(1 << 20, 128)) == lar.LAR_ERR_CAPACITY   # 2^31 slot tiles or more
 
 
 def test_append_refusals():
@@ -354,7 +358,7 @@ def _check_attention(c, hq, causal, start, workspace, seed, out_pad=2, hints=Tru
     q = _randn((T + out_pad, hq, d), dtype, seed) if q is None else q
     buf = torch.full((T + out_pad, hq + 1, d), 5.0, dtype=dtype, device=DEV)     # out is a view with a gap behind each token
     out = buf[:, :hq]
-    mc, ml = (max(c.n), max(c.lens)) if hints else (0, 0)
+    mc, ml = hints if isinstance(hints, tuple) else (max(c.n), max(c.lens)) if hints else (0, 0)
     ws = c.kv.attn_workspace(hq, T + out_pad, mc, ml) if workspace else None
     if ws is not None:
         ws.fill_(255)
@@ -379,6 +383,8 @@ def test_attention(dtype, layout, page, d, hkv, hq, n, lens):
         for workspace in (False, True):
             _check_attention(c, hq, causal, None, workspace, 11)
     _check_attention(c, hq, True, None, True, 12, hints=False)
+    for hints in ((1, 1), (10 ** 6, 10 ** 6)):            # bounds that do not hold choose another launch shape, no other result
+        _check_attention(c, hq, True, None, True, 12, hints=hints)
 
 
 @pytest.mark.gpu
@@ -428,6 +434,15 @@ def test_attention_of_many_ragged_prompts(d, causal):
     c.fill(start, 3)
     _check_attention(c, 8, causal, start, True, 5)
     _check_attention(c, 8, causal, start, False, 6)
+
+
+@pytest.mark.gpu
+def test_attention_of_as_many_sequences_as_there_may_be():
+    n = [1] * 1024
+    c = PagedCase(BF, 64, 1, 16, "nhd", n, [1 + i % 40 for i in range(1024)], seed=1)
+    c.fill(None, 2)
+    for hints in ((1, 40), (40, 40), (300, 40)):          # the kernels for few rows, for one row tile and for two
+        _check_attention(c, 4, True, None, True, 3, hints=hints)
 
 
 @pytest.mark.gpu
