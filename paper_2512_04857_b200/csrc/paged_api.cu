@@ -7,7 +7,7 @@
 #include <string.h>
 
 #include "host_util.h"
-#include "paged_attn_simt.cuh"
+#include "paged_attn_fp32.cuh"
 #include "paged_attn_few.cuh"
 #include "paged_attn_tc.cuh"
 #include "paged_host.h"
@@ -212,13 +212,14 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     return p;
 }
 
-using SimtFn = void (*)(const lar::PagedAttnArgs);
-template <int D, int BM>
-lar_status_t launch_simt(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    SimtFn fn = lar::paged_attn_simt_kernel<D, BM>;
-    constexpr int smem = lar::SimtShape<D, BM>::SMEM;
+// fp32 storage: row tiles of 64 (tensor cores, split tf32) or 16 (CUDA cores).
+template <int D>
+lar_status_t launch_fp32(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
+    void (*fn)(const lar::PagedAttnArgs) = p.bm == 64 ? lar::paged_attn_tf32_kernel<D> : lar::paged_attn_simt_kernel<D>;
+    const int smem = p.bm == 64 ? lar::Tf32Shape<D>::SMEM : lar::SimtShape<D>::SMEM;
+    const int threads = p.bm == 64 ? lar::Tf32Shape<D>::THREADS : lar::SimtShape<D>::THREADS;
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), lar::SimtShape<D, BM>::THREADS, smem, s>>>(a);
+    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), (unsigned)threads, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     if (p.splits > 1) {
         const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.n_kv_heads * a.group;
@@ -459,8 +460,7 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
         if (p.nr == 2) return d == 64 ? launch_tc<64, 0, 2>(*kv, a, p, s) : launch_tc<128, 0, 2>(*kv, a, p, s);
         return d == 64 ? launch_tc<64, 0, 1>(*kv, a, p, s) : launch_tc<128, 0, 1>(*kv, a, p, s);
     }
-    if (p.bm == 16) return d == 64 ? launch_simt<64, 16>(a, p, s) : launch_simt<128, 16>(a, p, s);
-    return d == 64 ? launch_simt<64, 64>(a, p, s) : launch_simt<128, 64>(a, p, s);
+    return d == 64 ? launch_fp32<64>(a, p, s) : launch_fp32<128>(a, p, s);
 }
 
 }  // extern "C"
