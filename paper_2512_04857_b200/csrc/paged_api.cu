@@ -212,14 +212,14 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     return p;
 }
 
-// fp32 storage: row tiles of 64 (tensor cores, split tf32) or 16 (CUDA cores).
+// fp32 storage: row tiles of 64 or 16.
 template <int D>
 lar_status_t launch_fp32(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    void (*fn)(const lar::PagedAttnArgs) = p.bm == 64 ? lar::paged_attn_tf32_kernel<D> : lar::paged_attn_simt_kernel<D>;
-    const int smem = p.bm == 64 ? lar::Tf32Shape<D>::SMEM : lar::SimtShape<D>::SMEM;
-    const int threads = p.bm == 64 ? lar::Tf32Shape<D>::THREADS : lar::SimtShape<D>::THREADS;
+    void (*fn)(const lar::PagedAttnArgs) = p.bm == 64 ? lar::paged_attn_tf32_kernel<D, false> : lar::paged_attn_tf32_kernel<D, true>;
+    const int smem = p.bm == 64 ? lar::Tf32Shape<D, false>::SMEM : lar::Tf32Shape<D, true>::SMEM;
+    constexpr int threads = lar::Tf32Shape<D, false>::THREADS;
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), (unsigned)threads, smem, s>>>(a);
+    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), threads, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     if (p.splits > 1) {
         const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.n_kv_heads * a.group;

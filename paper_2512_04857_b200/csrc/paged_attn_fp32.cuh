@@ -1,9 +1,10 @@
 // Chunk attention for fp32 storage.
 //
-// Two kernels: row tiles of 64 on the tensor cores, with every operand split in two tf32 numbers so that nothing fp32 storage is chosen for is
-// lost, and tiles of 16 rows (a decode step) on the CUDA cores, where the cache's bytes are what counts.  In both a CTA holds its query rows and walks
-// the unit's slots 64 at a time; K of the next step is copied (cp.async) while this step's P V runs, V while the next step's S is
-// formed.  Slots of a unit may be split over gridDim.z CTAs: they leave (O, m, l) in the workspace and combine_splits_kernel joins them.
+// A CTA holds its query rows and walks the unit's slots 64 at a time; K of the next step is copied (cp.async) while this step's P V
+// runs, V while the next step's S is formed.  Slots of a unit may be split over gridDim.z CTAs: they leave (O, m, l) in the
+// workspace and combine_splits_kernel joins them.
+//
+// The products run on the tensor cores with every operand split in two tf32 numbers, so that nothing fp32 storage is chosen for is lost:
 #pragma once
 #include "decode_stream.cuh"  // ldmatrix, ex2_approx
 #include "paged_attn.cuh"
@@ -113,22 +114,24 @@ struct Fp32Unit {
     }
 };
 
-// ------------------------------------------------------------------------------------------ 64 rows: split tf32
 // x = hi + lo with hi the nearest tf32 (11 significant bits, off by 2^-11 at most) and lo exact in fp32, of which the tensor core takes
 // the first 11 bits: hi + lo is x to 2^-21 of it.  A product is hi hi + hi lo + lo hi (lo lo is below 2^-22), each with fp32 accumulation (mma.sync m16n8k8): three
 // products where CUDA cores need one, at 276 TFLOP/s (measured) against 72: a third of that is still more, and a warp's
 // 16 rows cost it no shared-memory traffic per multiply-add.  tcgen05 would do the tf32 products at 4 times that rate, but wants its split
 // operands in shared memory: twice K and V written and read there for every step.
 //
-// A warp owns 16 rows: S (16 x 64), O (16 x D), running maximum and sum in registers.  P goes from the accumulators of S straight
-// into the A operand of P V: the operand's columns q and q + 4 (q = lane % 4) are taken to be slots 2 q and 2 q + 1 of a block of 8, the
-// accumulator's own pair, and V's rows are read in that order.  Rows are padded by 16 bytes: neither the 8 x 4 blocks of ldmatrix nor
-// the single words of V (slots 2 q, columns lane / 4) meet in a bank.
-template <int D>
+// FEW = false: a tile of 64 rows, 16 for each warp: S (16 x 64), O (16 x D), running maximum and sum in registers.  FEW = true (at
+// most 16 rows, a decode step): every warp has all of them and a quarter of the step's slots, with a running maximum of its own; the four
+// results are merged at the end.  Bound by the products, and with few rows by the cache's bytes.
+// P goes from the accumulators of S straight into the A operand of P V: the operand's columns q and q + 4 (q = lane % 4) are taken to be
+// slots 2 q and 2 q + 1 of a block of 8, the accumulator's own pair, and V's rows are read in that order.  Rows are padded by 16 bytes:
+// neither the 8 x 4 blocks of ldmatrix nor the single words of V (slots 2 q, columns lane / 4) meet in a bank.
+template <int D, bool FEW>
 struct Tf32Shape {
-    static constexpr int BM = 64, WARPS = 4, THREADS = WARPS * 32, RS = D + 4;
+    static constexpr int BM = FEW ? 16 : 64, WARPS = 4, THREADS = WARPS * 32, RS = D + 4;
+    static constexpr int NB = FEW ? 2 : 8;  // blocks of 8 slots of a warp in a step
     static constexpr int SMEM = (BM + 2 * kFp32Keys) * RS * 4;
-    static constexpr int PER_SM = D == 64 ? 4 : 2;
+    static constexpr int PER_SM = FEW ? (D == 64 ? 5 : 2) : (D == 64 ? 4 : 2);
 };
 
 // (integer rounding, not cvt.rna.tf32: conversions run at an eighth of the rate and would take longer than the products)
@@ -142,23 +145,24 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Four accumulators by one row operand; the three products of an accumulator lie four instructions apart.
-__device__ __forceinline__ void mma_split4(float (*c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&b)[8]) {
-    uint32_t h[8], l[8];
+// N accumulators by one row operand; the three products of an accumulator lie N instructions apart.
+template <int N>
+__device__ __forceinline__ void mma_split(float (*c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&b)[2 * N]) {
+    uint32_t h[2 * N], l[2 * N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) split_tf32(b[i], h[i], l[i]);
+    for (int i = 0; i < 2 * N; ++i) split_tf32(b[i], h[i], l[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mma_tf32(c[i], al, h[2 * i], h[2 * i + 1]);  // the small parts first
+    for (int i = 0; i < N; ++i) mma_tf32(c[i], al, h[2 * i], h[2 * i + 1]);  // the small parts first
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mma_tf32(c[i], ah, l[2 * i], l[2 * i + 1]);
+    for (int i = 0; i < N; ++i) mma_tf32(c[i], ah, l[2 * i], l[2 * i + 1]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mma_tf32(c[i], ah, h[2 * i], h[2 * i + 1]);
+    for (int i = 0; i < N; ++i) mma_tf32(c[i], ah, h[2 * i], h[2 * i + 1]);
 }
 
-template <int D>
-__global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) paged_attn_tf32_kernel(const PagedAttnArgs a) {
-    using S = Tf32Shape<D>;
-    constexpr int RS = S::RS, NB = kFp32Keys / 8;  // blocks of 8 slots
+template <int D, bool FEW>
+__global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>::PER_SM) paged_attn_tf32_kernel(const PagedAttnArgs a) {
+    using S = Tf32Shape<D, FEW>;
+    constexpr int RS = S::RS, NB = S::NB, GB = NB < 4 ? NB : 4;
     extern __shared__ __align__(16) float sm[];
     float* qs = sm;
     float* ks = qs + S::BM * RS;
@@ -171,15 +175,16 @@ __global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) p
         u.fetch<D>(a, ks, RS, a.kv.k_pool, u.b0 * kFp32Keys, true);
         u.fetch<D>(a, vs, RS, a.kv.v_pool, u.b0 * kFp32Keys, false);
     }
-    const int row0 = warp * 16 + qrow;  // this thread's rows: row0, row0 + 8
-    const bool active = warp * 16 < u.rows;
+    const int row_w = FEW ? 0 : warp * 16, slot_w = FEW ? warp * 16 : 0;  // the warp's first row, first slot of a step
+    const int row0 = row_w + qrow;  // this thread's rows: row0, row0 + 8
+    const bool active = row_w < u.rows;
     const int last[2] = {u.last_slot(a, row0), u.last_slot(a, row0 + 8)};
     const int min_last = u.last_slot(a, 0);
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[D / 8][4];
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    const uint32_t q_at = smem_u32(qs + (warp * 16 + (lane & 15)) * RS + (lane >> 4) * 4);
-    const uint32_t k_at = smem_u32(ks + ((lane & 7) + (lane >> 4) * 8) * RS + ((lane >> 3) & 1) * 4);
+    const uint32_t q_at = smem_u32(qs + (row_w + (lane & 15)) * RS + (lane >> 4) * 4);
+    const uint32_t k_at = smem_u32(ks + (slot_w + (lane & 7) + (lane >> 4) * 8) * RS + ((lane >> 3) & 1) * 4);
 
     for (int b = u.b0; b < u.b1; ++b) {
         const int j0 = b * kFp32Keys;
@@ -196,11 +201,11 @@ __global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) p
 #pragma unroll
                 for (int e = 0; e < 4; ++e) split_tf32(x[e], ah[e], al[e]);
 #pragma unroll
-                for (int i = 0; i < NB; i += 4) {
-                    uint32_t y[8];  // four blocks of 8 slots, two 4-element halves each
-                    ldmatrix_x4(k_at + (i * 8 * RS + k * 8) * 4, reinterpret_cast<uint32_t(&)[4]>(y[0]));
-                    ldmatrix_x4(k_at + ((i + 2) * 8 * RS + k * 8) * 4, reinterpret_cast<uint32_t(&)[4]>(y[4]));
-                    mma_split4(s + i, ah, al, y);
+                for (int i = 0; i < NB; i += GB) {
+                    uint32_t y[2 * GB];  // blocks of 8 slots, two 4-element halves each
+#pragma unroll
+                    for (int e = 0; e < GB; e += 2) ldmatrix_x4(k_at + ((i + e) * 8 * RS + k * 8) * 4, reinterpret_cast<uint32_t(&)[4]>(y[2 * e]));
+                    mma_split<GB>(s + i, ah, al, y);
                 }
             }
         }
@@ -213,7 +218,7 @@ __global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) p
                 for (int i = 0; i < NB; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int slot = j0 + i * 8 + 2 * quad + (e & 1);
+                        const int slot = j0 + slot_w + i * 8 + 2 * quad + (e & 1);
                         if (slot < u.lo || slot > last[e >> 1]) s[i][e] = -INFINITY;
                     }
             }
@@ -253,7 +258,7 @@ __global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) p
                 split_tf32(__float_as_uint(s[i][2]), ah[1], al[1]);
                 split_tf32(__float_as_uint(s[i][1]), ah[2], al[2]);
                 split_tf32(__float_as_uint(s[i][3]), ah[3], al[3]);
-                const float* v = vs + (i * 8 + 2 * quad) * RS + qrow;
+                const float* v = vs + (slot_w + i * 8 + 2 * quad) * RS + qrow;
 #pragma unroll
                 for (int n = 0; n < D / 8; n += 4) {
                     uint32_t y[8];
@@ -262,7 +267,7 @@ __global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) p
                         y[2 * e] = __float_as_uint(v[(n + e) * 8]);
                         y[2 * e + 1] = __float_as_uint(v[RS + (n + e) * 8]);
                     }
-                    mma_split4(o + n, ah, al, y);
+                    mma_split<4>(o + n, ah, al, y);
                 }
             }
         }
@@ -276,172 +281,50 @@ __global__ void __launch_bounds__(Tf32Shape<D>::THREADS, Tf32Shape<D>::PER_SM) p
     for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+    }
+    if constexpr (FEW) {
+        // the warps' parts side by side where K was (everybody is behind the last step's barrier, no copy is in flight)
+        constexpr int PS = D + 2;
+        static_assert(S::WARPS * S::BM * PS <= kFp32Keys * RS, "the parts fit where K was");
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float* p = ks + (warp * S::BM + row0 + 8 * r) * PS;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(p + n * 8 + 2 * quad) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
+            if (quad == 0) *reinterpret_cast<float2*>(p + D) = make_float2(m[r], l[r]);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < u.rows * (D / 2); i += S::THREADS) {
+            const int row = i / (D / 2), e = i % (D / 2) * 2;
+            const float* p = ks + row * PS;
+            float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+            for (int w = 0; w < S::WARPS; ++w) M = fmaxf(M, p[w * S::BM * PS + D]);
+            const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int w = 0; w < S::WARPS; ++w) {
+                const float2 ml = *reinterpret_cast<const float2*>(p + w * S::BM * PS + D), v = *reinterpret_cast<const float2*>(p + w * S::BM * PS + e);
+                const float f = ex2_approx(ml.x - ref);
+                L = fmaf(ml.y, f, L);
+                x = fmaf(v.x, f, x);
+                y = fmaf(v.y, f, y);
+            }
+            const float inv = a.n_splits > 1 ? 1.f : L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
+            *reinterpret_cast<float2*>(u.out_row(a, row, D) + e) = make_float2(x * inv, y * inv);
+            if (a.n_splits > 1 && e == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(M, L);
+        }
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
         const int row = row0 + 8 * r;
         if (row >= u.rows) continue;
-        const float inv = a.n_splits > 1 ? 1.f : l[r] > 0.f ? 1.0f / l[r] : l[r];  // nothing seen: 0; NaN stays NaN
+        const float inv = a.n_splits > 1 ? 1.f : l[r] > 0.f ? 1.0f / l[r] : l[r];
         float* dst = u.out_row(a, row, D) + 2 * quad;
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(o[n][2 * r] * inv, o[n][2 * r + 1] * inv);
         if (a.n_splits > 1 && quad == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(m[r], l[r]);
-    }
-}
-
-// ------------------------------------------------------------------------------------------ 16 rows: CUDA cores
-// S = Q K^T and O += P V as register tiles of 4 rows by 2 keys (columns), operands row by row in shared memory, Q and K padded by 16 bytes
-// (the 16-byte loads of the 8 lanes of a quarter warp fall into different banks).
-template <int D>
-struct SimtShape {
-    static constexpr int BM = 16, RT = 4;            // rows of a tile, of a thread: rg, rg + RG, ...
-    static constexpr int KG = 32, RG = BM / RT;      // threads along the keys, along the rows
-    static constexpr int THREADS = KG * RG;
-    static constexpr int KC = kFp32Keys / KG;        // keys of a thread: kg, kg + KG, ...
-    static constexpr int OC = D / KG;                // output columns of a thread
-    static constexpr int QS = D + 4, KS = D + 4, PS = BM + 4;
-    static constexpr int SMEM = (BM * QS + kFp32Keys * KS + kFp32Keys * D + kFp32Keys * PS) * 4;
-};
-
-template <int N>
-struct FVec;
-template <> struct FVec<2> { using type = float2; };
-template <> struct FVec<4> { using type = float4; };
-
-template <int N>
-__device__ __forceinline__ void load_vec(const float* p, float* v) {
-    *reinterpret_cast<typename FVec<N>::type*>(v) = *reinterpret_cast<const typename FVec<N>::type*>(p);
-}
-
-template <int D>
-__global__ void __launch_bounds__(SimtShape<D>::THREADS) paged_attn_simt_kernel(const PagedAttnArgs a) {
-    using S = SimtShape<D>;
-    constexpr int RT = S::RT;
-    extern __shared__ __align__(16) float sm[];
-    float* qs = sm;                      // [BM][QS]
-    float* ks = qs + S::BM * S::QS;      // [64][KS]
-    float* vs = ks + kFp32Keys * S::KS;  // [64][D]
-    float* pt = vs + kFp32Keys * D;      // [64][PS]
-    const int kg = threadIdx.x % S::KG, rg = threadIdx.x / S::KG;
-    Fp32Unit u;
-    if (!u.find(a)) return;
-    u.fetch_q<D>(a, qs, S::QS, S::BM);
-    if (u.b0 < u.b1) {
-        u.fetch<D>(a, ks, S::KS, a.kv.k_pool, u.b0 * kFp32Keys, true);
-        u.fetch<D>(a, vs, D, a.kv.v_pool, u.b0 * kFp32Keys, false);
-    }
-
-    uint64_t o[RT][S::OC / 2];  // pairs of columns
-    float m[RT], l[RT];
-    int last[RT];  // last slot each row sees
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        m[r] = -INFINITY;
-        l[r] = 0.f;
-        const int row = rg + S::RG * r;
-        last[r] = u.last_slot(a, row);
-#pragma unroll
-        for (int i = 0; i < S::OC / 2; ++i) o[r][i] = 0;
-    }
-
-    for (int b = u.b0; b < u.b1; ++b) {
-        const int j0 = b * kFp32Keys;
-        copy_wait<1>();   // K of this step (V may be on its way)
-        __syncthreads();
-        float s[RT][S::KC];
-        {
-            uint64_t acc[RT][S::KC];  // sums over the even and the odd elements of a row
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int k = 0; k < S::KC; ++k) acc[r][k] = 0;
-#pragma unroll 2
-            for (int d = 0; d < D; d += 4) {
-                ulonglong2 kv[S::KC];
-#pragma unroll
-                for (int k = 0; k < S::KC; ++k) kv[k] = *reinterpret_cast<const ulonglong2*>(ks + (kg + k * S::KG) * S::KS + d);
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const ulonglong2 qv = *reinterpret_cast<const ulonglong2*>(qs + (rg + S::RG * r) * S::QS + d);
-#pragma unroll
-                    for (int k = 0; k < S::KC; ++k) acc[r][k] = fma_f32x2(qv.y, kv[k].y, fma_f32x2(qv.x, kv[k].x, acc[r][k]));
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int k = 0; k < S::KC; ++k) {
-                    float even, odd;
-                    unpack_f32x2(acc[r][k], even, odd);
-                    s[r][k] = even + odd;
-                }
-        }
-        __syncthreads();  // K has been read
-        if (b + 1 < u.b1) u.fetch<D>(a, ks, S::KS, a.kv.k_pool, j0 + kFp32Keys, true);
-        else copy_commit();
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < S::KC; ++k) {
-                const int slot = j0 + kg + k * S::KG;
-                s[r][k] = slot >= u.lo && slot <= last[r] ? s[r][k] * a.scale_log2 : -INFINITY;
-                mx = fmaxf(mx, s[r][k]);
-            }
-#pragma unroll
-            for (int w = S::KG / 2; w >= 1; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-            const float mn = fmaxf(m[r], mx), ref = mn == -INFINITY ? 0.f : mn;  // (a row that has seen nothing yet)
-            const float corr = exp2f(m[r] - ref);
-            m[r] = mn;
-            float sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < S::KC; ++k) {
-                s[r][k] = exp2f(s[r][k] - ref);
-                sum += s[r][k];
-            }
-            l[r] = l[r] * corr + sum;  // (this thread's keys only: joined over the threads of the row at the end)
-#pragma unroll
-            for (int i = 0; i < S::OC / 2; ++i) o[r][i] = mul_f32x2(o[r][i], pack_f32x2(corr, corr));
-        }
-#pragma unroll
-        for (int k = 0; k < S::KC; ++k)
-#pragma unroll
-            for (int r = 0; r < RT; r += 4)
-                *reinterpret_cast<float4*>(pt + (kg + k * S::KG) * S::PS + rg * RT + r) = make_float4(s[r][k], s[r + 1][k], s[r + 2][k], s[r + 3][k]);
-        copy_wait<1>();   // V of this step
-        __syncthreads();
-#pragma unroll 4
-        for (int j = 0; j < kFp32Keys; ++j) {
-            float pv[RT];
-#pragma unroll
-            for (int r = 0; r < RT; r += 4) load_vec<4>(pt + j * S::PS + rg * RT + r, pv + r);
-            uint64_t vv[S::OC / 2];
-            load_vec<S::OC>(vs + j * D + kg * S::OC, reinterpret_cast<float*>(vv));
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int e = 0; e < S::OC / 2; ++e) o[r][e] = fma_f32x2(pack_f32x2(pv[r], pv[r]), vv[e], o[r][e]);
-        }
-        __syncthreads();  // V and P have been read
-        if (b + 1 < u.b1) u.fetch<D>(a, vs, D, a.kv.v_pool, j0 + kFp32Keys, false);
-        else copy_commit();
-    }
-    copy_commit();
-    copy_wait<0>();  // (nothing is in flight when the CTA ends)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-#pragma unroll
-        for (int w = S::KG / 2; w >= 1; w >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
-        const int row = rg + S::RG * r;
-        if (row >= u.rows) continue;
-        const float inv = a.n_splits > 1 ? 1.f : l[r] > 0.f ? 1.0f / l[r] : l[r];  // nothing seen: 0; NaN stays NaN
-        typename FVec<S::OC>::type v;
-#pragma unroll
-        for (int e = 0; e < S::OC / 2; ++e) {
-            float x, y;
-            unpack_f32x2(o[r][e], x, y);
-            reinterpret_cast<float*>(&v)[2 * e] = x * inv;
-            reinterpret_cast<float*>(&v)[2 * e + 1] = y * inv;
-        }
-        *reinterpret_cast<typename FVec<S::OC>::type*>(u.out_row(a, row, D) + kg * S::OC) = v;
-        if (a.n_splits > 1 && kg == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(m[r], l[r]);
     }
 }
 
