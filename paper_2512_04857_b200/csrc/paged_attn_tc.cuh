@@ -254,6 +254,23 @@ struct TcWork {
     }
 };
 
+// Transposes a 4 x 4 matrix of 16-byte pieces held a row per lane by four neighbouring lanes.
+__device__ __forceinline__ void quad_transpose(uint4 (&c)[4], int lane) {
+    auto swap = [&](uint4& a, uint4& b, int mask) {  // the lower lane gives b and keeps a, the upper one gives a and keeps b
+        const bool upper = (lane & mask) != 0;
+        uint4 s = upper ? a : b;
+        s.x = __shfl_xor_sync(0xffffffffu, s.x, mask);
+        s.y = __shfl_xor_sync(0xffffffffu, s.y, mask);
+        s.z = __shfl_xor_sync(0xffffffffu, s.z, mask);
+        s.w = __shfl_xor_sync(0xffffffffu, s.w, mask);
+        if (upper) a = s; else b = s;
+    };
+    swap(c[0], c[1], 1);
+    swap(c[2], c[3], 1);
+    swap(c[0], c[2], 2);
+    swap(c[1], c[3], 2);
+}
+
 // The whole warp waits, and gives up together (what follows are warp-wide instructions).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
@@ -498,7 +515,12 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                         const int c_lo = g.lo - base_slot, c_hi = last - base_slot;
 #pragma unroll
                         for (int c = 0; c < BN; ++c)
-                            if (c < c_lo || c > c_hi) s[c] = 0xff800000u;
+                            if (c > c_hi) s[c] = 0xff800000u;
+                        if (c_lo > 0) {
+#pragma unroll
+                            for (int c = 0; c < BN; ++c)
+                                if (c < c_lo) s[c] = 0xff800000u;
+                        }
                     }
                     float mx[4] = {m_used, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -572,10 +594,24 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             // the output rows, or this CTA's part of them
             if (n > 0 && !(ok = product_wait(steps - 1))) break;
             const bool mine = row < rows;
-            const long long tok = g.tok0 + tile * a.tq + t;
             const int slotp = blockIdx.x * 2 + (g.b0 > 0 ? 0 : 1);
             if (active) {
                 const float inv = g.whole ? (l > 0.f ? 1.0f / l : l) : 1.f;  // nothing seen: 0; NaN stays NaN
+                const size_t part = ((size_t)slotp * NT + tile) * ta.rows_cap + row;
+                // a thread has a row, but four neighbours write 64 bytes of one row together
+                unsigned long long own_row = 0;
+                if (mine)
+                    own_row = g.whole ? reinterpret_cast<unsigned long long>(a.out.p) + 2 * ((long long)(g.tok0 + tile * a.tq + t) * a.out.token_stride + (long long)(g.head * G + head_g) * a.out.head_stride)
+                                      : reinterpret_cast<unsigned long long>(a.part_o + part * D);
+                char* rows4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) rows4[i] = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, own_row, (lane & 28) + i));
+                auto put = [&](uint4 (&c)[4], int offset) {
+                    quad_transpose(c, lane);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (rows4[i]) *reinterpret_cast<uint4*>(rows4[i] + offset + (lane & 3) * 16) = c[i];
+                };
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
@@ -586,26 +622,28 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = 0;
                     }
-                    if (mine && g.whole) {
-                        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + tok * a.out.token_stride + (long long)(g.head * G + head_g) * a.out.head_stride + c;
+                    uint4 u[4];
+                    if (g.whole) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint4 u;
-                            u.x = pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-                            u.y = pack_bf16(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-                            u.z = pack_bf16(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-                            u.w = pack_bf16(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-                            *reinterpret_cast<uint4*>(dst + i) = u;
+                        for (int i = 0; i < 4; ++i) {
+                            u[i].x = pack_bf16(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
+                            u[i].y = pack_bf16(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
+                            u[i].z = pack_bf16(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
+                            u[i].w = pack_bf16(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
                         }
-                    } else if (mine) {
-                        float* dst = a.part_o + (((size_t)slotp * NT + tile) * ta.rows_cap + row) * D + c;
+                        put(u, c * 2);
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(dst + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        for (int h = 0; h < 32; h += 16) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) u[i] = make_uint4(o[h + 4 * i], o[h + 4 * i + 1], o[h + 4 * i + 2], o[h + 4 * i + 3]);
+                            put(u, (c + h) * 4);
+                        }
                     }
                     __syncwarp();  // (tcgen05.ld is a warp-wide instruction: all lanes together again)
                 }
                 if (mine && !g.whole) {
-                    float* ml = a.part_ml + (((size_t)slotp * NT + tile) * ta.rows_cap + row) * 2;
+                    float* ml = a.part_ml + part * 2;
                     ml[0] = m_used * sc;  // (-inf: nothing seen)
                     ml[1] = l;
                 }
