@@ -115,7 +115,7 @@ struct Fp32Unit {
 };
 
 // x = hi + lo with hi the nearest tf32 (11 significant bits, off by 2^-11 at most) and lo exact in fp32, of which the tensor core takes
-// the first 11 bits: hi + lo is x to 2^-21 of it.  A product is hi hi + hi lo + lo hi (lo lo is below 2^-22), each with fp32 accumulation (mma.sync m16n8k8): three
+// the first 11 bits: hi + lo is x to 2^-21 of it.  A product is hi hi + hi lo + lo hi (lo lo is below 2^-22; mma.sync m16n8k8): three
 // products where CUDA cores need one, at 276 TFLOP/s (measured) against 72: a third of that is still more, and a warp's
 // 16 rows cost it no shared-memory traffic per multiply-add.  tcgen05 would do the tf32 products at 4 times that rate, but wants its split
 // operands in shared memory: twice K and V written and read there for every step.
@@ -131,7 +131,7 @@ struct Tf32Shape {
     static constexpr int BM = FEW ? 16 : 64, WARPS = 4, THREADS = WARPS * 32, RS = D + 4;
     static constexpr int NB = FEW ? 2 : 8;  // blocks of 8 slots of a warp in a step
     static constexpr int SMEM = (BM + 2 * kFp32Keys) * RS * 4;
-    static constexpr int PER_SM = FEW ? (D == 64 ? 5 : 2) : (D == 64 ? 4 : 2);
+    static constexpr int PER_SM = D == 128 ? 2 : FEW ? 4 : 3;
 };
 
 // (integer rounding, not cvt.rna.tf32: conversions run at an eighth of the rate and would take longer than the products)
@@ -145,18 +145,25 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// N accumulators by one row operand; the three products of an accumulator lie N instructions apart.
+// N products by one row operand.  The tensor core's accumulation cuts its sum off instead of rounding it (an fp32 sum of many
+// products drifts towards zero: 2.4e-6 of the result where all 432 products of a row went into one accumulator), so the large products
+// and the small ones have accumulators of their own, of few products each, and are added up with rounded additions.
 template <int N>
-__device__ __forceinline__ void mma_split(float (*c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&b)[2 * N]) {
+__device__ __forceinline__ void mma_split(float (*big)[4], float (*small)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&b)[2 * N]) {
     uint32_t h[2 * N], l[2 * N];
 #pragma unroll
     for (int i = 0; i < 2 * N; ++i) split_tf32(b[i], h[i], l[i]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) mma_tf32(c[i], al, h[2 * i], h[2 * i + 1]);  // the small parts first
+    for (int i = 0; i < N; ++i) mma_tf32(small[i], al, h[2 * i], h[2 * i + 1]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) mma_tf32(c[i], ah, l[2 * i], l[2 * i + 1]);
+    for (int i = 0; i < N; ++i) mma_tf32(big[i], ah, h[2 * i], h[2 * i + 1]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) mma_tf32(c[i], ah, h[2 * i], h[2 * i + 1]);
+    for (int i = 0; i < N; ++i) mma_tf32(small[i], ah, l[2 * i], l[2 * i + 1]);
+}
+template <int N>
+__device__ __forceinline__ void clear_tiles(float (*c)[4]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
 }
 
 template <int D, bool FEW>
@@ -192,8 +199,9 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
         __syncthreads();
         float s[NB][4];
         if (active) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+            float small[NB][4];
+            clear_tiles<NB>(s);
+            clear_tiles<NB>(small);
 #pragma unroll 2
             for (int k = 0; k < D / 8; ++k) {
                 uint32_t x[4], ah[4], al[4];
@@ -205,9 +213,13 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
                     uint32_t y[2 * GB];  // blocks of 8 slots, two 4-element halves each
 #pragma unroll
                     for (int e = 0; e < GB; e += 2) ldmatrix_x4(k_at + ((i + e) * 8 * RS + k * 8) * 4, reinterpret_cast<uint32_t(&)[4]>(y[2 * e]));
-                    mma_split<GB>(s + i, ah, al, y);
+                    mma_split<GB>(s + i, small + i, ah, al, y);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[i][e] += small[i][e];
         }
         __syncthreads();  // K has been read
         if (b + 1 < u.b1) u.fetch<D>(a, ks, RS, a.kv.k_pool, j0 + kFp32Keys, true);
@@ -252,23 +264,30 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
         __syncthreads();
         if (active) {
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                uint32_t ah[4], al[4];
-                split_tf32(__float_as_uint(s[i][0]), ah[0], al[0]);
-                split_tf32(__float_as_uint(s[i][2]), ah[1], al[1]);
-                split_tf32(__float_as_uint(s[i][1]), ah[2], al[2]);
-                split_tf32(__float_as_uint(s[i][3]), ah[3], al[3]);
-                const float* v = vs + (slot_w + i * 8 + 2 * quad) * RS + qrow;
+            for (int n = 0; n < D / 8; n += 4) {  // four blocks of 8 columns at a time, summed over the step's slots on their own
+                float big[4][4], small[4][4];
+                clear_tiles<4>(big);
+                clear_tiles<4>(small);
 #pragma unroll
-                for (int n = 0; n < D / 8; n += 4) {
+                for (int i = 0; i < NB; ++i) {
+                    uint32_t ah[4], al[4];
+                    split_tf32(__float_as_uint(s[i][0]), ah[0], al[0]);
+                    split_tf32(__float_as_uint(s[i][2]), ah[1], al[1]);
+                    split_tf32(__float_as_uint(s[i][1]), ah[2], al[2]);
+                    split_tf32(__float_as_uint(s[i][3]), ah[3], al[3]);
+                    const float* v = vs + (slot_w + i * 8 + 2 * quad) * RS + qrow + n * 8;
                     uint32_t y[8];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        y[2 * e] = __float_as_uint(v[(n + e) * 8]);
-                        y[2 * e + 1] = __float_as_uint(v[RS + (n + e) * 8]);
+                        y[2 * e] = __float_as_uint(v[e * 8]);
+                        y[2 * e + 1] = __float_as_uint(v[RS + e * 8]);
                     }
-                    mma_split<4>(o + n, ah, al, y);
+                    mma_split<4>(big, FEW ? big : small, ah, al, y);  // (FEW: two blocks, six products in all)
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n + i][e] += FEW ? big[i][e] : big[i][e] + small[i][e];
             }
         }
         __syncthreads();  // V has been read
