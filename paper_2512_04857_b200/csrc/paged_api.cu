@@ -133,8 +133,8 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
 // ------------------------------------------------------------------------------------------ chunk attention
 struct AttnPlan {
     int tq;        // tokens of a row tile
-    int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows; 0: at most 16 rows, the kernel for few rows)
-    int nr;        // bf16, few rows: blocks of 8 rows
+    int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows; 0: the kernel for few rows)
+    int nr;        // bf16, few rows: blocks of 8 rows (two with 64-element rows only)
     int stages, grid, rows_cap;  // bf16: K/V ring, persistent CTAs, rows of a row tile
     int splits;    // bf16: 1 units stay whole, 2 they may be cut, 3 they are handed out on demand; fp32: CTAs along a unit's slots
     int bm, tiles; // fp32: rows of a tile, bound on the row tiles of all sequences
@@ -157,13 +157,17 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     const int d = k.head_dim;
     if (k.dtype == LAR_BF16) {
         constexpr size_t kSmem = 227 * 1024;
-        p.nt = chunk * group > 128 ? 2 : chunk * group > lar::kFewRows ? 1 : 0;
+        // Two row tiles above 128 rows, and with 128-element rows and long caches above 32 (one row tile leaves its two CTAs per SM two
+        // stages each; 16 x 4288 slots, one / two row tiles: 32 rows 62 / 65 us, 64 rows 75 / 66, 128 rows 78 / 69, 192 rows 120 / 74; 64 x 577
+        // slots, 64 rows 55 / 59; 64-element rows 44 / 55, 48 / 56, 72 / 68).
+        const int64_t rows = chunk * group;
+        p.nt = rows > 128 || (d == 128 && rows > 32 && len >= 2048) ? 2 : rows > lar::few_rows(d) ? 1 : 0;
         if (p.nt == 0) {
             p.tq = (int)chunk;
             p.rows_cap = p.tq * group;
             p.nr = p.rows_cap > 8 ? 2 : 1;
             p.smem = d == 64 ? (p.nr == 1 ? lar::FewShape<64, 1>::bytes(k.n_seqs) : lar::FewShape<64, 2>::bytes(k.n_seqs))
-                             : (p.nr == 1 ? lar::FewShape<128, 1>::bytes(k.n_seqs) : lar::FewShape<128, 2>::bytes(k.n_seqs));
+                             : lar::FewShape<128, 1>::bytes(k.n_seqs);
             const int fit = (int)(233472 / (p.smem + 1024)), want = d == 64 ? lar::FewShape<64, 1>::PER_SM : lar::FewShape<128, 1>::PER_SM;
             p.grid = (fit < want ? fit : want) * kSms;
             p.splits = split ? 2 : 1;
@@ -311,6 +315,14 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     lar_status_t st = make_maps(k, a, t.box_rows, m);
     if (st != LAR_OK) return st;
     constexpr auto fn = S::fn;
+    if (NT_ == 2) {
+        // the softmax warps take registers that the block has to have been launched with: a build that gives it fewer is refused
+        static const int regs = [] {
+            cudaFuncAttributes at;
+            return cudaFuncGetAttributes(&at, (const void*)S::fn) == cudaSuccess ? at.numRegs : 0;
+        }();
+        if (regs * 3 < 2 * lar::TcShape<D, 2>::SM_REGS + lar::TcShape<D, 2>::OTHER_REGS) return LAR_ERR_CUDA;
+    }
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
     fn<<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
     LAR_CUDA(cudaGetLastError());
@@ -457,7 +469,7 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     if (kv->dtype == LAR_BF16) {
         if (p.nt == 2) return d == 64 ? launch_tc<64, 2>(*kv, a, p, s) : launch_tc<128, 2>(*kv, a, p, s);
         if (p.nt == 1) return d == 64 ? launch_tc<64, 1>(*kv, a, p, s) : launch_tc<128, 1>(*kv, a, p, s);
-        if (p.nr == 2) return d == 64 ? launch_tc<64, 0, 2>(*kv, a, p, s) : launch_tc<128, 0, 2>(*kv, a, p, s);
+        if (p.nr == 2) return launch_tc<64, 0, 2>(*kv, a, p, s);
         return d == 64 ? launch_tc<64, 0, 1>(*kv, a, p, s) : launch_tc<128, 0, 1>(*kv, a, p, s);
     }
     return d == 64 ? launch_fp32<64>(a, p, s) : launch_fp32<128>(a, p, s);
