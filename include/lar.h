@@ -303,7 +303,8 @@ lar_status_t lar_attend_dense_noalloc(const void* q, const void* k, const void* 
  * over the cache.  They keep no state: the caller describes its cache in a lar_paged_kv_t (lar_cache_paged_view describes
  * a layer of the library's own cache the same way).  Device pointers belong to the device that is current at the call;
  * work is only enqueued on `stream`, nothing is allocated, and every call may be captured into a CUDA graph (launch
- * shapes depend on the host arguments alone; lengths, positions and page tables are read on the device at replay).
+ * shapes depend on the host arguments alone; lengths, positions and page tables are read on the device at replay).  At most
+ * 4096 heads and 2^26 tokens a call; no tokens: nothing is done.
  * ------------------------------------------------------------------------------------------------------------------ */
 
 /* Rotary position embedding with 1 to 4 position axes.  Pair i of a row of head_dim elements is turned by the angle

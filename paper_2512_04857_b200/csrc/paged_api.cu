@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kSms = 148;             // SMs of a B200 (launch shapes only)
 constexpr int64_t kMaxTokens = 1 << 26;
+constexpr int kMaxHeads = 4096;       // (the rotary kernel divides row numbers by multiplication: rows of two tokens x rows of one < 2^32)
 
 int elt_of(int dtype) { return dtype == LAR_BF16 ? 2 : 4; }
 bool is_dtype(int dtype) { return dtype == LAR_BF16 || dtype == LAR_FP32; }
@@ -60,7 +61,7 @@ bool rows_view(const lar_rows_t* r, int64_t tokens, int heads, int d, int elt, b
 bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, lar::PagedView& v) {
     if (!k || k->struct_size != sizeof(lar_paged_kv_t) || !is_dtype(k->dtype)) return false;
     if (k->n_seqs < 1 || k->n_kv_heads < 1 || !(k->head_dim == 64 || k->head_dim == 128)) return false;
-    if (k->n_kv_heads > (1 << 16)) return false;
+    if (k->n_kv_heads > kMaxHeads) return false;
     int shift = 4;
     while (shift < 8 && (1 << shift) != k->page_tokens) ++shift;
     if (shift == 8 || k->n_pages < 1 || k->table_cols < 1) return false;
@@ -122,7 +123,7 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
     if (slices > most) slices = most;
     a.rows_per_slice = (a.n_rows + slices - 1) / slices;
     slices = (a.n_rows + a.rows_per_slice - 1) / a.rows_per_slice;
-    a.rows_magic = (unsigned)((1ull << 32) / (unsigned)a.rows_per_slice + 1ull);
+    a.rows_magic = a.rows_per_slice > 1 ? (unsigned)((1ull << 32) / (unsigned)a.rows_per_slice + 1ull) : 0u;
     const size_t smem = (size_t)a.tokens_per_cta * (d + 2) * 4;
     if (slices > 65535) return LAR_ERR_CAPACITY;
     fn<<<dim3((unsigned)token_blocks, (unsigned)slices), lar::kRopeThreads, smem, s>>>(a);
@@ -353,11 +354,11 @@ lar_status_t paged_append(const lar_paged_kv_t& kv, const lar_rope_t* rope, cons
     memset(&a, 0, sizeof(a));
     if (!paged_view(&kv, n_tokens, cu_tokens, a.kv)) return LAR_ERR_INVALID_ARG;
     if (rope && (!rope_freqs(rope, 0, a.f) || rope->head_dim != kv.head_dim)) return LAR_ERR_INVALID_ARG;
+    if (n_tokens == 0) return LAR_OK;
     if ((rope != nullptr) != (pos != nullptr) || !aligned(pos, 4)) return LAR_ERR_INVALID_ARG;
     if (rope && rope->n_axes > 1 && pos_axis_stride < n_tokens) return LAR_ERR_INVALID_ARG;
-    if (n_q_heads < 0 || n_q_heads > (1 << 16) || (n_q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr)) return LAR_ERR_INVALID_ARG;
+    if (n_q_heads < 0 || n_q_heads > kMaxHeads || (n_q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr)) return LAR_ERR_INVALID_ARG;
     const int elt = elt_of(kv.dtype);
-    if (n_tokens == 0) return LAR_OK;
     if (q && (!rows_view(q, n_tokens, n_q_heads, kv.head_dim, elt, false, a.src[0]) ||
               !rows_view(q_out, n_tokens, n_q_heads, kv.head_dim, elt, true, a.dst[0])))
         return LAR_ERR_INVALID_ARG;
@@ -406,7 +407,7 @@ lar_status_t lar_rope_rotate(const lar_rope_t* rope, int dtype, const int32_t* p
     if (!rope_freqs(rope, inverse, a.f) || !is_dtype(dtype) || n_tokens < 0 || n_tokens > kMaxTokens) return LAR_ERR_INVALID_ARG;
     if (rope->n_axes > 1 && pos_axis_stride < n_tokens) return LAR_ERR_INVALID_ARG;
     const int elt = elt_of(dtype), d = rope->head_dim;
-    if (n_q_heads < 1 || n_q_heads > (1 << 16) || n_kv_heads < 0 || n_kv_heads > (1 << 16)) return LAR_ERR_INVALID_ARG;
+    if (n_q_heads < 1 || n_q_heads > kMaxHeads || n_kv_heads < 0 || n_kv_heads > kMaxHeads) return LAR_ERR_INVALID_ARG;
     if ((n_kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr)) return LAR_ERR_INVALID_ARG;
     if (n_tokens == 0) return LAR_OK;
     if (!pos || !aligned(pos, 4)) return LAR_ERR_INVALID_ARG;
@@ -443,7 +444,7 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     memset(&a, 0, sizeof(a));
     if (!paged_view(kv, n_tokens, cu_tokens, a.kv) || n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return LAR_ERR_INVALID_ARG;
     const int group = n_q_heads / kv->n_kv_heads;
-    if (group > 16 || kv->n_kv_heads > 65535) return LAR_ERR_INVALID_ARG;
+    if (group > 16) return LAR_ERR_INVALID_ARG;
     if (!(softmax_scale >= 0.f) || !isfinite(softmax_scale) || max_chunk < 0 || max_len < 0 || !aligned(kv_start, 4)) return LAR_ERR_INVALID_ARG;
     if (n_tokens == 0) return LAR_OK;
     const int elt = elt_of(kv->dtype), d = kv->head_dim;

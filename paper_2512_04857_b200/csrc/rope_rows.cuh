@@ -39,7 +39,7 @@ struct RopeRowsArgs {
     int heads[3];
     int n_rows;             // heads[0] + heads[1] + heads[2]
     int rows_per_slice;     // rows of a token that one CTA handles (grid.y slices)
-    unsigned rows_magic;    // floor(2^32 / rows_per_slice) + 1
+    unsigned rows_magic;    // floor(2^32 / rows_per_slice) + 1, which 32 bits do not hold for one row: 0
     int n_tokens, tokens_per_cta;
     PagedView kv;           // PAGED only
     // the library's own cache (PAGED, may be null): every unit's length and index map advance with the append
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_co
         for (int b = 0; b < kRopeBatch; ++b) {
             const int item = base + b * kRopeThreads + tid;
             const int r = item / IPR;
-            const int tl = (int)__umulhi((unsigned)r, a.rows_magic);
+            const int tl = a.rows_magic ? (int)__umulhi((unsigned)r, a.rows_magic) : r;
             const int rl = r - tl * a.rows_per_slice;
             tok[b] = item < n_items && rl < nr ? tl : -1;
             row[b] = row0 + rl;

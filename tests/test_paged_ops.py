@@ -84,7 +84,9 @@ def test_append_refusals():
     assert call(k=None) == INVALID and call(v=_r(None)) == INVALID and call(k=_r(4097, 128, 64)) == INVALID
     assert call(q=rows) == INVALID and call(q=rows, qo=rows) == INVALID and call(hq=2) == INVALID and call(hq=-1) == INVALID
     assert call(rope=lar.make_rope(128, (64,))) == INVALID  # another head_dim
-    assert call(n=7) == INVALID and call(cu=255) == INVALID and call(n=0) == lar.LAR_OK
+    assert call(n=7) == INVALID and call(cu=255) == INVALID
+    assert call(n=0) == lar.LAR_OK and call(n=0, pos=None, k=None) == lar.LAR_OK
+    assert call(kv=_kv(n_kv_heads=4097, table_head_stride=4, head_stride=0)) == INVALID and call(q=rows, qo=rows, hq=4097) == INVALID
 
 
 def test_rope_refusals():
@@ -178,6 +180,23 @@ def test_rotary_rows(dtype, interleaved, restart, axes, d):
         first = R.rotation_tolerance(dtype, ref[:, :hq], xq, interleaved)
         back = R.partner_sum(first, interleaved) + R.rotation_tolerance(dtype, xq.double(), ref[:, :hq].abs() + first, interleaved)
         _assert_close(q, xq.double(), back, "back")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hk", [(1, 0), (1, 1), (2, 0), (9, 8), (300, 7)])
+def test_rotary_rows_of_large_batches(hq, hk):
+    """Two tokens per CTA, with every count of rows that its division has to get right at the edges (one row among them)."""
+    n, d = 2401, 64
+    x, pos = _randn((n, hq + hk, d), F32, hq), _pos(1, n, hk)
+    rope, xd = lar.make_rope(d, (32,)), x.to(DEV)
+    q, k = xd[:, :hq], xd[:, hq:] if hk else None
+    qo, ko = torch.full_like(q, 9.0, memory_format=torch.contiguous_format), torch.full((n, hk, d), 9.0, device=DEV) if hk else None
+    lar.rope_rotate(rope, pos.to(DEV), q, qo, k, ko)
+    ref = R.rotate(x, pos, (32,), 10000.0, False, False)
+    tol = R.rotation_tolerance(F32, ref, x, False)
+    _assert_close(qo, ref[:, :hq], tol[:, :hq], "q")
+    if hk:
+        _assert_close(ko, ref[:, hq:], tol[:, hq:], "k")
 
 
 @pytest.mark.gpu
