@@ -12,6 +12,7 @@
 namespace lar {
 
 constexpr int kFp32Keys = 64;  // slots of a step
+constexpr int kFp32Threads = 128;
 
 // 16 bytes to shared memory, or zeros
 __device__ __forceinline__ void copy16_async(float* dst, const float* src, bool live) {
@@ -71,20 +72,30 @@ struct Fp32Unit {
         table = a.kv.table + seq * a.kv.table_seq_stride + head * a.kv.table_head_stride;
         return true;
     }
-    // The K or V rows of a step; slots outside [lo, hi) are zero whatever their memory holds.
+    // The K or V rows of a step; slots outside [lo, hi) are zero whatever their memory holds.  16 slots at a time: they lie in one page, so
+    // the table is read and the address formed once for them (one look-up per 16-byte piece cost as many instructions as the products).
     template <int D>
     __device__ __forceinline__ void fetch(const PagedAttnArgs& a, float* dst, int stride, const char* pool, int j0, bool report) const {
-        for (int i = threadIdx.x; i < kFp32Keys * (D / 4); i += blockDim.x) {
-            const int j = i / (D / 4), c = i % (D / 4), slot = j0 + j;
-            const float* src = reinterpret_cast<const float*>(pool);
-            bool live = slot >= lo && slot < hi;
-            if (live) {
-                const int page = table[slot >> a.kv.page_shift];
-                live = page >= 0 && page < a.kv.n_pages;
-                if (live) src += page * a.kv.page_stride + (slot & (a.kv.page_tokens - 1)) * a.kv.row_stride + head * a.kv.head_stride + c * 4;
-                else if (report && c == 0) paged_report(a.kv, kStPage);
+        constexpr int PIECES = D / 4, ROWS = kFp32Threads / PIECES;  // of a row; rows that the CTA copies at once
+        const int c = threadIdx.x % PIECES, r0 = threadIdx.x / PIECES;
+        const float* from = reinterpret_cast<const float*>(pool);
+#pragma unroll
+        for (int g = 0; g < kFp32Keys; g += 16) {
+            const int first = j0 + g;
+            const float* p = from;
+            bool page_ok = false;
+            if (first < hi && first + 16 > lo) {
+                const int page = table[first >> a.kv.page_shift];
+                page_ok = page >= 0 && page < a.kv.n_pages;
+                if (page_ok) p += page * a.kv.page_stride + (first & (a.kv.page_tokens - 1)) * a.kv.row_stride + head * a.kv.head_stride + c * 4;
+                else if (report && threadIdx.x == 0) paged_report(a.kv, kStPage);
             }
-            copy16_async(dst + j * stride + c * 4, src, live);
+#pragma unroll
+            for (int r = 0; r < 16; r += ROWS) {
+                const int slot = first + r + r0;
+                const bool live = page_ok && slot >= lo && slot < hi;
+                copy16_async(dst + (g + r + r0) * stride + c * 4, live ? p + (r + r0) * a.kv.row_stride : from, live);
+            }
         }
         copy_commit();
     }
@@ -128,7 +139,7 @@ struct Fp32Unit {
 // neither the 8 x 4 blocks of ldmatrix nor the single words of V (slots 2 q, columns lane / 4) meet in a bank.
 template <int D, bool FEW>
 struct Tf32Shape {
-    static constexpr int BM = FEW ? 16 : 64, WARPS = 4, THREADS = WARPS * 32, RS = D + 4;
+    static constexpr int BM = FEW ? 16 : 64, WARPS = 4, THREADS = kFp32Threads, RS = D + 4;
     static constexpr int NB = FEW ? 2 : 8;  // blocks of 8 slots of a warp in a step
     static constexpr int SMEM = (BM + 2 * kFp32Keys) * RS * 4;
     static constexpr int PER_SM = D == 128 ? 2 : FEW ? 4 : 3;
