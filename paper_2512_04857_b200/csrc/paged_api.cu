@@ -161,6 +161,11 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         // Two row tiles above 128 rows, and with 128-element rows and long caches above 32 (one row tile leaves its two CTAs per SM two
         // stages each; 16 x 4288 slots, one / two row tiles: 32 rows 62 / 65 us, 64 rows 75 / 66, 128 rows 78 / 69, 192 rows 120 / 74; 64 x 577
         // slots, 64 rows 55 / 59; 64-element rows 44 / 55, 48 / 56, 72 / 68).
+        // Units of few slots, or enough of them to fill the SMs, stay whole: joining costs a launch (one token, cut / whole: 1 to 64 sequences
+        // of up to 300 slots 8.3 / 7.7 to 12.1 / 9.0 us, 4 of up to 577 9.4 / 10.8, 64 of them 14.6 / 12.0, 37 of up to 1153 with 128-element
+        // rows 31 / 29).
+        const int64_t heads_with_tokens = with_tokens * k.n_kv_heads;
+        const bool cut = split && len > 384 && (len > 1280 || heads_with_tokens < 2 * kSms);
         const int64_t rows = chunk * group;
         p.nt = rows > 128 || (d == 128 && rows > 32 && len >= 2048) ? 2 : rows > lar::few_rows(d) ? 1 : 0;
         if (p.nt == 0) {
@@ -171,8 +176,8 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
                              : lar::FewShape<128, 1>::bytes(k.n_seqs);
             const int fit = (int)(233472 / (p.smem + 1024)), want = d == 64 ? lar::FewShape<64, 1>::PER_SM : lar::FewShape<128, 1>::PER_SM;
             p.grid = (fit < want ? fit : want) * kSms;
-            p.splits = split ? 2 : 1;
-            if (split) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
+            p.splits = cut ? 2 : 1;
+            if (cut) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
             return p;
         }
         p.tq = 128 / group;
@@ -192,12 +197,12 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
             p.smem = tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs);
         }
         p.grid = per_sm * kSms;
-        // One row tile: units are cut.  Two: whole units on demand where there are many, or where their lengths differ much (chunks
+        // One row tile: as above.  Two: whole units on demand where there are many, or where their lengths differ much (chunks
         // that make up much of their cache); long units are cut where a few rounds of whole ones would leave CTAs idle.
         const int64_t units = (n_tokens / (p.tq * p.nt) + with_tokens) * k.n_kv_heads;
         p.splits = 1;
-        if (split && (p.nt == 1 || (units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid)))) p.splits = 2;
-        else if (split && units > p.grid) p.splits = 3;
+        if (p.nt == 1 ? cut : split && (units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
+        else if (split && p.nt == 2 && units > p.grid) p.splits = 3;
         if (p.splits == 2) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         if (p.splits == 3) p.bytes = sizeof(int4);
         return p;
@@ -211,6 +216,9 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         int64_t s = (12 * kSms + units - 1) / units;  // four rounds of three CTAs per SM: the last one costs little
         if (s > (len + 255) / 256) s = (len + 255) / 256;  // at least 256 slots each
         if (s > 64) s = 64;
+        // Few rows: units that fill the SMs by themselves are not worth joining (one token, 8 KV heads, cut / whole: 64 sequences of up to 577
+        // slots of 64 elements 45.6 / 42.7 us, of up to 1153 73 / 78; 37 of up to 1153 slots of 128 elements 98 / 84, 16 of them 49 / 77).
+        if (p.bm == 16 && len <= (d == 64 ? 768 : 1280) && units >= (d == 64 ? 3 : 2) * kSms) s = 1;
         p.splits = s < 1 ? 1 : (int)s;
     }
     p.bytes = p.splits > 1 ? (size_t)p.splits * n_tokens * k.n_kv_heads * group * (d + 2) * sizeof(float) : 0;
