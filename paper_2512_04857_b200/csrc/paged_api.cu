@@ -161,11 +161,6 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         // Two row tiles above 128 rows, and with 128-element rows and long caches above 32 (one row tile leaves its two CTAs per SM two
         // stages each; 16 x 4288 slots, one / two row tiles: 32 rows 62 / 65 us, 64 rows 75 / 66, 128 rows 78 / 69, 192 rows 120 / 74; 64 x 577
         // slots, 64 rows 55 / 59; 64-element rows 44 / 55, 48 / 56, 72 / 68).
-        // Units of few slots, or enough of them to fill the SMs, stay whole: joining costs a launch (one token, cut / whole: 1 to 64 sequences
-        // of up to 300 slots 8.3 / 7.7 to 12.1 / 9.0 us, 4 of up to 577 9.4 / 10.8, 64 of them 14.6 / 12.0, 37 of up to 1153 with 128-element
-        // rows 31 / 29).
-        const int64_t heads_with_tokens = with_tokens * k.n_kv_heads;
-        const bool cut = split && len > 384 && (len > 1280 || heads_with_tokens < 2 * kSms);
         const int64_t rows = chunk * group;
         p.nt = rows > 128 || (d == 128 && rows > 32 && len >= 2048) ? 2 : rows > lar::few_rows(d) ? 1 : 0;
         if (p.nt == 0) {
@@ -176,6 +171,10 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
                              : lar::FewShape<128, 1>::bytes(k.n_seqs);
             const int fit = (int)(233472 / (p.smem + 1024)), want = d == 64 ? lar::FewShape<64, 1>::PER_SM : lar::FewShape<128, 1>::PER_SM;
             p.grid = (fit < want ? fit : want) * kSms;
+            // Units of few slots, or short ones that fill the SMs, stay whole: joining costs a launch (one token, 8 KV heads, cut / whole: 1 to
+            // 64 sequences of up to 300 slots 8.3 / 7.7 to 12.1 / 9.0 us; up to 577 slots: 4 sequences 9.4 / 10.8, 64 14.6 / 12.0; up to 1153:
+            // 37 15.2 / 17.9, 64 of unlike length 15.9 / 18.5).
+            const bool cut = split && len > 384 && (len > 640 || with_tokens * k.n_kv_heads < 2 * kSms);
             p.splits = cut ? 2 : 1;
             if (cut) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
             return p;
@@ -197,11 +196,13 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
             p.smem = tc_smem<1>(d, p.rows_cap, p.stages, k.n_seqs);
         }
         p.grid = per_sm * kSms;
-        // One row tile: as above.  Two: whole units on demand where there are many, or where their lengths differ much (chunks
+        // One row tile: cut above 1280 slots (8 tokens of 64-element rows, 8 KV heads, cut / whole: 37 sequences of up to 577 slots 22 / 14 us,
+        // up to 1153 28 / 20, up to 2000 36 / 31, of unlike length 29 / 30, up to 4100 43 / 54; 16 sequences 18 / 14, 22 / 20, 25 / 29,
+        // 34 / 52 at the same lengths).  Two: whole units on demand where there are many, or where their lengths differ much (chunks
         // that make up much of their cache); long units are cut where a few rounds of whole ones would leave CTAs idle.
         const int64_t units = (n_tokens / (p.tq * p.nt) + with_tokens) * k.n_kv_heads;
         p.splits = 1;
-        if (p.nt == 1 ? cut : split && (units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
+        if (split && (p.nt == 1 ? len > 1280 : units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
         else if (split && p.nt == 2 && units > p.grid) p.splits = 3;
         if (p.splits == 2) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         if (p.splits == 3) p.bytes = sizeof(int4);
