@@ -385,7 +385,8 @@ lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* r
  *                                               or            kv_start[s] .. lens[s] - 1  (causal = 0)
  * kv_start (device, int32, [n_seqs], or NULL: 0) masks left padding.  A row that sees no slot is zero; memory of slots that
  * no row of a sequence sees (behind lens, before kv_start) may hold anything.  Tokens that belong to no sequence are left alone.  A
- * non-finite value in a slot that some row of the chunk sees may reach every row of the chunk.  out overlaps nothing else.
+ * non-finite value in a slot that some row of the chunk sees may reach every row of the chunk, with fp32 storage an infinity as
+ * NaN (operands are split into two numbers).  out overlaps nothing else.
  * LAR_ERR_CAPACITY: bf16 with more than 1024 sequences, or 2^30 (query tile, cache tile) pairs or more.
  * Query head hq uses KV head hq / (n_q_heads / n_kv_heads); their ratio is 1..16.  softmax_scale 0 selects 1/sqrt(head_dim).
  * max_chunk and max_len bound the tokens of a chunk and the entries of a cache (0: not known); they only choose the launch

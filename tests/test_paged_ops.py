@@ -426,6 +426,22 @@ def test_attention_with_left_padding(dtype, n, lens, start):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout,page,d,hkv,hq", SHAPES)
+@pytest.mark.parametrize("n,lens,start", [(n, lens, None) for n, lens in LENGTHS] + [
+    ([20, 5, 1], [20, 70, 66], [7, 69, 65]),
+    ([40, 1, 9], [40, 64, 9], [200, 64, 9]),
+    ([2, 1, 3], [1300, 900, 40], [700, 0, 33]),
+])
+def test_attention_of_short_caches_in_long_tables(dtype, layout, page, d, hkv, hq, n, lens, start):
+    """Lengths that only the GPU knows: tables and bounds that allow long caches make the kernels cut the few slots there are."""
+    c = PagedCase(dtype, d, hkv, page, layout, n, lens, seed=d + page, extra_cols=1 + 8192 // page)
+    c.fill(start, 3)
+    for causal in (True, False):
+        _check_attention(c, hq, causal, start, True, 13, hints=(max(n), 10 ** 6))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("n,d", [([70, 1], 64), ([40, 9], 64), ([33, 1], 128), ([3, 1], 64), ([2, 8], 128)])
 def test_attention_of_extreme_logits(dtype, n, d):
     """Logits of several hundred either way: the running maximum has to be taken off, and to grow along the cache."""
