@@ -603,22 +603,23 @@ def test_prefill_of_the_librarys_cache_then_decode_steps():
 
 
 @pytest.mark.gpu
-def test_chunks_of_a_growing_cache_in_a_graph():
+@pytest.mark.parametrize("extra_cols,max_len", [(0, 310), (256, 8192)])     # units stay whole, and are cut and joined
+def test_chunks_of_a_growing_cache_in_a_graph(extra_cols, max_len):
     """Append and attention of chunks captured once and replayed with other lengths, positions and pages: the graph reads
     them on the device.  Two replays share the workspace, one behind the other; they run on a side stream."""
     hq, hkv, d, page, S = 4, 2, 64, 32, 3
     n, T = [4, 1, 7], 12
-    c = PagedCase(BF, d, hkv, page, "nhd", n, [300, 290, 310], extra_cols=0)
+    c = PagedCase(BF, d, hkv, page, "nhd", n, [300, 290, 310], extra_cols=extra_cols)
     c.fill(None, 1)
     rope, axes = lar.make_rope(d, (32,)), (32,)
     x, pos = torch.empty(T, hq + 2 * hkv, d, dtype=BF, device=DEV), torch.zeros(1, T, dtype=torch.int32, device=DEV)
     qo, out = torch.empty(T, hq, d, dtype=BF, device=DEV), torch.empty(T, hq, d, dtype=BF, device=DEV)
-    ws = c.kv.attn_workspace(hq, T, 7, 310)
+    ws = c.kv.attn_workspace(hq, T, 7, max_len)
     side = torch.cuda.Stream()
 
     def step():
         c.kv.append_rope(x[:, hq:hq + hkv], x[:, hq + hkv:], c.cu, rope, pos, x[:, :hq], qo)
-        c.kv.attn(qo, out, c.cu, max_chunk=7, max_len=310, workspace=ws)
+        c.kv.attn(qo, out, c.cu, max_chunk=7, max_len=max_len, workspace=ws)
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         step()
