@@ -208,32 +208,37 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         if (p.splits == 3) p.bytes = sizeof(int4);
         return p;
     }
-    p.bm = chunk * group <= 16 ? 16 : 64;
+    p.bm = chunk * group <= 8 ? 8 : chunk * group <= 16 ? 16 : 64;
     p.tq = p.bm / group;
-    p.tiles = (int)(n_tokens / p.tq + with_tokens);
+    const int64_t tiles = n_tokens / p.tq + with_tokens;
+    p.tiles = (int)(tiles < n_tokens ? tiles : n_tokens);
     p.splits = 1;
     if (split) {
         const int64_t units = (int64_t)p.tiles * k.n_kv_heads;
         int64_t s = (12 * kSms + units - 1) / units;  // four rounds of three CTAs per SM: the last one costs little
         if (s > (len + 255) / 256) s = (len + 255) / 256;  // at least 256 slots each
         if (s > 64) s = 64;
-        // Few rows: units that fill the SMs by themselves are not worth joining (one token, 8 KV heads, cut / whole: 64 sequences of up to 577
-        // slots of 64 elements 45.6 / 42.7 us, of up to 1153 73 / 78; 37 of up to 1153 slots of 128 elements 98 / 84, 16 of them 49 / 77).
-        if (p.bm == 16 && len <= (d == 64 ? 768 : 1280) && units >= (d == 64 ? 3 : 2) * kSms) s = 1;
+        // Few rows: short units that fill the SMs by themselves are not worth joining (one token, 8 KV heads, cut / whole: 37 sequences of up
+        // to 577 slots 25.8 / 24.3 us, with 128-element rows 42.5 / 39.8, 16 of them 31.6 / 42.1; 64 sequences 37.4 / 32.0, of up to 1153
+        // slots 60 / 58, with 128-element rows 103 / 112).
+        if (p.bm < 64 && len <= 768 && units >= 2 * kSms) s = 1;
         p.splits = s < 1 ? 1 : (int)s;
     }
     p.bytes = p.splits > 1 ? (size_t)p.splits * n_tokens * k.n_kv_heads * group * (d + 2) * sizeof(float) : 0;
     return p;
 }
 
-// fp32 storage: row tiles of 64 or 16.
+// fp32 storage: row tiles of 64, 16 or 8.
 template <int D>
 lar_status_t launch_fp32(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
-    void (*fn)(const lar::PagedAttnArgs) = p.bm == 64 ? lar::paged_attn_tf32_kernel<D, false> : lar::paged_attn_tf32_kernel<D, true>;
-    const int smem = p.bm == 64 ? lar::Tf32Shape<D, false>::SMEM : lar::Tf32Shape<D, true>::SMEM;
-    constexpr int threads = lar::Tf32Shape<D, false>::THREADS;
+    void (*fn)(const lar::PagedAttnArgs) = p.bm == 64   ? lar::paged_attn_tf32_kernel<D, false>
+                                           : p.bm == 16 ? lar::paged_attn_tf32_kernel<D, true>
+                                                        : lar::paged_attn_tf32_decode_kernel<D>;
+    const int smem = p.bm == 64   ? lar::Tf32Shape<D, false>::SMEM
+                     : p.bm == 16 ? lar::Tf32Shape<D, true>::SMEM
+                                  : lar::Tf32DecodeShape<D>::SMEM;
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), threads, smem, s>>>(a);
+    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), lar::kFp32Threads, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     if (p.splits > 1) {
         const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.n_kv_heads * a.group;

@@ -123,6 +123,29 @@ struct Fp32Unit {
         const int t = row / a.group, g = row - t * a.group;
         return reinterpret_cast<float*>(a.out.p) + (long long)(tok0 + t) * a.out.token_stride + (head * a.group + g) * a.out.head_stride;
     }
+    // The warps' parts (O, m, l of every row, PS floats each) into the result.
+    template <int D, int WARPS, int ROWS, int PS>
+    __device__ __forceinline__ void merge_warps(const PagedAttnArgs& a, const float* parts) const {
+        for (int i = threadIdx.x; i < rows * (D / 2); i += kFp32Threads) {
+            const int row = i / (D / 2), e = i % (D / 2) * 2;
+            const float* p = parts + row * PS;
+            float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) M = fmaxf(M, p[w * ROWS * PS + D]);
+            const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float2 ml = *reinterpret_cast<const float2*>(p + w * ROWS * PS + D), v = *reinterpret_cast<const float2*>(p + w * ROWS * PS + e);
+                const float f = ex2_approx(ml.x - ref);
+                L = fmaf(ml.y, f, L);
+                x = fmaf(v.x, f, x);
+                y = fmaf(v.y, f, y);
+            }
+            const float inv = a.n_splits > 1 ? 1.f : L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
+            *reinterpret_cast<float2*>(out_row(a, row, D) + e) = make_float2(x * inv, y * inv);
+            if (a.n_splits > 1 && e == 0) *reinterpret_cast<float2*>(a.part_ml + part_row(a, row) * 2) = make_float2(M, L);
+        }
+    }
 };
 
 // x = hi + lo with hi the nearest tf32 (11 significant bits, off by 2^-11 at most) and lo exact in fp32, of which the tensor core takes
@@ -325,25 +348,7 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
             if (quad == 0) *reinterpret_cast<float2*>(p + D) = make_float2(m[r], l[r]);
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < u.rows * (D / 2); i += S::THREADS) {
-            const int row = i / (D / 2), e = i % (D / 2) * 2;
-            const float* p = ks + row * PS;
-            float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
-#pragma unroll
-            for (int w = 0; w < S::WARPS; ++w) M = fmaxf(M, p[w * S::BM * PS + D]);
-            const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-            for (int w = 0; w < S::WARPS; ++w) {
-                const float2 ml = *reinterpret_cast<const float2*>(p + w * S::BM * PS + D), v = *reinterpret_cast<const float2*>(p + w * S::BM * PS + e);
-                const float f = ex2_approx(ml.x - ref);
-                L = fmaf(ml.y, f, L);
-                x = fmaf(v.x, f, x);
-                y = fmaf(v.y, f, y);
-            }
-            const float inv = a.n_splits > 1 ? 1.f : L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
-            *reinterpret_cast<float2*>(u.out_row(a, row, D) + e) = make_float2(x * inv, y * inv);
-            if (a.n_splits > 1 && e == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(M, L);
-        }
+        u.merge_warps<D, S::WARPS, S::BM, PS>(a, ks);
         return;
     }
 #pragma unroll
@@ -356,6 +361,173 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
         for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(o[n][2 * r] * inv, o[n][2 * r + 1] * inv);
         if (a.n_splits > 1 && quad == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(m[r], l[r]);
     }
+}
+
+// At most 8 rows of a KV head (a decode step).  The slots are the 16 rows of a product and the query rows its 8 columns (S^T = K q^T,
+// O^T = V^T P^T), so that few products are padding; as above every warp has all query rows and a quarter of a step's slots.  Bound by
+// the instructions that split K and V into tf32 numbers and by the cache's bytes (16 x 4288 slots, 8 KV heads of 4: 64-element rows 68 us
+// against 81 of the 16-row kernel above, 128-element rows 117 = 4.8 TB/s against 159; two such column blocks for 9 to 16 rows took
+// 95 us against 83 and 171 against 168).
+// P^T comes out of the accumulators transposed in 16-bit halves (movmatrix); its operand rows q and q + 4 (q = lane % 4) are taken to be
+// slots 2 q and 2 q + 1 of a block of 8.  The rows of V^T are taken in the order in which a lane finds four of them in 16 bytes.
+template <int D>
+struct Tf32DecodeShape {
+    static constexpr int ROWS = 8, WARPS = 4, RS = D + 4, KS = D / 8;
+    static constexpr int Q_FLOATS = KS * 32 * 4;  // the query rows as operands, split
+    static constexpr int SMEM = (Q_FLOATS + 2 * kFp32Keys * RS) * 4;
+    static constexpr int PER_SM = D == 128 ? 3 : 4;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kFp32Threads, Tf32DecodeShape<D>::PER_SM) paged_attn_tf32_decode_kernel(const PagedAttnArgs a) {
+    using S = Tf32DecodeShape<D>;
+    constexpr int RS = S::RS, KS = S::KS, OT = D / 16;
+    extern __shared__ __align__(16) float sm[];
+    uint4* qf = reinterpret_cast<uint4*>(sm);
+    float* ks = sm + S::Q_FLOATS;
+    float* vs = ks + kFp32Keys * RS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, qrow = lane >> 2;
+    Fp32Unit u;
+    if (!u.find(a)) return;
+    if (u.b0 < u.b1) {
+        u.fetch<D>(a, ks, RS, a.kv.k_pool, u.b0 * kFp32Keys, true);
+        u.fetch<D>(a, vs, RS, a.kv.v_pool, u.b0 * kFp32Keys, false);
+    }
+    // elements 8 k + quad and 8 k + quad + 4 of row qrow, the high parts, then the low ones; rows behind the last are zero
+    for (int i = threadIdx.x; i < KS * 32; i += kFp32Threads) {
+        const int l = i & 31, k = i >> 5, row = l >> 2;
+        uint32_t x0 = 0, x1 = 0;
+        if (row < u.rows) {
+            const int t = row / a.group, g = row - t * a.group;
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q.p) + (long long)(u.tok0 + t) * a.q.token_stride + (u.head * a.group + g) * a.q.head_stride + k * 8 + (l & 3);
+            x0 = p[0];
+            x1 = p[4];
+        }
+        uint4 f;
+        split_tf32(x0, f.x, f.z);
+        split_tf32(x1, f.y, f.w);
+        qf[i] = f;
+    }
+    const int slot_w = warp * 16;  // the warp's first slot of a step
+    const int last[2] = {u.last_slot(a, 2 * quad), u.last_slot(a, 2 * quad + 1)};
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[OT][4];
+    clear_tiles<OT>(o);
+    const int min_last = u.last_slot(a, 0);
+    const uint32_t k_at = smem_u32(ks + (slot_w + (lane & 15)) * RS + (lane >> 4) * 4);
+    const float* v_at = vs + (slot_w + 2 * quad) * RS + 4 * qrow;
+
+    for (int b = u.b0; b < u.b1; ++b) {
+        const int j0 = b * kFp32Keys;
+        copy_wait<1>();  // K of this step (V may be on its way)
+        __syncthreads();
+        float s[4];
+        {
+            float big[2][4], small[4][4];  // (accumulators of few products, and chains short enough)
+            clear_tiles<2>(big);
+            clear_tiles<4>(small);
+#pragma unroll 8
+            for (int k = 0; k < KS; ++k) {
+                uint32_t x[4], ah[4], al[4];
+                ldmatrix_x4(k_at + k * 32, x);  // slots 0-7 | 8-15, elements 8 k .. + 3, then the next four
+#pragma unroll
+                for (int e = 0; e < 4; ++e) split_tf32(x[e], ah[e], al[e]);
+                const uint4 q = qf[k * 32 + lane];
+                mma_tf32(small[k & 1], al, q.x, q.y);
+                mma_tf32(big[k & 1], ah, q.x, q.y);
+                mma_tf32(small[2 + (k & 1)], ah, q.z, q.w);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = big[0][e] + big[1][e] + ((small[0][e] + small[1][e]) + (small[2][e] + small[3][e]));
+        }
+        __syncthreads();  // K has been read
+        if (b + 1 < u.b1) u.fetch<D>(a, ks, RS, a.kv.k_pool, j0 + kFp32Keys, true);
+        else copy_commit();
+        // this thread: slots qrow (+ 8), rows 2 quad (+ 1)
+        if (j0 < u.lo || j0 + kFp32Keys - 1 > min_last) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int slot = j0 + slot_w + qrow + (e >> 1) * 8;
+                if (slot < u.lo || slot > last[e & 1]) s[e] = -INFINITY;
+            }
+        }
+        float corr[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float mx = fmaxf(s[e], s[2 + e]);
+#pragma unroll
+            for (int w = 4; w <= 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+            const float mn = fmaxf(m[e], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
+            corr[e] = ex2_approx(m[e] - ref);
+            m[e] = mn;
+            s[e] = ex2_approx(fmaf(s[e], a.scale_log2, -ref));
+            s[2 + e] = ex2_approx(fmaf(s[2 + e], a.scale_log2, -ref));
+            l[e] = l[e] * corr[e] + (s[e] + s[2 + e]);  // (this thread's slots: joined over the row's threads at the end)
+        }
+        uint32_t ph[2][2], pl[2][2];  // P^T of slots 0-7 | 8-15: slots 2 quad and 2 quad + 1 of row qrow
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t x = __float_as_uint(s[2 * h]), y = __float_as_uint(s[2 * h + 1]);
+            const uint32_t hi = movmatrix_trans(__byte_perm(x, y, 0x7632)), lo = movmatrix_trans(__byte_perm(x, y, 0x5410));
+            split_tf32(__byte_perm(lo, hi, 0x5410), ph[h][0], pl[h][0]);
+            split_tf32(__byte_perm(lo, hi, 0x7632), ph[h][1], pl[h][1]);
+        }
+        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+            for (int i = 0; i < OT; ++i) {
+                o[i][0] *= corr[0];
+                o[i][1] *= corr[1];
+                o[i][2] *= corr[0];
+                o[i][3] *= corr[1];
+            }
+        }
+        copy_wait<1>();  // V of this step
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) {  // elements 32 g + 4 qrow .. + 3: rows qrow and qrow + 8 of two products
+            float part[2][4];
+            clear_tiles<2>(part);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4 v0 = *reinterpret_cast<const uint4*>(v_at + h * 8 * RS + g * 32);
+                const uint4 v1 = *reinterpret_cast<const uint4*>(v_at + (h * 8 + 1) * RS + g * 32);
+                const uint32_t x[2][4] = {{v0.x, v0.y, v1.x, v1.y}, {v0.z, v0.w, v1.z, v1.w}};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t ah[4], al[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) split_tf32(x[i][e], ah[e], al[e]);
+                    mma_tf32(part[i], al, ph[h][0], ph[h][1]);  // (six products in all)
+                    mma_tf32(part[i], ah, pl[h][0], pl[h][1]);
+                    mma_tf32(part[i], ah, ph[h][0], ph[h][1]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[2 * g + i][e] += part[i][e];
+        }
+        __syncthreads();  // V has been read
+        if (b + 1 < u.b1) u.fetch<D>(a, vs, RS, a.kv.v_pool, j0 + kFp32Keys, false);
+        else copy_commit();
+    }
+    copy_commit();
+    copy_wait<0>();  // (nothing is in flight when the CTA ends)
+    // the warps' parts side by side where K was
+    constexpr int PS = D + 4;
+    static_assert(S::WARPS * S::ROWS * PS <= kFp32Keys * RS, "the parts fit where K was");
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int w = 4; w <= 16; w <<= 1) l[e] += __shfl_xor_sync(0xffffffffu, l[e], w);
+        float* p = ks + (warp * S::ROWS + 2 * quad + e) * PS;
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g)
+            *reinterpret_cast<float4*>(p + g * 32 + 4 * qrow) = make_float4(o[2 * g][e], o[2 * g][2 + e], o[2 * g + 1][e], o[2 * g + 1][2 + e]);
+        if (qrow == 0) *reinterpret_cast<float2*>(p + D) = make_float2(m[e], l[e]);
+    }
+    __syncthreads();
+    u.merge_warps<D, S::WARPS, S::ROWS, PS>(a, ks);
 }
 
 // Joins the splits of every row, in the order of the splits: one warp per (token, head).
