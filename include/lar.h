@@ -391,14 +391,16 @@ lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* r
  * Query head hq uses KV head hq / (n_q_heads / n_kv_heads); their ratio is 1..16.  softmax_scale 0 selects 1/sqrt(head_dim).
  * max_chunk and max_len bound the tokens of a chunk and the entries of a cache (0: not known); they only choose the launch
  * shape, never the result's correctness.
- * workspace (device, 16-byte aligned, lar_paged_attn_workspace_bytes of the same arguments, contents irrelevant) lets the
- * kernel spread the slots of a unit over several CTAs; NULL: it does not.  LAR_ERR_NOMEM: workspace_bytes is too small.
+ * workspace (device, 16-byte aligned, lar_paged_attn_workspace_bytes of these arguments or larger ones, contents irrelevant) lets
+ * the kernel spread the slots of a unit over several CTAs; NULL: it does not.  LAR_ERR_NOMEM: workspace_bytes is too small.
  * Calls that may overlap on the GPU need workspaces of their own (two graphs that share one are ordered by the caller). */
 lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads, int64_t n_tokens,
                             const int32_t* cu_tokens, const int32_t* kv_start, int causal, float softmax_scale, int max_chunk,
                             int max_len, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace lar_paged_attn wants for these arguments (0: none, or the arguments are invalid).  No CUDA call. */
+/* Bytes of workspace that suffice for lar_paged_attn with these arguments and for every smaller call: the same dtype, head_dim and head
+ * counts, no more sequences, tokens or table entries, max_chunk (0: n_tokens) and max_len (0: what the table holds) no larger.  One
+ * workspace of the largest call serves all of them.  0: none is used, or the arguments are invalid.  No CUDA call. */
 size_t lar_paged_attn_workspace_bytes(const lar_paged_kv_t* kv, int n_q_heads, int64_t n_tokens, int max_chunk, int max_len);
 
 /* Describes a layer of the library's own cache for lar_paged_attn (heads have pages of their own).  The pointers lie in the

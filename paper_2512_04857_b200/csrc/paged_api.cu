@@ -228,6 +228,44 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     return p;
 }
 
+// Workspace of a call and of every smaller one: the largest need over the launch shapes that attn_plan may choose for at most these
+// sequences, tokens, tokens of a chunk (0: n_tokens) and entries (0: what the table holds).  A call's own need goes up and down with its
+// sizes (fewer units are cut into more parts), and a program has one workspace for all of its calls.
+size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len) {
+    const int64_t chunk = max_chunk > 0 ? max_chunk : n_tokens;
+    const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
+    const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
+    const int d = k.head_dim;
+    if (k.dtype == LAR_BF16) {
+        lar_paged_kv_t one = k;  // (few sequences leave shared memory for most CTAs)
+        one.n_seqs = 1;
+        const int few = lar::few_rows(d);
+        size_t most = 0;
+        auto take = [&](size_t n) { most = n > most ? n : most; };
+        // few rows: each chunk length is a launch shape; where any length up to len is cut, one near len is
+        for (int64_t c = 1; c <= chunk && c * group <= few; ++c) {
+            AttnPlan p = attn_plan(one, group, 1, (int)c, len > 640 ? 641 : (int)len, true);
+            take(p.bytes);
+        }
+        // one row tile (of two CTAs per SM at most), then two: their rows are bounded by the 128 of a tile
+        const int64_t t1 = chunk < 128 / group ? chunk : 128 / group;
+        const size_t part = (size_t)(d + 2) * sizeof(float), rows = (size_t)(t1 * group + 7) / 8 * 8, rows2 = (size_t)(128 / group * group + 7) / 8 * 8;
+        if (chunk * group > few && len > 1280) take(2 * kSms * (sizeof(int4) + 2 * rows * part));
+        if (chunk * group > 128 || (d == 128 && chunk * group > 32 && len >= 2048))
+            take(len >= 2048 ? kSms * (sizeof(int4) + 4 * rows2 * part) : sizeof(int4));
+        return most;
+    }
+    // fp32: s splits of n tokens, s <= 12 kSms / units + 1 with at least n / tq * KV heads units, so that s n <= 12 kSms tq / KV heads + n; and
+    // two splits or more only where there are fewer than 12 kSms units
+    const int bm = chunk * group <= 8 ? 8 : chunk * group <= 16 ? 16 : 64;
+    const int64_t spread = 12ll * kSms * (bm / group) / k.n_kv_heads, n = n_tokens < spread ? n_tokens : spread;
+    int64_t s = (len + 255) / 256;
+    s = s > 64 ? 64 : s;
+    if (s < 2) return 0;
+    const int64_t rows = s * n < spread + n ? s * n : spread + n;
+    return (size_t)rows * k.n_kv_heads * group * (d + 2) * sizeof(float);
+}
+
 // fp32 storage: row tiles of 64, 16 or 8.
 template <int D>
 lar_status_t launch_fp32(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStream_t s) {
@@ -447,8 +485,8 @@ lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* r
 size_t lar_paged_attn_workspace_bytes(const lar_paged_kv_t* kv, int n_q_heads, int64_t n_tokens, int max_chunk, int max_len) {
     lar::PagedView v;
     if (n_tokens < 1 || n_q_heads < 1 || !paged_view(kv, n_tokens, kv ? kv->lens : nullptr, v)) return 0;
-    if (n_q_heads % kv->n_kv_heads || n_q_heads / kv->n_kv_heads > 16) return 0;
-    return attn_plan(*kv, n_q_heads / kv->n_kv_heads, n_tokens, max_chunk, max_len, true).bytes;
+    if (n_q_heads % kv->n_kv_heads || n_q_heads / kv->n_kv_heads > 16 || max_chunk < 0 || max_len < 0) return 0;
+    return attn_workspace_bound(*kv, n_q_heads / kv->n_kv_heads, n_tokens, max_chunk, max_len);
 }
 
 lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads, int64_t n_tokens,

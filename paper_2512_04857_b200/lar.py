@@ -439,7 +439,7 @@ class PagedKV:
               _ints(cu_tokens, self.n_seqs + 1, dev, "append_rope: cu_tokens"))
 
     def attn_workspace(self, n_q_heads, n_tokens, max_chunk=0, max_len=0):
-        """A workspace tensor for attn calls of these sizes (None where none is used)."""
+        """A workspace tensor for attn calls of these sizes and all smaller ones (None where none is used)."""
         import torch
         n = lib().lar_paged_attn_workspace_bytes(self.desc, n_q_heads, n_tokens, max_chunk, max_len)
         return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None

@@ -645,3 +645,60 @@ def test_chunks_of_a_growing_cache_in_a_graph(extra_cols, max_len):
         turned = R.rotate(xs[:, :hq], ps, axes, 10000.0, False, False)
         _assert_close(qo, turned, R.rotation_tolerance(BF, turned, xs[:, :hq], False), "q")
     assert int(c.status) == 0
+
+
+# --------------------------------------------------------------------------------------- one workspace for many calls
+WS_HEADS = [(1, 1), (2, 8), (4, 8), (8, 1), (3, 20), (16, 2)]        # (heads of a group, KV heads)
+
+
+@pytest.mark.parametrize("dtype", [lar.LAR_BF16, lar.LAR_FP32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group,hkv", WS_HEADS)
+def test_a_workspace_holds_for_smaller_calls(dtype, d, group, hkv):
+    """What is asked for a call covers every call with fewer sequences, tokens, tokens of a chunk and entries."""
+    def need(seqs, tokens, chunk, length):
+        kv = _kv(dtype=dtype, head_dim=d, n_seqs=seqs, n_kv_heads=hkv, n_pages=1 << 16, table_cols=1 << 11, row_stride=hkv * d,
+                 head_stride=d, page_stride=hkv * d * 32)
+        return lar.lib().lar_paged_attn_workspace_bytes(kv, group * hkv, tokens, chunk, length)
+    rng = random.Random(d + hkv)
+    pick = lambda hi: max(1, min(hi, int(hi ** rng.random() + 0.5)))
+    for _ in range(300):
+        seqs, chunk, length = pick(1024), pick(8192), pick(65536)
+        tokens = pick(seqs * chunk)
+        if rng.random() < 0.5:                                          # bounds that are not known: no chunk is longer than the batch
+            chunk, large = tokens, need(seqs, tokens, 0, 0)
+        else:
+            large = need(seqs, tokens, chunk, length)
+        for _ in range(4):
+            s, t, c, n = pick(seqs), pick(tokens), rng.choice([0, pick(chunk)]), pick(length)
+            if c == 0 and t > chunk:
+                continue
+            assert need(s, t, c, n) <= large, (seqs, tokens, chunk, length, s, t, c, n)
+    # 32 sequences of single tokens and 24 of them; a prompt and one token
+    assert need(24, 24, 1, 4288) <= need(32, 32, 1, 4288) <= need(222, 222, 1, 4288)
+    assert need(1, 1, 1, 4096) <= need(1, 4096, 4096, 4096) and need(1, 2048, 2048, 4096) <= need(1, 4096, 4096, 4096)
+    assert need(1, 1, -1, 0) == 0 and need(1, 1, 1, -1) == 0            # attn refuses these
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,hkv,hq", [(128, 2, 8), (64, 3, 3)])
+def test_one_workspace_for_a_prompt_and_what_follows(dtype, d, hkv, hq):
+    """Sized once for the largest call, then used for smaller ones of every launch shape (the fence behind it stays)."""
+    lens = [2600, 700, 130, 2100]
+    c = PagedCase(dtype, d, hkv, 64, "nhd", [600, 3, 0, 40], lens, seed=d)
+    for p, x in zip(c.pools, c.dev):
+        x.normal_()
+        p.copy_(x.cpu())
+    n_bytes = lar.lib().lar_paged_attn_workspace_bytes(c.kv.desc, hq, 643, 600, 2600)
+    buf = torch.full((n_bytes + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    ws = buf[:n_bytes]
+    for seqs, n in ((4, [600, 3, 0, 40]), (4, [1, 1, 1, 1]), (4, [300, 0, 0, 0]), (2, [40, 2]), (1, [1]), (1, [9]), (1, [200]), (4, [2, 0, 1, 2])):
+        part = lar.PagedKV(c.dev[0], c.dev[1], c.kv._keep[2][:seqs], c.lens_dev[:seqs], hkv, status=c.status)
+        cu = torch.tensor([0] + list(torch.tensor(n).cumsum(0)), dtype=torch.int32, device=DEV)
+        q = _randn((sum(n), hq, d), dtype, sum(n))
+        out = torch.full((sum(n), hq, d), 5.0, dtype=dtype, device=DEV)
+        part.attn(q.to(DEV), out, cu, max_chunk=max(n), max_len=2600, workspace=ws)
+        ref, mag, big = R.attention(q, c.rows(0), c.rows(1), n, lens[:seqs], None, True, hq // hkv, d ** -0.5)
+        _assert_close(out, ref, R.attention_tolerance(dtype, ref, mag, big, d, 2600), f"{n}")
+    assert int(c.status) == 0 and (buf[n_bytes:] == 0xA5).all()
