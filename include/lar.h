@@ -338,7 +338,8 @@ typedef struct lar_rows {
  * One table shared by the heads has table_head_stride = 0; heads with pages of their own have head_stride = 0.
  * lens[s * lens_stride] entries of sequence s are live.  A page number outside 0 .. n_pages - 1, or a token whose slot the
  * table does not hold, is never followed: its rows are not written, read as zeros, and status bit 64 is recorded in *status
- * (if given; lar_cache_poll_device_status reports it for the library's own caches). */
+ * (if given; lar_cache_poll_device_status reports it for the library's own caches).  Attention takes a length beyond the table as what
+ * the table holds, and a chunk of more tokens than its cache has entries as starting before slot 0, and records the bit for both. */
 typedef struct lar_paged_kv {
     uint32_t struct_size;      /* = sizeof(lar_paged_kv_t) */
     int32_t dtype;             /* lar_dtype_t */

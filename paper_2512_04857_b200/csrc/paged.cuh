@@ -38,9 +38,12 @@ __device__ __forceinline__ void chunk_of(const PagedView& v, int s, int& t0, int
     }
 }
 
-// Entries of a sequence's cache, kept inside what its table can address.
-__device__ __forceinline__ int live_len(const PagedView& v, int s) {
-    return min(max(v.lens[s * v.lens_stride], 0), v.table_cols << v.page_shift);
+// Entries of the cache of a sequence with n tokens, kept inside what its table can address.  Tokens whose slots lie outside that (a length
+// beyond the table, or of fewer entries than tokens) are recorded by the caller that says so.
+__device__ __forceinline__ int live_len(const PagedView& v, int s, int n, bool report) {
+    const int len = v.lens[s * v.lens_stride], cap = v.table_cols << v.page_shift;
+    if (report && n > 0 && (len < n || len > cap)) paged_report(v, kStPage);
+    return min(max(len, 0), cap);
 }
 
 }  // namespace lar

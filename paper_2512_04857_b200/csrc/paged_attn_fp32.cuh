@@ -58,7 +58,7 @@ struct Fp32Unit {
         chunk_of(a.kv, seq, t0, t1);
         tile = (t1 - t0 + a.tq - 1) / a.tq - 1 - tile;  // the tiles that see most first
         head = blockIdx.y;
-        len = live_len(a.kv, seq);
+        len = live_len(a.kv, seq, t1 - t0, threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0);
         tok0 = t0 + tile * a.tq;
         n_tok = min(a.tq, t1 - tok0);
         rows = n_tok * a.group;

@@ -702,3 +702,22 @@ def test_one_workspace_for_a_prompt_and_what_follows(dtype, d, hkv, hq):
         ref, mag, big = R.attention(q, c.rows(0), c.rows(1), n, lens[:seqs], None, True, hq // hkv, d ** -0.5)
         _assert_close(out, ref, R.attention_tolerance(dtype, ref, mag, big, d, 2600), f"{n}")
     assert int(c.status) == 0 and (buf[n_bytes:] == 0xA5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [[1, 0, 2], [40, 0, 9], [200, 0, 33]])     # few rows, one and two row tiles
+def test_attention_reports_slots_that_the_table_does_not_hold(dtype, n):
+    """A length beyond the table, below zero, or of fewer entries than the chunk has tokens leaves bit 64 in the status word."""
+    c = PagedCase(dtype, 64, 2, 32, "nhd", n, [256, 256, 256], extra_cols=0)
+    c.fill(None, 8)
+    q = _randn((sum(n), 2, 64), dtype, 9).to(DEV)
+    out = torch.empty_like(q)
+    ws = c.kv.attn_workspace(2, sum(n), max(n), 256)
+    for lens, want in (([256, 256, 256], 0), (n, 0), ([256, 10 ** 6, 256], 0), ([256, -3, 256], 0),    # (no tokens: nothing is looked up)
+                       ([257, 256, 256], 64), ([256, 0, n[2] - 1], 64), ([-1, 0, 256], 64), ([256, 0, -2 ** 31], 64), ([256, 0, 2 ** 31 - 1], 64)):
+        for causal in (True, False):
+            c.lens_dev.copy_(torch.tensor(lens))
+            c.kv.attn(q, out, c.cu, causal=causal, max_chunk=max(n), max_len=256, workspace=ws)
+            assert int(c.status) == want, (lens, causal)
+            c.status.zero_()
