@@ -6,6 +6,8 @@
 //
 // The products run on the tensor cores with every operand split in two tf32 numbers, so that nothing fp32 storage is chosen for is lost:
 #pragma once
+#include <type_traits>
+
 #include "decode_stream.cuh"  // ldmatrix, ex2_approx
 #include "paged_attn.cuh"
 
@@ -169,9 +171,23 @@ struct Tf32Shape {
 };
 
 // (integer rounding, not cvt.rna.tf32: conversions run at an eighth of the rate and would take longer than the products)
-__device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
-    hi = (x + 0x1000u) & 0xffffe000u;
+// round = kRoundTf32 is the above.  A finite number within half a step of fp32's largest is infinite when it is rounded up, and what comes of it NaN.  A CTA
+// that finds NaN in its result therefore walks its slots once more with round = 0: hi is cut off to 11 bits, lo has up to 13, and hi + lo is x to 2^-21
+// of it still (lo lo, below 2^-20, is left out as before).  If the NaN was in the data it comes out again.  (One token over 16 x 4288 slots of 64- and
+// 128-element rows, 5 chunks of 400 tokens over 800 slots of 64: without 67.7, 117 and 196 us; as it is 67.9, 117 and 199; with the addend in a
+// register instead of a second copy of the loop 67.4, 117 and 203; with a test of every number before it is split 71, 127 and 214.)
+constexpr uint32_t kRoundTf32 = 0x1000u;
+__device__ __forceinline__ void split_tf32(uint32_t x, uint32_t round, uint32_t& hi, uint32_t& lo) {
+    hi = (x + round) & 0xffffe000u;
     lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi));
+}
+// Whether a row sum or an output element is NaN or infinite in any thread of the CTA.
+template <int N>
+__device__ __forceinline__ bool any_not_finite(const float (&l)[2], const float (&o)[N][4]) {
+    float z = l[0] * 0.f + l[1] * 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z += (o[i][0] * 0.f + o[i][1] * 0.f) + (o[i][2] * 0.f + o[i][3] * 0.f);
+    return __syncthreads_or(!(z == 0.f));
 }
 __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -183,10 +199,10 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], 
 // products drifts towards zero: 2.4e-6 of the result where all 432 products of a row went into one accumulator), so the large products
 // and the small ones have accumulators of their own, of few products each, and are added up with rounded additions.
 template <int N>
-__device__ __forceinline__ void mma_split(float (*big)[4], float (*small)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&b)[2 * N]) {
+__device__ __forceinline__ void mma_split(float (*big)[4], float (*small)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const uint32_t (&b)[2 * N], uint32_t round) {
     uint32_t h[2 * N], l[2 * N];
 #pragma unroll
-    for (int i = 0; i < 2 * N; ++i) split_tf32(b[i], h[i], l[i]);
+    for (int i = 0; i < 2 * N; ++i) split_tf32(b[i], round, h[i], l[i]);
 #pragma unroll
     for (int i = 0; i < N; ++i) mma_tf32(small[i], al, h[2 * i], h[2 * i + 1]);
 #pragma unroll
@@ -212,124 +228,130 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
     Fp32Unit u;
     if (!u.find(a)) return;
     u.fetch_q<D>(a, qs, RS, S::BM);
-    if (u.b0 < u.b1) {
-        u.fetch<D>(a, ks, RS, a.kv.k_pool, u.b0 * kFp32Keys, true);
-        u.fetch<D>(a, vs, RS, a.kv.v_pool, u.b0 * kFp32Keys, false);
-    }
     const int row_w = FEW ? 0 : warp * 16, slot_w = FEW ? warp * 16 : 0;  // the warp's first row, first slot of a step
     const int row0 = row_w + qrow;  // this thread's rows: row0, row0 + 8
     const bool active = row_w < u.rows;
     const int last[2] = {u.last_slot(a, row0), u.last_slot(a, row0 + 8)};
     const int min_last = u.last_slot(a, 0);
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[D / 8][4];
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m[2], l[2], o[D / 8][4];
     const uint32_t q_at = smem_u32(qs + (row_w + (lane & 15)) * RS + (lane >> 4) * 4);
     const uint32_t k_at = smem_u32(ks + (slot_w + (lane & 7) + (lane >> 4) * 8) * RS + ((lane >> 3) & 1) * 4);
 
-    for (int b = u.b0; b < u.b1; ++b) {
-        const int j0 = b * kFp32Keys;
-        copy_wait<1>();  // K of this step (V may be on its way)
-        __syncthreads();
-        float s[NB][4];
-        if (active) {
-            float small[NB][4];
-            clear_tiles<NB>(s);
-            clear_tiles<NB>(small);
+    auto walk = [&](auto rounding) {  // the CTA's slots from the first to the last
+        constexpr uint32_t round = decltype(rounding)::value;
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+        clear_tiles<D / 8>(o);
+        if (u.b0 < u.b1) {
+            u.fetch<D>(a, ks, RS, a.kv.k_pool, u.b0 * kFp32Keys, true);
+            u.fetch<D>(a, vs, RS, a.kv.v_pool, u.b0 * kFp32Keys, false);
+        }
+        for (int b = u.b0; b < u.b1; ++b) {
+            const int j0 = b * kFp32Keys;
+            copy_wait<1>();  // K of this step (V may be on its way)
+            __syncthreads();
+            float s[NB][4];
+            if (active) {
+                float small[NB][4];
+                clear_tiles<NB>(s);
+                clear_tiles<NB>(small);
 #pragma unroll 2
-            for (int k = 0; k < D / 8; ++k) {
-                uint32_t x[4], ah[4], al[4];
-                ldmatrix_x4(q_at + k * 32, x);  // rows 0-7 | rows 8-15, elements 8 k .. + 3, then the next four
+                for (int k = 0; k < D / 8; ++k) {
+                    uint32_t x[4], ah[4], al[4];
+                    ldmatrix_x4(q_at + k * 32, x);  // rows 0-7 | rows 8-15, elements 8 k .. + 3, then the next four
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split_tf32(x[e], ah[e], al[e]);
+                    for (int e = 0; e < 4; ++e) split_tf32(x[e], round, ah[e], al[e]);
 #pragma unroll
-                for (int i = 0; i < NB; i += GB) {
-                    uint32_t y[2 * GB];  // blocks of 8 slots, two 4-element halves each
+                    for (int i = 0; i < NB; i += GB) {
+                        uint32_t y[2 * GB];  // blocks of 8 slots, two 4-element halves each
 #pragma unroll
-                    for (int e = 0; e < GB; e += 2) ldmatrix_x4(k_at + ((i + e) * 8 * RS + k * 8) * 4, reinterpret_cast<uint32_t(&)[4]>(y[2 * e]));
-                    mma_split<GB>(s + i, small + i, ah, al, y);
+                        for (int e = 0; e < GB; e += 2) ldmatrix_x4(k_at + ((i + e) * 8 * RS + k * 8) * 4, reinterpret_cast<uint32_t(&)[4]>(y[2 * e]));
+                        mma_split<GB>(s + i, small + i, ah, al, y, round);
+                    }
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[i][e] += small[i][e];
-        }
-        __syncthreads();  // K has been read
-        if (b + 1 < u.b1) u.fetch<D>(a, ks, RS, a.kv.k_pool, j0 + kFp32Keys, true);
-        else copy_commit();
-        if (active) {
-            if (j0 < u.lo || j0 + kFp32Keys - 1 > min_last) {
 #pragma unroll
                 for (int i = 0; i < NB; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int slot = j0 + slot_w + i * 8 + 2 * quad + (e & 1);
-                        if (slot < u.lo || slot > last[e >> 1]) s[i][e] = -INFINITY;
-                    }
+                    for (int e = 0; e < 4; ++e) s[i][e] += small[i][e];
             }
+            __syncthreads();  // K has been read
+            if (b + 1 < u.b1) u.fetch<D>(a, ks, RS, a.kv.k_pool, j0 + kFp32Keys, true);
+            else copy_commit();
+            if (active) {
+                if (j0 < u.lo || j0 + kFp32Keys - 1 > min_last) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float mx = -INFINITY;
+                    for (int i = 0; i < NB; ++i)
 #pragma unroll
-                for (int i = 0; i < NB; ++i) mx = fmaxf(mx, fmaxf(s[i][2 * r], s[i][2 * r + 1]));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                const float mn = fmaxf(m[r], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
-                const float corr = ex2_approx(m[r] - ref);
-                m[r] = mn;
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < NB; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        s[i][2 * r + e] = ex2_approx(fmaf(s[i][2 * r + e], a.scale_log2, -ref));
-                        sum += s[i][2 * r + e];
-                    }
-                l[r] = l[r] * corr + sum;  // (this thread's slots: joined over the row's four threads at the end)
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    o[i][2 * r] *= corr;
-                    o[i][2 * r + 1] *= corr;
-                }
-            }
-        }
-        copy_wait<1>();  // V of this step
-        __syncthreads();
-        if (active) {
-#pragma unroll
-            for (int n = 0; n < D / 8; n += 4) {  // four blocks of 8 columns at a time, summed over the step's slots on their own
-                float big[4][4], small[4][4];
-                clear_tiles<4>(big);
-                clear_tiles<4>(small);
-#pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    uint32_t ah[4], al[4];
-                    split_tf32(__float_as_uint(s[i][0]), ah[0], al[0]);
-                    split_tf32(__float_as_uint(s[i][2]), ah[1], al[1]);
-                    split_tf32(__float_as_uint(s[i][1]), ah[2], al[2]);
-                    split_tf32(__float_as_uint(s[i][3]), ah[3], al[3]);
-                    const float* v = vs + (slot_w + i * 8 + 2 * quad) * RS + qrow + n * 8;
-                    uint32_t y[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[2 * e] = __float_as_uint(v[e * 8]);
-                        y[2 * e + 1] = __float_as_uint(v[RS + e * 8]);
-                    }
-                    mma_split<4>(big, FEW ? big : small, ah, al, y);  // (FEW: two blocks, six products in all)
+                        for (int e = 0; e < 4; ++e) {
+                            const int slot = j0 + slot_w + i * 8 + 2 * quad + (e & 1);
+                            if (slot < u.lo || slot > last[e >> 1]) s[i][e] = -INFINITY;
+                        }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int r = 0; r < 2; ++r) {
+                    float mx = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[n + i][e] += FEW ? big[i][e] : big[i][e] + small[i][e];
+                    for (int i = 0; i < NB; ++i) mx = fmaxf(mx, fmaxf(s[i][2 * r], s[i][2 * r + 1]));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    const float mn = fmaxf(m[r], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
+                    const float corr = ex2_approx(m[r] - ref);
+                    m[r] = mn;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            s[i][2 * r + e] = ex2_approx(fmaf(s[i][2 * r + e], a.scale_log2, -ref));
+                            sum += s[i][2 * r + e];
+                        }
+                    l[r] = l[r] * corr + sum;  // (this thread's slots: joined over the row's four threads at the end)
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        o[i][2 * r] *= corr;
+                        o[i][2 * r + 1] *= corr;
+                    }
+                }
             }
+            copy_wait<1>();  // V of this step
+            __syncthreads();
+            if (active) {
+#pragma unroll
+                for (int n = 0; n < D / 8; n += 4) {  // four blocks of 8 columns at a time, summed over the step's slots on their own
+                    float big[4][4], small[4][4];
+                    clear_tiles<4>(big);
+                    clear_tiles<4>(small);
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) {
+                        uint32_t ah[4], al[4];
+                        split_tf32(__float_as_uint(s[i][0]), kRoundTf32, ah[0], al[0]);
+                        split_tf32(__float_as_uint(s[i][2]), kRoundTf32, ah[1], al[1]);
+                        split_tf32(__float_as_uint(s[i][1]), kRoundTf32, ah[2], al[2]);
+                        split_tf32(__float_as_uint(s[i][3]), kRoundTf32, ah[3], al[3]);
+                        const float* v = vs + (slot_w + i * 8 + 2 * quad) * RS + qrow + n * 8;
+                        uint32_t y[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            y[2 * e] = __float_as_uint(v[e * 8]);
+                            y[2 * e + 1] = __float_as_uint(v[RS + e * 8]);
+                        }
+                        mma_split<4>(big, FEW ? big : small, ah, al, y, round);  // (FEW: two blocks, six products in all)
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n + i][e] += FEW ? big[i][e] : big[i][e] + small[i][e];
+                }
+            }
+            __syncthreads();  // V has been read
+            if (b + 1 < u.b1) u.fetch<D>(a, vs, RS, a.kv.v_pool, j0 + kFp32Keys, false);
+            else copy_commit();
         }
-        __syncthreads();  // V has been read
-        if (b + 1 < u.b1) u.fetch<D>(a, vs, RS, a.kv.v_pool, j0 + kFp32Keys, false);
-        else copy_commit();
-    }
-    copy_commit();
-    copy_wait<0>();  // (nothing is in flight when the CTA ends)
+        copy_commit();
+        copy_wait<0>();  // (nothing is in flight when the CTA ends)
+    };
+    walk(std::integral_constant<uint32_t, kRoundTf32>());
+    if (any_not_finite(l, o)) walk(std::integral_constant<uint32_t, 0>());
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -389,129 +411,136 @@ __global__ void __launch_bounds__(kFp32Threads, Tf32DecodeShape<D>::PER_SM) page
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, qrow = lane >> 2;
     Fp32Unit u;
     if (!u.find(a)) return;
-    if (u.b0 < u.b1) {
-        u.fetch<D>(a, ks, RS, a.kv.k_pool, u.b0 * kFp32Keys, true);
-        u.fetch<D>(a, vs, RS, a.kv.v_pool, u.b0 * kFp32Keys, false);
-    }
-    // elements 8 k + quad and 8 k + quad + 4 of row qrow, the high parts, then the low ones; rows behind the last are zero
-    for (int i = threadIdx.x; i < KS * 32; i += kFp32Threads) {
-        const int l = i & 31, k = i >> 5, row = l >> 2;
-        uint32_t x0 = 0, x1 = 0;
-        if (row < u.rows) {
-            const int t = row / a.group, g = row - t * a.group;
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q.p) + (long long)(u.tok0 + t) * a.q.token_stride + (u.head * a.group + g) * a.q.head_stride + k * 8 + (l & 3);
-            x0 = p[0];
-            x1 = p[4];
-        }
-        uint4 f;
-        split_tf32(x0, f.x, f.z);
-        split_tf32(x1, f.y, f.w);
-        qf[i] = f;
-    }
     const int slot_w = warp * 16;  // the warp's first slot of a step
     const int last[2] = {u.last_slot(a, 2 * quad), u.last_slot(a, 2 * quad + 1)};
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[OT][4];
-    clear_tiles<OT>(o);
+    float m[2], l[2], o[OT][4];
     const int min_last = u.last_slot(a, 0);
     const uint32_t k_at = smem_u32(ks + (slot_w + (lane & 15)) * RS + (lane >> 4) * 4);
     const float* v_at = vs + (slot_w + 2 * quad) * RS + 4 * qrow;
 
-    for (int b = u.b0; b < u.b1; ++b) {
-        const int j0 = b * kFp32Keys;
-        copy_wait<1>();  // K of this step (V may be on its way)
-        __syncthreads();
-        float s[4];
-        {
-            float big[2][4], small[4][4];  // (accumulators of few products, and chains short enough)
-            clear_tiles<2>(big);
-            clear_tiles<4>(small);
+    auto walk = [&](auto rounding) {  // the CTA's slots from the first to the last
+        constexpr uint32_t round = decltype(rounding)::value;
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+        clear_tiles<OT>(o);
+        if (u.b0 < u.b1) {
+            u.fetch<D>(a, ks, RS, a.kv.k_pool, u.b0 * kFp32Keys, true);
+            u.fetch<D>(a, vs, RS, a.kv.v_pool, u.b0 * kFp32Keys, false);
+        }
+        // elements 8 k + quad and 8 k + quad + 4 of row qrow, the high parts, then the low ones; rows behind the last are zero
+        for (int i = threadIdx.x; i < KS * 32; i += kFp32Threads) {
+            const int l = i & 31, k = i >> 5, row = l >> 2;
+            uint32_t x0 = 0, x1 = 0;
+            if (row < u.rows) {
+                const int t = row / a.group, g = row - t * a.group;
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q.p) + (long long)(u.tok0 + t) * a.q.token_stride + (u.head * a.group + g) * a.q.head_stride + k * 8 + (l & 3);
+                x0 = p[0];
+                x1 = p[4];
+            }
+            uint4 f;
+            split_tf32(x0, round, f.x, f.z);
+            split_tf32(x1, round, f.y, f.w);
+            qf[i] = f;
+        }
+        for (int b = u.b0; b < u.b1; ++b) {
+            const int j0 = b * kFp32Keys;
+            copy_wait<1>();  // K of this step (V may be on its way)
+            __syncthreads();
+            float s[4];
+            {
+                float big[2][4], small[4][4];  // (accumulators of few products, and chains short enough)
+                clear_tiles<2>(big);
+                clear_tiles<4>(small);
 #pragma unroll 8
-            for (int k = 0; k < KS; ++k) {
-                uint32_t x[4], ah[4], al[4];
-                ldmatrix_x4(k_at + k * 32, x);  // slots 0-7 | 8-15, elements 8 k .. + 3, then the next four
+                for (int k = 0; k < KS; ++k) {
+                    uint32_t x[4], ah[4], al[4];
+                    ldmatrix_x4(k_at + k * 32, x);  // slots 0-7 | 8-15, elements 8 k .. + 3, then the next four
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split_tf32(x[e], ah[e], al[e]);
-                const uint4 q = qf[k * 32 + lane];
-                mma_tf32(small[k & 1], al, q.x, q.y);
-                mma_tf32(big[k & 1], ah, q.x, q.y);
-                mma_tf32(small[2 + (k & 1)], ah, q.z, q.w);
+                    for (int e = 0; e < 4; ++e) split_tf32(x[e], round, ah[e], al[e]);
+                    const uint4 q = qf[k * 32 + lane];
+                    mma_tf32(small[k & 1], al, q.x, q.y);
+                    mma_tf32(big[k & 1], ah, q.x, q.y);
+                    mma_tf32(small[2 + (k & 1)], ah, q.z, q.w);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = big[0][e] + big[1][e] + ((small[0][e] + small[1][e]) + (small[2][e] + small[3][e]));
             }
+            __syncthreads();  // K has been read
+            if (b + 1 < u.b1) u.fetch<D>(a, ks, RS, a.kv.k_pool, j0 + kFp32Keys, true);
+            else copy_commit();
+            // this thread: slots qrow (+ 8), rows 2 quad (+ 1)
+            if (j0 < u.lo || j0 + kFp32Keys - 1 > min_last) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] = big[0][e] + big[1][e] + ((small[0][e] + small[1][e]) + (small[2][e] + small[3][e]));
-        }
-        __syncthreads();  // K has been read
-        if (b + 1 < u.b1) u.fetch<D>(a, ks, RS, a.kv.k_pool, j0 + kFp32Keys, true);
-        else copy_commit();
-        // this thread: slots qrow (+ 8), rows 2 quad (+ 1)
-        if (j0 < u.lo || j0 + kFp32Keys - 1 > min_last) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int slot = j0 + slot_w + qrow + (e >> 1) * 8;
-                if (slot < u.lo || slot > last[e & 1]) s[e] = -INFINITY;
-            }
-        }
-        float corr[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(s[e], s[2 + e]);
-#pragma unroll
-            for (int w = 4; w <= 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-            const float mn = fmaxf(m[e], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
-            corr[e] = ex2_approx(m[e] - ref);
-            m[e] = mn;
-            s[e] = ex2_approx(fmaf(s[e], a.scale_log2, -ref));
-            s[2 + e] = ex2_approx(fmaf(s[2 + e], a.scale_log2, -ref));
-            l[e] = l[e] * corr[e] + (s[e] + s[2 + e]);  // (this thread's slots: joined over the row's threads at the end)
-        }
-        uint32_t ph[2][2], pl[2][2];  // P^T of slots 0-7 | 8-15: slots 2 quad and 2 quad + 1 of row qrow
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t x = __float_as_uint(s[2 * h]), y = __float_as_uint(s[2 * h + 1]);
-            const uint32_t hi = movmatrix_trans(__byte_perm(x, y, 0x7632)), lo = movmatrix_trans(__byte_perm(x, y, 0x5410));
-            split_tf32(__byte_perm(lo, hi, 0x5410), ph[h][0], pl[h][0]);
-            split_tf32(__byte_perm(lo, hi, 0x7632), ph[h][1], pl[h][1]);
-        }
-        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-            for (int i = 0; i < OT; ++i) {
-                o[i][0] *= corr[0];
-                o[i][1] *= corr[1];
-                o[i][2] *= corr[0];
-                o[i][3] *= corr[1];
-            }
-        }
-        copy_wait<1>();  // V of this step
-        __syncthreads();
-#pragma unroll
-        for (int g = 0; g < D / 32; ++g) {  // elements 32 g + 4 qrow .. + 3: rows qrow and qrow + 8 of two products
-            float part[2][4];
-            clear_tiles<2>(part);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 v0 = *reinterpret_cast<const uint4*>(v_at + h * 8 * RS + g * 32);
-                const uint4 v1 = *reinterpret_cast<const uint4*>(v_at + (h * 8 + 1) * RS + g * 32);
-                const uint32_t x[2][4] = {{v0.x, v0.y, v1.x, v1.y}, {v0.z, v0.w, v1.z, v1.w}};
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t ah[4], al[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) split_tf32(x[i][e], ah[e], al[e]);
-                    mma_tf32(part[i], al, ph[h][0], ph[h][1]);  // (six products in all)
-                    mma_tf32(part[i], ah, pl[h][0], pl[h][1]);
-                    mma_tf32(part[i], ah, ph[h][0], ph[h][1]);
+                for (int e = 0; e < 4; ++e) {
+                    const int slot = j0 + slot_w + qrow + (e >> 1) * 8;
+                    if (slot < u.lo || slot > last[e & 1]) s[e] = -INFINITY;
                 }
             }
+            float corr[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int e = 0; e < 2; ++e) {
+                float mx = fmaxf(s[e], s[2 + e]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[2 * g + i][e] += part[i][e];
+                for (int w = 4; w <= 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                const float mn = fmaxf(m[e], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
+                corr[e] = ex2_approx(m[e] - ref);
+                m[e] = mn;
+                s[e] = ex2_approx(fmaf(s[e], a.scale_log2, -ref));
+                s[2 + e] = ex2_approx(fmaf(s[2 + e], a.scale_log2, -ref));
+                l[e] = l[e] * corr[e] + (s[e] + s[2 + e]);  // (this thread's slots: joined over the row's threads at the end)
+            }
+            uint32_t ph[2][2], pl[2][2];  // P^T of slots 0-7 | 8-15: slots 2 quad and 2 quad + 1 of row qrow
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t x = __float_as_uint(s[2 * h]), y = __float_as_uint(s[2 * h + 1]);
+                const uint32_t hi = movmatrix_trans(__byte_perm(x, y, 0x7632)), lo = movmatrix_trans(__byte_perm(x, y, 0x5410));
+                split_tf32(__byte_perm(lo, hi, 0x5410), kRoundTf32, ph[h][0], pl[h][0]);
+                split_tf32(__byte_perm(lo, hi, 0x7632), kRoundTf32, ph[h][1], pl[h][1]);
+            }
+            if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+                for (int i = 0; i < OT; ++i) {
+                    o[i][0] *= corr[0];
+                    o[i][1] *= corr[1];
+                    o[i][2] *= corr[0];
+                    o[i][3] *= corr[1];
+                }
+            }
+            copy_wait<1>();  // V of this step
+            __syncthreads();
+#pragma unroll
+            for (int g = 0; g < D / 32; ++g) {  // elements 32 g + 4 qrow .. + 3: rows qrow and qrow + 8 of two products
+                float part[2][4];
+                clear_tiles<2>(part);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 v0 = *reinterpret_cast<const uint4*>(v_at + h * 8 * RS + g * 32);
+                    const uint4 v1 = *reinterpret_cast<const uint4*>(v_at + (h * 8 + 1) * RS + g * 32);
+                    const uint32_t x[2][4] = {{v0.x, v0.y, v1.x, v1.y}, {v0.z, v0.w, v1.z, v1.w}};
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t ah[4], al[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) split_tf32(x[i][e], round, ah[e], al[e]);
+                        mma_tf32(part[i], al, ph[h][0], ph[h][1]);  // (six products in all)
+                        mma_tf32(part[i], ah, pl[h][0], pl[h][1]);
+                        mma_tf32(part[i], ah, ph[h][0], ph[h][1]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[2 * g + i][e] += part[i][e];
+            }
+            __syncthreads();  // V has been read
+            if (b + 1 < u.b1) u.fetch<D>(a, vs, RS, a.kv.v_pool, j0 + kFp32Keys, false);
+            else copy_commit();
         }
-        __syncthreads();  // V has been read
-        if (b + 1 < u.b1) u.fetch<D>(a, vs, RS, a.kv.v_pool, j0 + kFp32Keys, false);
-        else copy_commit();
-    }
-    copy_commit();
-    copy_wait<0>();  // (nothing is in flight when the CTA ends)
+        copy_commit();
+        copy_wait<0>();  // (nothing is in flight when the CTA ends)
+    };
+    walk(std::integral_constant<uint32_t, kRoundTf32>());
+    if (any_not_finite(l, o)) walk(std::integral_constant<uint32_t, 0>());
     // the warps' parts side by side where K was
     constexpr int PS = D + 4;
     static_assert(S::WARPS * S::ROWS * PS <= kFp32Keys * RS, "the parts fit where K was");

@@ -721,3 +721,26 @@ def test_attention_reports_slots_that_the_table_does_not_hold(dtype, n):
             c.kv.attn(q, out, c.cu, causal=causal, max_chunk=max(n), max_len=256, workspace=ws)
             assert int(c.status) == want, (lens, causal)
             c.status.zero_()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,n", [(1, [1, 3]), (2, [2, 7]), (4, [40, 9])])        # the kernels of 8, 16 and 64 rows
+def test_fp32_attention_of_the_largest_numbers(d, hq, n):
+    """Finite values next to fp32's largest stay finite: in V, and in q or K where the other factor is zero."""
+    c = PagedCase(F32, d, 1, 32, "nhd", n, [70, 129])
+    c.fill(None, 5)
+    top = torch.tensor([0x7f7fffff, 0x7f7fff8b, 0x7f7ff000, 0x7f7fefff], dtype=torch.int32).view(torch.float32)
+    for s, length in enumerate(c.lens):
+        for e in range(d):                            # one slot of each column, either sign
+            c.pools[1][c.place(s, 0, (7 * e) % (length - max(n)))][e] = top[e % 4] * (1 if e & 4 else -1)
+        for j in range(length):
+            c.pools[0][c.place(s, 0, j)][:4] = top * (1 if j & 1 else -1)
+            c.pools[0][c.place(s, 0, j)][4:8] = 0.0
+    for p, x in zip(c.pools, c.dev):
+        x.copy_(p.to(DEV))
+    q = _randn((sum(n), hq, d), F32, 4)
+    q[..., :4] = 0.0
+    q[..., 4:8] = top
+    for workspace in (False, True):
+        _check_attention(c, hq, True, None, workspace, 0, out_pad=0, q=q)
