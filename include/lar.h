@@ -355,7 +355,7 @@ typedef struct lar_paged_kv {
     int64_t table_seq_stride, table_head_stride;  /* entries */
     const int32_t* lens;       /* device: live entries of each sequence, the tokens of the current chunks included */
     int64_t lens_stride;       /* entries */
-    uint32_t* status;          /* device word, or NULL */
+    uint32_t* status;          /* device word that takes status bits (64 as above, 4: see lar_paged_attn), or NULL: they are lost */
 } lar_paged_kv_t;
 
 /* cos and sin of every pair for n_rows positions: cos_sin (device, fp32) [n_rows, head_dim], the head_dim / 2 cosines of a
@@ -388,6 +388,8 @@ lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* r
  * no row of a sequence sees (behind lens, before kv_start) may hold anything.  Tokens that belong to no sequence are left alone.  A
  * non-finite value in a slot that some row of the chunk sees may reach every row of the chunk, with fp32 storage an infinity as
  * NaN (operands are split into two numbers).  out overlaps nothing else.
+ * With bf16 storage the kernel's waits are bounded (about a second): one that runs out, on a GPU that was held up for that long, ends the
+ * launch with output rows that are not valid and records status bit 4 in kv->status.  Pass a status word and read it with the results.
  * LAR_ERR_CAPACITY: bf16 with more than 1024 sequences, or 2^30 (query tile, cache tile) pairs or more.
  * Query head hq uses KV head hq / (n_q_heads / n_kv_heads); their ratio is 1..16.  softmax_scale 0 selects 1/sqrt(head_dim).
  * max_chunk and max_len bound the tokens of a chunk and the entries of a cache (0: not known); they only choose the launch

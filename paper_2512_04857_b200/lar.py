@@ -388,7 +388,7 @@ class PagedKV:
     page_table      int32 [seqs, columns], or [seqs, kv_heads, columns] where every head has pages of its own (the pools
                     then have one head)
     lens            int32 [seqs]: live entries, the tokens of the current chunks included
-    status          int32 [1] (or None): takes the status bits of pages and slots outside the cache
+    status          int32 [1] (None: the object keeps one of its own): takes the status bits, see poll_device_status
     """
 
     def __init__(self, k_pool, v_pool, page_table, lens, n_kv_heads, status=None):
@@ -404,6 +404,9 @@ class PagedKV:
         _require(lens.dtype == torch.int32 and lens.device == k_pool.device and tuple(lens.shape) == (seqs,), "PagedKV: lens")
         _require(status is None or (status.dtype in (torch.int32, torch.uint32) and status.device == k_pool.device and
                                     status.numel() == 1), "PagedKV: status")
+        if status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=k_pool.device)
+        self._status = status
         self._keep = (k_pool, v_pool, page_table, lens, status)
         self._set(lar_paged_kv_t(
             C.sizeof(lar_paged_kv_t), _dtype_of(k_pool), seqs, n_kv_heads, d, page_tokens, pages, page_table.shape[-1],
@@ -421,9 +424,19 @@ class PagedKV:
         import torch
         self, desc = cls.__new__(cls), lar_paged_kv_t()
         _chk(lib().lar_cache_paged_view(cache.handle, layer, desc), "lar_cache_paged_view")
-        self._keep = (cache,)
+        self._keep, self._status = (cache,), None
         self._set(desc, torch.bfloat16 if cache.cfg.dtype == LAR_BF16 else torch.float32, cache.slab.device)
         return self
+
+    def poll_device_status(self) -> int:
+        """Waits for the current stream, returns the status bits since the last poll and clears them: 64 a page or slot outside the
+        cache, 4 a wait of the bf16 attention ran into its limit and output rows are not valid (0 = clean)."""
+        if self._status is None:
+            return self._keep[0].poll_device_status()
+        bits = int(self._status.item()) & 0xffffffff
+        if bits:
+            self._status.zero_()
+        return bits
 
     def append_rope(self, k, v, cu_tokens=None, rope=None, pos=None, q=None, q_out=None):
         """Stores the chunks' keys (rotated by rope at pos [axes, tokens]) and values; q is rotated into q_out."""

@@ -744,3 +744,37 @@ def test_fp32_attention_of_the_largest_numbers(d, hq, n):
     q[..., 4:8] = top
     for workspace in (False, True):
         _check_attention(c, hq, True, None, workspace, 0, out_pad=0, q=q)
+
+
+# ------------------------------------------------------------------------------------------------------ status word
+def test_a_paged_cache_has_a_status_word_of_its_own():
+    """Where the caller gives none, the binding keeps one: a wait that ran out or a bad page is not lost."""
+    pool, table, lens = torch.zeros(4, 32, 2, 64), torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    kv = lar.PagedKV(pool, pool, table, lens, 2)
+    assert kv.desc.status and kv.poll_device_status() == 0
+    word = torch.zeros(1, dtype=torch.int32)
+    kv = lar.PagedKV(pool, pool, table, lens, 2, status=word)
+    assert kv.desc.status == word.data_ptr()
+    word.fill_(68)
+    assert kv.poll_device_status() == 68 and kv.poll_device_status() == 0 and int(word) == 0
+
+
+@pytest.mark.gpu
+def test_status_of_a_paged_cache_and_of_a_layer():
+    c = PagedCase(BF, 64, 2, 32, "nhd", [3], [40])
+    c.fill(None, 1)
+    kv = lar.PagedKV(c.dev[0], c.dev[1], c.kv._keep[2], c.lens_dev, 2)
+    q = _randn((3, 2, 64), BF, 1).to(DEV)
+    out = torch.empty_like(q)
+    kv.attn(q, out, c.cu)
+    assert kv.poll_device_status() == 0
+    kv._keep[2][0, 1] = -1
+    kv.attn(q, out, c.cu)
+    assert kv.poll_device_status() == 64 and kv.poll_device_status() == 0
+    cache = lar.Cache(lar.make_config(n_layers=1, batch=1, n_q_heads=2, n_kv_heads=2, head_dim=64, dtype="bf16", cond_len=3, line_width=8, n_lines=4,
+                                      anchor_len=8, recent_lines=1, budget_lines=4))
+    assert cache.paged_view(0).poll_device_status() == 0
+    view = cache.paged_view(0)
+    view.attn(q, out, c.cu)                                # an empty cache: the chunk is longer than it
+    assert view.poll_device_status() == 64 and cache.poll_device_status() == 0
+    cache.close()
