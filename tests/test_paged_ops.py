@@ -778,3 +778,94 @@ def test_status_of_a_paged_cache_and_of_a_layer():
     view.attn(q, out, c.cu)                                # an empty cache: the chunk is longer than it
     assert view.poll_device_status() == 64 and cache.poll_device_status() == 0
     cache.close()
+
+
+# ------------------------------------------------------------------------------------ views, and calls behind each other
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout", ["interleaved", "heads outermost", "one head's pages"])
+@pytest.mark.parametrize("d,hkv,hq,n", [(64, 2, 4, [1, 3]), (128, 2, 8, [1, 2]), (64, 3, 3, [40, 9]), (128, 2, 4, [150, 7]), (128, 1, 1, [1, 1])])
+def test_attention_of_views(dtype, layout, d, hkv, hq, n):
+    """q in a fused projection or head-major, out head-major, pools in one tensor or heads outermost, the table and the lengths
+    parts of larger tensors: strides of the tensor maps on the bf16 path."""
+    page, lens = 32, [300, 170]
+    T, cols = sum(n), 10
+    heads, per_head = (1, True) if layout == "one head's pages" else (hkv, False)
+    pages = 2 * cols * (hkv if per_head else 1)
+    base = _randn({"interleaved": (pages, 2, page, heads, d), "heads outermost": (2, heads, pages, page, d),
+                   "one head's pages": (pages, page, 2, 1, d)}[layout], dtype, 1)
+    dev = base.to(DEV)
+
+    def pools(x):
+        if layout == "interleaved":
+            return x[:, 0], x[:, 1]
+        if layout == "heads outermost":
+            return x[0].permute(1, 2, 0, 3), x[1].permute(1, 2, 0, 3)
+        return x[:, :, 0], x[:, :, 1]
+    ids = torch.randperm(pages, generator=torch.Generator().manual_seed(2)).int()
+    table = ids.view(2, hkv, cols) if per_head else ids.view(2, cols)
+    wide = torch.full((4, *table.shape[1:-1], cols + 3), -1, dtype=torch.int32)
+    wide[::2, ..., 1:cols + 1] = table
+    lens3 = torch.tensor([lens[0], -1, -1, lens[1]], dtype=torch.int32, device=DEV)
+    kv = lar.PagedKV(*pools(dev), wide.to(DEV)[::2, ..., 1:cols + 1], lens3[::3], hkv)
+    cu = torch.tensor([0, n[0], T], dtype=torch.int32, device=DEV)
+    kc, vc = pools(base)
+    at = lambda s, h, j: (int(table[s, h, j // page] if per_head else table[s, j // page]), j % page, 0 if per_head else h)
+    rows = lambda pool: (lambda s, h, a, b: torch.stack([pool[at(s, h, j)] for j in range(a, b)]))
+    fused, major = _randn((T, hq + 2 * hkv, d), dtype, 3), _randn((hq, T, d), dtype, 4)
+    for q, qd in ((fused[:, :hq], fused.to(DEV)[:, :hq]), (major.transpose(0, 1), major.to(DEV).transpose(0, 1))):
+        for workspace in (False, True):
+            out = torch.full((hq, T + 1, d), 5.0, dtype=dtype, device=DEV)
+            ws = kv.attn_workspace(hq, T, max(n), 300) if workspace else None
+            kv.attn(qd, out[:, :T].transpose(0, 1), cu, max_chunk=max(n), max_len=300, workspace=ws)
+            ref, mag, big = R.attention(q, rows(kc), rows(vc), n, lens, None, True, hq // hkv, d ** -0.5)
+            _assert_close(out[:, :T].transpose(0, 1), ref, R.attention_tolerance(dtype, ref, mag, big, d, 300), f"workspace {workspace}")
+            assert (out[:, T:] == 5.0).all()
+    assert kv.poll_device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [[1, 1, 1], [5, 0, 20], [160, 1, 90]])
+def test_unlike_calls_share_a_workspace_one_behind_the_other(dtype, n):
+    """Calls with other queries, lengths, caches and outputs queued on one workspace without a wait between them, eagerly and as
+    graphs on a side stream: parts left by the call before must not be met."""
+    hq, hkv, d = 8, 2, 64
+    T, ws = sum(n), None
+    calls = []
+    for i, lens in enumerate(([3000, 2500, 2900], [160, 1, 700], [2049, 2900, 90], [3000, 3000, 3000])):
+        c = PagedCase(dtype, d, hkv, 64, "nhd", n, lens, seed=i, extra_cols=50)
+        for p, x in zip(c.pools, c.dev):
+            x.normal_()
+            p.copy_(x.cpu())
+        q = _randn((T, hq, d), dtype, 70 + i)
+        ref, mag, big = R.attention(q, c.rows(0), c.rows(1), n, lens, None, True, hq // hkv, d ** -0.5)
+        calls.append((c, q.to(DEV), ref, R.attention_tolerance(dtype, ref, mag, big, d, 3000)))
+        ws = ws if ws is not None else c.kv.attn_workspace(hq, T, max(n), 3000)
+
+    def run(i, out):
+        c, q = calls[i][:2]
+        c.kv.attn(q, out, c.cu, max_chunk=max(n), max_len=3000, workspace=ws)
+    order = [0, 1, 2, 3, 1, 0, 3, 2, 2, 0]
+    outs = [torch.full((T, hq, d), 5.0, dtype=dtype, device=DEV) for _ in order]
+    ws.fill_(255)
+    for i, out in zip(order, outs):
+        run(i, out)
+    torch.cuda.synchronize()
+    check = lambda: [_assert_close(out, calls[i][2], calls[i][3], f"call {i}") for i, out in zip(order, outs)]
+    check()
+    side, graphs = torch.cuda.Stream(), []
+    for i, out in zip(order, outs):
+        out.fill_(5.0)
+    torch.cuda.synchronize()
+    for i, out in zip(order, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            run(i, out)
+        graphs.append(g)
+    with torch.cuda.stream(side):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    check()
+    assert all(int(c.status) == 0 for c, *_ in calls)
