@@ -11,6 +11,11 @@
 
 namespace lar {
 
+// The softmax's reference m is the largest logit itself, and a weight 2^((s - m) scale_log2): s - m is exact where it matters, however large the logits
+// are.  Scaled first, in one multiply-add per weight, the reference is off by half a step of its own, and from logits of 2^31 on that alone
+// makes every weight of a row 0 or infinite.
+__device__ __forceinline__ float softmax_ref(float m) { return m == -INFINITY ? 0.f : m; }  // (a row that has seen nothing yet)
+
 struct PagedAttnArgs {
     PagedView kv;
     RowsView q, out;

@@ -284,16 +284,16 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
                             for (int mt = 1; mt < S::MT; ++mt) mx = fmaxf(mx, fmaxf(s[mt][r][e], s[mt][r][2 + e]));
 #pragma unroll
                             for (int w = 4; w <= 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                            const float mn = fmaxf(m[r][e], mx * sc);
-                            ref[e] = mn == -INFINITY ? 0.f : mn;  // (a row that has seen nothing yet)
-                            corr[e] = ex2_approx(m[r][e] - ref[e]);
+                            const float mn = fmaxf(m[r][e], mx);
+                            ref[e] = softmax_ref(mn);
+                            corr[e] = ex2_approx((m[r][e] - ref[e]) * sc);
                             m[r][e] = mn;
                             l[r][e] *= corr[e];
                         }
 #pragma unroll
                         for (int mt = 0; mt < S::MT; ++mt) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[mt][r][e] = ex2_approx(fmaf(s[mt][r][e], sc, -ref[e & 1]));
+                            for (int e = 0; e < 4; ++e) s[mt][r][e] = ex2_approx((s[mt][r][e] - ref[e & 1]) * sc);
                             l[r][0] += s[mt][r][0] + s[mt][r][2];
                             l[r][1] += s[mt][r][1] + s[mt][r][3];
                             pb[mt][r][0] = movmatrix_trans(pack_bf16(s[mt][r][0], s[mt][r][1]));
@@ -371,12 +371,12 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
                     mw[w] = part[w * S::ROWS * S::PS + D];
                     M = fmaxf(M, mw[w]);
                 }
-                const float ref = M == -INFINITY ? 0.f : M;
+                const float ref = softmax_ref(M);
                 float L = 0.f;
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const float f = ex2_approx(mw[w] - ref);
+                    const float f = ex2_approx((mw[w] - ref) * a.scale_log2);
                     const float4 p = *reinterpret_cast<const float4*>(part + w * S::ROWS * S::PS + e);
                     L = fmaf(part[w * S::ROWS * S::PS + D + 1], f, L);
                     o.x = fmaf(p.x, f, o.x);

@@ -134,11 +134,11 @@ struct Fp32Unit {
             float M = -INFINITY, L = 0.f, x = 0.f, y = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) M = fmaxf(M, p[w * ROWS * PS + D]);
-            const float ref = M == -INFINITY ? 0.f : M;
+            const float ref = softmax_ref(M);
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
                 const float2 ml = *reinterpret_cast<const float2*>(p + w * ROWS * PS + D), v = *reinterpret_cast<const float2*>(p + w * ROWS * PS + e);
-                const float f = ex2_approx(ml.x - ref);
+                const float f = ex2_approx((ml.x - ref) * a.scale_log2);
                 L = fmaf(ml.y, f, L);
                 x = fmaf(v.x, f, x);
                 y = fmaf(v.y, f, y);
@@ -294,15 +294,15 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
                     for (int i = 0; i < NB; ++i) mx = fmaxf(mx, fmaxf(s[i][2 * r], s[i][2 * r + 1]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    const float mn = fmaxf(m[r], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
-                    const float corr = ex2_approx(m[r] - ref);
+                    const float mn = fmaxf(m[r], mx), ref = softmax_ref(mn);
+                    const float corr = ex2_approx((m[r] - ref) * a.scale_log2);
                     m[r] = mn;
                     float sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < NB; ++i)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            s[i][2 * r + e] = ex2_approx(fmaf(s[i][2 * r + e], a.scale_log2, -ref));
+                            s[i][2 * r + e] = ex2_approx((s[i][2 * r + e] - ref) * a.scale_log2);
                             sum += s[i][2 * r + e];
                         }
                     l[r] = l[r] * corr + sum;  // (this thread's slots: joined over the row's four threads at the end)
@@ -482,11 +482,11 @@ __global__ void __launch_bounds__(kFp32Threads, Tf32DecodeShape<D>::PER_SM) page
                 float mx = fmaxf(s[e], s[2 + e]);
 #pragma unroll
                 for (int w = 4; w <= 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                const float mn = fmaxf(m[e], mx * a.scale_log2), ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet)
-                corr[e] = ex2_approx(m[e] - ref);
+                const float mn = fmaxf(m[e], mx), ref = softmax_ref(mn);
+                corr[e] = ex2_approx((m[e] - ref) * a.scale_log2);
                 m[e] = mn;
-                s[e] = ex2_approx(fmaf(s[e], a.scale_log2, -ref));
-                s[2 + e] = ex2_approx(fmaf(s[2 + e], a.scale_log2, -ref));
+                s[e] = ex2_approx((s[e] - ref) * a.scale_log2);
+                s[2 + e] = ex2_approx((s[2 + e] - ref) * a.scale_log2);
                 l[e] = l[e] * corr[e] + (s[e] + s[2 + e]);  // (this thread's slots: joined over the row's threads at the end)
             }
             uint32_t ph[2][2], pl[2][2];  // P^T of slots 0-7 | 8-15: slots 2 quad and 2 quad + 1 of row qrow
@@ -570,13 +570,13 @@ __global__ void __launch_bounds__(128) combine_splits_kernel(const PagedAttnArgs
     if (a.kv.cu && (t < a.kv.cu[0] || t >= a.kv.cu[a.kv.n_seqs])) return;  // no sequence's token: left as it was
     float M = -INFINITY;
     for (int s = 0; s < a.n_splits; ++s) M = fmaxf(M, a.part_ml[((size_t)s * n_rows + row) * 2]);
-    const float ref = M == -INFINITY ? 0.f : M;
+    const float ref = softmax_ref(M);
     float L = 0.f, o[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) o[i] = 0.f;
     for (int s = 0; s < a.n_splits; ++s) {
         const size_t at = (size_t)s * n_rows + row;
-        const float f = exp2f(a.part_ml[at * 2] - ref);
+        const float f = exp2f((a.part_ml[at * 2] - ref) * a.scale_log2);
         L = fmaf(a.part_ml[at * 2 + 1], f, L);
 #pragma unroll
         for (int i = 0; i < PER; ++i) o[i] = fmaf(a.part_o[at * D + i * 32 + lane], f, o[i]);

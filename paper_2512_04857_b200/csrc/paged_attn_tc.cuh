@@ -548,7 +548,14 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                             tc_st32(tm_o + c, o);
                         }
                     }
-                    const float mref = m_used == -INFINITY ? 0.f : m_used * sc;
+                    // (here the reference is scaled first, a multiply-add per weight, unless it is so large that its rounding shows)
+                    float mref = softmax_ref(m_used) * sc;
+                    if (__any_sync(0xffffffffu, row < rows && fabsf(mref) > 16777216.f)) {
+                        const float ref = softmax_ref(m_used);
+#pragma unroll
+                        for (int c = 0; c < BN; ++c) s[c] = __float_as_uint(__uint_as_float(s[c]) - ref);
+                        mref = 0.f;
+                    }
                     const uint64_t sc2 = pack_f32x2(sc, sc), mr2 = pack_f32x2(-mref, -mref);
                     uint64_t sum2[2] = {0, 0};
 #pragma unroll
@@ -645,7 +652,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 }
                 if (mine && !g.whole) {
                     float* ml = a.part_ml + part * 2;
-                    ml[0] = m_used * sc;  // (-inf: nothing seen)
+                    ml[0] = m_used;  // (-inf: nothing seen)
                     ml[1] = l;
                 }
             }
@@ -857,8 +864,8 @@ __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant_
         for (int c = c0; c <= c1; ++c) {
             const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at(c) * 2);
             const float4 p = *reinterpret_cast<const float4*>(a.part_o + at(c) * D + e);
-            const float mn = fmaxf(M, ml.x), ref = mn == -INFINITY ? 0.f : mn;
-            const float f0 = ex2_approx(M - ref), f = ex2_approx(ml.x - ref);
+            const float mn = fmaxf(M, ml.x), ref = softmax_ref(mn);
+            const float f0 = ex2_approx((M - ref) * a.scale_log2), f = ex2_approx((ml.x - ref) * a.scale_log2);
             M = mn;
             L = fmaf(ml.y, f, L * f0);
             o.x = fmaf(p.x, f, o.x * f0);

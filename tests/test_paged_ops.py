@@ -869,3 +869,48 @@ def test_unlike_calls_share_a_workspace_one_behind_the_other(dtype, n):
     torch.cuda.synchronize()
     check()
     assert all(int(c.status) == 0 for c, *_ in calls)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,lens", [([1, 3], [700, 90]), ([1, 1], [3000, 2100]), ([12, 1], [700, 1500]), ([40, 2], [700, 1500]), ([150, 1], [2500, 700])])
+def test_attention_of_enormous_logits(dtype, d, n, lens):
+    """Logits of 10^9 to 10^30: the products are exact (one element of q is not zero) and lie so far apart that each row is the value
+    row of its largest logit -- and of the slots that share it, half and half."""
+    page, hq = 32, 2
+    for power in (0, 20, 70):                            # the largest logits: about 2^30, 2^50, 2^100
+        c = PagedCase(dtype, d, 1, page, "nhd", n, lens, seed=power)
+        c.fill(None, 5)
+        g = torch.Generator().manual_seed(power)
+        best = []
+        for s, length in enumerate(lens):
+            keys = torch.randperm(length, generator=g).float().bfloat16().float() + 4096.0      # (some are equal once rounded)
+            keys = keys.bfloat16().float()
+            best.append(keys)
+            for j in range(length):
+                row = c.pools[0][c.place(s, 0, j)]
+                row.zero_()
+                row[3] = keys[j] * 2.0 ** (17 + power // 2)
+        for p, x in zip(c.pools, c.dev):
+            x.copy_(p.to(DEV))
+        T = sum(n)
+        q = torch.zeros(T, hq, d, dtype=dtype)
+        q[:, 0, 3], q[:, 1, 3] = 2.0 ** (power - power // 2 + 3), -(2.0 ** (power - power // 2 + 3))
+        for workspace in (False, True):
+            out = torch.full((T, hq, d), 5.0, dtype=dtype, device=DEV)
+            ws = c.kv.attn_workspace(hq, T, max(n), max(lens)) if workspace else None
+            c.kv.attn(q.to(DEV), out, c.cu, max_chunk=max(n), max_len=max(lens), workspace=ws)
+            t = 0
+            for s, a in enumerate(n):
+                V = c.rows(1)(s, 0, 0, lens[s]).double()
+                for i in range(a):
+                    seen = best[s][:lens[s] - a + i + 1]
+                    for h, top in ((0, seen.max()), (1, seen.min())):
+                        at = (seen == top).nonzero()[:, 0]
+                        ref = V[at].mean(0)
+                        # weights are 1 each: the sum of the value rows (fp32, in 22 bits each) and its quotient, rounded to the storage type
+                        tol = V[at].abs().mean(0) * (2.0 ** -20) + (ref.abs() * 2.0 ** -8 if dtype == BF else 0) + 1e-12
+                        _assert_close(out[t + i, h], ref, tol, f"2^{power} seq {s} token {i} head {h} workspace {workspace}")
+                t += a
+    assert int(c.status) == 0
