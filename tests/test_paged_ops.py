@@ -914,3 +914,52 @@ def test_attention_of_enormous_logits(dtype, d, n, lens):
                         _assert_close(out[t + i, h], ref, tol, f"2^{power} seq {s} token {i} head {h} workspace {workspace}")
                 t += a
     assert int(c.status) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [[1, 1], [9, 1], [40, 5]])
+def test_offsets_beyond_32_bits(dtype, n):
+    """Pages, tokens and heads that lie 2^30 and 2^31 elements apart: appended to and attended over."""
+    if torch.cuda.get_device_properties(0).total_memory < 60 << 30:
+        pytest.skip("needs 35 GB")
+    d, hkv, hq, page, far = 64, 2, 4, 64, 1 << 30
+    T, lens = sum(n), [300, 3 * page]
+    buf = torch.empty(4 * far + (1 << 23), dtype=dtype, device=DEV)
+    pool = lambda at: buf.as_strided((5, page, hkv, d), (far, hkv * d, d, 1), at)
+    rows = lambda heads, at: buf.as_strided((T, heads, d), (heads * d, far, 1) if heads == 4 else (heads * d, d, 1), at)
+    table = torch.tensor([[4, 1, 3, 0, 2], [-1] * 5], dtype=torch.int32)
+    table[1, :3] = torch.tensor([2, 4, 3])                # (pages of their own and pages shared with the first sequence)
+    kp, vp = pool(0), pool(1 << 20)
+    q, qo, out = rows(hq, 2 << 20), rows(hq, 3 << 20), rows(hq, 4 << 20)
+    k, v = rows(hkv, 5 << 20), rows(hkv, (5 << 20) + (4 * far))
+    host = {}
+    for name, x in (("kp", kp), ("vp", vp), ("q", q), ("k", k), ("v", v)):
+        host[name] = _randn(tuple(x.shape), dtype, len(host))
+        x.copy_(host[name].to(DEV))
+    start = [0, 128]                                      # (what the second sequence sees lies in its own rows)
+    c = torch.tensor([0, n[0], T], dtype=torch.int32, device=DEV)
+    kv = lar.PagedKV(kp, vp, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), hkv)
+    rope, pos = lar.make_rope(d, (32,)), _pos(1, T, 5)
+    kv.append_rope(k, v, c, rope, pos.to(DEV), q, qo)
+    turned = {x: R.rotate(host[x], pos, (32,), 10000.0, False, False) for x in ("q", "k")}
+    _assert_close(qo, turned["q"], R.rotation_tolerance(dtype, turned["q"], host["q"], False), "q")
+    t = 0
+    tol = torch.zeros(5, page, hkv, d, dtype=torch.float64)
+    for s, a in enumerate(n):
+        for i in range(a):
+            j = lens[s] - a + i
+            at = int(table[s, j // page]), j % page
+            host["kp"][at], host["vp"][at] = turned["k"][t].to(dtype), host["v"][t]
+            tol[at] = R.rotation_tolerance(dtype, turned["k"][t:t + 1], host["k"][t:t + 1], False)[0] + turned["k"][t].abs() * 2.0 ** -8 * (dtype == BF)
+            t += 1
+    assert torch.equal(vp.cpu(), host["vp"])
+    _assert_close(kp, host["kp"].double(), tol + 1e-12 * (tol > 0), "keys")
+    seen = [kp.cpu(), vp.cpu()]
+    get = lambda which: (lambda s, h, a, b: torch.stack([seen[which][int(table[s, j // page]), j % page, h] for j in range(a, b)]))
+    ref, mag, big = R.attention(qo.cpu(), get(0), get(1), n, lens, start, True, hq // hkv, d ** -0.5)
+    for workspace in (False, True):
+        ws = kv.attn_workspace(hq, T, max(n), 300) if workspace else None
+        kv.attn(qo, out, c, kv_start=torch.tensor(start, dtype=torch.int32, device=DEV), max_chunk=max(n), max_len=300, workspace=ws)
+        _assert_close(out, ref, R.attention_tolerance(dtype, ref, mag, big, d, 300), "out")
+    assert kv.poll_device_status() == 0
