@@ -388,7 +388,8 @@ lar_status_t lar_paged_append_rope(const lar_paged_kv_t* kv, const lar_rope_t* r
  * no row of a sequence sees (behind lens, before kv_start) may hold anything.  Tokens that belong to no sequence are left alone.  A
  * non-finite value in a slot that some row of the chunk sees may reach every row of the chunk, with fp32 storage an infinity as
  * NaN (operands are split into two numbers).  out overlaps nothing else.
- * With bf16 storage the kernel's waits are bounded (about a second): one that runs out, on a GPU that was held up for that long, ends the
+ * Logits, softmax and sums are fp32; with bf16 storage the weights are rounded to bf16 for the product with V, as the decode step does, and
+ * the result once more.  With bf16 storage the kernel's waits are bounded (about a second): one that runs out, on a GPU that was held up for that long, ends the
  * launch with output rows that are not valid and records status bit 4 in kv->status.  Pass a status word and read it with the results.
  * LAR_ERR_CAPACITY: bf16 with more than 1024 sequences, or 2^30 (query tile, cache tile) pairs or more.
  * Query head hq uses KV head hq / (n_q_heads / n_kv_heads); their ratio is 1..16.  softmax_scale 0 selects 1/sqrt(head_dim).

@@ -125,7 +125,6 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
     slices = (a.n_rows + a.rows_per_slice - 1) / a.rows_per_slice;
     a.rows_magic = a.rows_per_slice > 1 ? (unsigned)((1ull << 32) / (unsigned)a.rows_per_slice + 1ull) : 0u;
     const size_t smem = (size_t)a.tokens_per_cta * (d + 2) * 4;
-    if (slices > 65535) return LAR_ERR_CAPACITY;
     fn<<<dim3((unsigned)token_blocks, (unsigned)slices), lar::kRopeThreads, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     return LAR_OK;
@@ -134,7 +133,7 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
 // ------------------------------------------------------------------------------------------ chunk attention
 struct AttnPlan {
     int tq;        // tokens of a row tile
-    int nt;        // bf16: row tiles of a CTA (2: chunks of more than 128 rows; 0: the kernel for few rows)
+    int nt;        // bf16: row tiles of a CTA (0: the kernel for few rows)
     int nr;        // bf16, few rows: blocks of 8 rows (two with 64-element rows only)
     int stages, grid, rows_cap;  // bf16: K/V ring, persistent CTAs, rows of a row tile
     int splits;    // bf16: 1 units stay whole, 2 they may be cut, 3 they are handed out on demand; fp32: CTAs along a unit's slots

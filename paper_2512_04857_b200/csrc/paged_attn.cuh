@@ -1,4 +1,4 @@
-// Attention of a chunk of new tokens over a paged K/V cache: what the two kernels share.
+// Attention of a chunk of new tokens over a paged K/V cache: what its kernels share.
 //
 //   out[t, h] = sum_j p_j V_j,  p = softmax_j(scale q[t, h] . K_j),  j over the slots start[s] .. last(t)
 //
@@ -40,18 +40,13 @@ __device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 
-// Row tiles of a sequence / slots [lo, hi) that any row of a tile of it may see.
+// Row tiles of a sequence.
 __device__ __forceinline__ int tiles_of(const PagedAttnArgs& a, int s) {
     int t0, t1;
     chunk_of(a.kv, s, t0, t1);

@@ -4,7 +4,8 @@
 // runs, V while the next step's S is formed.  Slots of a unit may be split over gridDim.z CTAs: they leave (O, m, l) in the
 // workspace and combine_splits_kernel joins them.
 //
-// The products run on the tensor cores with every operand split in two tf32 numbers, so that nothing fp32 storage is chosen for is lost:
+// The products run on the tensor cores with every operand split in two tf32 numbers (see Tf32Shape), so that what fp32 storage is chosen for is
+// kept.
 #pragma once
 #include <type_traits>
 
@@ -153,8 +154,8 @@ struct Fp32Unit {
 // x = hi + lo with hi the nearest tf32 (11 significant bits, off by 2^-11 at most) and lo exact in fp32, of which the tensor core takes
 // the first 11 bits: hi + lo is x to 2^-21 of it.  A product is hi hi + hi lo + lo hi (lo lo is below 2^-22; mma.sync m16n8k8): three
 // products where CUDA cores need one, at 276 TFLOP/s (measured) against 72: a third of that is still more, and a warp's
-// 16 rows cost it no shared-memory traffic per multiply-add.  tcgen05 would do the tf32 products at 4 times that rate, but wants its split
-// operands in shared memory: twice K and V written and read there for every step.
+// 16 rows cost it no shared-memory traffic per multiply-add.  tcgen05 has about three times that rate for tf32
+// (half of its bf16 rate) but wants the split operands in shared memory, K and V twice for every step: not built, not measured.
 //
 // FEW = false: a tile of 64 rows, 16 for each warp: S (16 x 64), O (16 x D), running maximum and sum in registers.  FEW = true (at
 // most 16 rows, a decode step): every warp has all of them and a quarter of the step's slots, with a running maximum of its own; the four

@@ -3,7 +3,7 @@
 // chain logits -> exponentials -> P -> product).
 //
 // A row tile is up to 128 (token, head of the group) rows of one KV head.  A CTA works on NT of them at a time:
-//   NT = 2  chunks of more than 128 rows: 256 rows share every K/V tile of 128 slots; while the softmax of one row tile runs on its warps, the
+//   NT = 2  chunks of more than 128 rows, of 128-element rows over long caches more than 32: up to 256 rows share every K/V tile of 128 slots; while the softmax of one row tile runs on its warps, the
 //           tensor cores work for the other.  4096 tokens of 32 / 8 heads of 128 over 32768 slots: 1.69 ms, 1.2 PFLOP/s.
 //   NT = 1  fewer rows: K/V tiles of 64 slots, two logit buffers (the logits of the next tile are formed while the softmax of this
 //           one runs) and two CTAs per SM, since what counts is that the cache streams without a pause.
@@ -17,6 +17,10 @@
 // The output accumulator is rescaled only where a row's maximum has grown by more than 2^8 since its last rescaling (P then
 // reaches 2^8 at most, far inside the range of bf16 and fp32; the factor cancels in the final division), so the
 // accumulator hardly ever leaves TMEM.
+//
+// P is rounded to bf16 for the product with V (both operands of a product have one type; the library's decode kernel does the same), the row sum is
+// of the weights before that rounding, in fp32.  Relative error against 64 bits, all of a result: 1.9e-3 to 2.4e-3, where rounding the result
+// alone gives 1.6e-3 to 1.7e-3 (paged_attn_few.cuh alike).  Logits, maximum, sum and accumulator are fp32.
 //
 // Slots outside [start, len) of a tile hold memory that may be anything: keys are masked by selection, and the value rows
 // are cleared in shared memory before the product (0 * NaN would reach the output).
@@ -135,9 +139,6 @@ __device__ __forceinline__ void tc_st32(uint32_t tmem, const uint32_t* r) {
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Shared-memory matrix descriptors, 128-byte swizzle.  K-major rows of 128 bytes (64 elements of the contracted dimension): groups of 8 rows
-// lie 1024 bytes apart.  Slots-as-K (V): 64 columns per 128-byte row, column blocks lead_bytes apart, groups of 8 slots 1024 apart.
-// low word: address / 16 | column-block distance / 16 << 16; high word: group distance / 16 | version 1 << 14 | 128-byte swizzle << 29
 // Position in the ring of stages: which stage, and the parity of this use of it.
 struct RingPos {
     int st = 0;
@@ -674,6 +675,10 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         // holds up nothing of the other
         if (lane == 0) {
             constexpr uint32_t id_s = tc_idesc(BN, false), id_o = tc_idesc(D, true);
+            // Shared-memory matrix descriptors, 128-byte swizzle.  K-major rows of 128 bytes (64 elements of the contracted dimension): groups of
+            // 8 rows lie 1024 bytes apart.  Slots-as-K (V): 64 columns per 128-byte row, column blocks BN * 128 bytes apart, groups of 8 slots
+            // 1024 apart.  Low word: address / 16 | column-block distance / 16 << 16; high word: group distance / 16 | version 1 << 14 |
+            // 128-byte swizzle << 29.
             constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
             constexpr uint32_t kStage = S::STAGE_BYTES >> 4;
             const int tile = warp == S::SM_WARPS ? 0 : 1;
