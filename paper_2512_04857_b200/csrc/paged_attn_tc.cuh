@@ -549,15 +549,13 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                             tc_st32(tm_o + c, o);
                         }
                     }
-                    // (here the reference is scaled first, a multiply-add per weight, unless it is so large that its rounding shows)
-                    float mref = softmax_ref(m_used) * sc;
-                    if (__any_sync(0xffffffffu, row < rows && fabsf(mref) > 16777216.f)) {
-                        const float ref = softmax_ref(m_used);
-#pragma unroll
-                        for (int c = 0; c < BN; ++c) s[c] = __float_as_uint(__uint_as_float(s[c]) - ref);
-                        mref = 0.f;
-                    }
-                    const uint64_t sc2 = pack_f32x2(sc, sc), mr2 = pack_f32x2(-mref, -mref);
+                    // Here the reference is scaled first, so that a weight is one multiply-add: it is off by half a step of its own, a factor of all
+                    // weights of the row that cancels.  From 2^31 on the factor itself leaves fp32's range; logits that differ at all then differ by
+                    // 2^7 scaled, and whatever the scale, only those that equal the reference count: it is taken as a power of two, which
+                    // makes the scaled reference exact.  (12 prompts of 340 to 4160 tokens 465 -> 468 us; with a branch that subtracts first where it matters, 471.)
+                    const float ref = softmax_ref(m_used);
+                    const float sr = fabsf(ref * sc) < 2147483648.f ? sc : __uint_as_float(__float_as_uint(sc) & 0x7f800000u);
+                    const uint64_t sc2 = pack_f32x2(sr, sr), mr2 = pack_f32x2(-ref * sr, -ref * sr);
                     uint64_t sum2[2] = {0, 0};
 #pragma unroll
                     for (int c = 0; c < BN; c += 64) {
