@@ -278,6 +278,25 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
 }
 
+// The reference of a row, scaled before it is subtracted, so that a weight is one multiply-add.  Its rounding is a factor common to all weights that were
+// formed with it: it cancels in a row that keeps its reference; a change of reference takes the ratio of the scaled ones, and what leaves the CTA as a part
+// is freed of it.  From 2^31 on the factor itself leaves fp32's range.  Logits that differ at all then differ by 2^7 scaled, so that only those equal to
+// the reference count whatever the scale, and a power of two for it makes the scaled reference exact.  (12 prompts of 340 to 4160 tokens 466 us, 466 with
+// the scaled reference alone, 471 with a branch that subtracts first where it matters.)
+struct ScaledRef {
+    float m, sc, scale, scaled;
+    __device__ __forceinline__ ScaledRef(float largest, float sc_) : m(softmax_ref(largest)), sc(sc_) {
+        scale = fabsf(m * sc) < 2147483648.f ? sc : __uint_as_float(__float_as_uint(sc) & 0x7f800000u);
+        scaled = __fmul_rn(m, scale);
+    }
+    // what weights formed with this reference are to be multiplied by for a larger one
+    __device__ __forceinline__ float ratio_to(float larger) const {
+        const ScaledRef to(larger, sc);
+        return ex2_approx(scale == sc && to.scale == sc ? scaled - to.scaled : (m - larger) * sc);
+    }
+    __device__ __forceinline__ float rounding() const { return ex2_approx(-fmaf(m, scale, -scaled)); }
+};
+
 template <int D, int NT>
 __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
     using S = TcShape<D, NT>;
@@ -536,7 +555,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                     } else if (__any_sync(0xffffffffu, grow)) {
                         if (!(ok = product_wait(steps - 1))) break;
                         product_over = true;
-                        const float f = grow ? ex2_approx((m_used - m_new) * sc) : 1.f;
+                        const float f = !grow ? 1.f : m_used == -INFINITY ? 0.f : ScaledRef(m_used, sc).ratio_to(m_new);
                         l *= f;
                         if (grow) m_used = m_new;
 #pragma unroll 1
@@ -549,13 +568,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                             tc_st32(tm_o + c, o);
                         }
                     }
-                    // Here the reference is scaled first, so that a weight is one multiply-add: it is off by half a step of its own, a factor of all
-                    // weights of the row that cancels.  From 2^31 on the factor itself leaves fp32's range; logits that differ at all then differ by
-                    // 2^7 scaled, and whatever the scale, only those that equal the reference count: it is taken as a power of two, which
-                    // makes the scaled reference exact.  (12 prompts of 340 to 4160 tokens 465 -> 468 us; with a branch that subtracts first where it matters, 471.)
-                    const float ref = softmax_ref(m_used);
-                    const float sr = fabsf(ref * sc) < 2147483648.f ? sc : __uint_as_float(__float_as_uint(sc) & 0x7f800000u);
-                    const uint64_t sc2 = pack_f32x2(sr, sr), mr2 = pack_f32x2(-ref * sr, -ref * sr);
+                    const ScaledRef ref(m_used, sc);
+                    const uint64_t sc2 = pack_f32x2(ref.scale, ref.scale), mr2 = pack_f32x2(-ref.scaled, -ref.scaled);
                     uint64_t sum2[2] = {0, 0};
 #pragma unroll
                     for (int c = 0; c < BN; c += 64) {
@@ -603,7 +617,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             const bool mine = row < rows;
             const int slotp = blockIdx.x * 2 + (g.b0 > 0 ? 0 : 1);
             if (active) {
-                const float inv = g.whole ? (l > 0.f ? 1.0f / l : l) : 1.f;  // nothing seen: 0; NaN stays NaN
+                // nothing seen: 0; NaN stays NaN.  Parts are joined by their references as they are.
+                const float inv = g.whole ? (l > 0.f ? 1.0f / l : l) : ScaledRef(m_used, sc).rounding();
                 const size_t part = ((size_t)slotp * NT + tile) * ta.rows_cap + row;
                 // a thread has a row, but four neighbours write 64 bytes of one row together
                 unsigned long long own_row = 0;
@@ -643,6 +658,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
 #pragma unroll
                         for (int h = 0; h < 32; h += 16) {
 #pragma unroll
+                            for (int i = 0; i < 16; ++i) o[h + i] = __float_as_uint(__uint_as_float(o[h + i]) * inv);
+#pragma unroll
                             for (int i = 0; i < 4; ++i) u[i] = make_uint4(o[h + 4 * i], o[h + 4 * i + 1], o[h + 4 * i + 2], o[h + 4 * i + 3]);
                             put(u, (c + h) * 4);
                         }
@@ -652,7 +669,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 if (mine && !g.whole) {
                     float* ml = a.part_ml + part * 2;
                     ml[0] = m_used;  // (-inf: nothing seen)
-                    ml[1] = l;
+                    ml[1] = l * inv;
                 }
             }
             if (!g.whole && g.b0 == 0) {

@@ -1,6 +1,7 @@
 """Rotary positions with several axes, the append to a paged cache and the chunk attention over it, against plain 64-bit
 forms on the sizes and masks where they can go wrong; refusals run without a GPU."""
 import ctypes as C
+import math
 import random
 
 import pytest
@@ -963,3 +964,44 @@ def test_offsets_beyond_32_bits(dtype, n):
         kv.attn(qo, out, c, kv_start=torch.tensor(start, dtype=torch.int32, device=DEV), max_chunk=max(n), max_len=300, workspace=ws)
         _assert_close(out, ref, R.attention_tolerance(dtype, ref, mag, big, d, 300), "out")
     assert kv.poll_device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,length", [(1, 3000), (9, 700), (12, 1500), (40, 1500), (150, 2500)])
+@pytest.mark.parametrize("base,step", [(2.0 ** 20, 1.0), (2.0 ** 26, 8.0), (2.0 ** 29, 64.0), (-(2.0 ** 29), 64.0)])
+def test_attention_of_large_logits_that_lie_close(dtype, d, n, length, base, step):
+    """Logits base + step k (exact in fp32) with k growing along the cache, and values that shrink as the weights grow: slots of
+    every level count, so the references of all tiles, parts and splits have to agree far below the logits' own rounding."""
+    c = PagedCase(dtype, d, 1, 64, "nhd", [n], [length], seed=n)
+    c.fill(None, 6)
+    scale = 0.125
+    levels = 6
+    level = torch.arange(length) * levels // length                       # 0 .. levels - 1
+    for j in range(length):
+        at = c.place(0, 0, j)
+        c.pools[0][at] = 0.0
+        c.pools[0][at][0], c.pools[0][at][1] = base / 1024, step / 8 * float(level[j])
+        c.pools[1][at] *= math.exp(-step * scale * float(level[j]))
+    for p, x in zip(c.pools, c.dev):
+        x.copy_(p.to(DEV))
+    q = torch.zeros(n, 2, d, dtype=dtype)
+    q[..., 0], q[..., 1] = 1024.0, 8.0
+    V = c.rows(1)(0, 0, 0, length).double()
+    weight = torch.exp(step * scale * (level - (levels - 1)).double())
+    # A weight's argument is at most step scale levels, rounded a few times; sums of 3000 terms and the tensor core's cut-off sums
+    # (2^-21 each); bf16: weights rounded once, and the result.
+    rel = step * scale * levels * 2.0 ** -21 + 3000 * 2.0 ** -24 + 2.0 ** -16
+    for workspace in (False, True):
+        out = torch.full((n, 2, d), 5.0, dtype=dtype, device=DEV)
+        ws = c.kv.attn_workspace(2, n, n, length) if workspace else None
+        c.kv.attn(q.to(DEV), out, c.cu, softmax_scale=scale, max_chunk=n, max_len=length, workspace=ws)
+        for i in range(n):
+            hi = length - n + i + 1
+            w = weight[:hi] / weight[:hi].sum()
+            ref, mag = w @ V[:hi], w @ V[:hi].abs()
+            tol = mag * rel + (mag * 2.0 ** -8 + ref.abs() * 2.0 ** -8 if dtype == BF else 0)
+            _assert_close(out[i, 0], ref, tol, f"token {i} workspace {workspace}")
+            assert torch.equal(out[i, 0], out[i, 1])
+    assert int(c.status) == 0
