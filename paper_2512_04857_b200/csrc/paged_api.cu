@@ -16,6 +16,7 @@
 namespace {
 
 constexpr int kSms = 148;             // SMs of a B200 (launch shapes only)
+constexpr size_t kMaxSmem = 227 * 1024;  // shared memory of a CTA
 constexpr int64_t kMaxTokens = 1 << 26;
 constexpr int kMaxHeads = 4096;       // (the rotary kernel divides row numbers by multiplication: rows of two tokens x rows of one < 2^32)
 
@@ -156,7 +157,6 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     const int64_t with_tokens = n_tokens < k.n_seqs ? n_tokens : k.n_seqs;
     const int d = k.head_dim;
     if (k.dtype == LAR_BF16) {
-        constexpr size_t kSmem = 227 * 1024;
         // Two row tiles above 128 rows, and with 128-element rows and long caches above 32 (one row tile leaves its two CTAs per SM two
         // stages each; 16 x 4288 slots, one / two row tiles: 32 rows 62 / 65 us, 64 rows 75 / 66, 128 rows 78 / 69, 192 rows 120 / 74; 64 x 577
         // slots, 64 rows 55 / 59; 64-element rows 44 / 55, 48 / 56, 72 / 68).
@@ -184,7 +184,7 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         int per_sm = 1;
         if (p.nt == 2) {
             p.stages = lar::kTcMaxStages;
-            while (p.stages > 1 && tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs) > kSmem) --p.stages;
+            while (p.stages > 1 && tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs) > kMaxSmem) --p.stages;
             p.smem = tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs);
         } else {
             // two CTAs per SM, unless the lengths of very many sequences leave no room for two stages each
@@ -364,9 +364,12 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
         t.a.part_ml = reinterpret_cast<float*>(t.records + p.grid);
         t.a.part_o = t.a.part_ml + (size_t)p.grid * 2 * NT * p.rows_cap * 2;
     }
+    // First of all a call of the runtime, which makes the device's context current in a thread that has made none: encoding a tensor map is a
+    // call of the driver and fails without one.
+    constexpr auto fn = S::fn;
+    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
     lar_status_t st = make_maps(k, a, t.box_rows, m);
     if (st != LAR_OK) return st;
-    constexpr auto fn = S::fn;
     if (NT_ == 2) {
         // the softmax warps take registers that the block has to have been launched with: a build that gives it fewer is refused
         static const int regs = [] {
@@ -375,7 +378,6 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
         }();
         if (regs * 3 < 2 * lar::TcShape<D, 2>::SM_REGS + lar::TcShape<D, 2>::OTHER_REGS) return LAR_ERR_CUDA;
     }
-    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
     fn<<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
     LAR_CUDA(cudaGetLastError());
     if (t.split) {

@@ -3,6 +3,7 @@ forms on the sizes and masks where they can go wrong; refusals run without a GPU
 import ctypes as C
 import math
 import random
+import threading
 
 import pytest
 import torch
@@ -1005,3 +1006,28 @@ def test_attention_of_large_logits_that_lie_close(dtype, d, n, length, base, ste
             _assert_close(out[i, 0], ref, tol, f"token {i} workspace {workspace}")
             assert torch.equal(out[i, 0], out[i, 1])
     assert int(c.status) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n", [(BF, 1), (BF, 40), (BF, 160), (F32, 1)])
+def test_first_call_of_a_thread(dtype, n):
+    """A thread that has made no CUDA call yet: attention (a tensor map is encoded), append and rotation."""
+    c = PagedCase(dtype, 64, 1, 64, "nhd", [n], [300])
+    c.fill(None, 1)
+    q, pos, rope = _randn((n, 2, 64), dtype, 1).to(DEV), torch.zeros(1, n, dtype=torch.int32, device=DEV), lar.make_rope(64, (32,))
+    want, out, k = torch.empty_like(q), torch.empty_like(q), c.dev[0].new_zeros(n, 1, 64)
+    c.kv.attn(q, want, c.cu)
+    errors = []
+
+    def call(what):
+        try:
+            what()
+        except Exception as e:                                        # noqa: BLE001 -- shown by the test
+            errors.append(e)
+    for what in (lambda: c.kv.attn(q, out, c.cu), lambda: lar.rope_rotate(rope, pos, q, q), lambda: c.kv.append_rope(k, k, c.cu, rope, pos)):
+        t = threading.Thread(target=call, args=(what,))
+        t.start()
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    assert torch.equal(out, want)
