@@ -367,7 +367,8 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     // First of all a call of the runtime, which makes the device's context current in a thread that has made none: encoding a tensor map is a
     // call of the driver and fails without one.
     constexpr auto fn = S::fn;
-    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem));
+    // (The limit is the same whatever a call launches with: another thread's call may come between this one and the launch.)
+    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem));
     lar_status_t st = make_maps(k, a, t.box_rows, m);
     if (st != LAR_OK) return st;
     if (NT_ == 2) {

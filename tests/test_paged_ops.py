@@ -1031,3 +1031,42 @@ def test_first_call_of_a_thread(dtype, n):
     torch.cuda.synchronize()
     assert not errors, errors
     assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 20, 160])                              # few rows, one and two row tiles
+def test_attention_from_two_threads(n):
+    """Calls of one kernel with different amounts of shared memory from two threads at once, on streams and outputs of their own."""
+    d, hkv, hq = 64, 1, 4
+    work, fn = [], lar._fast().lar_paged_attn
+    for seqs, length in ((1, 300), (900, 200)):
+        pools = [torch.randn(seqs * 5, 64, hkv, d, device=DEV, generator=torch.Generator(DEV).manual_seed(seqs + i)).to(BF) for i in range(2)]
+        table = torch.arange(seqs * 5, dtype=torch.int32, device=DEV).view(seqs, 5)
+        kv = lar.PagedKV(*pools, table, torch.full((seqs,), length, dtype=torch.int32, device=DEV), hkv)
+        T = 900                                                          # (the few tokens of one of the calls keep the GPU's queue short)
+        cu = (torch.arange(seqs + 1, device=DEV) * n).clamp(max=T).int()
+        q = torch.randn(T, hq, d, device=DEV).to(BF)
+        outs = [torch.zeros_like(q) for _ in range(2)]
+        kv.attn(q, outs[0], cu, max_chunk=n, max_len=length)
+        work.append((kv, q, cu, outs, length, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    errors = []
+
+    def loop(kv, q, cu, outs, length, stream):
+        try:
+            with torch.cuda.stream(stream):
+                kv.attn(q, outs[1], cu, max_chunk=n, max_len=length)
+            rows = [lar.lar_rows_t(x.data_ptr(), x.stride(0), x.stride(1)) for x in (q, outs[1])]
+            args = (kv._at, C.addressof(rows[0]), C.addressof(rows[1]), hq, q.shape[0], cu.data_ptr(), None, 1, 0.0, n, length, None, 0, stream.cuda_stream)
+            errors.extend(s for s in (fn(*args) for _ in range(4000)) if s)
+        except Exception as e:                                        # noqa: BLE001 -- shown by the test
+            errors.append(e)
+    threads = [threading.Thread(target=loop, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, (len(errors), errors[:4])
+    for kv, q, cu, outs, length, stream in work:
+        assert torch.equal(outs[0], outs[1]) and kv.poll_device_status() == 0
