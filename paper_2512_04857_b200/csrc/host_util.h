@@ -7,6 +7,7 @@
 #include <stdlib.h>
 
 namespace lar {
+constexpr int kMaxSmem = 227 * 1024;  // dynamic shared memory a CTA can have
 int& last_cuda_error();  // cudaError_t of the last failed runtime call in this thread (defined in lar_api.cu)
 }
 

@@ -707,14 +707,14 @@ lar_status_t lar_cache_create(const lar_config_t* cfg, void* dev_slab, size_t sl
     if (ce == cudaSuccess) ce = cudaMemset(c->slab + L.off_kpool, 0, L.stride_pool * cfg->n_layers);
     if (ce == cudaSuccess) ce = cudaMemset(c->slab + L.off_vpool, 0, L.stride_pool * cfg->n_layers);
     if (ce == cudaSuccess) ce = cudaMemset(c->slab + L.off_tickets, 0, L.tickets_bytes);
-    if (ce == cudaSuccess)
-        ce = cudaFuncSetAttribute(cfg->dtype == LAR_BF16 ? (const void*)decode_stream_fn(*cfg, d.group) : (const void*)decode_fn(*cfg, d.group),
-                                  cudaFuncAttributeMaxDynamicSharedMemorySize, plan.decode_smem_bytes);
-    if (ce == cudaSuccess && cfg->dtype == LAR_BF16)  // (the variant for views of larger tensors / the rotary embedding)
-        ce = cudaFuncSetAttribute((const void*)decode_stream_fn(*cfg, d.group, true), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  plan.decode_smem_bytes);
-    if (ce == cudaSuccess && d.compressing)
-        ce = cudaFuncSetAttribute((const void*)line_end_fn(*cfg, d.group), cudaFuncAttributeMaxDynamicSharedMemorySize, plan.line_end_smem_bytes);
+    // The limit belongs to the kernel, not to this cache: every cache sets the same, all the shared memory of a CTA, so that one that needs less takes
+    // nothing from those that share the kernel.
+    auto allow_smem = [&](const void* fn) {
+        if (ce == cudaSuccess) ce = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, lar::kMaxSmem);
+    };
+    allow_smem(cfg->dtype == LAR_BF16 ? (const void*)decode_stream_fn(*cfg, d.group) : (const void*)decode_fn(*cfg, d.group));
+    if (cfg->dtype == LAR_BF16) allow_smem((const void*)decode_stream_fn(*cfg, d.group, true));  // (the variant for views of larger tensors / the rotary embedding)
+    if (d.compressing) allow_smem((const void*)line_end_fn(*cfg, d.group));
     if (ce == cudaSuccess) ce = cudaStreamCreateWithFlags(&c->s_in, cudaStreamNonBlocking);
     if (ce == cudaSuccess) ce = cudaStreamCreateWithFlags(&c->s_out, cudaStreamNonBlocking);
     if (ce == cudaSuccess) ce = cudaEventCreateWithFlags(&c->e_fork, cudaEventDisableTiming);

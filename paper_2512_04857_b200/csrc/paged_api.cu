@@ -16,7 +16,6 @@
 namespace {
 
 constexpr int kSms = 148;             // SMs of a B200 (launch shapes only)
-constexpr size_t kMaxSmem = 227 * 1024;  // shared memory of a CTA
 constexpr int64_t kMaxTokens = 1 << 26;
 constexpr int kMaxHeads = 4096;       // (the rotary kernel divides row numbers by multiplication: rows of two tokens x rows of one < 2^32)
 
@@ -184,7 +183,7 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
         int per_sm = 1;
         if (p.nt == 2) {
             p.stages = lar::kTcMaxStages;
-            while (p.stages > 1 && tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs) > kMaxSmem) --p.stages;
+            while (p.stages > 1 && tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs) > lar::kMaxSmem) --p.stages;
             p.smem = tc_smem<2>(d, p.rows_cap, p.stages, k.n_seqs);
         } else {
             // two CTAs per SM, unless the lengths of very many sequences leave no room for two stages each
@@ -368,7 +367,7 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, con
     // call of the driver and fails without one.
     constexpr auto fn = S::fn;
     // (The limit is the same whatever a call launches with: another thread's call may come between this one and the launch.)
-    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem));
+    LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, lar::kMaxSmem));
     lar_status_t st = make_maps(k, a, t.box_rows, m);
     if (st != LAR_OK) return st;
     if (NT_ == 2) {
