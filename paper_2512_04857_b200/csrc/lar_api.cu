@@ -830,7 +830,8 @@ lar_status_t lar_append_kv_rope(lar_cache_t* c, int layer, const lar_rope_t* rop
     if (bad_layer(c, layer) || n_tokens < 1) return LAR_ERR_INVALID_ARG;
     LayerShadow& sh = c->sh[layer];
     // the prefill only: a visual token's key is rotated by lar_decode_step_rope
-    if (c->cfg.cond_len < 1 || sh.prefilled) return LAR_ERR_BAD_STATE;
+    // (it takes the layer as empty: with the call-order checks off, steps may have come before)
+    if (c->cfg.cond_len < 1 || sh.prefilled || sh.v > 0 || sh.n_tok > 0) return LAR_ERR_BAD_STATE;
     if (n_tokens != c->cfg.cond_len) return LAR_ERR_INVALID_ARG;
     lar_paged_kv_t kv;
     lar_status_t st = lar_cache_paged_view(c, layer, &kv);

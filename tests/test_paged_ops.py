@@ -1070,3 +1070,21 @@ def test_attention_from_two_threads(n):
     assert not errors, (len(errors), errors[:4])
     for kv, q, cu, outs, length, stream in work:
         assert torch.equal(outs[0], outs[1]) and kv.poll_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_rotated_prefill_refuses_a_layer_that_is_not_empty():
+    """With the call-order checks off a step may come before the prefix: the prefill would take its rows for its own."""
+    cfg = lar.make_config(n_layers=2, batch=1, n_q_heads=2, n_kv_heads=2, head_dim=64, dtype="bf16", cond_len=3, line_width=8, n_lines=4, anchor_len=8,
+                          recent_lines=1, budget_lines=4, flags=lar.LAR_FLAG_NO_HOST_CHECKS)
+    cache = lar.Cache(cfg)
+    x = torch.zeros(1, 2, 64, dtype=BF, device=DEV)
+    rows = torch.zeros(3, 2, 64, dtype=BF, device=DEV)
+    cache.decode_step(0, x, x, x, torch.empty_like(x))
+    with pytest.raises(lar.LarError) as e:
+        cache.append_kv_rope(0, rows, rows, 3)
+    assert e.value.status == lar.LAR_ERR_BAD_STATE
+    assert (cache.get_state(0)[0] == 1).all()
+    cache.append_kv_rope(1, rows, rows, 3)
+    assert (cache.get_state(1)[0] == 3).all()
+    cache.close()
