@@ -158,7 +158,8 @@ AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max
     if (k.dtype == LAR_BF16) {
         // Two row tiles above 128 rows, and with 128-element rows and long caches above 32 (one row tile leaves its two CTAs per SM two
         // stages each; 16 x 4288 slots, one / two row tiles: 32 rows 62 / 65 us, 64 rows 75 / 66, 128 rows 78 / 69, 192 rows 120 / 74; 64 x 577
-        // slots, 64 rows 55 / 59; 64-element rows 44 / 55, 48 / 56, 72 / 68).
+        // slots, 64 rows 55 / 59; 64-element rows 44 / 55, 48 / 56, 72 / 68).  All of it with 8 KV heads: how few units a call has is not looked at, here and in
+        // what is cut below (one sequence of 300 tokens over 1500 slots: 40 units on 148 SMs).
         const int64_t rows = chunk * group;
         p.nt = rows > 128 || (d == 128 && rows > 32 && len >= 2048) ? 2 : rows > lar::few_rows(d) ? 1 : 0;
         if (p.nt == 0) {
