@@ -241,7 +241,8 @@ def prepare(case, seed):
             else:
                 codes = torch.zeros(shape, device=DEV, dtype=torch.uint8).view(torch.float8_e4m3fn)
                 scale = torch.zeros(shape[:-1], device=DEV, dtype=torch.uint8)
-            st[name + "_pool"], st[name + "_scale"] = turn(codes), turn(scale)
+            # the bytes of a page's slots lie side by side: [pages, heads, page]
+            st[name + "_pool"], st[name + "_scale"] = turn(codes), turn(scale).transpose(1, 2).contiguous().transpose(1, 2)
         if case["op"] == "store":
             st.update(k=k, v=v, pos=_positions(case, cu[-1], gen), **_norm_params(case, gen))
             st.update({x + "_rows": torch.empty(cu[-1], hkv, d, device=DEV, dtype=_dtype(case)) for x in "kv"})
@@ -251,7 +252,7 @@ def prepare(case, seed):
             st["kv"] = lar.PagedKV(st["k_pool"], st["v_pool"], table, st["lens"], hkv)
             st["workspace"] = st["kv"].attn_shared_workspace(hq, cu[-1], case["groups"], st["max_chunk"], st["max_len"], st["max_pre"])
         else:
-            st["kv"] = lar.PagedKV8(st["k_pool"], st["v_pool"], st["k_scale"], st["v_scale"], table, st["lens"], hkv)
+            st["kv"] = lar.PagedKV8(st["k_pool"], st["v_pool"], st["k_scale"].transpose(1, 2), st["v_scale"].transpose(1, 2), table, st["lens"], hkv)
             if case["op"] == "store":
                 _own_norms(case, st)
             else:
