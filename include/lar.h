@@ -419,6 +419,85 @@ lar_status_t lar_append_kv_rope(lar_cache_t* c, int layer, const lar_rope_t* rop
                                 const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q, const lar_rows_t* q_out,
                                 int n_tokens, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Norms of q and k per head, caches held in 8 bits, attention over slots that sequences share.  As the calls above: no state,
+ * no allocation, work is only enqueued on `stream`, launch shapes depend on the host arguments alone (graph capture).
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* Norm of every head's row x of head_dim elements:
+ *     LAR_NORM_RMS    y = x / sqrt(mean(x^2) + eps) * weight + bias
+ *     LAR_NORM_LAYER  y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias
+ * weight and bias (device, 16-byte aligned, of weight_dtype; NULL: ones / zeros): element i of head h at h * head_stride + i
+ * (head_stride a multiple of 16 bytes; 0: one row for all heads).  Sums and products are fp32; a row that is also rotated is rounded once, at the
+ * end.  eps lies in [1e-12, 1].  A row with an element that is not finite becomes NaN or zeros as the formula has it. */
+#define LAR_NORM_RMS 0
+#define LAR_NORM_LAYER 1
+typedef struct lar_head_norm {
+    uint32_t struct_size;  /* = sizeof(lar_head_norm_t) */
+    int32_t kind;
+    int32_t weight_dtype;  /* LAR_BF16 or LAR_FP32, whatever the rows are */
+    float eps;
+    const void* weight;
+    const void* bias;
+    int64_t head_stride;   /* elements */
+} lar_head_norm_t;
+
+/* lar_rope_rotate with norms before the rotation, in the same pass: q_norm and k_norm (NULL: rows are not normalised) for the rows of q and of k.
+ * rope and pos NULL: norms alone. */
+lar_status_t lar_norm_rope_rotate(const lar_head_norm_t* q_norm, const lar_head_norm_t* k_norm, const lar_rope_t* rope, int dtype, int head_dim,
+                                  const int32_t* pos, int64_t pos_axis_stride, int64_t n_tokens, const lar_rows_t* q, const lar_rows_t* q_out,
+                                  int n_q_heads, const lar_rows_t* k, const lar_rows_t* k_out, int n_kv_heads, void* stream);
+
+/* lar_paged_append_rope with norms before the rotation (q_norm needs q). */
+lar_status_t lar_paged_append_norm_rope(const lar_paged_kv_t* kv, const lar_head_norm_t* q_norm, const lar_head_norm_t* k_norm, const lar_rope_t* rope,
+                                        const int32_t* pos, int64_t pos_axis_stride, const lar_rows_t* k, const lar_rows_t* v,
+                                        const lar_rows_t* q, const lar_rows_t* q_out, int n_q_heads, int64_t n_tokens, const int32_t* cu_tokens,
+                                        void* stream);
+
+/* lar_append_kv_rope with norms before the rotation. */
+lar_status_t lar_append_kv_norm_rope(lar_cache_t* c, int layer, const lar_head_norm_t* q_norm, const lar_head_norm_t* k_norm, const lar_rope_t* rope,
+                                     const int32_t* pos, int64_t pos_axis_stride, const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q,
+                                     const lar_rows_t* q_out, int n_tokens, void* stream);
+
+/* A paged cache in 8 bits: kv as above with dtype LAR_E4M3 (pools of one-byte codes; strides in elements are bytes, multiples of 16), and a byte b
+ * for every row: the byte of row r of page p and head h is scale[p * scale_page_stride + h * scale_head_stride + r] (16-byte aligned, strides
+ * multiples of 16; heads with pages of their own have scale_head_stride = 0).  An element is  e4m3(code) * 2^(b - 127);  a row is stored
+ * with the smallest power 2^(b - 127), at least 2^-117, for which none of its elements exceeds 448 times it, codes rounded to nearest even (an element
+ * below 2^-15 of the row's largest to a multiple of 2^-18 of it); a row of zeros has b = 127.  A row with an element that is not
+ * finite is stored as b = 255 and reads as NaN. */
+#define LAR_E4M3 2
+typedef struct lar_paged_q8 {
+    uint32_t struct_size;  /* = sizeof(lar_paged_q8_t) */
+    uint32_t reserved;     /* 0 */
+    lar_paged_kv_t kv;
+    uint8_t* k_scale;      /* device */
+    uint8_t* v_scale;
+    int64_t scale_page_stride, scale_head_stride;
+} lar_paged_q8_t;
+
+/* lar_paged_append_norm_rope into an 8-bit cache; q, k, v are rows of rows_dtype (LAR_BF16 or LAR_FP32), rounded once: to 8 bits, q to its type. */
+lar_status_t lar_paged_q8_append(const lar_paged_q8_t* cache, int rows_dtype, const lar_head_norm_t* q_norm, const lar_head_norm_t* k_norm,
+                                 const lar_rope_t* rope, const int32_t* pos, int64_t pos_axis_stride, const lar_rows_t* k, const lar_rows_t* v,
+                                 const lar_rows_t* q, const lar_rows_t* q_out, int n_q_heads, int64_t n_tokens, const int32_t* cu_tokens,
+                                 void* stream);
+
+/* Reads the newest entries of every sequence back as rows [n_rows][n_kv_heads][head_dim] of rows_dtype, exactly what is stored: sequence s gives
+ * the rows cu_rows[s] .. cu_rows[s + 1] - 1 (as cu_tokens of an append: NULL: n_rows / n_seqs each), the i-th of T of them slot
+ * lens[s] - T + i.  Rows that belong to no sequence are left alone. */
+lar_status_t lar_paged_q8_read(const lar_paged_q8_t* cache, int rows_dtype, const lar_rows_t* k_out, const lar_rows_t* v_out, int64_t n_rows,
+                               const int32_t* cu_rows, void* stream);
+
+/* lar_paged_attn over an 8-bit cache, q and out of rows_dtype.  Few rows per KV head (up to 16) are computed from the codes; for longer chunks the
+ * live entries are first read into the workspace, as rows of rows_dtype, as many sequences at a time as 256 MB hold (at least one), and the attention
+ * runs over those: such a call needs its workspace (LAR_ERR_NOMEM with NULL).  LAR_ERR_CAPACITY: more than 1024 sequences, and as lar_paged_attn.
+ * The waits of every kernel are bounded, also with fp32 rows: status bit 4. */
+lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads,
+                               int64_t n_tokens, const int32_t* cu_tokens, const int32_t* kv_start, int causal, float softmax_scale,
+                               int max_chunk, int max_len, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that suffice for lar_paged_q8_attn with these arguments and every smaller call, as lar_paged_attn_workspace_bytes. */
+size_t lar_paged_q8_attn_workspace_bytes(const lar_paged_q8_t* cache, int rows_dtype, int n_q_heads, int64_t n_tokens, int max_chunk, int max_len);
+
 const char* lar_status_str(lar_status_t s);
 int lar_last_cuda_error(void); /* cudaError_t of the last failed runtime call in this thread, 0 if none */
 

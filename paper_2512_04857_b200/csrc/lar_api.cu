@@ -827,6 +827,12 @@ lar_status_t lar_cache_paged_view(lar_cache_t* c, int layer, lar_paged_kv_t* out
 lar_status_t lar_append_kv_rope(lar_cache_t* c, int layer, const lar_rope_t* rope, const int32_t* pos, int64_t pos_axis_stride,
                                 const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q, const lar_rows_t* q_out,
                                 int n_tokens, void* stream) {
+    return lar_append_kv_norm_rope(c, layer, nullptr, nullptr, rope, pos, pos_axis_stride, k, v, q, q_out, n_tokens, stream);
+}
+
+lar_status_t lar_append_kv_norm_rope(lar_cache_t* c, int layer, const lar_head_norm_t* q_norm, const lar_head_norm_t* k_norm, const lar_rope_t* rope,
+                                     const int32_t* pos, int64_t pos_axis_stride, const lar_rows_t* k, const lar_rows_t* v, const lar_rows_t* q,
+                                     const lar_rows_t* q_out, int n_tokens, void* stream) {
     if (bad_layer(c, layer) || n_tokens < 1) return LAR_ERR_INVALID_ARG;
     LayerShadow& sh = c->sh[layer];
     // the prefill only: a visual token's key is rotated by lar_decode_step_rope
@@ -841,8 +847,8 @@ lar_status_t lar_append_kv_rope(lar_cache_t* c, int layer, const lar_rope_t* rop
     oc.index_map = lv.index_map;
     oc.state = lv.state;
     oc.cap_pad = c->d.cap_pad;
-    st = lar::paged_append(kv, rope, pos, pos_axis_stride, k, v, q, q_out, q ? c->cfg.n_q_heads : 0,
-                           (int64_t)c->cfg.batch * n_tokens, nullptr, &oc, stream);
+    st = lar::paged_append_norm(kv, q_norm, k_norm, rope, pos, pos_axis_stride, k, v, q, q_out, q ? c->cfg.n_q_heads : 0,
+                                (int64_t)c->cfg.batch * n_tokens, nullptr, &oc, stream);
     if (st != LAR_OK) return st;
     c->launches++;
     c->last_layer = layer;

@@ -12,20 +12,13 @@
 #include "paged_attn_tc.cuh"
 #include "paged_host.h"
 #include "rope_rows.cuh"
+#include "tensor_map.h"
 
-namespace {
+namespace lar {
 
-constexpr int kSms = 148;             // SMs of a B200 (launch shapes only)
-constexpr int64_t kMaxTokens = 1 << 26;
-constexpr int kMaxHeads = 4096;       // (the rotary kernel divides row numbers by multiplication: rows of two tokens x rows of one < 2^32)
-
-int elt_of(int dtype) { return dtype == LAR_BF16 ? 2 : 4; }
-bool is_dtype(int dtype) { return dtype == LAR_BF16 || dtype == LAR_FP32; }
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-bool rope_freqs(const lar_rope_t* r, int inverse, lar::RopeFreqs& f) {
+bool rope_freqs(const lar_rope_t* r, int inverse, RopeFreqs& f) {
     if (!r || r->struct_size != sizeof(lar_rope_t)) return false;
-    if (!(r->head_dim == 64 || r->head_dim == 128) || r->n_axes < 1 || r->n_axes > lar::kRopeMaxAxes) return false;
+    if (!(r->head_dim == 64 || r->head_dim == 128) || r->n_axes < 1 || r->n_axes > kRopeMaxAxes) return false;
     if (!(r->theta > 0.0) || !isfinite(r->theta)) return false;
     const int half = r->head_dim / 2;
     const double ln = log(r->theta);
@@ -45,7 +38,7 @@ bool rope_freqs(const lar_rope_t* r, int inverse, lar::RopeFreqs& f) {
 }
 
 // Rows of [tokens][heads][d].  Strides of an extent of one do not matter; output rows may not overlap.
-bool rows_view(const lar_rows_t* r, int64_t tokens, int heads, int d, int elt, bool output, lar::RowsView& v) {
+bool rows_view(const lar_rows_t* r, int64_t tokens, int heads, int d, int elt, bool output, RowsView& v) {
     if (!r || !r->data || !aligned(r->data, 16)) return false;
     v.p = static_cast<char*>(r->data);
     v.token_stride = tokens > 1 ? r->token_stride : (int64_t)heads * d;
@@ -58,15 +51,15 @@ bool rows_view(const lar_rows_t* r, int64_t tokens, int heads, int d, int elt, b
     return true;
 }
 
-bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, lar::PagedView& v) {
-    if (!k || k->struct_size != sizeof(lar_paged_kv_t) || !is_dtype(k->dtype)) return false;
+bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, PagedView& v, bool q8) {
+    if (!k || k->struct_size != sizeof(lar_paged_kv_t) || !(q8 ? k->dtype == LAR_E4M3 : is_dtype(k->dtype))) return false;
     if (k->n_seqs < 1 || k->n_kv_heads < 1 || !(k->head_dim == 64 || k->head_dim == 128)) return false;
     if (k->n_kv_heads > kMaxHeads) return false;
     int shift = 4;
     while (shift < 8 && (1 << shift) != k->page_tokens) ++shift;
     if (shift == 8 || k->n_pages < 1 || k->table_cols < 1) return false;
     if ((int64_t)k->table_cols * k->page_tokens > (1ll << 30)) return false;
-    const int elt = elt_of(k->dtype);
+    const int elt = q8 ? 1 : elt_of(k->dtype);
     if (!k->k_pool || !k->v_pool || !aligned(k->k_pool, 16) || !aligned(k->v_pool, 16)) return false;
     const int64_t strides[3] = {k->page_stride, k->row_stride, k->head_stride};
     for (int64_t s : strides)
@@ -101,17 +94,8 @@ bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, la
     return true;
 }
 
-// ------------------------------------------------------------------------------------------ rotary rows
-using RopeFn = void (*)(const lar::RopeRowsArgs);
-template <typename T, int D, bool PAGED>
-RopeFn rope_fn_pairs(bool inter) { return inter ? lar::rope_rows_kernel<T, D, true, PAGED> : lar::rope_rows_kernel<T, D, false, PAGED>; }
-template <bool PAGED>
-RopeFn rope_fn(int dtype, int d, bool inter) {
-    if (dtype == LAR_BF16) return d == 64 ? rope_fn_pairs<__nv_bfloat16, 64, PAGED>(inter) : rope_fn_pairs<__nv_bfloat16, 128, PAGED>(inter);
-    return d == 64 ? rope_fn_pairs<float, 64, PAGED>(inter) : rope_fn_pairs<float, 128, PAGED>(inter);
-}
-
-lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream_t s) {
+// Launch shape of the rotary kernels: token blocks x slices of a token's rows.
+dim3 rope_grid(RopeRowsArgs& a) {
     a.n_rows = a.heads[0] + a.heads[1] + a.heads[2];
     // One token per CTA while the batch is small, its rows dealt to enough CTAs that every SM has some; two tokens per CTA for
     // large batches (66560 tokens of 40 rows: 204 us, against 214 us with one and 203 us with four; 5193 tokens of fp32: 19.4,
@@ -124,8 +108,29 @@ lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream
     a.rows_per_slice = (a.n_rows + slices - 1) / slices;
     slices = (a.n_rows + a.rows_per_slice - 1) / a.rows_per_slice;
     a.rows_magic = a.rows_per_slice > 1 ? (unsigned)((1ull << 32) / (unsigned)a.rows_per_slice + 1ull) : 0u;
+    return dim3((unsigned)token_blocks, (unsigned)slices);
+}
+
+}  // namespace lar
+
+namespace {
+
+using namespace lar;
+
+// ------------------------------------------------------------------------------------------ rotary rows
+using RopeFn = void (*)(const lar::RopeRowsArgs);
+template <typename T, int D, bool PAGED>
+RopeFn rope_fn_pairs(bool inter) { return inter ? lar::rope_rows_kernel<T, D, true, PAGED> : lar::rope_rows_kernel<T, D, false, PAGED>; }
+template <bool PAGED>
+RopeFn rope_fn(int dtype, int d, bool inter) {
+    if (dtype == LAR_BF16) return d == 64 ? rope_fn_pairs<__nv_bfloat16, 64, PAGED>(inter) : rope_fn_pairs<__nv_bfloat16, 128, PAGED>(inter);
+    return d == 64 ? rope_fn_pairs<float, 64, PAGED>(inter) : rope_fn_pairs<float, 128, PAGED>(inter);
+}
+
+lar_status_t launch_rope_rows(lar::RopeRowsArgs& a, RopeFn fn, int d, cudaStream_t s) {
+    const dim3 grid = rope_grid(a);
     const size_t smem = (size_t)a.tokens_per_cta * (d + 2) * 4;
-    fn<<<dim3((unsigned)token_blocks, (unsigned)slices), lar::kRopeThreads, smem, s>>>(a);
+    fn<<<grid, lar::kRopeThreads, smem, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     return LAR_OK;
 }
@@ -285,48 +290,19 @@ lar_status_t launch_fp32(const lar::PagedAttnArgs& a, const AttnPlan& p, cudaStr
     return LAR_OK;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-lar_status_t encode_4d(EncodeTiledFn encode, CUtensorMap* m, void* p, const cuuint64_t (&dim)[4], const int64_t (&stride)[3],
-                       const cuuint32_t (&box)[4]) {
-    const cuuint32_t one[4] = {1, 1, 1, 1};
-    const cuuint64_t st[3] = {(cuuint64_t)stride[0] * 2, (cuuint64_t)stride[1] * 2, (cuuint64_t)stride[2] * 2};
-    if (encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, p, dim, st, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
-        lar::last_cuda_error() = (int)cudaErrorInvalidValue;
-        return LAR_ERR_CUDA;
-    }
-    return LAR_OK;
-}
-
 lar_status_t make_maps(const lar_paged_kv_t& k, const lar::PagedAttnArgs& a, int box_rows, lar::TcMaps& m) {
-    static const EncodeTiledFn encode = [] {
-        void* fp = nullptr;
-        cudaDriverEntryPointQueryResult res;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fp, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            fp = nullptr;
-        }
-        return reinterpret_cast<EncodeTiledFn>(fp);
-    }();
-    if (!encode) {
-        lar::last_cuda_error() = (int)cudaErrorNotSupported;
-        return LAR_ERR_CUDA;
-    }
     const cuuint64_t d = (cuuint64_t)k.head_dim;
     const cuuint64_t qdim[4] = {d, (cuuint64_t)a.group, (cuuint64_t)k.n_kv_heads, (cuuint64_t)a.kv.n_tokens};
     const int64_t qst[3] = {a.q.head_stride, a.q.head_stride * a.group, a.q.token_stride};
     const cuuint32_t qbox[4] = {64, (cuuint32_t)a.group, 1, (cuuint32_t)a.tq};
-    lar_status_t st = encode_4d(encode, &m.q, a.q.p, qdim, qst, qbox);
+    lar_status_t st = encode_map_4d(&m.q, kMapBf16, 128, a.q.p, qdim, qst, qbox);
     const int heads = k.head_stride > 0 ? k.n_kv_heads : 1;  // heads with pages of their own: every page is one head's
     const int64_t page_stride = k.n_pages > 1 ? k.page_stride : k.row_stride * k.page_tokens * heads;
     const cuuint64_t kdim[4] = {d, (cuuint64_t)k.page_tokens, (cuuint64_t)heads, (cuuint64_t)k.n_pages};
     const int64_t kst[3] = {k.row_stride, heads > 1 ? k.head_stride : page_stride, page_stride};
     const cuuint32_t kbox[4] = {64, (cuuint32_t)box_rows, 1, 1};
-    if (st == LAR_OK) st = encode_4d(encode, &m.k, k.k_pool, kdim, kst, kbox);
-    if (st == LAR_OK) st = encode_4d(encode, &m.v, k.v_pool, kdim, kst, kbox);
+    if (st == LAR_OK) st = encode_map_4d(&m.k, kMapBf16, 128, k.k_pool, kdim, kst, kbox);
+    if (st == LAR_OK) st = encode_map_4d(&m.v, kMapBf16, 128, k.v_pool, kdim, kst, kbox);
     return st;
 }
 

@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_rows_kernel(const __grid_co
 
 // cos and sin of every pair for a list of positions: [n_rows][cos D/2 | sin D/2].  Bound by the fp64 products and the sines, not by the bytes: 66560 rows of
 // 128 take 64 us (35 MB), 4160 rows 6.7 us; a step's 16 rows are one launch, 2.5 us.
-__global__ void __launch_bounds__(kRopeThreads) rope_table_kernel(const __grid_constant__ RopeFreqs f, const int* pos, long long pos_axis_stride,
+static __global__ void __launch_bounds__(kRopeThreads) rope_table_kernel(const __grid_constant__ RopeFreqs f, const int* pos, long long pos_axis_stride,
                                                                   int n_rows, int half, float* out) {
     const long long n = (long long)n_rows * half;
     for (long long idx = (long long)blockIdx.x * kRopeThreads + threadIdx.x; idx < n; idx += (long long)gridDim.x * kRopeThreads) {

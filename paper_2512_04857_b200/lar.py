@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(_HERE, "liblar.so")
 
 LAR_OK, LAR_ERR_INVALID_ARG, LAR_ERR_BAD_STATE, LAR_ERR_CAPACITY, LAR_ERR_CUDA, LAR_ERR_NOMEM, \
     LAR_ERR_DEVICE_CHECK = range(7)
-LAR_BF16, LAR_FP32 = 0, 1
+LAR_BF16, LAR_FP32, LAR_E4M3 = 0, 1, 2
+LAR_NORM_RMS, LAR_NORM_LAYER = 0, 1
 LAR_FLAG_NO_HOST_CHECKS, LAR_FLAG_PDL, LAR_FLAG_SHUFFLE_PAGES, LAR_FLAG_TILE_RANGES = 0x1, 0x2, 0x4, 0x8
 LAR_FLAG_SCORE_CACHE_NORM = 0x10
 LAR_FLAG_HOST_DEFER_OUT = 0x20
@@ -62,6 +63,16 @@ class lar_paged_kv_t(C.Structure):
                 ("lens_stride", C.c_int64), ("status", C.c_void_p)]
 
 
+class lar_head_norm_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("kind", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("head_stride", C.c_int64)]
+
+
+class lar_paged_q8_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("reserved", C.c_uint32), ("kv", lar_paged_kv_t), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("scale_page_stride", C.c_int64), ("scale_head_stride", C.c_int64)]
+
+
 class LarError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -85,6 +96,7 @@ def lib():
     L = C.CDLL(LIB_PATH)
     vp, ip, cfgp, planp = C.c_void_p, C.c_int, C.POINTER(lar_config_t), C.POINTER(lar_plan_t)
     ropep, rowsp, kvp = C.POINTER(lar_rope_t), C.POINTER(lar_rows_t), C.POINTER(lar_paged_kv_t)
+    normp, q8p = C.POINTER(lar_head_norm_t), C.POINTER(lar_paged_q8_t)
     sigs = {
         "lar_plan_query": (C.c_int, [cfgp, planp]),
         "lar_cache_slab_bytes": (C.c_size_t, [cfgp]),
@@ -113,6 +125,13 @@ def lib():
         "lar_paged_attn_workspace_bytes": (C.c_size_t, [kvp, ip, C.c_int64, ip, ip]),
         "lar_cache_paged_view": (C.c_int, [vp, ip, kvp]),
         "lar_append_kv_rope": (C.c_int, [vp, ip, ropep, vp, C.c_int64, rowsp, rowsp, rowsp, rowsp, ip, vp]),
+        "lar_norm_rope_rotate": (C.c_int, [normp, normp, ropep, ip, ip, vp, C.c_int64, C.c_int64, rowsp, rowsp, ip, rowsp, rowsp, ip, vp]),
+        "lar_paged_append_norm_rope": (C.c_int, [kvp, normp, normp, ropep, vp, C.c_int64, rowsp, rowsp, rowsp, rowsp, ip, C.c_int64, vp, vp]),
+        "lar_append_kv_norm_rope": (C.c_int, [vp, ip, normp, normp, ropep, vp, C.c_int64, rowsp, rowsp, rowsp, rowsp, ip, vp]),
+        "lar_paged_q8_append": (C.c_int, [q8p, ip, normp, normp, ropep, vp, C.c_int64, rowsp, rowsp, rowsp, rowsp, ip, C.c_int64, vp, vp]),
+        "lar_paged_q8_read": (C.c_int, [q8p, ip, rowsp, rowsp, C.c_int64, vp, vp]),
+        "lar_paged_q8_attn": (C.c_int, [q8p, ip, rowsp, rowsp, ip, C.c_int64, vp, vp, ip, C.c_float, ip, ip, vp, C.c_size_t, vp]),
+        "lar_paged_q8_attn_workspace_bytes": (C.c_size_t, [q8p, ip, ip, C.c_int64, ip, ip]),
         "lar_status_str": (C.c_char_p, [C.c_int]),
         "lar_last_cuda_error": (C.c_int, []),
     }
@@ -287,8 +306,9 @@ def _fast():
     if _FAST is None:
         import torch
         typed, raw = lib(), C.CDLL(LIB_PATH)
-        names = ("lar_rope_table", "lar_rope_rotate", "lar_paged_append_rope", "lar_paged_attn", "lar_append_kv_rope")
-        plain = {C.POINTER(t): C.c_void_p for t in (lar_rope_t, lar_rows_t, lar_paged_kv_t)}
+        names = ("lar_rope_table", "lar_rope_rotate", "lar_paged_append_rope", "lar_paged_attn", "lar_append_kv_rope", "lar_norm_rope_rotate",
+                 "lar_paged_append_norm_rope", "lar_append_kv_norm_rope", "lar_paged_q8_append", "lar_paged_q8_read", "lar_paged_q8_attn")
+        plain = {C.POINTER(t): C.c_void_p for t in (lar_rope_t, lar_rows_t, lar_paged_kv_t, lar_head_norm_t, lar_paged_q8_t)}
         for name in names:
             fn = getattr(raw, name)
             fn.restype, fn.argtypes = C.c_int, [plain.get(a, a) for a in getattr(typed, name).argtypes]
@@ -380,6 +400,51 @@ def rope_rotate(rope, pos, q, q_out, k=None, k_out=None, inverse=False):
           None if k is None else _rows(k_out, n, hk, d, dt, dev, "rope_rotate: k_out"), hk, int(inverse))
 
 
+class HeadNorm:
+    """Norm of every head's row: kind "rms" or "layer"; weight and bias (None: ones / zeros) [head_dim], or [heads, head_dim] with a row for each
+    head, bf16 or fp32 whatever the rows are.  Keeps the tensors alive."""
+
+    def __init__(self, kind, weight=None, bias=None, eps=1e-6):
+        _require(kind in ("rms", "layer"), f"HeadNorm: kind {kind!r}")
+        given = [x for x in (weight, bias) if x is not None]
+        code, stride = LAR_FP32, 0
+        self.head_dim = self.heads = self.dev = None
+        for x in given:
+            code, self.dev = _dtype_of(x), _device_of(x)
+            _require(x.dim() in (1, 2) and x.stride(-1) == 1 and x.dtype == given[0].dtype and x.shape == given[0].shape and
+                     x.stride() == given[0].stride() and x.device == given[0].device, "HeadNorm: weight and bias")
+            self.head_dim = x.shape[-1]
+            if x.dim() == 2:
+                self.heads, stride = x.shape[0], x.stride(0)
+        self._keep = (weight, bias)
+        self.desc = lar_head_norm_t(C.sizeof(lar_head_norm_t), LAR_NORM_LAYER if kind == "layer" else LAR_NORM_RMS, code, float(eps),
+                                    _ptr(weight), _ptr(bias), stride)
+        self._at = C.addressof(self.desc)
+
+
+def _norm(norm, heads, d, dev, what):
+    """Address of a HeadNorm's description, or None."""
+    if norm is None:
+        return None
+    if norm.head_dim not in (None, d) or norm.heads not in (None, heads) or norm.dev not in (None, dev):
+        raise LarError(LAR_ERR_INVALID_ARG, f"{what}: a norm of {heads} heads of {d} elements on the same GPU is expected")
+    return norm._at
+
+
+def norm_rope_rotate(rope, pos, q, q_out, k=None, k_out=None, q_norm=None, k_norm=None):
+    """rope_rotate with norms of q's and k's rows before the rotation, in one pass (rope and pos None: norms alone)."""
+    code, dt, dev = _dtype_of(q), q.dtype, _device_of(q)
+    n, hq, d = q.shape
+    _require((rope is None) == (pos is None) and (k is None) == (k_out is None), "norm_rope_rotate: shapes")
+    at, stride = (None, 0) if pos is None else _positions(pos, rope, n, dev, "norm_rope_rotate")
+    hk = 0 if k is None else k.shape[1]
+    _call("lar_norm_rope_rotate", dev, _norm(q_norm, hq, d, dev, "norm_rope_rotate: q_norm"), _norm(k_norm, hk, d, dev, "norm_rope_rotate: k_norm"),
+          None if rope is None else C.addressof(rope), code, d, at, stride, n, _rows(q, n, hq, d, dt, dev, "norm_rope_rotate: q"),
+          _rows(q_out, n, hq, d, dt, dev, "norm_rope_rotate: q_out"), hq,
+          None if k is None else _rows(k, n, hk, d, dt, dev, "norm_rope_rotate: k"),
+          None if k is None else _rows(k_out, n, hk, d, dt, dev, "norm_rope_rotate: k_out"), hk)
+
+
 class PagedKV:
     """A paged K/V cache in the caller's tensors.
 
@@ -409,10 +474,14 @@ class PagedKV:
         self._status = status
         self._keep = (k_pool, v_pool, page_table, lens, status)
         self._set(lar_paged_kv_t(
-            C.sizeof(lar_paged_kv_t), _dtype_of(k_pool), seqs, n_kv_heads, d, page_tokens, pages, page_table.shape[-1],
+            C.sizeof(lar_paged_kv_t), self._code(k_pool), seqs, n_kv_heads, d, page_tokens, pages, page_table.shape[-1],
             k_pool.stride(0), k_pool.stride(1), 0 if per_head else k_pool.stride(2), k_pool.data_ptr(), v_pool.data_ptr(),
             page_table.data_ptr(), page_table.stride(0), page_table.stride(1) if per_head else 0, lens.data_ptr(),
             lens.stride(0), _ptr(status)), k_pool.dtype, k_pool.device)
+
+    @staticmethod
+    def _code(pool):
+        return _dtype_of(pool)
 
     def _set(self, desc, dtype, device):
         self.desc, self._at, self.dtype, self.device = desc, C.addressof(desc), dtype, device
@@ -451,6 +520,23 @@ class PagedKV:
               None if q is None else _rows(q_out, n, hq, d, dt, dev, "append_rope: q_out"), hq, n,
               _ints(cu_tokens, self.n_seqs + 1, dev, "append_rope: cu_tokens"))
 
+    def append_norm_rope(self, k, v, cu_tokens=None, rope=None, pos=None, q=None, q_out=None, q_norm=None, k_norm=None):
+        """append_rope with norms of q's and k's rows (HeadNorm) before the rotation, in the same pass."""
+        _fast()
+        self._append("lar_paged_append_norm_rope", (self._at,), self.dtype, k, v, cu_tokens, rope, pos, q, q_out, q_norm, k_norm)
+
+    def _append(self, name, first, dt, k, v, cu_tokens, rope, pos, q, q_out, q_norm, k_norm):
+        n, hkv, d, dev = k.shape[0], self.n_kv_heads, self.head_dim, _device_of(k)
+        _require((rope is None) == (pos is None) and (q is None) == (q_out is None) and dev == self.device.index, "append_norm_rope")
+        at, stride = (None, 0) if pos is None else _positions(pos, rope, n, dev, "append_norm_rope")
+        hq = 0 if q is None else q.shape[1]
+        _call(name, dev, *first, _norm(q_norm, hq, d, dev, "append_norm_rope: q_norm"), _norm(k_norm, hkv, d, dev, "append_norm_rope: k_norm"),
+              None if rope is None else C.addressof(rope), at, stride,
+              _rows(k, n, hkv, d, dt, dev, "append_norm_rope: k"), _rows(v, n, hkv, d, dt, dev, "append_norm_rope: v"),
+              None if q is None else _rows(q, n, hq, d, dt, dev, "append_norm_rope: q"),
+              None if q is None else _rows(q_out, n, hq, d, dt, dev, "append_norm_rope: q_out"), hq, n,
+              _ints(cu_tokens, self.n_seqs + 1, dev, "append_norm_rope: cu_tokens"))
+
     def attn_workspace(self, n_q_heads, n_tokens, max_chunk=0, max_len=0):
         """A workspace tensor for attn calls of these sizes and all smaller ones (None where none is used)."""
         import torch
@@ -468,6 +554,75 @@ class PagedKV:
             _require(workspace.get_device() == dev and workspace.is_contiguous(), "attn: workspace")
             ws_at, ws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         _call("lar_paged_attn", dev, self._at, _rows(q, n, hq, d, dt, dev, "attn: q"), _rows(out, n, hq, d, dt, dev, "attn: out"),
+              hq, n, _ints(cu_tokens, self.n_seqs + 1, dev, "attn: cu_tokens"), _ints(kv_start, self.n_seqs, dev, "attn: kv_start"),
+              int(causal), softmax_scale, max_chunk, max_len, ws_at, ws)
+
+
+class PagedKV8(PagedKV):
+    """A paged K/V cache in 8 bits, in the caller's tensors (see lar_paged_q8_t for what an element is).
+
+    k_pool, v_pool    float8_e4m3fn or uint8, shaped and strided as PagedKV's
+    k_scale, v_scale  uint8 [pages, heads, page_tokens], the bytes of a page's slots side by side; strides multiples of 16
+    page_table, lens, status as PagedKV's
+
+    The rows that go in and come out (k, v, q, out) are bf16 or fp32, whichever the call's tensors are.
+    """
+
+    def __init__(self, k_pool, v_pool, k_scale, v_scale, page_table, lens, n_kv_heads, status=None):
+        import torch
+        codes = (torch.float8_e4m3fn, torch.uint8)
+        _require(k_pool.dtype in codes and v_pool.dtype in codes, "PagedKV8: pools")
+        k8, v8 = k_pool.view(torch.uint8), v_pool.view(torch.uint8)
+        pages, page_tokens, heads = k_pool.shape[:3]
+        for x in (k_scale, v_scale):
+            _require(x.dtype == torch.uint8 and x.shape == (pages, heads, page_tokens) and x.stride() == k_scale.stride() and
+                     x.stride(2) == 1 and x.device == k_pool.device, "PagedKV8: scales")
+        super().__init__(k8, v8, page_table, lens, n_kv_heads, status)
+        self._keep += (k_pool, v_pool, k_scale, v_scale)
+        self.desc = lar_paged_q8_t(C.sizeof(lar_paged_q8_t), 0, self.desc, k_scale.data_ptr(), v_scale.data_ptr(), k_scale.stride(0),
+                                   0 if page_table.dim() == 3 else k_scale.stride(1))
+        self._at = C.addressof(self.desc)
+
+    @staticmethod
+    def _code(x):
+        return LAR_E4M3
+
+    @classmethod
+    def of_cache(cls, cache, layer):
+        raise LarError(LAR_ERR_INVALID_ARG, "PagedKV8.of_cache: the library's own caches are not held in 8 bits")
+
+    def append_rope(self, k, v, cu_tokens=None, rope=None, pos=None, q=None, q_out=None):
+        """Stores the chunks' keys (rotated by rope at pos [axes, tokens]) and values in 8 bits; q is rotated into q_out."""
+        self.append_norm_rope(k, v, cu_tokens, rope, pos, q, q_out)
+
+    def append_norm_rope(self, k, v, cu_tokens=None, rope=None, pos=None, q=None, q_out=None, q_norm=None, k_norm=None):
+        """append_rope with norms of q's and k's rows (HeadNorm) before the rotation, in the same pass."""
+        self._append("lar_paged_q8_append", (self._at, _dtype_of(k)), k.dtype, k, v, cu_tokens, rope, pos, q, q_out, q_norm, k_norm)
+
+    def read(self, k_out, v_out, cu_rows=None):
+        """The newest entries of every sequence, as many as it has rows in k_out and v_out [rows, kv_heads, head_dim] (bf16 or fp32)."""
+        code, n, hkv, d, dt, dev = _dtype_of(k_out), k_out.shape[0], self.n_kv_heads, self.head_dim, k_out.dtype, _device_of(k_out)
+        _require(dev == self.device.index, "read: the cache lies on another GPU")
+        _call("lar_paged_q8_read", dev, self._at, code, _rows(k_out, n, hkv, d, dt, dev, "read: k_out"), _rows(v_out, n, hkv, d, dt, dev, "read: v_out"),
+              n, _ints(cu_rows, self.n_seqs + 1, dev, "read: cu_rows"))
+
+    def attn_workspace(self, n_q_heads, n_tokens, max_chunk=0, max_len=0, dtype=None):
+        """A workspace tensor for attn calls of these sizes and all smaller ones with rows of dtype (None: bf16); None where none is used."""
+        import torch
+        code = LAR_BF16 if dtype in (None, torch.bfloat16) else LAR_FP32
+        _require(dtype in (None, torch.bfloat16, torch.float32), "attn_workspace: dtype")
+        n = lib().lar_paged_q8_attn_workspace_bytes(self.desc, code, n_q_heads, n_tokens, max_chunk, max_len)
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+    def attn(self, q, out, cu_tokens=None, causal=True, kv_start=None, softmax_scale=0.0, max_chunk=0, max_len=0, workspace=None):
+        """Attention of the chunks' queries [tokens, heads, head_dim] (bf16 or fp32) over the cache; see lar_paged_q8_attn."""
+        code, n, hq, d, dt, dev = _dtype_of(q), q.shape[0], q.shape[1], self.head_dim, q.dtype, _device_of(q)
+        _require(dev == self.device.index, "attn: the cache lies on another GPU")
+        ws_at, ws = None, 0
+        if workspace is not None:
+            _require(workspace.get_device() == dev and workspace.is_contiguous(), "attn: workspace")
+            ws_at, ws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _call("lar_paged_q8_attn", dev, self._at, code, _rows(q, n, hq, d, dt, dev, "attn: q"), _rows(out, n, hq, d, dt, dev, "attn: out"),
               hq, n, _ints(cu_tokens, self.n_seqs + 1, dev, "attn: cu_tokens"), _ints(kv_start, self.n_seqs, dev, "attn: kv_start"),
               int(causal), softmax_scale, max_chunk, max_len, ws_at, ws)
 
@@ -514,15 +669,18 @@ class Cache:
     def append_kv(self, layer, k, v, n_tokens):
         lar_append_kv(self.handle, layer, k, v, n_tokens, self._stream())
 
-    def append_kv_rope(self, layer, k, v, n_tokens, rope=None, pos=None, q=None, q_out=None):
-        """The prefill with rotated keys: k, v, q are [batch * n_tokens, heads, head_dim], sequence by sequence."""
+    def append_kv_rope(self, layer, k, v, n_tokens, rope=None, pos=None, q=None, q_out=None, q_norm=None, k_norm=None):
+        """The prefill with rotated keys: k, v, q are [batch * n_tokens, heads, head_dim], sequence by sequence.  q_norm, k_norm (HeadNorm): norms
+        of the rows before the rotation."""
         _fast()
         n, hq, hkv, d, dt, dev = (self.cfg.batch * n_tokens, self.cfg.n_q_heads, self.cfg.n_kv_heads, self.cfg.head_dim,
                                   k.dtype, _device_of(k))
         _require((rope is None) == (pos is None) and (q is None) == (q_out is None) and _dtype_of(k) == self.cfg.dtype and
                  dev == self.slab.get_device(), "append_kv_rope")
         at, stride = (None, 0) if pos is None else _positions(pos, rope, n, dev, "append_kv_rope")
-        _call("lar_append_kv_rope", dev, self.handle, layer, None if rope is None else C.addressof(rope), at, stride,
+        hq = hq if q is not None else 0
+        _call("lar_append_kv_norm_rope", dev, self.handle, layer, _norm(q_norm, hq, d, dev, "append_kv_rope: q_norm"),
+              _norm(k_norm, hkv, d, dev, "append_kv_rope: k_norm"), None if rope is None else C.addressof(rope), at, stride,
               _rows(k, n, hkv, d, dt, dev, "append_kv_rope: k"), _rows(v, n, hkv, d, dt, dev, "append_kv_rope: v"),
               None if q is None else _rows(q, n, hq, d, dt, dev, "append_kv_rope: q"),
               None if q is None else _rows(q_out, n, hq, d, dt, dev, "append_kv_rope: q_out"), n_tokens)
