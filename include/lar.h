@@ -498,6 +498,23 @@ lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, cons
 /* Bytes of workspace that suffice for lar_paged_q8_attn with these arguments and every smaller call, as lar_paged_attn_workspace_bytes. */
 size_t lar_paged_q8_attn_workspace_bytes(const lar_paged_q8_t* cache, int rows_dtype, int n_q_heads, int64_t n_tokens, int max_chunk, int max_len);
 
+/* lar_paged_attn (bf16 and fp32 caches, no kv_start) for sequences that have their first slots in common: many images of one prompt.  Group g is the sequences
+ * cu_groups[g] .. cu_groups[g + 1] - 1 (device, int32, [n_groups + 1], ascending), and their first shared_lens[g] slots (device, int32, [n_groups]) hold the
+ * same keys and values: the same pages in every table, or copies; those of the group's first sequence are read, once for all of its tokens.
+ * Every sequence of a group that has tokens holds the slots in common before its chunk; of a length that says more, only what the shortest of the group's caches
+ * held before its chunk is taken as common.  Sequences of no group share nothing.  shared_lens need not be multiples of page_tokens.
+ * The result is that of lar_paged_attn up to rounding.  max_shared bounds shared_lens (0: not known) and chooses the launch shape only.  Chunks of more than
+ * 128 rows per KV head, and calls with workspace NULL, go through lar_paged_attn: a read of a slot serves that many rows there already.
+ * workspace: lar_paged_attn_shared_workspace_bytes of these arguments or larger ones; as lar_paged_attn otherwise. */
+lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads, int64_t n_tokens,
+                                   const int32_t* cu_tokens, int n_groups, const int32_t* cu_groups, const int32_t* shared_lens, int causal,
+                                   float softmax_scale, int max_chunk, int max_len, int max_shared, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* Bytes of workspace that suffice for lar_paged_attn_shared with these arguments and every smaller call, as lar_paged_attn_workspace_bytes. */
+size_t lar_paged_attn_shared_workspace_bytes(const lar_paged_kv_t* kv, int n_q_heads, int64_t n_tokens, int n_groups, int max_chunk, int max_len,
+                                             int max_shared);
+
 const char* lar_status_str(lar_status_t s);
 int lar_last_cuda_error(void); /* cudaError_t of the last failed runtime call in this thread, 0 if none */
 

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "liblar.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("lar_api.cu", "paged_api.cu", "norm_api.cu", "paged_q8_api.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("lar_api.cu", "paged_api.cu", "norm_api.cu", "paged_q8_api.cu", "paged_shared_api.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))] + \
     [os.path.join(ROOT, "include", "lar.h")]
 

@@ -21,6 +21,7 @@ struct PagedView {
     const int* cu;   // [n_seqs + 1], or null: every sequence has chunk tokens
     int chunk;
     int n_tokens;
+    const int* row_of;  // row of the page table of each sequence, or null: its own number (groups of sequences with slots in common)
 };
 
 __device__ __forceinline__ void paged_report(const PagedView& v, unsigned bits) {

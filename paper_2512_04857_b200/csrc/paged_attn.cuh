@@ -26,6 +26,9 @@ struct PagedAttnArgs {
     float* part_o;     // partial results of units whose slots are spread over several CTAs
     float* part_ml;
     int n_splits;
+    int parts;         // fp32: rows are left as parts (split, or joined with another call's)
+    float* row_o;      // kernels with PART: (O, m, l) of every (token, head) instead of its output row
+    float* row_ml;
 };
 
 // two fp32 operations in one instruction

@@ -40,7 +40,8 @@ struct FewShape {
     static __host__ __device__ int bytes(int n_seqs) { return FIXED + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
 };
 
-template <int D, int NR>
+// PART: the rows of all units, cut or not, are left as (O, m, l) for a kernel that joins them with those over other slots.
+template <int D, int NR, bool PART = false>
 __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER_SM) paged_attn_few_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
     using S = FewShape<D, NR>;
     using Work = TcWork<1, S::KT, D>;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
             int t1;
             chunk_of(a.kv, s, v.t0, t1);
             v.n = t1 - v.t0;
-            v.len = live_len(a.kv, s, v.n, blockIdx.x == 0);
+            v.len = live_len(a.kv, s, v.n, blockIdx.x == 0 && !(PART && a.kv.row_of));
             v.lo = a.start ? max(a.start[s], 0) : 0;
             info[s] = v;
             sum += (v.n + a.tq - 1) / a.tq * a.kv.n_kv_heads * (ta.split ? Work::items_of_unit(v) : 1);
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
         while (ok && work.next(g)) {
             const int n = g.nb, len = min(g.len, cap), lo = g.lo;
             if (n == 0) continue;
-            const int* table = a.kv.table + g.seq * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
+            const int* table = a.kv.table + (PART && a.kv.row_of ? a.kv.row_of[g.seq] : g.seq) * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
             const int head_c = a.kv.head_stride > 0 ? g.head : 0;
             int slot = g.jb * KT + box_slot;  // first slot of this lane's box
             auto page_of = [&](int slot) {
@@ -384,7 +385,12 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
                     o.z = fmaf(p.z, f, o.z);
                     o.w = fmaf(p.w, f, o.w);
                 }
-                if (g.whole) {
+                if (PART && g.whole) {
+                    const int t = row / G;
+                    const size_t at = (size_t)(g.tok0 + t) * (a.kv.n_kv_heads * G) + g.head * G + row - t * G;
+                    *reinterpret_cast<float4*>(a.row_o + at * D + e) = o;
+                    if (e == 0) *reinterpret_cast<float2*>(a.row_ml + at * 2) = make_float2(M, L);
+                } else if (g.whole) {
                     const float inv = L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
                     const int t = row / G;
                     __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + (long long)(g.tok0 + t) * a.out.token_stride +

@@ -61,7 +61,7 @@ struct Fp32Unit {
         chunk_of(a.kv, seq, t0, t1);
         tile = (t1 - t0 + a.tq - 1) / a.tq - 1 - tile;  // the tiles that see most first
         head = blockIdx.y;
-        len = live_len(a.kv, seq, t1 - t0, threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0);
+        len = live_len(a.kv, seq, t1 - t0, threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && !a.kv.row_of);
         tok0 = t0 + tile * a.tq;
         n_tok = min(a.tq, t1 - tok0);
         rows = n_tok * a.group;
@@ -72,7 +72,7 @@ struct Fp32Unit {
         const int per = (end - first + a.n_splits - 1) / a.n_splits;
         b0 = min(end, first + (int)blockIdx.z * per);
         b1 = min(end, b0 + per);
-        table = a.kv.table + seq * a.kv.table_seq_stride + head * a.kv.table_head_stride;
+        table = a.kv.table + (a.kv.row_of ? a.kv.row_of[seq] : seq) * a.kv.table_seq_stride + head * a.kv.table_head_stride;
         return true;
     }
     // The K or V rows of a step; slots outside [lo, hi) are zero whatever their memory holds.  16 slots at a time: they lie in one page, so
@@ -122,7 +122,7 @@ struct Fp32Unit {
         return ((size_t)blockIdx.z * a.kv.n_tokens + tok0 + t) * hq + head * a.group + g;
     }
     __device__ __forceinline__ float* out_row(const PagedAttnArgs& a, int row, int d) const {
-        if (a.n_splits > 1) return a.part_o + part_row(a, row) * d;
+        if (a.parts) return a.part_o + part_row(a, row) * d;
         const int t = row / a.group, g = row - t * a.group;
         return reinterpret_cast<float*>(a.out.p) + (long long)(tok0 + t) * a.out.token_stride + (head * a.group + g) * a.out.head_stride;
     }
@@ -144,9 +144,9 @@ struct Fp32Unit {
                 x = fmaf(v.x, f, x);
                 y = fmaf(v.y, f, y);
             }
-            const float inv = a.n_splits > 1 ? 1.f : L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
+            const float inv = a.parts ? 1.f : L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
             *reinterpret_cast<float2*>(out_row(a, row, D) + e) = make_float2(x * inv, y * inv);
-            if (a.n_splits > 1 && e == 0) *reinterpret_cast<float2*>(a.part_ml + part_row(a, row) * 2) = make_float2(M, L);
+            if (a.parts && e == 0) *reinterpret_cast<float2*>(a.part_ml + part_row(a, row) * 2) = make_float2(M, L);
         }
     }
 };
@@ -378,11 +378,11 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
     for (int r = 0; r < 2; ++r) {
         const int row = row0 + 8 * r;
         if (row >= u.rows) continue;
-        const float inv = a.n_splits > 1 ? 1.f : l[r] > 0.f ? 1.0f / l[r] : l[r];
+        const float inv = a.parts ? 1.f : l[r] > 0.f ? 1.0f / l[r] : l[r];
         float* dst = u.out_row(a, row, D) + 2 * quad;
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(o[n][2 * r] * inv, o[n][2 * r + 1] * inv);
-        if (a.n_splits > 1 && quad == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(m[r], l[r]);
+        if (a.parts && quad == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(m[r], l[r]);
     }
 }
 

@@ -297,7 +297,8 @@ struct ScaledRef {
     __device__ __forceinline__ float rounding() const { return ex2_approx(-fmaf(m, scale, -scaled)); }
 };
 
-template <int D, int NT>
+// PART: the rows of all units, cut or not, are left as (O, m, l) for a kernel that joins them with those over other slots.
+template <int D, int NT, bool PART = false>
 __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ TcMaps maps) {
     using S = TcShape<D, NT>;
     constexpr int BN = S::BN, HALVES = S::HALVES;
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             int t1;
             chunk_of(a.kv, s, v.t0, t1);
             v.n = t1 - v.t0;
-            v.len = live_len(a.kv, s, v.n, blockIdx.x == 0);
+            v.len = live_len(a.kv, s, v.n, blockIdx.x == 0 && !(PART && a.kv.row_of));
             v.lo = a.start ? max(a.start[s], 0) : 0;
             info[s] = v;
             sum += (v.n + NT * a.tq - 1) / (NT * a.tq) * a.kv.n_kv_heads * (by_tiles ? Work::items_of_unit(v) : 1);
@@ -618,11 +619,15 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             const int slotp = blockIdx.x * 2 + (g.b0 > 0 ? 0 : 1);
             if (active) {
                 // nothing seen: 0; NaN stays NaN.  Parts are joined by their references as they are.
-                const float inv = g.whole ? (l > 0.f ? 1.0f / l : l) : ScaledRef(m_used, sc).rounding();
+                const bool done = g.whole && !PART;
+                const float inv = done ? (l > 0.f ? 1.0f / l : l) : ScaledRef(m_used, sc).rounding();
                 const size_t part = ((size_t)slotp * NT + tile) * ta.rows_cap + row;
                 // a thread has a row, but four neighbours write 64 bytes of one row together
                 unsigned long long own_row = 0;
-                if (mine)
+                const size_t all = (size_t)(g.tok0 + tile * a.tq + t) * (a.kv.n_kv_heads * G) + g.head * G + head_g;  // (PART)
+                if (PART && mine && g.whole)
+                    own_row = reinterpret_cast<unsigned long long>(a.row_o + all * D);
+                else if (mine)
                     own_row = g.whole ? reinterpret_cast<unsigned long long>(a.out.p) + 2 * ((long long)(g.tok0 + tile * a.tq + t) * a.out.token_stride + (long long)(g.head * G + head_g) * a.out.head_stride)
                                       : reinterpret_cast<unsigned long long>(a.part_o + part * D);
                 char* rows4[4];
@@ -645,7 +650,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                         for (int i = 0; i < 32; ++i) o[i] = 0;
                     }
                     uint4 u[4];
-                    if (g.whole) {
+                    if (done) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             u[i].x = pack_bf16(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
@@ -666,8 +671,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                     }
                     __syncwarp();  // (tcgen05.ld is a warp-wide instruction: all lanes together again)
                 }
-                if (mine && !g.whole) {
-                    float* ml = a.part_ml + part * 2;
+                if (mine && !done) {
+                    float* ml = PART && g.whole ? a.row_ml + all * 2 : a.part_ml + part * 2;
                     ml[0] = m_used;  // (-inf: nothing seen)
                     ml[1] = l * inv;
                 }
@@ -824,7 +829,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                 }
             }
             if (!ok) break;
-            const int* table = a.kv.table + g.seq * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
+            const int* table = a.kv.table + (PART && a.kv.row_of ? a.kv.row_of[g.seq] : g.seq) * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
             const int head_c = a.kv.head_stride > 0 ? g.head : 0;
             const int nmax = g.nb, len = min(g.len, cap), lo = g.lo;
             int slot = g.jb * BN + box_slot;  // first slot of this lane's box
@@ -867,7 +872,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
 }
 
 // Adds up the parts of the units that range boundaries cut, in the order of the CTAs that left them.
-template <int D, int NT>
+template <int D, int NT, bool PART = false>
 __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant__ TcArgs ta) {
     grid_dep_wait();
     const PagedAttnArgs& a = ta.a;
@@ -895,6 +900,12 @@ __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant_
         }
         const float inv = L > 0.f ? 1.0f / L : L;
         const int h = rec.z * a.group + unit_row - t * a.group;
+        if (PART) {
+            const size_t to = (size_t)(rec.x + t) * (a.kv.n_kv_heads * a.group) + h;
+            *reinterpret_cast<float4*>(a.row_o + to * D + e) = o;
+            if (e == 0) *reinterpret_cast<float2*>(a.row_ml + to * 2) = make_float2(M, L);
+            continue;
+        }
         __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + (long long)(rec.x + t) * a.out.token_stride + (long long)h * a.out.head_stride + e;
         *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
     }

@@ -132,6 +132,8 @@ def lib():
         "lar_paged_q8_read": (C.c_int, [q8p, ip, rowsp, rowsp, C.c_int64, vp, vp]),
         "lar_paged_q8_attn": (C.c_int, [q8p, ip, rowsp, rowsp, ip, C.c_int64, vp, vp, ip, C.c_float, ip, ip, vp, C.c_size_t, vp]),
         "lar_paged_q8_attn_workspace_bytes": (C.c_size_t, [q8p, ip, ip, C.c_int64, ip, ip]),
+        "lar_paged_attn_shared": (C.c_int, [kvp, rowsp, rowsp, ip, C.c_int64, vp, ip, vp, vp, ip, C.c_float, ip, ip, ip, vp, C.c_size_t, vp]),
+        "lar_paged_attn_shared_workspace_bytes": (C.c_size_t, [kvp, ip, C.c_int64, ip, ip, ip, ip]),
         "lar_status_str": (C.c_char_p, [C.c_int]),
         "lar_last_cuda_error": (C.c_int, []),
     }
@@ -307,7 +309,8 @@ def _fast():
         import torch
         typed, raw = lib(), C.CDLL(LIB_PATH)
         names = ("lar_rope_table", "lar_rope_rotate", "lar_paged_append_rope", "lar_paged_attn", "lar_append_kv_rope", "lar_norm_rope_rotate",
-                 "lar_paged_append_norm_rope", "lar_append_kv_norm_rope", "lar_paged_q8_append", "lar_paged_q8_read", "lar_paged_q8_attn")
+                 "lar_paged_append_norm_rope", "lar_append_kv_norm_rope", "lar_paged_q8_append", "lar_paged_q8_read", "lar_paged_q8_attn",
+                 "lar_paged_attn_shared")
         plain = {C.POINTER(t): C.c_void_p for t in (lar_rope_t, lar_rows_t, lar_paged_kv_t, lar_head_norm_t, lar_paged_q8_t)}
         for name in names:
             fn = getattr(raw, name)
@@ -558,6 +561,29 @@ class PagedKV:
               int(causal), softmax_scale, max_chunk, max_len, ws_at, ws)
 
 
+    def attn_shared_workspace(self, n_q_heads, n_tokens, n_groups, max_chunk=0, max_len=0, max_shared=0):
+        """A workspace tensor for attn_shared calls of these sizes and all smaller ones (None where none is used)."""
+        import torch
+        n = lib().lar_paged_attn_shared_workspace_bytes(self.desc, n_q_heads, n_tokens, n_groups, max_chunk, max_len, max_shared)
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+    def attn_shared(self, q, out, cu_groups, shared_lens, cu_tokens=None, causal=True, softmax_scale=0.0, max_chunk=0, max_len=0, max_shared=0,
+                    workspace=None):
+        """attn for sequences that have their first slots in common, in groups: cu_groups int32 [groups + 1] sequences, shared_lens int32 [groups] slots;
+        see lar_paged_attn_shared."""
+        _fast()
+        n, hq, d, dt, dev = q.shape[0], q.shape[1], self.head_dim, self.dtype, _device_of(q)
+        _require(dev == self.device.index, "attn_shared: the cache lies on another GPU")
+        groups = shared_lens.shape[0]
+        ws_at, ws = None, 0
+        if workspace is not None:
+            _require(workspace.get_device() == dev and workspace.is_contiguous(), "attn_shared: workspace")
+            ws_at, ws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _call("lar_paged_attn_shared", dev, self._at, _rows(q, n, hq, d, dt, dev, "attn_shared: q"), _rows(out, n, hq, d, dt, dev, "attn_shared: out"),
+              hq, n, _ints(cu_tokens, self.n_seqs + 1, dev, "attn_shared: cu_tokens"), groups, _ints(cu_groups, groups + 1, dev, "attn_shared: cu_groups"),
+              _ints(shared_lens, groups, dev, "attn_shared: shared_lens"), int(causal), softmax_scale, max_chunk, max_len, max_shared, ws_at, ws)
+
+
 class PagedKV8(PagedKV):
     """A paged K/V cache in 8 bits, in the caller's tensors (see lar_paged_q8_t for what an element is).
 
@@ -590,6 +616,11 @@ class PagedKV8(PagedKV):
     @classmethod
     def of_cache(cls, cache, layer):
         raise LarError(LAR_ERR_INVALID_ARG, "PagedKV8.of_cache: the library's own caches are not held in 8 bits")
+
+    def attn_shared(self, *args, **kwargs):
+        raise LarError(LAR_ERR_INVALID_ARG, "PagedKV8.attn_shared: caches of bf16 and fp32 only")
+
+    attn_shared_workspace = attn_shared
 
     def append_rope(self, k, v, cu_tokens=None, rope=None, pos=None, q=None, q_out=None):
         """Stores the chunks' keys (rotated by rope at pos [axes, tokens]) and values in 8 bits; q is rotated into q_out."""
