@@ -41,10 +41,18 @@ NormFn norm_fn(int dtype, int d, bool inter) {
 }
 
 lar_status_t launch_norm(NormRopeArgs& a, NormFn fn, int d, cudaStream_t s) {
-    a.any_norm = a.norm[0].on || a.norm[1].on;
-    a.any_layer = a.norm[0].layer || a.norm[1].layer;
-    const dim3 grid = rope_grid(a.r);
-    fn<<<grid, kRopeThreads, (size_t)a.r.tokens_per_cta * (d + 2) * 4, s>>>(a);
+    // Small batches (below 16 * kSms) as in rope_grid, a token per CTA with its rows dealt to enough CTAs that every SM has some; large ones up to eight tokens per CTA,
+    // so that the rows of a kind fill the threads' batches.
+    dim3 grid = rope_grid(a.r);
+    int64_t tokens = a.r.n_tokens / (8 * kSms);
+    tokens = tokens > 8 ? 8 : tokens;
+    if (tokens > 1) {
+        a.r.tokens_per_cta = (int)tokens;
+        a.r.rows_per_slice = a.r.n_rows;
+        grid = dim3((unsigned)((a.r.n_tokens + tokens - 1) / tokens), 1);
+        for (int i = 0; i < 3; ++i) a.magic[i] = a.r.heads[i] > 1 ? (unsigned)((1ull << 32) / (unsigned)a.r.heads[i] + 1ull) : 0u;
+    }
+    fn<<<grid, kRopeThreads, (size_t)a.r.tokens_per_cta * (d + d / 2 + 2) * 4, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     return LAR_OK;
 }

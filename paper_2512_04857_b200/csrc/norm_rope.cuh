@@ -9,10 +9,27 @@
 // (fp32) threads of a row are neighbours in a warp, so that the row's sums are three or four shuffles, taken with the row in registers: the
 // mean first and the squares of what is left after it, not the difference of two large sums.  Weights come through L1.
 #pragma once
+#include "paged_attn.cuh"  // two fp32 operations in one instruction
 #include "paged_q8.cuh"
 #include "rope_rows.cuh"
 
 namespace lar {
+
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float sum_of(uint64_t v) {
+    float a, b;
+    unpack_f32x2(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN where one is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
 struct HeadNormView {
     const char* weight;  // null: ones
@@ -26,7 +43,7 @@ struct NormRopeArgs {
     RopeRowsArgs r;
     HeadNormView norm[2];  // of q, of k
     Q8View q8;             // DEST 2 only
-    int any_norm, any_layer;
+    unsigned magic[3];     // floor(2^32 / heads) + 1 of each kind of row (0: one head), where a CTA has several tokens; else 0
 };
 
 // E parameters of a norm as fp32 (16 or 8 bytes)
@@ -57,168 +74,260 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
     constexpr int E = Elt<T>::kPerChunk;  // elements of a 16-byte chunk
     constexpr int IPR = D / (2 * E);      // threads of a row
     constexpr int HP = D / 2;
+    constexpr int B = 16 / E;             // items (32 bytes each) that a thread has at a time: 32 registers once unpacked
+    constexpr int CS = D + HP;            // per token: cosines, sines, sines negated
     const RopeRowsArgs& a = na.r;
-    extern __shared__ __align__(16) float cs[];  // [tokens_per_cta][cos HP | sin HP], then the tokens' slots and sequences
-    int* slot_of = reinterpret_cast<int*>(cs + a.tokens_per_cta * D);
+    extern __shared__ __align__(16) float cs[];  // [tokens_per_cta][CS], then the tokens' slots and sequences
+    int* slot_of = reinterpret_cast<int*>(cs + a.tokens_per_cta * CS);
     int* seq_of = slot_of + a.tokens_per_cta;
 
     const int tid = threadIdx.x;
     const int t0 = blockIdx.x * a.tokens_per_cta;
     const int nt = min(a.tokens_per_cta, a.n_tokens - t0);
-    const int row0 = blockIdx.y * a.rows_per_slice;
-    const int nr = min(a.rows_per_slice, a.n_rows - row0);
-    const int n_items = nt * a.rows_per_slice * IPR;
+    const int row0 = blockIdx.y * a.rows_per_slice, row1 = min(row0 + a.rows_per_slice, a.n_rows);
     const int c = tid & (IPR - 1);
     const int o_lo = INTER ? 2 * c * E : c * E, o_hi = INTER ? (2 * c + 1) * E : HP + c * E;
-    auto row_sum = [](float v) {
-#pragma unroll
-        for (int o = 1; o < IPR; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
-    };
 
     bool ready = false;
-    for (int base = 0; base < n_items; base += kRopeThreads * kRopeBatch) {
-        uint4 lo[kRopeBatch], hi[kRopeBatch];
-        int tok[kRopeBatch], row[kRopeBatch];
+    // q, k and v rows one kind behind the other: what depends on the kind is the same for all threads
+    int first = 0;  // first row of the kind
+#pragma unroll 1
+    for (int which = 0; which < 3; ++which) {
+        const int h0 = max(row0 - first, 0), m = min(row1 - first, a.heads[which]) - h0;  // heads h0 .. h0 + m - 1 of this CTA
+        first += a.heads[which];
+        if (m <= 0) continue;
+        const int n_items = nt * m * IPR;
+        const HeadNormView& h = na.norm[which & 1];
+        const bool on = which < 2 && h.on, layer = on && h.layer, turn = which < 2 && a.pos;
+        const unsigned magic = na.magic[which];  // of m, where a CTA has several tokens
+        const RowsView& from = a.src[which];
+        char* pool = which == 1 ? a.kv.k_pool : a.kv.v_pool;
+#pragma unroll 1
+        for (int base = 0; base < n_items; base += kRopeThreads * B) {
+            uint4 lo[B], hi[B];
+            int tok[B], head[B];
+            long long at[B], scale_at[B];  // element of the pool (-1: the row is not written), its scale byte
 #pragma unroll
-        for (int b = 0; b < kRopeBatch; ++b) {
-            const int item = base + b * kRopeThreads + tid;
-            const int r = item / IPR;
-            const int tl = a.rows_magic ? (int)__umulhi((unsigned)r, a.rows_magic) : r;
-            const int rl = r - tl * a.rows_per_slice;
-            tok[b] = item < n_items && rl < nr ? tl : -1;
-            row[b] = row0 + rl;
-            lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
-            if (tok[b] >= 0) {
-                const int which = row[b] < a.heads[0] ? 0 : row[b] < a.heads[0] + a.heads[1] ? 1 : 2;
-                const int head = row[b] - (which > 0 ? a.heads[0] : 0) - (which > 1 ? a.heads[1] : 0);
-                const RowsView& s = a.src[which];
-                const T* p = reinterpret_cast<const T*>(s.p) + (long long)(t0 + tl) * s.token_stride + head * s.head_stride;
-                lo[b] = *reinterpret_cast<const uint4*>(p + o_lo);
-                hi[b] = *reinterpret_cast<const uint4*>(p + o_hi);
-            }
-        }
-        if (!ready) {  // sines, cosines and slots of the CTA's tokens, while the first rows are on the way
-            ready = true;
-            if (a.pos) {
-                const int i = tid & (HP - 1);
-                const double f = a.f.turns[i];
-                const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
-                for (int tl = tid / HP; tl < nt; tl += kRopeThreads / HP) {
-                    const float2 v = cos_sin_of(f, p[tl]);
-                    cs[tl * D + i] = v.x;
-                    cs[tl * D + HP + i] = v.y;
+            for (int b = 0; b < B; ++b) {
+                const int item = base + b * kRopeThreads + tid, r = item / IPR;
+                const int tl = magic ? (int)__umulhi((unsigned)r, magic) : a.tokens_per_cta > 1 ? r : 0;
+                tok[b] = item < n_items ? tl : -1;
+                head[b] = h0 + r - tl * m;
+                lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
+                if (tok[b] >= 0) {
+                    const T* p = reinterpret_cast<const T*>(from.p) + (t0 + tl) * from.token_stride + head[b] * from.head_stride;
+                    lo[b] = *reinterpret_cast<const uint4*>(p + o_lo);
+                    hi[b] = *reinterpret_cast<const uint4*>(p + o_hi);
                 }
             }
-            if (DEST) find_slots<kRopeThreads>(a.kv, a.state ? a.base_len : -1, t0, nt, slot_of, seq_of);
-            __syncthreads();
-        }
+            if (!ready) {  // sines, cosines and slots of the CTA's tokens, while the first rows are on the way
+                ready = true;
+                if (a.pos) {
+                    const int i = tid & (HP - 1);
+                    const double f = a.f.turns[i];
+                    const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
+                    for (int tl = tid / HP; tl < nt; tl += kRopeThreads / HP) {
+                        const float2 v = cos_sin_of(f, p[tl]);
+                        cs[tl * CS + i] = v.x;
+                        cs[tl * CS + HP + i] = v.y;
+                        cs[tl * CS + D + i] = -v.y;
+                    }
+                }
+                if (DEST) find_slots<kRopeThreads>(a.kv, a.state ? a.base_len : -1, t0, nt, slot_of, seq_of);
+                __syncthreads();
+            }
 #pragma unroll
-        for (int b = 0; b < kRopeBatch; ++b) {
-            // (all lanes stay together to the stores: the row sums are warp-wide)
-            const bool valid = tok[b] >= 0;
-            const int which = row[b] < a.heads[0] ? 0 : row[b] < a.heads[0] + a.heads[1] ? 1 : 2;
-            const int head = row[b] - (which > 0 ? a.heads[0] : 0) - (which > 1 ? a.heads[1] : 0);
-            float x[2 * E];  // the low chunk, then the high one
-            {
+            for (int b = 0; b < B; ++b) {
+                at[b] = scale_at[b] = 0;
+                if (DEST && tok[b] >= 0) {
+                    const int slot = slot_of[tok[b]], seq = seq_of[tok[b]];
+                    if (which == 0) {
+                        if (seq < 0) at[b] = -1;
+                    } else if (slot < 0) {
+                        at[b] = -1;
+                    } else {
+                        const int page = a.kv.table[seq * a.kv.table_seq_stride + head[b] * a.kv.table_head_stride + (slot >> a.kv.page_shift)];
+                        at[b] = page * a.kv.page_stride + (slot & (a.kv.page_tokens - 1)) * a.kv.row_stride + head[b] * a.kv.head_stride;
+                        if (page < 0 || page >= a.kv.n_pages) {
+                            at[b] = -1;
+                            if (c == 0) paged_report(a.kv, kStPage);
+                        }
+                        if (DEST == 2) scale_at[b] = page * na.q8.page_stride + head[b] * na.q8.head_stride + (slot & (a.kv.page_tokens - 1));
+                    }
+                }
+            }
+            if (DEST == 1 && which == 2) {  // values as they are: a pass through fp32 could touch the bits of a NaN
+#pragma unroll
+                for (int b = 0; b < B; ++b)
+                    if (tok[b] >= 0 && at[b] >= 0) {
+                        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(pool) + at[b] + o_lo) = lo[b];
+                        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(pool) + at[b] + o_hi) = hi[b];
+                    }
+                continue;
+            }
+            uint64_t x[B][E];  // two elements each: the low chunk, then the high one
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
                 float u[E], v[E];
                 Elt<T>::unpack(lo[b], u);
                 Elt<T>::unpack(hi[b], v);
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    x[i] = u[i];
-                    x[E + i] = v[i];
+                for (int i = 0; i < E / 2; ++i) {
+                    x[b][i] = pack_f32x2(u[2 * i], u[2 * i + 1]);
+                    x[b][E / 2 + i] = pack_f32x2(v[2 * i], v[2 * i + 1]);
                 }
             }
-            if (na.any_norm) {
-                const HeadNormView& h = na.norm[which == 0 ? 0 : 1];
-                const bool on = valid && which < 2 && h.on;
-                const bool layer = h.layer != 0;
-                float mean = 0.f, up = 1.f, ss = 0.f;
-                for (;;) {
-                    float y = 0.f;
-                    if (na.any_layer) {
+            if (on) {
+                // The row sums, one step for all rows of the batch at a time.  (Warp-wide: lanes without a row have zeros.)
+                float mean[B], ss[B], up[B];
+                auto sums = [&]() {
 #pragma unroll
-                        for (int i = 0; i < 2 * E; ++i) y += x[i];
-                        y = row_sum(y);
-                        mean = layer ? y * (1.0f / D) : 0.f;
-                    }
-                    y = 0.f;
+                    for (int b = 0; b < B; ++b) {
+                        uint64_t y = x[b][0];
 #pragma unroll
-                    for (int i = 0; i < 2 * E; ++i) {
-                        const float z = x[i] - mean;
-                        y = fmaf(z, z, y);
+                        for (int i = 1; i < E; ++i) y = add_f32x2(y, x[b][i]);
+                        mean[b] = sum_of(y);
                     }
-                    ss = row_sum(y);
-                    // squares beyond fp32: once more with the row scaled down (eps is nothing beside such a row)
-                    const bool again = on && up == 1.f && !(ss <= 3.4e38f);
-                    if (!__any_sync(0xffffffffu, again)) break;
-                    if (again) {
-                        up = 0x1p-80f;
 #pragma unroll
-                        for (int i = 0; i < 2 * E; ++i) x[i] *= up;
+                    for (int o = 1; o < IPR; o <<= 1)
+#pragma unroll
+                        for (int b = 0; b < B; ++b) mean[b] += __shfl_xor_sync(0xffffffffu, mean[b], o);
+#pragma unroll
+                    for (int b = 0; b < B; ++b) {
+                        mean[b] *= -1.0f / D;
+#pragma unroll
+                        for (int i = 0; i < E; ++i) x[b][i] = add_f32x2(x[b][i], pack_f32x2(mean[b], mean[b]));
                     }
+                };
+                auto squares = [&]() {
+#pragma unroll
+                    for (int b = 0; b < B; ++b) {
+                        uint64_t y = mul_f32x2(x[b][0], x[b][0]);
+#pragma unroll
+                        for (int i = 1; i < E; ++i) y = fma_f32x2(x[b][i], x[b][i], y);
+                        ss[b] = sum_of(y);
+                    }
+#pragma unroll
+                    for (int o = 1; o < IPR; o <<= 1)
+#pragma unroll
+                        for (int b = 0; b < B; ++b) ss[b] += __shfl_xor_sync(0xffffffffu, ss[b], o);
+                };
+                if (layer) sums();
+                squares();
+                bool beyond = false;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    up[b] = 1.f;
+                    beyond |= !(ss[b] <= 3.4e38f);
                 }
-                if (on) {
-                    const float f = rsqrtf(fmaf(ss, 1.0f / D, h.eps * up * up));
+                if (__any_sync(0xffffffffu, beyond)) {
+                    // squares (or the sum) beyond fp32: once more from the rows times 2^-80, beside which eps is nothing
 #pragma unroll
-                    for (int i = 0; i < 2 * E; ++i) x[i] = (x[i] - mean) * f;
-                    const long long at = head * h.head_stride;
-                    float w[E];
-                    if (h.weight) {
-                        norm_params<E>(h.weight, at + o_lo, h.bf16, w);
+                    for (int b = 0; b < B; ++b) {
+                        if (!(ss[b] <= 3.4e38f)) up[b] = 0x1p-80f;
+                        float u[E], v[E];
+                        Elt<T>::unpack(lo[b], u);
+                        Elt<T>::unpack(hi[b], v);
 #pragma unroll
-                        for (int i = 0; i < E; ++i) x[i] *= w[i];
-                        norm_params<E>(h.weight, at + o_hi, h.bf16, w);
-#pragma unroll
-                        for (int i = 0; i < E; ++i) x[E + i] *= w[i];
+                        for (int i = 0; i < E / 2; ++i) {
+                            x[b][i] = pack_f32x2(u[2 * i] * up[b], u[2 * i + 1] * up[b]);
+                            x[b][E / 2 + i] = pack_f32x2(v[2 * i] * up[b], v[2 * i + 1] * up[b]);
+                        }
                     }
-                    if (h.bias) {
-                        norm_params<E>(h.bias, at + o_lo, h.bf16, w);
+                    if (layer) sums();
+                    squares();
+                }
 #pragma unroll
-                        for (int i = 0; i < E; ++i) x[i] += w[i];
-                        norm_params<E>(h.bias, at + o_hi, h.bf16, w);
+                for (int b = 0; b < B; ++b) {
+                    if (tok[b] < 0) continue;
+                    const float f = rsqrtf(fmaf(ss[b], 1.0f / D, h.eps * up[b] * up[b]));
+                    const uint64_t f2 = pack_f32x2(f, f);
+                    const long long wat = head[b] * h.head_stride;
 #pragma unroll
-                        for (int i = 0; i < E; ++i) x[E + i] += w[i];
+                    for (int half = 0; half < 2; ++half) {
+                        uint64_t* y = x[b] + half * (E / 2);
+                        const int o = half ? o_hi : o_lo;
+                        float w[E];
+#pragma unroll
+                        for (int i = 0; i < E / 2; ++i) y[i] = mul_f32x2(y[i], f2);
+                        if (h.weight && h.bias) {
+                            float add[E];
+                            norm_params<E>(h.weight, wat + o, h.bf16, w);
+                            norm_params<E>(h.bias, wat + o, h.bf16, add);
+#pragma unroll
+                            for (int i = 0; i < E / 2; ++i) y[i] = fma_f32x2(y[i], pack_f32x2(w[2 * i], w[2 * i + 1]), pack_f32x2(add[2 * i], add[2 * i + 1]));
+                        } else if (h.weight) {
+                            norm_params<E>(h.weight, wat + o, h.bf16, w);
+#pragma unroll
+                            for (int i = 0; i < E / 2; ++i) y[i] = mul_f32x2(y[i], pack_f32x2(w[2 * i], w[2 * i + 1]));
+                        } else if (h.bias) {
+                            norm_params<E>(h.bias, wat + o, h.bf16, w);
+#pragma unroll
+                            for (int i = 0; i < E / 2; ++i) y[i] = add_f32x2(y[i], pack_f32x2(w[2 * i], w[2 * i + 1]));
+                        }
                     }
                 }
             }
-            if (a.pos && valid && which < 2) {
-                const float* cosv = cs + tok[b] * D + c * E;
-                const float* sinv = cosv + HP;
+            if (turn) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) {  // pair i of the thread: (2 i, 2 i + 1) where pairs interleave, else (i, E + i)
-                    float& p = INTER ? x[2 * i] : x[i];
-                    float& q = INTER ? x[2 * i + 1] : x[E + i];
-                    const float2 u = turn_pair(p, q, cosv[i], sinv[i]);
-                    p = u.x;
-                    q = u.y;
+                for (int b = 0; b < B; ++b) {
+                    if (tok[b] < 0) continue;
+                    const float* cosv = cs + tok[b] * CS + c * E;
+#pragma unroll
+                    for (int i = 0; i < E / 2; i += 2) {
+                        const float4 co = *reinterpret_cast<const float4*>(cosv + 2 * i), si = *reinterpret_cast<const float4*>(cosv + HP + 2 * i);
+                        if (INTER) {  // pairs 2 i .. 2 i + 3 of the thread
+                            const float cc[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float p, q;
+                                unpack_f32x2(x[b][2 * i + j], p, q);
+                                x[b][2 * i + j] = pack_f32x2(fmaf(p, cc[j], -(q * sn[j])), fmaf(q, cc[j], p * sn[j]));
+                            }
+                        } else {
+                            const float4 ns = *reinterpret_cast<const float4*>(cosv + D + 2 * i);
+                            auto turn2 = [](uint64_t& p, uint64_t& q, uint64_t co, uint64_t si, uint64_t ns) {
+                                const uint64_t u = fma_f32x2(p, co, mul_f32x2(q, ns));
+                                q = fma_f32x2(q, co, mul_f32x2(p, si));
+                                p = u;
+                            };
+                            turn2(x[b][i], x[b][E / 2 + i], pack_f32x2(co.x, co.y), pack_f32x2(si.x, si.y), pack_f32x2(ns.x, ns.y));
+                            turn2(x[b][i + 1], x[b][E / 2 + i + 1], pack_f32x2(co.z, co.w), pack_f32x2(si.z, si.w), pack_f32x2(ns.z, ns.w));
+                        }
+                    }
                 }
             }
-            int byte = 0;
-            if (DEST == 2) {
-                unsigned largest = 0;
+            int byte[B];
+            if (DEST == 2 && which > 0) {
+                float largest[B];
 #pragma unroll
-                for (int i = 0; i < 2 * E; ++i) largest = max(largest, __float_as_uint(x[i]) & 0x7fffffffu);
+                for (int b = 0; b < B; ++b) {
+                    largest[b] = 0.f;
 #pragma unroll
-                for (int o = 1; o < IPR; o <<= 1) largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-                byte = q8_byte(largest);
-            }
-            if (!valid || (DEST && (which > 0 ? slot_of[tok[b]] : seq_of[tok[b]]) < 0)) continue;
-            if (DEST && which > 0) {
-                const int slot = slot_of[tok[b]], in_page = slot & (a.kv.page_tokens - 1);
-                const int page = a.kv.table[seq_of[tok[b]] * a.kv.table_seq_stride + head * a.kv.table_head_stride + (slot >> a.kv.page_shift)];
-                if (page < 0 || page >= a.kv.n_pages) {
-                    if (c == 0) paged_report(a.kv, kStPage);
-                    continue;
+                    for (int i = 0; i < E; ++i) {
+                        float p, q;
+                        unpack_f32x2(x[b][i], p, q);
+                        largest[b] = max_nan(max_nan(largest[b], fabsf(p)), fabsf(q));
+                    }
                 }
-                const long long at = page * a.kv.page_stride + in_page * a.kv.row_stride + head * a.kv.head_stride;
-                char* pool = which == 1 ? a.kv.k_pool : a.kv.v_pool;
-                if (DEST == 2) {
+#pragma unroll
+                for (int o = 1; o < IPR; o <<= 1)
+#pragma unroll
+                    for (int b = 0; b < B; ++b) largest[b] = max_nan(largest[b], __shfl_xor_sync(0xffffffffu, largest[b], o));
+#pragma unroll
+                for (int b = 0; b < B; ++b) byte[b] = q8_byte(__float_as_uint(largest[b]));
+            }
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                if (tok[b] < 0 || at[b] < 0) continue;
+                float y[2 * E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) unpack_f32x2(x[b][i], y[2 * i], y[2 * i + 1]);
+                if (DEST == 2 && which > 0) {
                     unsigned codes[E / 2];
 #pragma unroll
-                    for (int i = 0; i < E / 2; ++i) codes[i] = q8_codes4(x + 4 * i, byte);
-                    char* p = pool + at;
+                    for (int i = 0; i < E / 2; ++i) codes[i] = q8_codes4(y + 4 * i, byte[b]);
+                    char* p = pool + at[b];
                     if (INTER && E == 8) {
                         *reinterpret_cast<uint4*>(p + o_lo) = make_uint4(codes[0], codes[1], codes[E / 2 - 2], codes[E / 2 - 1]);
                     } else if (INTER) {
@@ -230,31 +339,27 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
                         *reinterpret_cast<unsigned*>(p + o_lo) = codes[0];
                         *reinterpret_cast<unsigned*>(p + o_hi) = codes[E / 2 - 1];
                     }
-                    if (c == 0) (which == 1 ? na.q8.k_scale : na.q8.v_scale)[page * na.q8.page_stride + head * na.q8.head_stride + in_page] = (unsigned char)byte;
+                    if (c == 0) {
+                        (which == 1 ? na.q8.k_scale : na.q8.v_scale)[scale_at[b]] = (unsigned char)byte[b];
+                    }
                     continue;
+                }
+                T* dst;
+                if (DEST == 1 && which > 0) {
+                    dst = reinterpret_cast<T*>(pool) + at[b];
+                } else {
+                    const RowsView& to = a.dst[which];
+                    dst = reinterpret_cast<T*>(to.p) + (t0 + tok[b]) * to.token_stride + head[b] * to.head_stride;
                 }
                 float u[E], v[E];
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    u[i] = x[i];
-                    v[i] = x[E + i];
+                    u[i] = y[i];
+                    v[i] = y[E + i];
                 }
-                T* dst = reinterpret_cast<T*>(pool) + at;
-                // (values are copied as they are: a pass through fp32 could touch the bits of a NaN)
-                *reinterpret_cast<uint4*>(dst + o_lo) = which == 2 ? lo[b] : PackRow<T>::pack(u);
-                *reinterpret_cast<uint4*>(dst + o_hi) = which == 2 ? hi[b] : PackRow<T>::pack(v);
-                continue;
+                *reinterpret_cast<uint4*>(dst + o_lo) = PackRow<T>::pack(u);
+                *reinterpret_cast<uint4*>(dst + o_hi) = PackRow<T>::pack(v);
             }
-            float u[E], v[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                u[i] = x[i];
-                v[i] = x[E + i];
-            }
-            const RowsView& d = a.dst[which];
-            T* dst = reinterpret_cast<T*>(d.p) + (long long)(t0 + tok[b]) * d.token_stride + head * d.head_stride;
-            *reinterpret_cast<uint4*>(dst + o_lo) = PackRow<T>::pack(u);
-            *reinterpret_cast<uint4*>(dst + o_hi) = PackRow<T>::pack(v);
         }
     }
     if (DEST == 1 && a.state) {

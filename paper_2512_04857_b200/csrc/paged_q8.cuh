@@ -35,9 +35,10 @@ __device__ __forceinline__ unsigned q8_codes4(const float* x, int byte) {
     float y[4];
     const float f = q8_inverse(byte);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        y[i] = byte == kQ8NaN ? 0.f : x[i] * f;
-        if (byte == kQ8MaxByte) y[i] = fminf(fmaxf(y[i], -240.f), 240.f);  // (256 * 2^120 is beyond fp32)
+    for (int i = 0; i < 4; ++i) y[i] = x[i] * f;
+    if (byte >= kQ8MaxByte) {  // 256 * 2^120 is beyond fp32; a row that is not finite has codes of zero
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = byte == kQ8NaN ? 0.f : fminf(fmaxf(y[i], -240.f), 240.f);
     }
     const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
     const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(y[2], y[3]), __NV_SATFINITE, __NV_E4M3);
