@@ -41,18 +41,17 @@ NormFn norm_fn(int dtype, int d, bool inter) {
 }
 
 lar_status_t launch_norm(NormRopeArgs& a, NormFn fn, int d, cudaStream_t s) {
-    // Small batches (below 16 * kSms) as in rope_grid, a token per CTA with its rows dealt to enough CTAs that every SM has some; large ones up to eight tokens per CTA,
-    // so that the rows of a kind fill the threads' batches.
+    // Small batches as in rope_grid, a token per CTA with its rows dealt to enough CTAs that every SM has some; large ones up to eight tokens per CTA,
+    // so that a thread's token serves it for several rows.
     dim3 grid = rope_grid(a.r);
-    int64_t tokens = a.r.n_tokens / (8 * kSms);
-    tokens = tokens > 8 ? 8 : tokens;
-    if (tokens > 1) {
-        a.r.tokens_per_cta = (int)tokens;
+    a.shift = 0;
+    while (a.shift < 3 && a.r.n_tokens >= (16 << a.shift) * kSms) ++a.shift;
+    if (a.shift > 0) {
+        a.r.tokens_per_cta = 1 << a.shift;
         a.r.rows_per_slice = a.r.n_rows;
-        grid = dim3((unsigned)((a.r.n_tokens + tokens - 1) / tokens), 1);
-        for (int i = 0; i < 3; ++i) a.magic[i] = a.r.heads[i] > 1 ? (unsigned)((1ull << 32) / (unsigned)a.r.heads[i] + 1ull) : 0u;
+        grid = dim3((unsigned)((a.r.n_tokens + a.r.tokens_per_cta - 1) >> a.shift), 1);
     }
-    fn<<<grid, kRopeThreads, (size_t)a.r.tokens_per_cta * (d + d / 2 + 2) * 4, s>>>(a);
+    fn<<<grid, kRopeThreads, 0, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     return LAR_OK;
 }

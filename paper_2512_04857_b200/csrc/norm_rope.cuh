@@ -43,8 +43,10 @@ struct NormRopeArgs {
     RopeRowsArgs r;
     HeadNormView norm[2];  // of q, of k
     Q8View q8;             // DEST 2 only
-    unsigned magic[3];     // floor(2^32 / heads) + 1 of each kind of row (0: one head), where a CTA has several tokens; else 0
+    int shift;             // log2 of the tokens of a CTA
 };
+
+constexpr int kNormTokens = 8;  // tokens of a CTA at most
 
 // E parameters of a norm as fp32 (16 or 8 bytes)
 template <int E>
@@ -70,99 +72,122 @@ __device__ __forceinline__ void norm_params(const char* p, long long at, int bf1
 
 // DEST: 0 rows, 1 pages of the rows' type, 2 pages of 8 bits
 template <typename T, int D, bool INTER, int DEST>
-__global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_constant__ NormRopeArgs na) {
+__global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const __grid_constant__ NormRopeArgs na) {
     constexpr int E = Elt<T>::kPerChunk;  // elements of a 16-byte chunk
     constexpr int IPR = D / (2 * E);      // threads of a row
     constexpr int HP = D / 2;
     constexpr int B = 16 / E;             // items (32 bytes each) that a thread has at a time: 32 registers once unpacked
-    constexpr int CS = D + HP;            // per token: cosines, sines, sines negated
+    constexpr int GROUPS = kRopeThreads / IPR;  // rows that the CTA has at a time, once
     const RopeRowsArgs& a = na.r;
-    extern __shared__ __align__(16) float cs[];  // [tokens_per_cta][CS], then the tokens' slots and sequences
-    int* slot_of = reinterpret_cast<int*>(cs + a.tokens_per_cta * CS);
-    int* seq_of = slot_of + a.tokens_per_cta;
+    __shared__ __align__(16) float cs[kNormTokens][D];  // cosines, sines
+    __shared__ int slot_of[kNormTokens], seq_of[kNormTokens];
 
     const int tid = threadIdx.x;
-    const int t0 = blockIdx.x * a.tokens_per_cta;
+    const int t0 = blockIdx.x * a.tokens_per_cta;  // (a power of two of tokens: 1 << na.shift)
     const int nt = min(a.tokens_per_cta, a.n_tokens - t0);
     const int row0 = blockIdx.y * a.rows_per_slice, row1 = min(row0 + a.rows_per_slice, a.n_rows);
     const int c = tid & (IPR - 1);
     const int o_lo = INTER ? 2 * c * E : c * E, o_hi = INTER ? (2 * c + 1) * E : HP + c * E;
+    // a thread stays with its token and goes through heads
+    const int tl = (tid / IPR) & (a.tokens_per_cta - 1), step = GROUPS >> na.shift, own = (tid / IPR) >> na.shift;
+    const bool live = tl < nt;
+    const long long t = t0 + tl;
+    int slot = -1, seq = -1;
 
-    bool ready = false;
     // q, k and v rows one kind behind the other: what depends on the kind is the same for all threads
-    int first = 0;  // first row of the kind
+    auto heads_of = [&](int which, int& h0, int& h1) {  // heads h0 .. h1 - 1 of this CTA
+        const int first = which > 1 ? a.heads[0] + a.heads[1] : which > 0 ? a.heads[0] : 0;
+        h0 = max(row0 - first, 0);
+        h1 = min(row1 - first, a.heads[which]);
+    };
+    auto fetch = [&](int which, int g, int h1, uint4 (&lo)[B], uint4 (&hi)[B]) {
+        const T* from = reinterpret_cast<const T*>(a.src[which].p) + t * a.src[which].token_stride;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int head = g + b * step + own;
+            lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
+            if (live && head < h1) {
+                const T* p = from + head * a.src[which].head_stride;
+                lo[b] = *reinterpret_cast<const uint4*>(p + o_lo);
+                hi[b] = *reinterpret_cast<const uint4*>(p + o_hi);
+            }
+        }
+    };
+    int which = 0, h0, h1;
+    for (heads_of(which, h0, h1); h1 <= h0 && which < 2; heads_of(++which, h0, h1)) {}
+    uint4 next_lo[B], next_hi[B];
+    fetch(which, h0, h1, next_lo, next_hi);
+    // sines, cosines and slots of the CTA's tokens, while the first rows are on the way
+    if (a.pos) {
+        const int i = tid & (HP - 1);
+        const double f = a.f.turns[i];
+        const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
+        for (int l = tid / HP; l < nt; l += kRopeThreads / HP) {
+            const float2 v = cos_sin_of(f, p[l]);
+            cs[l][i] = v.x;
+            cs[l][HP + i] = v.y;
+        }
+    }
+    if (DEST) find_slots<kRopeThreads>(a.kv, a.state ? a.base_len : -1, t0, nt, slot_of, seq_of);
+    __syncthreads();
+    if (DEST && live) {
+        slot = slot_of[tl];
+        seq = seq_of[tl];
+    }
+    int g0 = h0;
 #pragma unroll 1
-    for (int which = 0; which < 3; ++which) {
-        const int h0 = max(row0 - first, 0), m = min(row1 - first, a.heads[which]) - h0;  // heads h0 .. h0 + m - 1 of this CTA
-        first += a.heads[which];
-        if (m <= 0) continue;
-        const int n_items = nt * m * IPR;
+    while (which < 3) {
         const HeadNormView& h = na.norm[which & 1];
         const bool on = which < 2 && h.on, layer = on && h.layer, turn = which < 2 && a.pos;
-        const unsigned magic = na.magic[which];  // of m, where a CTA has several tokens
-        const RowsView& from = a.src[which];
         char* pool = which == 1 ? a.kv.k_pool : a.kv.v_pool;
-#pragma unroll 1
-        for (int base = 0; base < n_items; base += kRopeThreads * B) {
+        {
             uint4 lo[B], hi[B];
-            int tok[B], head[B];
+            int head[B];
+            bool has[B];
             long long at[B], scale_at[B];  // element of the pool (-1: the row is not written), its scale byte
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                const int item = base + b * kRopeThreads + tid, r = item / IPR;
-                const int tl = magic ? (int)__umulhi((unsigned)r, magic) : a.tokens_per_cta > 1 ? r : 0;
-                tok[b] = item < n_items ? tl : -1;
-                head[b] = h0 + r - tl * m;
-                lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
-                if (tok[b] >= 0) {
-                    const T* p = reinterpret_cast<const T*>(from.p) + (t0 + tl) * from.token_stride + head[b] * from.head_stride;
-                    lo[b] = *reinterpret_cast<const uint4*>(p + o_lo);
-                    hi[b] = *reinterpret_cast<const uint4*>(p + o_hi);
-                }
+                head[b] = g0 + b * step + own;
+                has[b] = live && head[b] < h1;
+                lo[b] = next_lo[b];
+                hi[b] = next_hi[b];
             }
-            if (!ready) {  // sines, cosines and slots of the CTA's tokens, while the first rows are on the way
-                ready = true;
-                if (a.pos) {
-                    const int i = tid & (HP - 1);
-                    const double f = a.f.turns[i];
-                    const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
-                    for (int tl = tid / HP; tl < nt; tl += kRopeThreads / HP) {
-                        const float2 v = cos_sin_of(f, p[tl]);
-                        cs[tl * CS + i] = v.x;
-                        cs[tl * CS + HP + i] = v.y;
-                        cs[tl * CS + D + i] = -v.y;
-                    }
-                }
-                if (DEST) find_slots<kRopeThreads>(a.kv, a.state ? a.base_len : -1, t0, nt, slot_of, seq_of);
-                __syncthreads();
+            // the next rows are on the way while these are worked on
+            int nwhich = which, ng = g0 + step * B, nh1 = h1;
+            if (ng >= h1) {
+                nh1 = ng = 0;
+                while (nh1 <= ng && ++nwhich < 3) heads_of(nwhich, ng, nh1);
             }
+            if (nwhich < 3) fetch(nwhich, ng, nh1, next_lo, next_hi);
 #pragma unroll
             for (int b = 0; b < B; ++b) {
                 at[b] = scale_at[b] = 0;
-                if (DEST && tok[b] >= 0) {
-                    const int slot = slot_of[tok[b]], seq = seq_of[tok[b]];
-                    if (which == 0) {
-                        if (seq < 0) at[b] = -1;
-                    } else if (slot < 0) {
+                if (!DEST || !has[b]) continue;
+                if (which == 0) {
+                    if (seq < 0) at[b] = -1;
+                } else if (slot < 0) {
+                    at[b] = -1;
+                } else {
+                    const int page = a.kv.table[seq * a.kv.table_seq_stride + head[b] * a.kv.table_head_stride + (slot >> a.kv.page_shift)];
+                    const int in_page = slot & (a.kv.page_tokens - 1);
+                    at[b] = page * a.kv.page_stride + in_page * a.kv.row_stride + head[b] * a.kv.head_stride;
+                    if (DEST == 2) scale_at[b] = page * na.q8.page_stride + head[b] * na.q8.head_stride + in_page;
+                    if (page < 0 || page >= a.kv.n_pages) {
                         at[b] = -1;
-                    } else {
-                        const int page = a.kv.table[seq * a.kv.table_seq_stride + head[b] * a.kv.table_head_stride + (slot >> a.kv.page_shift)];
-                        at[b] = page * a.kv.page_stride + (slot & (a.kv.page_tokens - 1)) * a.kv.row_stride + head[b] * a.kv.head_stride;
-                        if (page < 0 || page >= a.kv.n_pages) {
-                            at[b] = -1;
-                            if (c == 0) paged_report(a.kv, kStPage);
-                        }
-                        if (DEST == 2) scale_at[b] = page * na.q8.page_stride + head[b] * na.q8.head_stride + (slot & (a.kv.page_tokens - 1));
+                        if (c == 0) paged_report(a.kv, kStPage);
                     }
                 }
             }
             if (DEST == 1 && which == 2) {  // values as they are: a pass through fp32 could touch the bits of a NaN
 #pragma unroll
                 for (int b = 0; b < B; ++b)
-                    if (tok[b] >= 0 && at[b] >= 0) {
+                    if (has[b] && at[b] >= 0) {
                         *reinterpret_cast<uint4*>(reinterpret_cast<T*>(pool) + at[b] + o_lo) = lo[b];
                         *reinterpret_cast<uint4*>(reinterpret_cast<T*>(pool) + at[b] + o_hi) = hi[b];
                     }
+                which = nwhich;
+                g0 = ng;
+                h1 = nh1;
                 continue;
             }
             uint64_t x[B][E];  // two elements each: the low chunk, then the high one
@@ -221,7 +246,8 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
                     beyond |= !(ss[b] <= 3.4e38f);
                 }
                 if (__any_sync(0xffffffffu, beyond)) {
-                    // squares (or the sum) beyond fp32: once more from the rows times 2^-80, beside which eps is nothing
+                    // squares (or the sum) beyond fp32: once more from the rows (not written yet) times 2^-80, beside which eps is nothing
+                    fetch(which, g0, h1, lo, hi);
 #pragma unroll
                     for (int b = 0; b < B; ++b) {
                         if (!(ss[b] <= 3.4e38f)) up[b] = 0x1p-80f;
@@ -239,7 +265,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
                 }
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
-                    if (tok[b] < 0) continue;
+                    if (!has[b]) continue;
                     const float f = rsqrtf(fmaf(ss[b], 1.0f / D, h.eps * up[b] * up[b]));
                     const uint64_t f2 = pack_f32x2(f, f);
                     const long long wat = head[b] * h.head_stride;
@@ -269,32 +295,38 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
                 }
             }
             if (turn) {
+                const uint64_t minus = pack_f32x2(-1.f, -1.f);
 #pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    if (tok[b] < 0) continue;
-                    const float* cosv = cs + tok[b] * CS + c * E;
+                for (int i = 0; i < E / 2; i += 2) {
+                    const float4 u = *reinterpret_cast<const float4*>(&cs[tl][c * E + 2 * i]), v = *reinterpret_cast<const float4*>(&cs[tl][HP + c * E + 2 * i]);
+                    const uint64_t co[2] = {pack_f32x2(u.x, u.y), pack_f32x2(u.z, u.w)}, si[2] = {pack_f32x2(v.x, v.y), pack_f32x2(v.z, v.w)};
 #pragma unroll
-                    for (int i = 0; i < E / 2; i += 2) {
-                        const float4 co = *reinterpret_cast<const float4*>(cosv + 2 * i), si = *reinterpret_cast<const float4*>(cosv + HP + 2 * i);
-                        if (INTER) {  // pairs 2 i .. 2 i + 3 of the thread
-                            const float cc[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                float p, q;
-                                unpack_f32x2(x[b][2 * i + j], p, q);
-                                x[b][2 * i + j] = pack_f32x2(fmaf(p, cc[j], -(q * sn[j])), fmaf(q, cc[j], p * sn[j]));
+                        for (int b = 0; b < B; ++b) {
+                            // two pairs: side by side in the operands where pairs interleave, in the same place of both halves else
+                            uint64_t& y0 = x[b][INTER ? 2 * (i + j) : i + j];
+                            uint64_t& y1 = x[b][INTER ? 2 * (i + j) + 1 : E / 2 + i + j];
+                            uint64_t p = y0, q = y1;
+                            if (INTER) {
+                                float p0, q0, p1, q1;
+                                unpack_f32x2(y0, p0, q0);
+                                unpack_f32x2(y1, p1, q1);
+                                p = pack_f32x2(p0, p1);
+                                q = pack_f32x2(q0, q1);
                             }
-                        } else {
-                            const float4 ns = *reinterpret_cast<const float4*>(cosv + D + 2 * i);
-                            auto turn2 = [](uint64_t& p, uint64_t& q, uint64_t co, uint64_t si, uint64_t ns) {
-                                const uint64_t u = fma_f32x2(p, co, mul_f32x2(q, ns));
-                                q = fma_f32x2(q, co, mul_f32x2(p, si));
-                                p = u;
-                            };
-                            turn2(x[b][i], x[b][E / 2 + i], pack_f32x2(co.x, co.y), pack_f32x2(si.x, si.y), pack_f32x2(ns.x, ns.y));
-                            turn2(x[b][i + 1], x[b][E / 2 + i + 1], pack_f32x2(co.z, co.w), pack_f32x2(si.z, si.w), pack_f32x2(ns.z, ns.w));
+                            const uint64_t x2 = fma_f32x2(mul_f32x2(q, si[j]), minus, mul_f32x2(p, co[j])), z2 = fma_f32x2(q, co[j], mul_f32x2(p, si[j]));
+                            if (INTER) {
+                                float p0, q0, p1, q1;
+                                unpack_f32x2(x2, p0, p1);
+                                unpack_f32x2(z2, q0, q1);
+                                y0 = pack_f32x2(p0, q0);
+                                y1 = pack_f32x2(p1, q1);
+                            } else {
+                                y0 = x2;
+                                y1 = z2;
+                            }
                         }
-                    }
                 }
             }
             int byte[B];
@@ -319,7 +351,7 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
             }
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                if (tok[b] < 0 || at[b] < 0) continue;
+                if (!has[b] || at[b] < 0) continue;
                 float y[2 * E];
 #pragma unroll
                 for (int i = 0; i < E; ++i) unpack_f32x2(x[b][i], y[2 * i], y[2 * i + 1]);
@@ -344,13 +376,8 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
                     }
                     continue;
                 }
-                T* dst;
-                if (DEST == 1 && which > 0) {
-                    dst = reinterpret_cast<T*>(pool) + at[b];
-                } else {
-                    const RowsView& to = a.dst[which];
-                    dst = reinterpret_cast<T*>(to.p) + (t0 + tok[b]) * to.token_stride + head[b] * to.head_stride;
-                }
+                T* dst = DEST == 1 && which > 0 ? reinterpret_cast<T*>(pool) + at[b]
+                                                : reinterpret_cast<T*>(a.dst[which].p) + t * a.dst[which].token_stride + head[b] * a.dst[which].head_stride;
                 float u[E], v[E];
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
@@ -360,6 +387,9 @@ __global__ void __launch_bounds__(kRopeThreads) norm_rope_kernel(const __grid_co
                 *reinterpret_cast<uint4*>(dst + o_lo) = PackRow<T>::pack(u);
                 *reinterpret_cast<uint4*>(dst + o_hi) = PackRow<T>::pack(v);
             }
+            which = nwhich;
+            g0 = ng;
+            h1 = nh1;
         }
     }
     if (DEST == 1 && a.state) {
