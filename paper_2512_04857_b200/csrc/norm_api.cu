@@ -40,18 +40,42 @@ NormFn norm_fn(int dtype, int d, bool inter) {
     return d == 64 ? norm_fn_pairs<float, 64, DEST>(inter) : norm_fn_pairs<float, 128, DEST>(inter);
 }
 
-lar_status_t launch_norm(NormRopeArgs& a, NormFn fn, int d, cudaStream_t s) {
-    // Small batches as in rope_grid, a token per CTA with its rows dealt to enough CTAs that every SM has some; large ones up to eight tokens per CTA,
-    // so that a thread's token serves it for several rows.
-    dim3 grid = rope_grid(a.r);
-    a.shift = 0;
-    while (a.shift < 3 && a.r.n_tokens >= (16 << a.shift) * kSms) ++a.shift;
-    if (a.shift > 0) {
-        a.r.tokens_per_cta = 1 << a.shift;
-        a.r.rows_per_slice = a.r.n_rows;
-        grid = dim3((unsigned)((a.r.n_tokens + a.r.tokens_per_cta - 1) >> a.shift), 1);
+lar_status_t launch_norm(NormRopeArgs& a, NormFn fn, int d, int elt, cudaStream_t s) {
+    const int ipr = d * elt / 32;  // threads of a row
+    // The number of threads that leaves fewest of them without a row.  A kind whose heads a CTA holds several times over has as many tokens in a pass; one
+    // with more heads takes several CTAs.
+    int threads = 0, best_rows = 0;
+    double best = 0.0;
+    for (int n = kNormThreads; n >= 128; n -= 32) {
+        const int rows = n / ipr;
+        double used = 0.0, all = 0.0;
+        for (int i = 0; i < 3; ++i) {
+            const int heads = a.r.heads[i];
+            if (heads == 0) continue;
+            const int slices = (heads + rows - 1) / rows, per = (heads + slices - 1) / slices;
+            used += heads;
+            all += (double)slices * rows / (rows / per);
+        }
+        if (used / all > best + 1e-9) {
+            best = used / all;
+            threads = n;
+            best_rows = rows;
+        }
     }
-    fn<<<grid, kRopeThreads, 0, s>>>(a);
+    int slices = 0;
+    for (int i = 0; i < 3; ++i) {
+        const int heads = a.r.heads[i];
+        if (heads == 0) continue;
+        a.slices[i] = (heads + best_rows - 1) / best_rows;
+        a.heads[i] = (heads + a.slices[i] - 1) / a.slices[i];
+        a.at_once[i] = best_rows / a.heads[i];
+        slices += a.slices[i];
+    }
+    // Tokens of a CTA: what it sets up serves all of them, but there should be some rounds of CTAs.
+    int64_t tokens = (int64_t)a.r.n_tokens * slices / (8 * kSms);
+    tokens = tokens < 1 ? 1 : tokens > kNormTokens ? kNormTokens : tokens;
+    a.tokens = (int)tokens;
+    fn<<<dim3((unsigned)((a.r.n_tokens + tokens - 1) / tokens), (unsigned)slices), threads, 0, s>>>(a);
     LAR_CUDA(cudaGetLastError());
     return LAR_OK;
 }
@@ -116,7 +140,7 @@ lar_status_t paged_append_norm(const lar_paged_kv_t& kv, const lar_head_norm_t* 
         a.r.state = own->state;
         a.r.cap_pad = own->cap_pad;
     }
-    return launch_norm(a, norm_fn<1>(kv.dtype, kv.head_dim, rope && rope->interleaved), kv.head_dim, (cudaStream_t)stream);
+    return launch_norm(a, norm_fn<1>(kv.dtype, kv.head_dim, rope && rope->interleaved), kv.head_dim, elt_of(kv.dtype), (cudaStream_t)stream);
 }
 
 }  // namespace lar
@@ -146,7 +170,7 @@ lar_status_t lar_norm_rope_rotate(const lar_head_norm_t* q_norm, const lar_head_
     a.r.heads[0] = n_q_heads;
     a.r.heads[1] = n_kv_heads;
     a.r.n_tokens = (int)n_tokens;
-    return launch_norm(a, norm_fn<0>(dtype, head_dim, rope && rope->interleaved), head_dim, (cudaStream_t)stream);
+    return launch_norm(a, norm_fn<0>(dtype, head_dim, rope && rope->interleaved), head_dim, elt, (cudaStream_t)stream);
 }
 
 lar_status_t lar_paged_append_norm_rope(const lar_paged_kv_t* kv, const lar_head_norm_t* q_norm, const lar_head_norm_t* k_norm, const lar_rope_t* rope,
@@ -168,7 +192,7 @@ lar_status_t lar_paged_q8_append(const lar_paged_q8_t* cache, int rows_dtype, co
     if (!append_args(a, rows_dtype, cache->kv.n_kv_heads, d, q_norm, k_norm, rope, pos, pos_axis_stride, k, v, q, q_out, n_q_heads, n_tokens))
         return LAR_ERR_INVALID_ARG;
     if (n_tokens == 0) return LAR_OK;
-    return launch_norm(a, norm_fn<2>(rows_dtype, d, rope && rope->interleaved), d, (cudaStream_t)stream);
+    return launch_norm(a, norm_fn<2>(rows_dtype, d, rope && rope->interleaved), d, elt_of(rows_dtype), (cudaStream_t)stream);
 }
 
 lar_status_t lar_paged_q8_read(const lar_paged_q8_t* cache, int rows_dtype, const lar_rows_t* k_out, const lar_rows_t* v_out, int64_t n_rows,

@@ -4,10 +4,12 @@
 //   rms:    y = x / sqrt(mean(x^2) + eps) * w  (+ bias)        layer:  y = (x - mean(x)) / sqrt(mean((x - mean)^2) + eps) * w  (+ bias)
 //   then the pairs of y are turned as in rope_rows.cuh, and the result is rounded once, to the storage type or to 8 bits.
 //
-// Bound: HBM bytes (each row once in, once out; about ten operations per element).  The work is dealt out as in rope_rows.cuh: a CTA has
-// one or two tokens, a thread 16 bytes of each half of a row (or 32 bytes side by side where pairs interleave).  The D / 16 (bf16) or D / 8
-// (fp32) threads of a row are neighbours in a warp, so that the row's sums are three or four shuffles, taken with the row in registers: the
-// mean first and the squares of what is left after it, not the difference of two large sums.  Weights come through L1.
+// Bound: HBM bytes (each row once in, once out), as long as an element costs few instructions.  So a CTA has rows of one kind (q, k or v: what depends on the
+// kind is the same for all its threads) and a thread stays with one head, of which it has 16 bytes of each half of a row (or 32 bytes side by side
+// where pairs interleave), and goes through tokens: weights, biases and pointers are in registers from the start, and the CTA's sines, cosines and
+// slots in shared memory behind one barrier.  The D / 16 (bf16) or D / 8 (fp32) threads of a row are neighbours in a warp: the row's sums are
+// a few shuffles, taken with the row in registers, the mean first and the squares of what is left after it, not the difference of two large sums.  fp32
+// arithmetic goes two elements to an instruction.  While a token is worked on the next two are on the way.
 #pragma once
 #include "paged_attn.cuh"  // two fp32 operations in one instruction
 #include "paged_q8.cuh"
@@ -43,10 +45,14 @@ struct NormRopeArgs {
     RopeRowsArgs r;
     HeadNormView norm[2];  // of q, of k
     Q8View q8;             // DEST 2 only
-    int shift;             // log2 of the tokens of a CTA
+    int at_once[3];        // tokens of a pass of a CTA, of each kind of row
+    int slices[3];         // CTAs that the heads of a kind take
+    int heads[3];          // heads of a CTA
+    int tokens;            // of a CTA
 };
 
-constexpr int kNormTokens = 8;  // tokens of a CTA at most
+constexpr int kNormThreads = 256;  // of a CTA at most
+constexpr int kNormTokens = 32;
 
 // E parameters of a norm as fp32 (16 or 8 bytes)
 template <int E>
@@ -70,296 +76,233 @@ __device__ __forceinline__ void norm_params(const char* p, long long at, int bf1
     }
 }
 
+// Slot and sequence of token t, by a warp, as find_slots: the number of sequences that end at or before it.
+__device__ __forceinline__ void find_slot(const PagedView& kv, int base_len, int t, int* slot_of, int* seq_of) {
+    const int lane = threadIdx.x & 31;
+    int s = 0;
+    if (kv.cu) {
+        for (int j = lane; j < kv.n_seqs; j += 32) s += kv.cu[j + 1] <= t;
+        s = __reduce_add_sync(0xffffffffu, s);
+    } else {
+        s = t / kv.chunk;
+    }
+    if (lane == 0) {
+        int slot = -1, b0 = 0, b1 = 0;
+        if (s < kv.n_seqs) chunk_of(kv, s, b0, b1);
+        if (t < b0 || t >= b1) {
+            s = -1;
+        } else {
+            slot = base_len >= 0 ? base_len + (t - b0) : kv.lens[s * kv.lens_stride] - (b1 - t);
+            if (slot < 0 || slot >= (kv.table_cols << kv.page_shift)) {
+                paged_report(kv, kStPage);
+                slot = -1;
+            }
+        }
+        *slot_of = slot;
+        *seq_of = s;
+    }
+}
+
 // DEST: 0 rows, 1 pages of the rows' type, 2 pages of 8 bits
 template <typename T, int D, bool INTER, int DEST>
-__global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const __grid_constant__ NormRopeArgs na) {
-    constexpr int E = Elt<T>::kPerChunk;  // elements of a 16-byte chunk
-    constexpr int IPR = D / (2 * E);      // threads of a row
-    constexpr int HP = D / 2;
-    constexpr int B = 16 / E;             // items (32 bytes each) that a thread has at a time: 32 registers once unpacked
-    constexpr int GROUPS = kRopeThreads / IPR;  // rows that the CTA has at a time, once
-    const RopeRowsArgs& a = na.r;
-    __shared__ __align__(16) float cs[kNormTokens][D];  // cosines, sines
-    __shared__ int slot_of[kNormTokens], seq_of[kNormTokens];
+struct NormRope {
+    static constexpr int E = Elt<T>::kPerChunk;  // elements of a 16-byte chunk
+    static constexpr int IPR = D / (2 * E);      // threads of a row
+    static constexpr int HP = D / 2;
 
-    const int tid = threadIdx.x;
-    const int t0 = blockIdx.x * a.tokens_per_cta;  // (a power of two of tokens: 1 << na.shift)
-    const int nt = min(a.tokens_per_cta, a.n_tokens - t0);
-    const int row0 = blockIdx.y * a.rows_per_slice, row1 = min(row0 + a.rows_per_slice, a.n_rows);
-    const int c = tid & (IPR - 1);
-    const int o_lo = INTER ? 2 * c * E : c * E, o_hi = INTER ? (2 * c + 1) * E : HP + c * E;
-    // a thread stays with its token and goes through heads
-    const int tl = (tid / IPR) & (a.tokens_per_cta - 1), step = GROUPS >> na.shift, own = (tid / IPR) >> na.shift;
-    const bool live = tl < nt;
-    const long long t = t0 + tl;
-    int slot = -1, seq = -1;
-
-    // q, k and v rows one kind behind the other: what depends on the kind is the same for all threads
-    auto heads_of = [&](int which, int& h0, int& h1) {  // heads h0 .. h1 - 1 of this CTA
-        const int first = which > 1 ? a.heads[0] + a.heads[1] : which > 0 ? a.heads[0] : 0;
-        h0 = max(row0 - first, 0);
-        h1 = min(row1 - first, a.heads[which]);
+    struct Shared {
+        float cs[kNormTokens][D];  // cosines, sines
+        int slot_of[kNormTokens], seq_of[kNormTokens];
     };
-    auto fetch = [&](int which, int g, int h1, uint4 (&lo)[B], uint4 (&hi)[B]) {
-        const T* from = reinterpret_cast<const T*>(a.src[which].p) + t * a.src[which].token_stride;
+
+    static __device__ __forceinline__ float row_sum(float v) {
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const int head = g + b * step + own;
-            lo[b] = hi[b] = make_uint4(0, 0, 0, 0);
-            if (live && head < h1) {
-                const T* p = from + head * a.src[which].head_stride;
-                lo[b] = *reinterpret_cast<const uint4*>(p + o_lo);
-                hi[b] = *reinterpret_cast<const uint4*>(p + o_hi);
-            }
-        }
-    };
-    int which = 0, h0, h1;
-    for (heads_of(which, h0, h1); h1 <= h0 && which < 2; heads_of(++which, h0, h1)) {}
-    uint4 next_lo[B], next_hi[B];
-    fetch(which, h0, h1, next_lo, next_hi);
-    // sines, cosines and slots of the CTA's tokens, while the first rows are on the way
-    if (a.pos) {
-        const int i = tid & (HP - 1);
-        const double f = a.f.turns[i];
-        const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
-        for (int l = tid / HP; l < nt; l += kRopeThreads / HP) {
-            const float2 v = cos_sin_of(f, p[l]);
-            cs[l][i] = v.x;
-            cs[l][HP + i] = v.y;
+        for (int o = 1; o < IPR; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    static __device__ __forceinline__ void unpack(const uint4& lo, const uint4& hi, float up, uint64_t (&x)[E]) {
+        float u[E], v[E];
+        Elt<T>::unpack(lo, u);
+        Elt<T>::unpack(hi, v);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            x[i] = pack_f32x2(u[2 * i] * up, u[2 * i + 1] * up);
+            x[E / 2 + i] = pack_f32x2(v[2 * i] * up, v[2 * i + 1] * up);
         }
     }
-    if (DEST) find_slots<kRopeThreads>(a.kv, a.state ? a.base_len : -1, t0, nt, slot_of, seq_of);
-    __syncthreads();
-    if (DEST && live) {
-        slot = slot_of[tl];
-        seq = seq_of[tl];
-    }
-    int g0 = h0;
-#pragma unroll 1
-    while (which < 3) {
-        const HeadNormView& h = na.norm[which & 1];
-        const bool on = which < 2 && h.on, layer = on && h.layer, turn = which < 2 && a.pos;
-        char* pool = which == 1 ? a.kv.k_pool : a.kv.v_pool;
-        {
-            uint4 lo[B], hi[B];
-            int head[B];
-            bool has[B];
-            long long at[B], scale_at[B];  // element of the pool (-1: the row is not written), its scale byte
-#pragma unroll
-            for (int b = 0; b < B; ++b) {
-                head[b] = g0 + b * step + own;
-                has[b] = live && head[b] < h1;
-                lo[b] = next_lo[b];
-                hi[b] = next_hi[b];
+
+    // The rows of one kind of the CTA's tokens.
+    template <int KIND>
+    static __device__ __forceinline__ void rows(const NormRopeArgs& na, Shared& sh, int slice) {
+        const RopeRowsArgs& a = na.r;
+        const HeadNormView& h = na.norm[KIND & 1];
+        const bool on = KIND < 2 && h.on, layer = on && h.layer, turn = KIND < 2 && a.pos;
+        const int tid = threadIdx.x, c = tid & (IPR - 1), group = tid / IPR;
+        const int sub = group / na.heads[KIND], head = slice * na.heads[KIND] + group - sub * na.heads[KIND];
+        const bool has = sub < na.at_once[KIND] && head < a.heads[KIND];
+        const int t0 = blockIdx.x * na.tokens, t1 = min(t0 + na.tokens, a.n_tokens), step = na.at_once[KIND];
+        const int o_lo = INTER ? 2 * c * E : c * E, o_hi = INTER ? (2 * c + 1) * E : HP + c * E;
+        int t = t0 + sub;
+        const T* from = reinterpret_cast<const T*>(a.src[KIND].p) + head * a.src[KIND].head_stride + t * a.src[KIND].token_stride;
+        const long long from_step = step * a.src[KIND].token_stride;
+        auto fetch = [&](int t, uint4& lo, uint4& hi) {
+            if (has && t < t1) {
+                lo = *reinterpret_cast<const uint4*>(from + o_lo);
+                hi = *reinterpret_cast<const uint4*>(from + o_hi);
             }
-            // the next rows are on the way while these are worked on
-            int nwhich = which, ng = g0 + step * B, nh1 = h1;
-            if (ng >= h1) {
-                nh1 = ng = 0;
-                while (nh1 <= ng && ++nwhich < 3) heads_of(nwhich, ng, nh1);
-            }
-            if (nwhich < 3) fetch(nwhich, ng, nh1, next_lo, next_hi);
+            from += from_step;
+        };
+        uint4 lo[2], hi[2];  // two tokens on the way
+        lo[0] = lo[1] = hi[0] = hi[1] = make_uint4(0, 0, 0, 0);
+        fetch(t, lo[0], hi[0]);
+        fetch(t + step, lo[1], hi[1]);
+        uint64_t w[E], add[E];  // two elements each: the low chunk, then the high one
+        if (on) {
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                at[b] = scale_at[b] = 0;
-                if (!DEST || !has[b]) continue;
-                if (which == 0) {
-                    if (seq < 0) at[b] = -1;
-                } else if (slot < 0) {
-                    at[b] = -1;
-                } else {
-                    const int page = a.kv.table[seq * a.kv.table_seq_stride + head[b] * a.kv.table_head_stride + (slot >> a.kv.page_shift)];
-                    const int in_page = slot & (a.kv.page_tokens - 1);
-                    at[b] = page * a.kv.page_stride + in_page * a.kv.row_stride + head[b] * a.kv.head_stride;
-                    if (DEST == 2) scale_at[b] = page * na.q8.page_stride + head[b] * na.q8.head_stride + in_page;
-                    if (page < 0 || page >= a.kv.n_pages) {
-                        at[b] = -1;
-                        if (c == 0) paged_report(a.kv, kStPage);
-                    }
-                }
-            }
-            if (DEST == 1 && which == 2) {  // values as they are: a pass through fp32 could touch the bits of a NaN
-#pragma unroll
-                for (int b = 0; b < B; ++b)
-                    if (has[b] && at[b] >= 0) {
-                        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(pool) + at[b] + o_lo) = lo[b];
-                        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(pool) + at[b] + o_hi) = hi[b];
-                    }
-                which = nwhich;
-                g0 = ng;
-                h1 = nh1;
-                continue;
-            }
-            uint64_t x[B][E];  // two elements each: the low chunk, then the high one
-#pragma unroll
-            for (int b = 0; b < B; ++b) {
+            for (int half = 0; half < 2; ++half) {
                 float u[E], v[E];
-                Elt<T>::unpack(lo[b], u);
-                Elt<T>::unpack(hi[b], v);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    u[i] = 1.f;
+                    v[i] = 0.f;
+                }
+                if (has) {
+                    const long long at = head * h.head_stride + (half ? o_hi : o_lo);
+                    if (h.weight) norm_params<E>(h.weight, at, h.bf16, u);
+                    if (h.bias) norm_params<E>(h.bias, at, h.bf16, v);
+                }
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) {
-                    x[b][i] = pack_f32x2(u[2 * i], u[2 * i + 1]);
-                    x[b][E / 2 + i] = pack_f32x2(v[2 * i], v[2 * i + 1]);
+                    w[half * (E / 2) + i] = pack_f32x2(u[2 * i], u[2 * i + 1]);
+                    add[half * (E / 2) + i] = pack_f32x2(v[2 * i], v[2 * i + 1]);
                 }
             }
+        }
+        // sines, cosines and slots of the CTA's tokens
+        if (turn) {
+            const int i = tid & (HP - 1);
+            const double f = a.f.turns[i];
+            const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
+            for (int l = tid / HP; l < t1 - t0; l += blockDim.x / HP) {
+                const float2 v = cos_sin_of(f, p[l]);
+                sh.cs[l][i] = v.x;
+                sh.cs[l][HP + i] = v.y;
+            }
+        }
+        if (DEST)
+            for (int l = tid >> 5; l < t1 - t0; l += blockDim.x >> 5)
+                find_slot(a.kv, a.state ? a.base_len : -1, t0 + l, &sh.slot_of[l], &sh.seq_of[l]);
+        __syncthreads();
+
+        const bool paged = DEST && KIND > 0;
+        T* to = nullptr;
+        long long to_step = 0;
+        if (!paged) {
+            to = reinterpret_cast<T*>(a.dst[KIND].p) + head * a.dst[KIND].head_stride + t * a.dst[KIND].token_stride;
+            to_step = step * a.dst[KIND].token_stride;
+        }
+        const int* table = a.kv.table + head * a.kv.table_head_stride;
+        char* pool = KIND == 1 ? a.kv.k_pool : a.kv.v_pool;
+        auto work = [&](const uint4& lo, const uint4& hi) {
+            uint64_t x[E];
+            unpack(lo, hi, 1.f, x);
             if (on) {
-                // The row sums, one step for all rows of the batch at a time.  (Warp-wide: lanes without a row have zeros.)
-                float mean[B], ss[B], up[B];
+                float ss, up = 1.f;
                 auto sums = [&]() {
+                    if (layer) {
+                        uint64_t y = x[0];
 #pragma unroll
-                    for (int b = 0; b < B; ++b) {
-                        uint64_t y = x[b][0];
+                        for (int i = 1; i < E; ++i) y = add_f32x2(y, x[i]);
+                        const float mean = row_sum(sum_of(y)) * (-1.0f / D);
+                        const uint64_t m2 = pack_f32x2(mean, mean);
 #pragma unroll
-                        for (int i = 1; i < E; ++i) y = add_f32x2(y, x[b][i]);
-                        mean[b] = sum_of(y);
+                        for (int i = 0; i < E; ++i) x[i] = add_f32x2(x[i], m2);
                     }
+                    uint64_t y = mul_f32x2(x[0], x[0]);
 #pragma unroll
-                    for (int o = 1; o < IPR; o <<= 1)
-#pragma unroll
-                        for (int b = 0; b < B; ++b) mean[b] += __shfl_xor_sync(0xffffffffu, mean[b], o);
-#pragma unroll
-                    for (int b = 0; b < B; ++b) {
-                        mean[b] *= -1.0f / D;
-#pragma unroll
-                        for (int i = 0; i < E; ++i) x[b][i] = add_f32x2(x[b][i], pack_f32x2(mean[b], mean[b]));
-                    }
+                    for (int i = 1; i < E; ++i) y = fma_f32x2(x[i], x[i], y);
+                    ss = row_sum(sum_of(y));
                 };
-                auto squares = [&]() {
-#pragma unroll
-                    for (int b = 0; b < B; ++b) {
-                        uint64_t y = mul_f32x2(x[b][0], x[b][0]);
-#pragma unroll
-                        for (int i = 1; i < E; ++i) y = fma_f32x2(x[b][i], x[b][i], y);
-                        ss[b] = sum_of(y);
-                    }
-#pragma unroll
-                    for (int o = 1; o < IPR; o <<= 1)
-#pragma unroll
-                        for (int b = 0; b < B; ++b) ss[b] += __shfl_xor_sync(0xffffffffu, ss[b], o);
-                };
-                if (layer) sums();
-                squares();
-                bool beyond = false;
-#pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    up[b] = 1.f;
-                    beyond |= !(ss[b] <= 3.4e38f);
+                sums();
+                if (__any_sync(0xffffffffu, !(ss <= 3.4e38f))) {
+                    // squares (or the sum) beyond fp32: once more from the row times 2^-80, beside which eps is nothing
+                    if (!(ss <= 3.4e38f)) up = 0x1p-80f;
+                    unpack(lo, hi, up, x);
+                    sums();
                 }
-                if (__any_sync(0xffffffffu, beyond)) {
-                    // squares (or the sum) beyond fp32: once more from the rows (not written yet) times 2^-80, beside which eps is nothing
-                    fetch(which, g0, h1, lo, hi);
+                const float f = rsqrtf(fmaf(ss, 1.0f / D, h.eps * up * up));
+                const uint64_t f2 = pack_f32x2(f, f);
 #pragma unroll
-                    for (int b = 0; b < B; ++b) {
-                        if (!(ss[b] <= 3.4e38f)) up[b] = 0x1p-80f;
-                        float u[E], v[E];
-                        Elt<T>::unpack(lo[b], u);
-                        Elt<T>::unpack(hi[b], v);
-#pragma unroll
-                        for (int i = 0; i < E / 2; ++i) {
-                            x[b][i] = pack_f32x2(u[2 * i] * up[b], u[2 * i + 1] * up[b]);
-                            x[b][E / 2 + i] = pack_f32x2(v[2 * i] * up[b], v[2 * i + 1] * up[b]);
-                        }
-                    }
-                    if (layer) sums();
-                    squares();
-                }
-#pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    if (!has[b]) continue;
-                    const float f = rsqrtf(fmaf(ss[b], 1.0f / D, h.eps * up[b] * up[b]));
-                    const uint64_t f2 = pack_f32x2(f, f);
-                    const long long wat = head[b] * h.head_stride;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        uint64_t* y = x[b] + half * (E / 2);
-                        const int o = half ? o_hi : o_lo;
-                        float w[E];
-#pragma unroll
-                        for (int i = 0; i < E / 2; ++i) y[i] = mul_f32x2(y[i], f2);
-                        if (h.weight && h.bias) {
-                            float add[E];
-                            norm_params<E>(h.weight, wat + o, h.bf16, w);
-                            norm_params<E>(h.bias, wat + o, h.bf16, add);
-#pragma unroll
-                            for (int i = 0; i < E / 2; ++i) y[i] = fma_f32x2(y[i], pack_f32x2(w[2 * i], w[2 * i + 1]), pack_f32x2(add[2 * i], add[2 * i + 1]));
-                        } else if (h.weight) {
-                            norm_params<E>(h.weight, wat + o, h.bf16, w);
-#pragma unroll
-                            for (int i = 0; i < E / 2; ++i) y[i] = mul_f32x2(y[i], pack_f32x2(w[2 * i], w[2 * i + 1]));
-                        } else if (h.bias) {
-                            norm_params<E>(h.bias, wat + o, h.bf16, w);
-#pragma unroll
-                            for (int i = 0; i < E / 2; ++i) y[i] = add_f32x2(y[i], pack_f32x2(w[2 * i], w[2 * i + 1]));
-                        }
-                    }
-                }
+                for (int i = 0; i < E; ++i) x[i] = fma_f32x2(mul_f32x2(x[i], f2), w[i], add[i]);
             }
+            const int l = min(t - t0, kNormTokens - 1);
             if (turn) {
                 const uint64_t minus = pack_f32x2(-1.f, -1.f);
+                const float* cosv = &sh.cs[l][c * E];
 #pragma unroll
                 for (int i = 0; i < E / 2; i += 2) {
-                    const float4 u = *reinterpret_cast<const float4*>(&cs[tl][c * E + 2 * i]), v = *reinterpret_cast<const float4*>(&cs[tl][HP + c * E + 2 * i]);
+                    const float4 u = *reinterpret_cast<const float4*>(cosv + 2 * i), v = *reinterpret_cast<const float4*>(cosv + HP + 2 * i);
                     const uint64_t co[2] = {pack_f32x2(u.x, u.y), pack_f32x2(u.z, u.w)}, si[2] = {pack_f32x2(v.x, v.y), pack_f32x2(v.z, v.w)};
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int b = 0; b < B; ++b) {
-                            // two pairs: side by side in the operands where pairs interleave, in the same place of both halves else
-                            uint64_t& y0 = x[b][INTER ? 2 * (i + j) : i + j];
-                            uint64_t& y1 = x[b][INTER ? 2 * (i + j) + 1 : E / 2 + i + j];
-                            uint64_t p = y0, q = y1;
-                            if (INTER) {
-                                float p0, q0, p1, q1;
-                                unpack_f32x2(y0, p0, q0);
-                                unpack_f32x2(y1, p1, q1);
-                                p = pack_f32x2(p0, p1);
-                                q = pack_f32x2(q0, q1);
-                            }
-                            const uint64_t x2 = fma_f32x2(mul_f32x2(q, si[j]), minus, mul_f32x2(p, co[j])), z2 = fma_f32x2(q, co[j], mul_f32x2(p, si[j]));
-                            if (INTER) {
-                                float p0, q0, p1, q1;
-                                unpack_f32x2(x2, p0, p1);
-                                unpack_f32x2(z2, q0, q1);
-                                y0 = pack_f32x2(p0, q0);
-                                y1 = pack_f32x2(p1, q1);
-                            } else {
-                                y0 = x2;
-                                y1 = z2;
-                            }
+                    for (int j = 0; j < 2; ++j) {
+                        // two pairs: side by side in the operands where pairs interleave, in the same place of both halves else
+                        uint64_t& y0 = x[INTER ? 2 * (i + j) : i + j];
+                        uint64_t& y1 = x[INTER ? 2 * (i + j) + 1 : E / 2 + i + j];
+                        uint64_t p = y0, q = y1;
+                        if (INTER) {
+                            float p0, q0, p1, q1;
+                            unpack_f32x2(y0, p0, q0);
+                            unpack_f32x2(y1, p1, q1);
+                            p = pack_f32x2(p0, p1);
+                            q = pack_f32x2(q0, q1);
                         }
-                }
-            }
-            int byte[B];
-            if (DEST == 2 && which > 0) {
-                float largest[B];
-#pragma unroll
-                for (int b = 0; b < B; ++b) {
-                    largest[b] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        float p, q;
-                        unpack_f32x2(x[b][i], p, q);
-                        largest[b] = max_nan(max_nan(largest[b], fabsf(p)), fabsf(q));
+                        const uint64_t x2 = fma_f32x2(mul_f32x2(q, si[j]), minus, mul_f32x2(p, co[j])), z2 = fma_f32x2(q, co[j], mul_f32x2(p, si[j]));
+                        y0 = x2;
+                        y1 = z2;
+                        if (INTER) {
+                            float p0, q0, p1, q1;
+                            unpack_f32x2(x2, p0, p1);
+                            unpack_f32x2(z2, q0, q1);
+                            y0 = pack_f32x2(p0, q0);
+                            y1 = pack_f32x2(p1, q1);
+                        }
                     }
                 }
-#pragma unroll
-                for (int o = 1; o < IPR; o <<= 1)
-#pragma unroll
-                    for (int b = 0; b < B; ++b) largest[b] = max_nan(largest[b], __shfl_xor_sync(0xffffffffu, largest[b], o));
-#pragma unroll
-                for (int b = 0; b < B; ++b) byte[b] = q8_byte(__float_as_uint(largest[b]));
             }
+            int byte = 0;
+            if (DEST == 2 && paged) {
+                float largest = 0.f;
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                if (!has[b] || at[b] < 0) continue;
-                float y[2 * E];
+                for (int i = 0; i < E; ++i) {
+                    float p, q;
+                    unpack_f32x2(x[i], p, q);
+                    largest = max_nan(max_nan(largest, fabsf(p)), fabsf(q));
+                }
 #pragma unroll
-                for (int i = 0; i < E; ++i) unpack_f32x2(x[b][i], y[2 * i], y[2 * i + 1]);
-                if (DEST == 2 && which > 0) {
+                for (int o = 1; o < IPR; o <<= 1) largest = max_nan(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+                byte = q8_byte(__float_as_uint(largest));
+            }
+            if (!has || t >= t1) return;
+            T* dst = to;
+            if (DEST && !paged && sh.seq_of[l] < 0) return;
+            if (paged) {
+                const int slot = sh.slot_of[l];
+                if (slot < 0) return;
+                const int page = table[sh.seq_of[l] * a.kv.table_seq_stride + (slot >> a.kv.page_shift)];
+                if (page < 0 || page >= a.kv.n_pages) {
+                    if (c == 0) paged_report(a.kv, kStPage);
+                    return;
+                }
+                const int in_page = slot & (a.kv.page_tokens - 1);
+                const long long at = page * a.kv.page_stride + in_page * a.kv.row_stride + head * a.kv.head_stride;
+                if (DEST == 2) {
+                    float y[2 * E];
                     unsigned codes[E / 2];
 #pragma unroll
-                    for (int i = 0; i < E / 2; ++i) codes[i] = q8_codes4(y + 4 * i, byte[b]);
-                    char* p = pool + at[b];
+                    for (int i = 0; i < E; ++i) unpack_f32x2(x[i], y[2 * i], y[2 * i + 1]);
+#pragma unroll
+                    for (int i = 0; i < E / 2; ++i) codes[i] = q8_codes4(y + 4 * i, byte);
+                    char* p = pool + at;
                     if (INTER && E == 8) {
                         *reinterpret_cast<uint4*>(p + o_lo) = make_uint4(codes[0], codes[1], codes[E / 2 - 2], codes[E / 2 - 1]);
                     } else if (INTER) {
@@ -371,37 +314,64 @@ __global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const __grid
                         *reinterpret_cast<unsigned*>(p + o_lo) = codes[0];
                         *reinterpret_cast<unsigned*>(p + o_hi) = codes[E / 2 - 1];
                     }
-                    if (c == 0) {
-                        (which == 1 ? na.q8.k_scale : na.q8.v_scale)[scale_at[b]] = (unsigned char)byte[b];
-                    }
-                    continue;
+                    if (c == 0) (KIND == 1 ? na.q8.k_scale : na.q8.v_scale)[page * na.q8.page_stride + head * na.q8.head_stride + in_page] = (unsigned char)byte;
+                    return;
                 }
-                T* dst = DEST == 1 && which > 0 ? reinterpret_cast<T*>(pool) + at[b]
-                                                : reinterpret_cast<T*>(a.dst[which].p) + t * a.dst[which].token_stride + head[b] * a.dst[which].head_stride;
-                float u[E], v[E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    u[i] = y[i];
-                    v[i] = y[E + i];
+                dst = reinterpret_cast<T*>(pool) + at;
+                if (KIND == 2) {  // values as they are: a pass through fp32 could touch the bits of a NaN
+                    *reinterpret_cast<uint4*>(dst + o_lo) = lo;
+                    *reinterpret_cast<uint4*>(dst + o_hi) = hi;
+                    return;
                 }
-                *reinterpret_cast<uint4*>(dst + o_lo) = PackRow<T>::pack(u);
-                *reinterpret_cast<uint4*>(dst + o_hi) = PackRow<T>::pack(v);
             }
-            which = nwhich;
-            g0 = ng;
-            h1 = nh1;
+            float u[E], v[E];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                unpack_f32x2(x[i], u[2 * i], u[2 * i + 1]);
+                unpack_f32x2(x[E / 2 + i], v[2 * i], v[2 * i + 1]);
+            }
+            *reinterpret_cast<uint4*>(dst + o_lo) = PackRow<T>::pack(u);
+            *reinterpret_cast<uint4*>(dst + o_hi) = PackRow<T>::pack(v);
+        };
+        const int passes = (t1 - t0 + step - 1) / step;
+#pragma unroll 1
+        for (int p = 0; p < passes; p += 2) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint4 x = lo[j], y = hi[j];
+                fetch(t + 2 * step, lo[j], hi[j]);
+                if (p + j < passes) work(x, y);
+                t += step;
+                to += to_step;
+            }
         }
     }
-    if (DEST == 1 && a.state) {
+};
+
+template <typename T, int D, bool INTER, int DEST>
+__global__ void __launch_bounds__(kNormThreads, 2) norm_rope_kernel(const __grid_constant__ NormRopeArgs na) {
+    using R = NormRope<T, D, INTER, DEST>;
+    __shared__ __align__(16) typename R::Shared sh;
+    const RopeRowsArgs& a = na.r;
+    int y = blockIdx.y;
+    if (y < na.slices[0]) {
+        R::template rows<0>(na, sh, y);
+    } else if ((y -= na.slices[0]) < na.slices[1]) {
+        R::template rows<1>(na, sh, y);
+    } else if (DEST) {
+        R::template rows<2>(na, sh, y - na.slices[1]);
+    }
+    if (DEST == 1 && a.state && blockIdx.y == gridDim.y - 1) {
         // the library's own cache: the index map's entries of the tokens; the last one sets the unit's length
-        for (int i = tid; i < nt * a.kv.n_kv_heads && blockIdx.y == 0; i += kRopeThreads) {
-            const int tl = i / a.kv.n_kv_heads, head = i - tl * a.kv.n_kv_heads;
-            if (slot_of[tl] < 0) continue;
-            const int unit = seq_of[tl] * a.kv.n_kv_heads + head;
-            a.index_map[(size_t)unit * a.cap_pad + slot_of[tl]] = slot_of[tl];
-            if (slot_of[tl] == a.base_len + a.kv.chunk - 1) {
+        const int t0 = blockIdx.x * na.tokens, nt = min(na.tokens, a.n_tokens - t0);
+        for (int i = threadIdx.x; i < nt * a.kv.n_kv_heads; i += blockDim.x) {
+            const int l = i / a.kv.n_kv_heads, head = i - l * a.kv.n_kv_heads, slot = sh.slot_of[l];
+            if (slot < 0) continue;
+            const int unit = sh.seq_of[l] * a.kv.n_kv_heads + head;
+            a.index_map[(size_t)unit * a.cap_pad + slot] = slot;
+            if (slot == a.base_len + a.kv.chunk - 1) {
                 UnitState ns;
-                ns.len = slot_of[tl] + 1;
+                ns.len = slot + 1;
                 ns.n_tok = 0;
                 a.state[unit] = ns;
             }
