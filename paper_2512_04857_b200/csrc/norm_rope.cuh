@@ -6,10 +6,10 @@
 //
 // Bound: HBM bytes (each row once in, once out), as long as an element costs few instructions.  So a CTA has rows of one kind (q, k or v: what depends on the
 // kind is the same for all its threads) and a thread stays with one head, of which it has 16 bytes of each half of a row (or 32 bytes side by side
-// where pairs interleave), and goes through tokens: weights, biases and pointers are in registers from the start, and the CTA's sines, cosines and
-// slots in shared memory behind one barrier.  The D / 16 (bf16) or D / 8 (fp32) threads of a row are neighbours in a warp: the row's sums are
+// where pairs interleave), and goes through tokens: its pointers are in registers from the start, and weights, biases, sines, cosines and slots of the
+// CTA in shared memory behind one barrier (weights in registers leave room for half the warps: 275 us on 66560 tokens of 40 rows, layer norm).  The D / 16 (bf16) or D / 8 (fp32) threads of a row are neighbours in a warp: the row's sums are
 // a few shuffles, taken with the row in registers, the mean first and the squares of what is left after it, not the difference of two large sums.  fp32
-// arithmetic goes two elements to an instruction.  While a token is worked on the next two are on the way.
+// arithmetic goes two elements to an instruction.  While a token is worked on the next one is on the way.
 #pragma once
 #include "paged_attn.cuh"  // two fp32 operations in one instruction
 #include "paged_q8.cuh"
@@ -52,7 +52,7 @@ struct NormRopeArgs {
 };
 
 constexpr int kNormThreads = 256;  // of a CTA at most
-constexpr int kNormTokens = 32;
+constexpr int kNormTokens = 24;   // tokens of a CTA at most (with the weights of 256 threads just within 48 KB)
 
 // E parameters of a norm as fp32 (16 or 8 bytes)
 template <int E>
@@ -110,9 +110,12 @@ struct NormRope {
     static constexpr int IPR = D / (2 * E);      // threads of a row
     static constexpr int HP = D / 2;
 
+    static constexpr int NP = E;                 // pieces of four parameters that a thread has: weights and biases in turn
+
     struct Shared {
         float cs[kNormTokens][D];  // cosines, sines
         int slot_of[kNormTokens], seq_of[kNormTokens];
+        float4 params[kNormThreads * NP];  // [head][piece][thread of the row]
     };
 
     static __device__ __forceinline__ float row_sum(float v) {
@@ -147,17 +150,15 @@ struct NormRope {
         const long long from_step = step * a.src[KIND].token_stride;
         auto fetch = [&](int t, uint4& lo, uint4& hi) {
             if (has && t < t1) {
-                lo = *reinterpret_cast<const uint4*>(from + o_lo);
-                hi = *reinterpret_cast<const uint4*>(from + o_hi);
+                lo = __ldcg(reinterpret_cast<const uint4*>(from + o_lo));
+                hi = __ldcg(reinterpret_cast<const uint4*>(from + o_hi));
             }
             from += from_step;
         };
-        uint4 lo[2], hi[2];  // two tokens on the way
-        lo[0] = lo[1] = hi[0] = hi[1] = make_uint4(0, 0, 0, 0);
-        fetch(t, lo[0], hi[0]);
-        fetch(t + step, lo[1], hi[1]);
-        uint64_t w[E], add[E];  // two elements each: the low chunk, then the high one
-        if (on) {
+        uint4 next_lo = make_uint4(0, 0, 0, 0), next_hi = next_lo;  // of the next token, on the way
+        fetch(t, next_lo, next_hi);
+        if (on && sub == 0) {
+            // weights and biases, a thread's 16 bytes side by side with its neighbours'
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 float u[E], v[E];
@@ -172,12 +173,14 @@ struct NormRope {
                     if (h.bias) norm_params<E>(h.bias, at, h.bf16, v);
                 }
 #pragma unroll
-                for (int i = 0; i < E / 2; ++i) {
-                    w[half * (E / 2) + i] = pack_f32x2(u[2 * i], u[2 * i + 1]);
-                    add[half * (E / 2) + i] = pack_f32x2(v[2 * i], v[2 * i + 1]);
+                for (int i = 0; i < E; i += 4) {
+                    float4* p = sh.params + (group * NP + (half * E + i) / 2) * IPR + c;
+                    p[0] = make_float4(u[i], u[i + 1], u[i + 2], u[i + 3]);
+                    p[IPR] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                 }
             }
         }
+        const float4* params = sh.params + (group - sub * na.heads[KIND]) * NP * IPR + c;
         // sines, cosines and slots of the CTA's tokens
         if (turn) {
             const int i = tid & (HP - 1);
@@ -233,7 +236,11 @@ struct NormRope {
                 const float f = rsqrtf(fmaf(ss, 1.0f / D, h.eps * up * up));
                 const uint64_t f2 = pack_f32x2(f, f);
 #pragma unroll
-                for (int i = 0; i < E; ++i) x[i] = fma_f32x2(mul_f32x2(x[i], f2), w[i], add[i]);
+                for (int i = 0; i < E; i += 2) {
+                    const float4 w = params[i * IPR], v = params[(i + 1) * IPR];
+                    x[i] = fma_f32x2(mul_f32x2(x[i], f2), pack_f32x2(w.x, w.y), pack_f32x2(v.x, v.y));
+                    x[i + 1] = fma_f32x2(mul_f32x2(x[i + 1], f2), pack_f32x2(w.z, w.w), pack_f32x2(v.z, v.w));
+                }
             }
             const int l = min(t - t0, kNormTokens - 1);
             if (turn) {
@@ -330,26 +337,23 @@ struct NormRope {
                 unpack_f32x2(x[i], u[2 * i], u[2 * i + 1]);
                 unpack_f32x2(x[E / 2 + i], v[2 * i], v[2 * i + 1]);
             }
-            *reinterpret_cast<uint4*>(dst + o_lo) = PackRow<T>::pack(u);
-            *reinterpret_cast<uint4*>(dst + o_hi) = PackRow<T>::pack(v);
+            __stcg(reinterpret_cast<uint4*>(dst + o_lo), PackRow<T>::pack(u));
+            __stcg(reinterpret_cast<uint4*>(dst + o_hi), PackRow<T>::pack(v));
         };
         const int passes = (t1 - t0 + step - 1) / step;
 #pragma unroll 1
-        for (int p = 0; p < passes; p += 2) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint4 x = lo[j], y = hi[j];
-                fetch(t + 2 * step, lo[j], hi[j]);
-                if (p + j < passes) work(x, y);
-                t += step;
-                to += to_step;
-            }
+        for (int p = 0; p < passes; ++p) {
+            const uint4 lo = next_lo, hi = next_hi;
+            fetch(t + step, next_lo, next_hi);
+            work(lo, hi);
+            t += step;
+            to += to_step;
         }
     }
 };
 
 template <typename T, int D, bool INTER, int DEST>
-__global__ void __launch_bounds__(kNormThreads, 2) norm_rope_kernel(const __grid_constant__ NormRopeArgs na) {
+__global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const __grid_constant__ NormRopeArgs na) {
     using R = NormRope<T, D, INTER, DEST>;
     __shared__ __align__(16) typename R::Shared sh;
     const RopeRowsArgs& a = na.r;
