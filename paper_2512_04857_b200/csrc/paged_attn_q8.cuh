@@ -16,6 +16,7 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include "join_parts.cuh"
 #include "paged_attn_tc.cuh"
 #include "paged_q8.cuh"
 
@@ -23,35 +24,56 @@ namespace lar {
 
 constexpr int kQ8Rows = 16;  // rows of a unit up to which the kernel below is taken
 
+// A step of a CTA's work, worked out by the producer: some slot tiles of one unit.
+struct alignas(16) Q8Seg {
+    int tok0, n_tok, head, slot0;  // tokens of the unit, slot of the first
+    int lo, len, jb, nb;           // live slots of the sequence; first tile and tiles of this step (-1: no more work)
+    int whole, b0, last_cta, pad;  // nothing of the unit lies in other CTAs; tiles before this step's; the CTA with its last one
+};
+
 template <typename T, int D, int NR>
 struct Q8Shape {
-    static constexpr int KT = 32;                 // slots of a tile
     static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
+    // Slots of a tile (64 instead of 32, one token over 16 x 4288 slots: 25 instead of 27 us, 3 x 65537 slots 68 instead of 75; 16 rows of 64 fp32
+    // elements 40 instead of 44; of 128, where the registers do not hold it, 66 instead of 57).
+    static constexpr int KT = TERMS == 2 && NR == 2 && D == 128 ? 32 : 64;
     static constexpr int MT = KT / 16, KS = D / 16;
     static constexpr int TILE_BYTES = KT * D, STAGE_BYTES = 2 * TILE_BYTES, SCALE_BYTES = 2 * KT;
+    static constexpr int SCALE_PITCH = KT / 16 * 128;  // of a stage: a copy's destination is 128-byte aligned, and a page has 16 slots at least
     static constexpr int W = 4, THREADS = (W + 2) * 32;  // producer, consumers, epilogue
-    static constexpr int NS = 8;                  // stages: a multiple of W, a stage is always read by the same consumer
-    static constexpr int PER_SM = 2;
+    static constexpr int NS = KT == 64 ? 4 : 8;  // stages: a multiple of W, a stage is always read by the same consumer
+    static constexpr int PER_SM = D == 64 && NR == 1 ? 3 : 2;  // (64 x 577 slots, 20 heads of 64, 1 to 8 tokens: 27 us with three CTAs, 31 with two)
     static constexpr int ROWS = 8 * NR;
+    static constexpr int QS = 4;                  // units that the producer is ahead by at most
     static constexpr int Q_SLOT = ROWS * D * (int)sizeof(T);
     static constexpr int PS = D + 4;              // floats of a partial row: O, m, l, padding
     static constexpr int PBUFS = NR == 1 ? 2 : 1;
     static constexpr int PBUF_FLOATS = W * ROWS * PS;
-    static constexpr int FIXED = 1024 + NS * (STAGE_BYTES + SCALE_BYTES) + 2 * Q_SLOT + PBUFS * PBUF_FLOATS * 4 + 32 * 8;
+    static constexpr int FIXED = 1024 + NS * (STAGE_BYTES + SCALE_PITCH) + QS * (Q_SLOT + (int)sizeof(Q8Seg)) + PBUFS * PBUF_FLOATS * 4 + 32 * 8;
     static __host__ __device__ int bytes(int n_seqs) { return FIXED + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
 };
 
 struct Q8Maps {
     CUtensorMap q;     // {d, heads of a group, KV heads, tokens}, box d x group x 1 x tq, rows of T
-    CUtensorMap k, v;  // {d, rows of a page, heads, pages} of bytes, box d x min(page, 32) x 1 x 1, swizzled by d bytes
+    CUtensorMap kv;    // {d, rows of a page, heads, pages, 2} of bytes, box d x min(page, KT) x 1 x 1 x 2, swizzled by d bytes: K and V rows with one
+                       // copy (issuing copies is what bounds a producer), the pool with the lower address first
+    CUtensorMap scale; // {rows of a page, heads, pages, 2} of bytes, box min(page, KT) x 1 x 1 x 2
+    int v_first, v_scale_first;
 };
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, int v, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(bar)
+        : "memory");
+}
 
 // Two fp16 numbers from each half of four codes.
 __device__ __forceinline__ void q8_halves(uint32_t codes, uint32_t& lo, uint32_t& hi) {
     asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -84,7 +106,7 @@ struct OutRow<float> {
 
 template <typename T, int D, int NR>
 __global__ void __launch_bounds__(Q8Shape<T, D, NR>::THREADS, Q8Shape<T, D, NR>::PER_SM)
-paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ Q8View q8, const __grid_constant__ Q8Maps maps) {
+paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ Q8Maps maps) {
     using S = Q8Shape<T, D, NR>;
     using Work = TcWork<1, S::KT, D>;
     constexpr int KT = S::KT, W = S::W, NS = S::NS, TERMS = S::TERMS, KS = S::KS, MT = S::MT;
@@ -93,19 +115,20 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* gbase = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t ring = base, scales = base + NS * S::STAGE_BYTES;
-    unsigned char* gscales = gbase + NS * S::STAGE_BYTES;   // per stage: KT bytes of K, KT of V
-    unsigned char* gq = gscales + NS * S::SCALE_BYTES;
-    const uint32_t qring = scales + NS * S::SCALE_BYTES;
-    float* pbuf = reinterpret_cast<float*>(gq + 2 * S::Q_SLOT);
+    unsigned char* gscales = gbase + NS * S::STAGE_BYTES;
+    unsigned char* gq = gscales + NS * S::SCALE_PITCH;
+    const uint32_t qring = scales + NS * S::SCALE_PITCH;
+    Q8Seg* segs_at = reinterpret_cast<Q8Seg*>(gq + S::QS * S::Q_SLOT);
+    float* pbuf = reinterpret_cast<float*>(segs_at + S::QS);
     uint64_t* bars = reinterpret_cast<uint64_t*>(pbuf + S::PBUFS * S::PBUF_FLOATS);
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int st) { return bar0 + 8u * st; };
     auto empty = [&](int st) { return bar0 + 8u * (8 + st); };
     auto q_full = [&](int i) { return bar0 + 8u * (16 + i); };
-    auto q_empty = [&](int i) { return bar0 + 8u * (18 + i); };
-    auto p_full = [&](int i) { return bar0 + 8u * (20 + i); };
-    auto p_empty = [&](int i) { return bar0 + 8u * (22 + i); };
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 24);
+    auto q_empty = [&](int i) { return bar0 + 8u * (20 + i); };
+    auto p_full = [&](int i) { return bar0 + 8u * (24 + i); };
+    auto p_empty = [&](int i) { return bar0 + 8u * (26 + i); };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 28);
     SeqInfo* info = reinterpret_cast<SeqInfo*>(bars + 32);
     int* pre = reinterpret_cast<int*>(info + a.kv.n_seqs);
     int* wsum = pre + 2 * (a.kv.n_seqs + 1);
@@ -116,9 +139,11 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
             mbar_init(full(i), 1);
             mbar_init(empty(i), 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < S::QS; ++i) {
             mbar_init(q_full(i), 1);
-            mbar_init(q_empty(i), W);
+            mbar_init(q_empty(i), W + 1);  // consumers and epilogue
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(p_full(i), W);
             mbar_init(p_empty(i), 1);
         }
@@ -174,25 +199,21 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
     }
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ producer: lanes 0, 1 K and 2, 3 V, a page (or part of one) each
+        // ------------------------------------------------------------------ producer: a lane for every page (or part of one) of a tile
         int issued = 0, segs = 0;
         RingPos kv;
         bool ok = true;
-        const int nbox = KT / ta.box_rows;  // 1 or 2
-        const int is_v = (lane >> 1) & 1, box = lane & 1;
-        const bool boxes = lane < 4 && box < nbox;
-        const int box_slot = box * ta.box_rows, row_mask = a.kv.page_tokens - 1;
+        const int nbox = KT / ta.box_rows;  // at most 4
+        const bool boxes = lane < nbox;
+        const int box_slot = lane * ta.box_rows, row_mask = a.kv.page_tokens - 1;
         const int cap = a.kv.table_cols << a.kv.page_shift;
-        const uint32_t dst0 = ring + is_v * S::TILE_BYTES + box_slot * D, sdst0 = scales + is_v * KT + box_slot;
-        const CUtensorMap* map = is_v ? &maps.v : &maps.k;
-        const unsigned char* scale_pool = is_v ? q8.v_scale : q8.k_scale;
-        TcSeg g;
-        while (ok && work.next(g)) {
-            const int n = g.nb, len = min(g.len, cap), lo = g.lo;
-            if (n == 0) continue;
+        const uint32_t dst0 = ring + box_slot * 2 * D, sdst0 = scales + lane * 128;
+        TcSeg g = {};
+        for (;;) {
+            const bool more = work.next(g);
+            const int n = more ? g.nb : 0, len = min(g.len, cap), lo = g.lo;
             const int* table = a.kv.table + g.seq * a.kv.table_seq_stride + g.head * a.kv.table_head_stride;
             const int head_c = a.kv.head_stride > 0 ? g.head : 0;
-            const unsigned char* sbase = scale_pool + g.head * q8.head_stride;
             int slot = g.jb * KT + box_slot;  // first slot of this lane's box
             auto page_of = [&](int slot) {
                 int page = a.kv.n_pages;  // outside the tensor: the box is filled with zeros
@@ -203,38 +224,44 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                 }
                 return page;
             };
-            int page = page_of(slot);
-            const int qs = segs & 1;
-            if (segs >= 2 && !(ok = warp_wait(q_empty(qs), ((segs >> 1) - 1) & 1, abort_flag))) break;
+            int page = n > 0 ? page_of(slot) : 0;
+            const int qs = segs % S::QS;
+            if (segs >= S::QS && !(ok = warp_wait(q_empty(qs), (segs / S::QS - 1) & 1, abort_flag))) break;
             ++segs;
             if (lane == 0) {
-                mbar_expect_tx(q_full(qs), (uint32_t)(a.tq * a.group * D * (int)sizeof(T)));
-                tma_load_4d(qring + qs * S::Q_SLOT, &maps.q, 0, 0, g.head, g.tok0, q_full(qs));
+                Q8Seg u;
+                u.tok0 = g.tok0; u.n_tok = g.n_tok; u.head = g.head; u.slot0 = g.slot0;
+                u.lo = g.lo; u.len = g.len; u.jb = g.jb; u.nb = more ? n : -1;
+                u.whole = g.whole; u.b0 = g.b0; u.pad = 0;
+                u.last_cta = more && !g.whole ? (int)(((long long)g.unit_end * n_ranges + total - 1) / total - 1) : 0;
+                segs_at[qs] = u;
+                if (n > 0) {
+                    mbar_expect_tx(q_full(qs), (uint32_t)(a.tq * a.group * D * (int)sizeof(T)));
+                    tma_load_4d(qring + qs * S::Q_SLOT, &maps.q, 0, 0, g.head, g.tok0, q_full(qs));
+                } else {
+                    mbar_arrive(q_full(qs));
+                }
             }
+            if (!more) break;
             for (int j = 0; j < n; ++j) {
                 const int page_next = j + 1 < n ? page_of(slot + KT) : 0;
                 if (issued >= NS && !(ok = warp_wait(empty(kv.st), kv.ph ^ 1, abort_flag))) break;
-                const bool there = boxes && page < a.kv.n_pages;
-                const uint32_t sdst = sdst0 + kv.st * S::SCALE_BYTES;
-                if (boxes && !there) {  // codes of zero: any finite scale
-                    for (int i = 0; i < ta.box_rows; i += 16)
-                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(sdst + i), "r"(0x7f7f7f7f) : "memory");
-                    fence_proxy_async_smem();  // (before a later copy to the same place)
-                }
-                const int copies = __popc(__ballot_sync(0xffffffffu, there));
-                if (lane == 0) mbar_expect_tx(full(kv.st), (uint32_t)(S::STAGE_BYTES + copies * ta.box_rows));
+                if (lane == 0) mbar_expect_tx(full(kv.st), (uint32_t)(S::STAGE_BYTES + S::SCALE_BYTES));
                 __syncwarp();
-                if (boxes) tma_load_4d(dst0 + kv.st * S::STAGE_BYTES, map, 0, slot & row_mask, head_c, page, full(kv.st));
-                if (there) bulk_g2s(sdst, sbase + page * q8.page_stride + (slot & row_mask), (uint32_t)ta.box_rows, full(kv.st));
+                if (boxes) {
+                    tma_load_5d(dst0 + kv.st * S::STAGE_BYTES, &maps.kv, 0, slot & row_mask, head_c, page, 0, full(kv.st));
+                    tma_load_4d(sdst0 + kv.st * S::SCALE_PITCH, &maps.scale, slot & row_mask, head_c, page, 0, full(kv.st));
+                }
                 ++issued;
                 kv.next(NS);
                 slot += KT;
                 page = page_next;
             }
+            if (!ok) break;
         }
         if (!ok && lane == 0) {
             // given up: the copies in flight land before the CTA's shared memory goes to somebody else
-            for (int i = segs > 2 ? segs - 2 : 0; i < segs; ++i) mbar_wait_bounded(q_full(i & 1), (i >> 1) & 1);
+            for (int i = segs > S::QS ? segs - S::QS : 0; i < segs; ++i) mbar_wait_bounded(q_full(i % S::QS), (i / S::QS) & 1);
             for (int i = issued > NS ? issued - NS : 0; i < issued; ++i) mbar_wait_bounded(full(i % NS), (i / NS) & 1);
         }
         __syncwarp();
@@ -242,16 +269,24 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
         // ------------------------------------------------------------------ consumers
         const int cw = warp - 1, quad = lane & 3, qrow = lane >> 2;  // fragment coordinates
         const int G = a.group;
-        int t = cw, t_base = 0;   // next tile of this warp, first tile of the segment (in the CTA's list)
-        int segs = 0, all_segs = 0;
+        const unsigned by_group = 65536u / G + 1u;  // (a row's token: row / G of at most 16 rows)
+        int t = cw, t_base = 0;   // next tile of this warp, first tile of the step (in the CTA's list)
         RingPos rp;
         rp.st = cw;
         bool ok = true;
-        // byte offset of 16-byte chunk c of row r of a tile (128- or 64-byte swizzle)
+        // A stage holds one copy behind the other, each the rows of a page (or part of one) of one pool and then of the other: where 16 slots of a tile lie
+        const uint32_t box_bytes = ta.box_rows * D, k_at = maps.v_first ? box_bytes : 0, v_at = maps.v_first ? 0 : box_bytes;
+        const int ks_at = maps.v_scale_first ? ta.box_rows : 0, vs_at = maps.v_scale_first ? 0 : ta.box_rows;
+        const int box_mask = ta.box_rows - 1, box_shift = __ffs(ta.box_rows) - 1;
+        auto block = [&](int mt) { return (uint32_t)((16 * mt & ~box_mask) * 2 + (16 * mt & box_mask)); };  // rows before the block
+        // byte offset of 16-byte chunk c of row r of a block (128- or 64-byte swizzle)
         auto off = [](int r, int c) { return (uint32_t)(D == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); };
-        TcSeg g;
-        while (ok && work.next(g)) {
+        for (int seg = 0;; ++seg) {
+            const int qs = seg % S::QS;
+            if (!(ok = warp_wait(q_full(qs), (seg / S::QS) & 1, abort_flag))) break;
+            const Q8Seg g = segs_at[qs];
             const int n = g.nb;
+            if (n < 0) break;
             // per row of this thread (8 r + 2 quad + e): largest logit, sum, reference of the weights, accumulator (element 16 k + 2 qrow: e, + 1: 2 + e)
             float m[NR][2], l[NR][2], vr[NR][2], o[NR][KS][4];
             float qs_row[NR][2], sc[NR][2];  // power of two that q was divided by, softmax scale of the divided logits
@@ -264,16 +299,16 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     m[r][e] = vr[r][e] = -INFINITY;
                     l[r][e] = 0.f;
                     qs_row[r][e] = sc[r][e] = 0.f;
-                    last[r][e] = row >= g.n_tok * G ? -1 : a.causal ? min(g.slot0 + row / G, g.len - 1) : g.len - 1;
+                    last[r][e] = row >= g.n_tok * G ? -1 : a.causal ? min(g.slot0 + (int)(row * by_group >> 16), g.len - 1) : g.len - 1;
                 }
 #pragma unroll
                 for (int k = 0; k < KS; ++k) o[r][k][0] = o[r][k][1] = o[r][k][2] = o[r][k][3] = 0.f;
             }
             const int min_last = a.causal ? min(g.slot0, g.len - 1) : g.len - 1;
-            if (n > 0) {
-                const int qs = segs & 1;
-                if (!(ok = warp_wait(q_full(qs), (segs >> 1) & 1, abort_flag))) break;
-                ++segs;
+            if (n == 0) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_empty(qs));
+            } else {
                 uint32_t qf[TERMS][NR][KS][2];  // B operand: column = row of the unit, elements 4 quad .. + 3 of each 16
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
@@ -315,14 +350,14 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     if (!(ok = warp_wait(full(st), rp.ph, abort_flag))) break;
                     rp.skip(W, NS);
                     const int base_slot = (g.jb + t - t_base) * KT;
-                    const uint32_t kt = ring + st * S::STAGE_BYTES, vt = kt + S::TILE_BYTES;
+                    const uint32_t tile = ring + st * S::STAGE_BYTES;
                     const bool ragged = base_slot < g.lo || base_slot + KT > g.len;
                     if (ragged) {
                         // values of slots that are not live: their weight is 0, but 0 * NaN is not
                         for (int i = lane; i < KT * (D / 16); i += 32) {
                             const int r = i / (D / 16);
                             if (base_slot + r < g.lo || base_slot + r >= g.len)
-                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + i * 16), "r"(0) : "memory");
+                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + v_at + (block(r >> 4) + (r & 15)) * D + i % (D / 16) * 16), "r"(0) : "memory");
                         }
                         __syncwarp();
                     }
@@ -332,35 +367,39 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const int at = st * S::SCALE_BYTES + 16 * mt + qrow + 8 * h, vb = gscales[at + KT];
-                            kf[mt][h] = q8_scale(gscales[at]);
+                            const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at];
+                            kf[mt][h] = q8_scale(gscales[at + ks_at]);
                             ve[mt][h] = vb == kQ8NaN ? INFINITY : (float)(vb - 127);
                         }
                     // S^T[slot][row]
                     float s[MT][NR][4];
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
+                    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int r = 0; r < NR; ++r) s[mt][r][0] = s[mt][r][1] = s[mt][r][2] = s[mt][r][3] = 0.f;
 #pragma unroll
-                        for (int k = 0; k < KS; k += 2) {
+                    for (int k = 0; k < KS; k += 2)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
                             uint32_t f[4], x[4], y[4];  // 8 slots x 16 codes each: slots 0-7, 8-15 of chunk k, then of chunk k + 1
-                            ldmatrix_x4(kt + off(16 * mt + (lane & 15), k + (lane >> 4)), f);
+                            ldmatrix_x4(tile + k_at + block(mt) * D + off(lane & 15, k + (lane >> 4)), f);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) q8_halves(f[i], x[i], y[i]);
 #pragma unroll
-                            for (int r = 0; r < NR; ++r)
+                            for (int u = 0; u < TERMS; ++u)
 #pragma unroll
-                                for (int u = 0; u < TERMS; ++u) {
-                                    mma_f16(s[mt][r], x[0], x[1], y[0], y[1], qf[u][r][k][0], qf[u][r][k][1]);
-                                    mma_f16(s[mt][r], x[2], x[3], y[2], y[3], qf[u][r][k + 1][0], qf[u][r][k + 1][1]);
-                                }
+                                for (int r = 0; r < NR; ++r) mma_f16(s[mt][r], x[0], x[1], y[0], y[1], qf[u][r][k][0], qf[u][r][k][1]);
+#pragma unroll
+                            for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+                                for (int r = 0; r < NR; ++r) mma_f16(s[mt][r], x[2], x[3], y[2], y[3], qf[u][r][k + 1][0], qf[u][r][k + 1][1]);
                         }
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int r = 0; r < NR; ++r)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) s[mt][r][e] *= kf[mt][e >> 1];
-                    }
                     if (base_slot < g.lo || base_slot + KT - 1 > min_last) {
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
@@ -375,21 +414,30 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                                         if (slot < g.lo || slot > last[r][e]) s[mt][r][2 * h + e] = -INFINITY;
                             }
                     }
-                    uint32_t pb[TERMS][MT][NR][2];  // weights^T as B operand
+                    // The softmax, one step for all columns at a time: a shuffle's latency is that of many instructions.
+                    float mx[NR][2], top[NR][2], of[NR][2];
 #pragma unroll
-                    for (int r = 0; r < NR; ++r) {
-                        float of[2];
+                    for (int r = 0; r < NR; ++r)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float mx = fmaxf(s[0][r][e], s[0][r][2 + e]);
+                            mx[r][e] = fmaxf(s[0][r][e], s[0][r][2 + e]);
 #pragma unroll
-                            for (int mt = 1; mt < MT; ++mt) mx = fmaxf(mx, fmaxf(s[mt][r][e], s[mt][r][2 + e]));
+                            for (int mt = 1; mt < MT; ++mt) mx[r][e] = fmaxf(mx[r][e], fmaxf(s[mt][r][e], s[mt][r][2 + e]));
+                        }
 #pragma unroll
-                            for (int w = 4; w <= 16; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                            const float mn = fmaxf(m[r][e], mx), ref = softmax_ref(mn);
-                            const float shift = (m[r][e] - ref) * sc[r][e];
+                    for (int w = 4; w <= 16; w <<= 1)
+#pragma unroll
+                        for (int r = 0; r < NR; ++r)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) mx[r][e] = fmaxf(mx[r][e], __shfl_xor_sync(0xffffffffu, mx[r][e], w));
+#pragma unroll
+                    for (int r = 0; r < NR; ++r)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float mn = fmaxf(m[r][e], mx[r][e]), ref = softmax_ref(mn), shift = (m[r][e] - ref) * sc[r][e];
                             m[r][e] = mn;
-                            float sum = 0.f, top = -INFINITY;
+                            vr[r][e] += shift;
+                            float sum = 0.f, most = -INFINITY;
 #pragma unroll
                             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -398,14 +446,27 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                                     x = (x - ref) * sc[r][e];
                                     sum += ex2_approx(x);
                                     x += ve[mt][h];
-                                    top = fmaxf(top, x);
+                                    most = fmaxf(most, x);
                                 }
                             l[r][e] = fmaf(l[r][e], ex2_approx(shift), sum);
+                            top[r][e] = most;
+                        }
 #pragma unroll
-                            for (int w = 4; w <= 16; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-                            const float was = vr[r][e] + shift, vn = fmaxf(was, top), vref = softmax_ref(vn);
-                            of[e] = ex2_approx(was - vref);
+                    for (int w = 4; w <= 16; w <<= 1)
+#pragma unroll
+                        for (int r = 0; r < NR; ++r)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) top[r][e] = fmaxf(top[r][e], __shfl_xor_sync(0xffffffffu, top[r][e], w));
+                    uint32_t pb[TERMS][MT][NR][2];  // weights^T as B operand
+                    bool moved = false;
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float vn = fmaxf(vr[r][e], top[r][e]), vref = softmax_ref(vn);
+                            of[r][e] = ex2_approx(vr[r][e] - vref);
                             vr[r][e] = vn;
+                            moved |= of[r][e] != 1.f;
 #pragma unroll
                             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -423,15 +484,17 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                                     pb[TERMS - 1][mt][r][h] = movmatrix_trans(pack_f16(w0 - hi.x, w1 - hi.y));
                                 }
                             }
-                        if (__any_sync(0xffffffffu, of[0] != 1.f || of[1] != 1.f)) {
+                    }
+                    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                        for (int r = 0; r < NR; ++r)
 #pragma unroll
                             for (int k = 0; k < KS; ++k) {
-                                o[r][k][0] *= of[0];
-                                o[r][k][1] *= of[1];
-                                o[r][k][2] *= of[0];
-                                o[r][k][3] *= of[1];
+                                o[r][k][0] *= of[r][0];
+                                o[r][k][1] *= of[r][1];
+                                o[r][k][2] *= of[r][0];
+                                o[r][k][3] *= of[r][1];
                             }
-                        }
                     }
                     // O^T[element][row] += V^T w^T
 #pragma unroll
@@ -446,18 +509,20 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
                             uint32_t f[4];  // slots 0-7, 8-15 of chunk k, then of chunk k + 1
-                            ldmatrix_x4_trans(vt + off(16 * mt + (lane & 15), k + (lane >> 4)), f);
+                            ldmatrix_x4_trans(tile + v_at + block(mt) * D + off(lane & 15, k + (lane >> 4)), f);
+                            uint32_t v[2][4];
 #pragma unroll
                             for (int c = 0; c < 2; ++c) {
-                                uint32_t a0, a1, a2, a3;
-                                q8_halves(__byte_perm(f[2 * c], 0, 0x3120), a0, a1);
-                                q8_halves(__byte_perm(f[2 * c + 1], 0, 0x3120), a2, a3);
-#pragma unroll
-                                for (int r = 0; r < NR; ++r)
-#pragma unroll
-                                    for (int u = 0; u < TERMS; ++u)
-                                        mma_f16(TERMS == 2 ? add[c][r] : o[r][k + c], a0, a1, a2, a3, pb[u][mt][r][0], pb[u][mt][r][1]);
+                                q8_halves(__byte_perm(f[2 * c], 0, 0x3120), v[c][0], v[c][1]);
+                                q8_halves(__byte_perm(f[2 * c + 1], 0, 0x3120), v[c][2], v[c][3]);
                             }
+#pragma unroll
+                            for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                                    for (int r = 0; r < NR; ++r)
+                                        mma_f16(TERMS == 2 ? add[c][r] : o[r][k + c], v[c][0], v[c][1], v[c][2], v[c][3], pb[u][mt][r][0], pb[u][mt][r][1]);
                         }
                         if (TERMS == 2) {
 #pragma unroll
@@ -474,8 +539,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                 t_base += n;
             }
             // this warp's part of the unit
-            const int pb = all_segs % S::PBUFS, turn = all_segs / S::PBUFS;
-            ++all_segs;
+            const int pb = seg % S::PBUFS, turn = seg / S::PBUFS;
             if (turn > 0 && !(ok = warp_wait(p_empty(pb), (turn - 1) & 1, abort_flag))) break;
             float* part = pbuf + pb * S::PBUF_FLOATS + cw * S::ROWS * S::PS;
 #pragma unroll
@@ -500,12 +564,16 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
         // ------------------------------------------------------------------ epilogue
         constexpr int LPR = D / 4;  // lanes of a row, four elements each
         const int G = a.group;
-        int all_segs = 0;
+        const unsigned by_group = 65536u / G + 1u;
         bool ok = true, recorded = false;
-        TcSeg g;
-        while (ok && work.next(g)) {
-            const int pb = all_segs % S::PBUFS, turn = all_segs / S::PBUFS;
-            ++all_segs;
+        for (int seg = 0;; ++seg) {
+            const int qs = seg % S::QS;
+            if (!(ok = warp_wait(q_full(qs), (seg / S::QS) & 1, abort_flag))) break;
+            const Q8Seg g = segs_at[qs];
+            if (g.nb < 0) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_empty(qs));
+            const int pb = seg % S::PBUFS, turn = seg / S::PBUFS;
             if (!(ok = warp_wait(p_full(pb), turn & 1, abort_flag))) break;
             const int slotp = blockIdx.x * 2 + (g.b0 > 0 ? 0 : 1), e = (lane % LPR) * 4;
             for (int row = lane / LPR; row < g.n_tok * G; row += 32 / LPR) {
@@ -531,7 +599,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                 }
                 if (g.whole) {
                     const float inv = L > 0.f ? 1.0f / L : L;  // nothing seen: 0; NaN stays NaN
-                    const int t = row / G;
+                    const int t = (int)(row * by_group >> 16);
                     OutRow<T>::put(a.out.p, (long long)(g.tok0 + t) * a.out.token_stride + (long long)(g.head * G + row - t * G) * a.out.head_stride + e, o, inv);
                 } else {
                     const size_t at = (size_t)slotp * ta.rows_cap + row;
@@ -541,7 +609,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
             }
             if (!g.whole && g.b0 == 0) {
                 // the unit goes on in the next CTAs: up to the one that holds its last tile
-                if (lane == 0) ta.records[blockIdx.x] = make_int4(g.tok0, g.n_tok, g.head, (int)(((long long)g.unit_end * n_ranges + total - 1) / total - 1));
+                if (lane == 0) ta.records[blockIdx.x] = make_int4(g.tok0, g.n_tok, g.head, g.last_cta);
                 recorded = true;
             }
             __syncwarp();
@@ -551,36 +619,6 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
     }
     __syncthreads();
     if (tid == 0 && *abort_flag) paged_report(a.kv, kStWaitLimit);
-}
-
-// Adds up the parts of the units that range boundaries cut, in the order of the CTAs that left them.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) q8_join_kernel(const __grid_constant__ TcArgs ta) {
-    grid_dep_wait();
-    const PagedAttnArgs& a = ta.a;
-    const int4 rec = ta.records[blockIdx.x];  // first token, tokens, head, last CTA
-    const int c0 = blockIdx.x, c1 = min(rec.w, (int)gridDim.x - 1);
-    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rec.y * a.group * (D / 4); i += gridDim.y * blockDim.x) {
-        const int row = i / (D / 4), e = (i - row * (D / 4)) * 4, t = row / a.group;
-        auto at = [&](int c) { return (size_t)(c * 2 + (c == c0 ? 1 : 0)) * ta.rows_cap + row; };
-        float M = -INFINITY, L = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at(c) * 2);
-            const float4 p = *reinterpret_cast<const float4*>(a.part_o + at(c) * D + e);
-            const float mn = fmaxf(M, ml.x), ref = softmax_ref(mn);
-            const float f0 = ex2_approx((M - ref) * a.scale_log2), f = ex2_approx((ml.x - ref) * a.scale_log2);
-            M = mn;
-            L = fmaf(ml.y, f, L * f0);
-            o.x = fmaf(p.x, f, o.x * f0);
-            o.y = fmaf(p.y, f, o.y * f0);
-            o.z = fmaf(p.z, f, o.z * f0);
-            o.w = fmaf(p.w, f, o.w * f0);
-        }
-        const int h = rec.z * a.group + row - t * a.group;
-        OutRow<T>::put(a.out.p, (long long)(rec.x + t) * a.out.token_stride + (long long)h * a.out.head_stride + e, o, L > 0.f ? 1.0f / L : L);
-    }
 }
 
 struct Q8UnpackArgs {

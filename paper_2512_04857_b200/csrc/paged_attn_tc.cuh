@@ -386,7 +386,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         if (tid == 0) out[0] = 0;
         __syncthreads();
     };
-    if (ta.split) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
+    if (PART) {  // (own slots: behind the kernel that makes start; slots in common: beside the one of the own slots, see the end)
+        if (!a.kv.row_of) grid_dep_wait();
+        grid_dep_launch();
+    }
+    if (!PART && ta.split) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
     const bool by_tiles = NT == 1 && ta.split;  // every unit may be cut: its slot tiles are all that is counted
     {
         int sum = 0;
@@ -869,10 +873,11 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
     tc_fence_after();
     if (warp == S::SM_WARPS) tc_dealloc(tmem, S::TMEM_COLS);
     if (tid == 0 && *abort_flag) paged_report(a.kv, kStWaitLimit);
+    if (PART && a.kv.row_of) grid_dep_wait();  // (who waits for this kernel's end has waited for the other's)
 }
 
 // Adds up the parts of the units that range boundaries cut, in the order of the CTAs that left them.
-template <int D, int NT, bool PART = false>
+template <int D, int NT>
 __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant__ TcArgs ta) {
     grid_dep_wait();
     const PagedAttnArgs& a = ta.a;
@@ -900,12 +905,6 @@ __global__ void __launch_bounds__(128) join_ranges_kernel(const __grid_constant_
         }
         const float inv = L > 0.f ? 1.0f / L : L;
         const int h = rec.z * a.group + unit_row - t * a.group;
-        if (PART) {
-            const size_t to = (size_t)(rec.x + t) * (a.kv.n_kv_heads * a.group) + h;
-            *reinterpret_cast<float4*>(a.row_o + to * D + e) = o;
-            if (e == 0) *reinterpret_cast<float2*>(a.row_ml + to * 2) = make_float2(M, L);
-            continue;
-        }
         __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.out.p) + (long long)(rec.x + t) * a.out.token_stride + (long long)h * a.out.head_stride + e;
         *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
     }

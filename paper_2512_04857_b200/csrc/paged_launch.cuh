@@ -12,6 +12,8 @@
 
 namespace lar {
 
+constexpr int kPartItems = 3;  // slot tiles that a range has at least where its rows are joined with others anyway
+
 struct AttnPlan {
     int tq;        // tokens of a row tile
     int nt;        // bf16: row tiles of a CTA (0: the kernel for few rows)
@@ -28,7 +30,8 @@ size_t tc_smem(int d, int rows_cap, int stages, int n_seqs) {
     return d == 64 ? TcSmem<64, NT>::bytes(rows_cap, stages, n_seqs) : TcSmem<128, NT>::bytes(rows_cap, stages, n_seqs);
 }
 
-inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, bool split) {
+// least: fp32, slots that a CTA has at least where a unit's slots are spread over several.
+inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, bool split, int64_t least = 256) {
     AttnPlan p;
     memset(&p, 0, sizeof(p));
     const int64_t chunk = max_chunk > 0 ? max_chunk : (n_tokens + k.n_seqs - 1) / k.n_seqs;
@@ -96,7 +99,7 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
     if (split) {
         const int64_t units = (int64_t)p.tiles * k.n_kv_heads;
         int64_t s = (12 * kSms + units - 1) / units;  // four rounds of three CTAs per SM: the last one costs little
-        if (s > (len + 255) / 256) s = (len + 255) / 256;  // at least 256 slots each
+        if (s > (len + least - 1) / least) s = (len + least - 1) / least;
         if (s > 64) s = 64;
         // Few rows: short units that fill the SMs by themselves are not worth joining (one token, 8 KV heads, cut / whole: 37 sequences of up
         // to 577 slots 25.8 / 24.3 us, with 128-element rows 42.5 / 39.8, 16 of them 31.6 / 42.1; 64 sequences 37.4 / 32.0, of up to 1153
@@ -111,7 +114,7 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
 // Workspace of a call and of every smaller one: the largest need over the launch shapes that attn_plan may choose for at most these
 // sequences, tokens, tokens of a chunk (0: n_tokens) and entries (0: what the table holds).  A call's own need goes up and down with its
 // sizes (fewer units are cut into more parts), and a program has one workspace for all of its calls.
-inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len) {
+inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, int64_t least = 256) {
     const int64_t chunk = max_chunk > 0 ? max_chunk : n_tokens;
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
@@ -139,7 +142,7 @@ inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n
     // two splits or more only where there are fewer than 12 kSms units
     const int bm = chunk * group <= 8 ? 8 : chunk * group <= 16 ? 16 : 64;
     const int64_t spread = 12ll * kSms * (bm / group) / k.n_kv_heads, n = n_tokens < spread ? n_tokens : spread;
-    int64_t s = (len + 255) / 256;
+    int64_t s = (len + least - 1) / least;
     s = s > 64 ? 64 : s;
     if (s < 2) return 0;
     const int64_t rows = s * n < spread + n ? s * n : spread + n;
@@ -171,14 +174,14 @@ inline lar_status_t make_maps(const lar_paged_kv_t& k, const PagedAttnArgs& a, i
     const cuuint64_t qdim[4] = {d, (cuuint64_t)a.group, (cuuint64_t)k.n_kv_heads, (cuuint64_t)a.kv.n_tokens};
     const int64_t qst[3] = {a.q.head_stride, a.q.head_stride * a.group, a.q.token_stride};
     const cuuint32_t qbox[4] = {64, (cuuint32_t)a.group, 1, (cuuint32_t)a.tq};
-    lar_status_t st = encode_map_4d(&m.q, kMapBf16, 128, a.q.p, qdim, qst, qbox);
+    lar_status_t st = encode_map<4>(&m.q, kMapBf16, 128, a.q.p, qdim, qst, qbox);
     const int heads = k.head_stride > 0 ? k.n_kv_heads : 1;  // heads with pages of their own: every page is one head's
     const int64_t page_stride = k.n_pages > 1 ? k.page_stride : k.row_stride * k.page_tokens * heads;
     const cuuint64_t kdim[4] = {d, (cuuint64_t)k.page_tokens, (cuuint64_t)heads, (cuuint64_t)k.n_pages};
     const int64_t kst[3] = {k.row_stride, heads > 1 ? k.head_stride : page_stride, page_stride};
     const cuuint32_t kbox[4] = {64, (cuuint32_t)box_rows, 1, 1};
-    if (st == LAR_OK) st = encode_map_4d(&m.k, kMapBf16, 128, k.k_pool, kdim, kst, kbox);
-    if (st == LAR_OK) st = encode_map_4d(&m.v, kMapBf16, 128, k.v_pool, kdim, kst, kbox);
+    if (st == LAR_OK) st = encode_map<4>(&m.k, kMapBf16, 128, k.k_pool, kdim, kst, kbox);
+    if (st == LAR_OK) st = encode_map<4>(&m.v, kMapBf16, 128, k.v_pool, kdim, kst, kbox);
     return st;
 }
 
@@ -206,7 +209,7 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const PagedAttnArgs& a, const At
     t.rows_cap = p.rows_cap;
     t.box_rows = k.page_tokens < S::BN ? k.page_tokens : S::BN;
     t.split = p.splits == 2;
-    t.min_items = 6;
+    t.min_items = PART ? kPartItems : 6;
     if (p.splits == 3) {
         t.counter = reinterpret_cast<int*>(a.part_o);
         LAR_CUDA(cudaMemsetAsync(t.counter, 0, sizeof(int), s));
@@ -231,20 +234,25 @@ lar_status_t launch_tc(const lar_paged_kv_t& k, const PagedAttnArgs& a, const At
         }();
         if (regs * 3 < 2 * TcShape<D, 2>::SM_REGS + TcShape<D, 2>::OTHER_REGS) return LAR_ERR_CUDA;
     }
-    fn<<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
-    LAR_CUDA(cudaGetLastError());
-    if (t.split) {
-        cudaLaunchConfig_t lc;
-        memset(&lc, 0, sizeof(lc));
+    // A kernel whose rows are joined elsewhere is launched before its predecessor's end: it waits for it by itself (the joining kernel likewise).
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)p.grid, 1, 1);
+    lc.blockDim = dim3(S::THREADS, 1, 1);
+    lc.dynamicSmemBytes = p.smem;
+    lc.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &at;
+    lc.numAttrs = PART ? 1 : 0;
+    LAR_CUDA(cudaLaunchKernelEx(&lc, fn, (const TcArgs)t, (const TcMaps)m));
+    if (t.split && !PART) {
         lc.gridDim = dim3((unsigned)p.grid, (unsigned)((NT * p.rows_cap * (D / 4) + 511) / 512), 1);
         lc.blockDim = dim3(128, 1, 1);
-        lc.stream = s;
-        cudaLaunchAttribute at;
-        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at.val.programmaticStreamSerializationAllowed = 1;
-        lc.attrs = &at;
+        lc.dynamicSmemBytes = 0;
         lc.numAttrs = 1;
-        LAR_CUDA(cudaLaunchKernelEx(&lc, join_ranges_kernel<D, NT, PART>, (const TcArgs)t));
+        LAR_CUDA(cudaLaunchKernelEx(&lc, join_ranges_kernel<D, NT>, (const TcArgs)t));
     }
     return LAR_OK;
 }

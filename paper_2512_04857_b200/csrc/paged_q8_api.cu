@@ -47,10 +47,12 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
         p.rows_cap = p.tq * group;
         p.nr = p.rows_cap > 8 ? 2 : 1;
         p.smem = rows_dtype == LAR_BF16 ? few_smem<__nv_bfloat16>(d, p.nr, k.n_seqs) : few_smem<float>(d, p.nr, k.n_seqs);
-        const int fit = (int)(233472 / (p.smem + 1024)), want = 2;
+        const int fit = (int)(233472 / (p.smem + 1024)), want = d == 64 && p.nr == 1 ? 3 : 2;  // Q8Shape::PER_SM
         p.grid = (fit < want ? fit : want) * kSms;
-        // Units of few slots, or short ones that fill the SMs, stay whole: joining costs a launch.
-        p.split = split && len > 384 && (len > 640 || with_tokens * k.n_kv_heads < 2 * kSms);
+        // Units of few slots, or short ones in some number, stay whole: joining costs a launch (one token, 8 KV heads of 128, cut / whole: up to 300 slots 4
+        // sequences 10.3 / 9.5 us, 64 20.5 / 17.3; up to 577: 4 sequences 10.3 / 12.3, 16 13.6 / 13.0, 64 27.4 / 24.7; up to 1153: 64 of unlike
+        // length 25.4 / 28.7, with 20 heads 46.6 / 57.9).
+        p.split = split && len > 384 && (len > 640 || with_tokens * k.n_kv_heads < kSms / 2);
         if (p.split) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         return p;
     }
@@ -85,7 +87,7 @@ lar_paged_kv_t unpacked(const lar_paged_kv_t& k, int rows_dtype, const Q8Plan& p
 }
 
 template <typename T, int D, int NR>
-lar_status_t launch_few(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q8View& q8, const Q8Plan& p, cudaStream_t s) {
+lar_status_t launch_few(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q8Plan& p, cudaStream_t s) {
     using S = Q8Shape<T, D, NR>;
     const lar_paged_kv_t& k = c.kv;
     TcArgs t;
@@ -94,7 +96,7 @@ lar_status_t launch_few(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q
     t.rows_cap = p.rows_cap;
     t.box_rows = k.page_tokens < S::KT ? k.page_tokens : S::KT;
     t.split = p.split;
-    t.min_items = 6;
+    t.min_items = 192 / S::KT;
     if (t.split) {  // records, then (m, l), then O of every CTA's two parts
         t.records = reinterpret_cast<int4*>(a.part_o);
         t.a.part_ml = reinterpret_cast<float*>(t.records + p.grid);
@@ -107,37 +109,44 @@ lar_status_t launch_few(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q
     const cuuint64_t qdim[4] = {(cuuint64_t)D, (cuuint64_t)a.group, (cuuint64_t)k.n_kv_heads, (cuuint64_t)a.kv.n_tokens};
     const int64_t qst[3] = {a.q.head_stride, a.q.head_stride * a.group, a.q.token_stride};
     const cuuint32_t qbox[4] = {(cuuint32_t)D, (cuuint32_t)a.group, 1, (cuuint32_t)a.tq};
-    lar_status_t st = encode_map_4d(&m.q, sizeof(T) == 2 ? kMapBf16 : kMapFp32, 0, a.q.p, qdim, qst, qbox);
+    lar_status_t st = encode_map<4>(&m.q, sizeof(T) == 2 ? kMapBf16 : kMapFp32, 0, a.q.p, qdim, qst, qbox);
     const int heads = k.head_stride > 0 ? k.n_kv_heads : 1;  // heads with pages of their own: every page is one head's
     const int64_t page_stride = k.n_pages > 1 ? k.page_stride : k.row_stride * k.page_tokens * heads;
-    const cuuint64_t kdim[4] = {(cuuint64_t)D, (cuuint64_t)k.page_tokens, (cuuint64_t)heads, (cuuint64_t)k.n_pages};
-    const int64_t kst[3] = {k.row_stride, heads > 1 ? k.head_stride : page_stride, page_stride};
-    const cuuint32_t kbox[4] = {(cuuint32_t)D, (cuuint32_t)t.box_rows, 1, 1};
-    if (st == LAR_OK) st = encode_map_4d(&m.k, kMapBytes, D, k.k_pool, kdim, kst, kbox);
-    if (st == LAR_OK) st = encode_map_4d(&m.v, kMapBytes, D, k.v_pool, kdim, kst, kbox);
+    const int64_t scale_stride = k.n_pages > 1 ? c.scale_page_stride : (int64_t)k.page_tokens * heads;
+    char *kp = static_cast<char*>(k.k_pool), *vp = static_cast<char*>(k.v_pool);
+    m.v_first = vp < kp;
+    m.v_scale_first = c.v_scale < c.k_scale;
+    const cuuint64_t dim[5] = {(cuuint64_t)D, (cuuint64_t)k.page_tokens, (cuuint64_t)heads, (cuuint64_t)k.n_pages, 2};
+    const int64_t kst[4] = {k.row_stride, heads > 1 ? k.head_stride : page_stride, page_stride, m.v_first ? kp - vp : vp - kp};
+    const cuuint32_t kbox[5] = {(cuuint32_t)D, (cuuint32_t)t.box_rows, 1, 1, 2};
+    if (st == LAR_OK) st = encode_map<5>(&m.kv, kMapBytes, D, m.v_first ? vp : kp, dim, kst, kbox, k.row_stride == D ? 256 : D);  // (what lies beside a row is another head's)
+    const cuuint64_t sdim[4] = {dim[1], dim[2], dim[3], 2};
+    const int64_t sst[3] = {heads > 1 ? c.scale_head_stride : scale_stride, scale_stride, m.v_scale_first ? c.k_scale - c.v_scale : c.v_scale - c.k_scale};
+    const cuuint32_t sbox[4] = {(cuuint32_t)t.box_rows, 1, 1, 2};
+    if (st == LAR_OK) st = encode_map<4>(&m.scale, kMapBytes, 0, m.v_scale_first ? c.v_scale : c.k_scale, sdim, sst, sbox);
     if (st != LAR_OK) return st;
-    fn<<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, q8, m);
+    fn<<<(unsigned)p.grid, S::THREADS, p.smem, s>>>(t, m);
     LAR_CUDA(cudaGetLastError());
     if (t.split) {
         cudaLaunchConfig_t lc;
         memset(&lc, 0, sizeof(lc));
-        lc.gridDim = dim3((unsigned)p.grid, (unsigned)((p.rows_cap * (D / 4) + 511) / 512), 1);
-        lc.blockDim = dim3(128, 1, 1);
+        lc.gridDim = dim3((unsigned)p.grid, join_ctas(p.rows_cap), 1);
+        lc.blockDim = dim3(kJoinThreads, 1, 1);
         lc.stream = s;
         cudaLaunchAttribute at;
         at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at.val.programmaticStreamSerializationAllowed = 1;
         lc.attrs = &at;
         lc.numAttrs = 1;
-        LAR_CUDA(cudaLaunchKernelEx(&lc, q8_join_kernel<T, D>, (const TcArgs)t));
+        LAR_CUDA(cudaLaunchKernelEx(&lc, join_parts_kernel<T, D, 1>, (const TcArgs)t));
     }
     return LAR_OK;
 }
 
 template <typename T>
-lar_status_t launch_few_of(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q8View& q8, const Q8Plan& p, cudaStream_t s) {
-    if (c.kv.head_dim == 64) return p.nr == 1 ? launch_few<T, 64, 1>(c, a, q8, p, s) : launch_few<T, 64, 2>(c, a, q8, p, s);
-    return p.nr == 1 ? launch_few<T, 128, 1>(c, a, q8, p, s) : launch_few<T, 128, 2>(c, a, q8, p, s);
+lar_status_t launch_few_of(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q8Plan& p, cudaStream_t s) {
+    if (c.kv.head_dim == 64) return p.nr == 1 ? launch_few<T, 64, 1>(c, a, p, s) : launch_few<T, 64, 2>(c, a, p, s);
+    return p.nr == 1 ? launch_few<T, 128, 1>(c, a, p, s) : launch_few<T, 128, 2>(c, a, p, s);
 }
 
 }  // namespace
@@ -205,7 +214,7 @@ lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, cons
         a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d)) * 1.4426950408889634f;
         a.n_splits = 1;
         a.part_o = static_cast<float*>(workspace);
-        return rows_dtype == LAR_BF16 ? launch_few_of<__nv_bfloat16>(*cache, a, q8, p, s) : launch_few_of<float>(*cache, a, q8, p, s);
+        return rows_dtype == LAR_BF16 ? launch_few_of<__nv_bfloat16>(*cache, a, p, s) : launch_few_of<float>(*cache, a, p, s);
     }
     for (int s0 = 0; s0 < k.n_seqs; s0 += p.batch) {
         const int n = k.n_seqs - s0 < p.batch ? k.n_seqs - s0 : p.batch;

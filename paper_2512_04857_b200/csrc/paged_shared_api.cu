@@ -15,6 +15,9 @@ using namespace lar;
 // share a read).
 constexpr int kSharedRows = 128;
 
+// fp32: slots in common that a CTA has at least (16 tokens of 4 heads a group, 2 groups, 4 KV heads, up to 4160 slots in common: 54 us with 256).
+constexpr int64_t kSharedLeast = 64;
+
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct SharedPlan {
@@ -42,8 +45,14 @@ SharedPlan shared_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int
     p.apart = chunk * group <= kSharedRows && n_tokens * group <= (int64_t)k.n_seqs * kSharedRows;
     if (!p.apart) return p;
     const int64_t per_group = (n_tokens + n_groups - 1) / n_groups;
-    p.pass[0] = attn_plan(groups_of(k, n_groups), group, n_tokens, (int)per_group, max_shared > 0 && max_shared < cap ? max_shared : (int)cap, true);
+    p.pass[0] = attn_plan(groups_of(k, n_groups), group, n_tokens, (int)per_group, max_shared > 0 && max_shared < cap ? max_shared : (int)cap, true, kSharedLeast);
     p.pass[1] = attn_plan(k, group, n_tokens, (int)chunk, (int)own_len(cap, max_len, max_shared), true);
+    if (k.dtype == LAR_BF16)
+        for (AttnPlan& w : p.pass)
+            if (w.splits == 3) {  // (whole units round-robin: the counter of units on demand is cleared by a copy between the kernels)
+                w.splits = 1;
+                w.bytes = 0;
+            }
     p.ints = up256(((size_t)n_groups * 3 + 1 + k.n_seqs) * sizeof(int));
     const size_t row = (size_t)hq * (d + 2) * sizeof(float);
     if (k.dtype == LAR_BF16) {
@@ -80,7 +89,7 @@ size_t lar_paged_attn_shared_workspace_bytes(const lar_paged_kv_t* kv, int n_q_h
     const int64_t most = (int64_t)kv->n_seqs * kSharedRows / group, n = n_tokens < most ? n_tokens : most;
     if (n < 1) return whole;
     const size_t row = (size_t)n_q_heads * (d + 2) * sizeof(float), ints = up256(((size_t)n_groups * 3 + 1 + kv->n_seqs) * sizeof(int));
-    const size_t a = attn_workspace_bound(groups_of(*kv, n_groups), group, n, (int)n, max_shared);
+    const size_t a = attn_workspace_bound(groups_of(*kv, n_groups), group, n, (int)n, max_shared, kSharedLeast);
     const size_t b = attn_workspace_bound(*kv, group, n, (int)(chunk < n ? chunk : n), max_len);
     // (fp32: one part at least; the bounds hold from two parts on)
     const size_t rows = (size_t)n * row;
@@ -133,10 +142,13 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
     j.cu = pr.cu;
     j.n_groups = n_groups;
     j.hq = n_q_heads;
+    j.group = group;
     j.scale_log2 = a.scale_log2;
     const lar_paged_kv_t kg = groups_of(*kv, n_groups);
-    for (int w = 0; w < 2; ++w) {
+    // The own slots first: as their CTAs end, those of the slots in common take their place.
+    for (int w = 1; w >= 0; --w) {
         const AttnPlan& plan = p.pass[w];
+        SharedPass& left = j.pass[w];
         PagedAttnArgs b = a;
         b.tq = plan.tq;
         b.n_splits = plan.splits;
@@ -157,27 +169,45 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
             b.row_ml = b.row_o + (size_t)n_tokens * n_q_heads * d;
             at += p.rows;
             b.part_o = reinterpret_cast<float*>(at);
-            at += w == 0 ? p.ws0 : p.ws1;
-            j.o[w] = b.row_o;
-            j.ml[w] = b.row_ml;
-            j.parts[w] = 1;
+            left.row_o = b.row_o;
+            left.row_ml = b.row_ml;
+            left.parts = 1;
+            left.nt = plan.nt == 2 ? 2 : 1;
+            left.tq = plan.tq;
+            left.rows_cap = plan.rows_cap;
+            if (plan.splits == 2) {  // as launch_tc lays it out
+                left.ranges = plan.grid;
+                left.records = reinterpret_cast<const int4*>(at);
+                left.part_ml = reinterpret_cast<const float*>(left.records + plan.grid);
+                left.part_o = left.part_ml + (size_t)plan.grid * 2 * left.nt * plan.rows_cap * 2;
+            }
             st = launch_bf16<true>(w == 0 ? kg : *kv, b, plan, s);
         } else {
             b.part_o = reinterpret_cast<float*>(at);
             b.part_ml = b.part_o + (size_t)plan.splits * n_tokens * n_q_heads * d;
-            at += w == 0 ? p.ws0 : p.ws1;
-            j.o[w] = b.part_o;
-            j.ml[w] = b.part_ml;
-            j.parts[w] = plan.splits;
+            left.row_o = b.part_o;
+            left.row_ml = b.part_ml;
+            left.parts = plan.splits;
             st = d == 64 ? launch_fp32<64>(b, plan, s, false) : launch_fp32<128>(b, plan, s, false);
         }
+        at += w == 0 ? p.ws0 : p.ws1;
         if (st != LAR_OK) return st;
     }
-    const int64_t threads = n_tokens * n_q_heads * (d / 4);
+    const int64_t warps = n_tokens * n_q_heads, ctas = (warps + kSharedJoinThreads / 32 - 1) / (kSharedJoinThreads / 32);
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)(ctas < 8 * kSms ? ctas : 8 * kSms), 1, 1);
+    lc.blockDim = dim3(kSharedJoinThreads, 1, 1);
+    lc.dynamicSmemBytes = (size_t)(j.pass[0].ranges + j.pass[1].ranges) * sizeof(int4);
+    lc.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = kv->dtype == LAR_BF16 ? 1 : 0;
     void (*fn)(const SharedJoinArgs) = kv->dtype == LAR_BF16 ? (d == 64 ? shared_join_kernel<__nv_bfloat16, 64> : shared_join_kernel<__nv_bfloat16, 128>)
                                                              : (d == 64 ? shared_join_kernel<float, 64> : shared_join_kernel<float, 128>);
-    fn<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(j);
-    LAR_CUDA(cudaGetLastError());
+    LAR_CUDA(cudaLaunchKernelEx(&lc, fn, (const SharedJoinArgs)j));
     return LAR_OK;
 }
 
