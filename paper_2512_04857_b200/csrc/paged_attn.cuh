@@ -29,6 +29,7 @@ struct PagedAttnArgs {
     int parts;         // fp32: rows are left as parts (split, or joined with another call's)
     float* row_o;      // kernels with PART: (O, m, l) of every (token, head) instead of its output row
     float* row_ml;
+    int2* row_ref;     // where a row's unit is cut: first range + 65536 * last, place among a range's rows; else -1 (row_o, row_ml hold the row)
 };
 
 // two fp32 operations in one instruction

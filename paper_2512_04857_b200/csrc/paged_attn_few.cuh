@@ -389,6 +389,11 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
                     o.z = fmaf(p.z, f, o.z);
                     o.w = fmaf(p.w, f, o.w);
                 }
+                if (PART && e == 0 && g.b0 == 0) {
+                    const int t = row / G;
+                    a.row_ref[(size_t)(g.tok0 + t) * (a.kv.n_kv_heads * G) + g.head * G + row - t * G] =
+                        make_int2(g.whole ? -1 : (int)blockIdx.x + 65536 * (int)(((long long)g.unit_end * n_ranges + total - 1) / total - 1), row);
+                }
                 if (PART && g.whole) {
                     const int t = row / G;
                     const size_t at = (size_t)(g.tok0 + t) * (a.kv.n_kv_heads * G) + g.head * G + row - t * G;

@@ -675,6 +675,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
                     }
                     __syncwarp();  // (tcgen05.ld is a warp-wide instruction: all lanes together again)
                 }
+                if (PART && mine && g.b0 == 0) a.row_ref[all] = make_int2(g.whole ? -1 : (int)blockIdx.x + 65536 * g.unit_end, tile * ta.rows_cap + row);
                 if (mine && !done) {
                     float* ml = PART && g.whole ? a.row_ml + all * 2 : a.part_ml + part * 2;
                     ml[0] = m_used;  // (-inf: nothing seen)

@@ -12,7 +12,8 @@
 
 namespace lar {
 
-constexpr int kPartItems = 3;  // slot tiles that a range has at least where its rows are joined with others anyway
+// Where rows are joined with others anyway: slot tiles that a range has at least (bf16), slots that a CTA has (fp32).
+constexpr int kPartItems = 3, kPartSlots = 64;
 
 struct AttnPlan {
     int tq;        // tokens of a row tile
@@ -30,8 +31,8 @@ size_t tc_smem(int d, int rows_cap, int stages, int n_seqs) {
     return d == 64 ? TcSmem<64, NT>::bytes(rows_cap, stages, n_seqs) : TcSmem<128, NT>::bytes(rows_cap, stages, n_seqs);
 }
 
-// least: fp32, slots that a CTA has at least where a unit's slots are spread over several.
-inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, bool split, int64_t least = 256) {
+// joined: the rows are joined with others behind the kernel anyway, so that cutting a unit costs no launch.
+inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, bool split, bool joined = false) {
     AttnPlan p;
     memset(&p, 0, sizeof(p));
     const int64_t chunk = max_chunk > 0 ? max_chunk : (n_tokens + k.n_seqs - 1) / k.n_seqs;
@@ -57,7 +58,7 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
             // Units of few slots, or short ones that fill the SMs, stay whole: joining costs a launch (one token, 8 KV heads, cut / whole: 1 to
             // 64 sequences of up to 300 slots 8.3 / 7.7 to 12.1 / 9.0 us; up to 577 slots: 4 sequences 9.4 / 10.8, 64 14.6 / 12.0; up to 1153:
             // 37 15.2 / 17.9, 64 of unlike length 15.9 / 18.5).
-            const bool cut = split && len > 384 && (len > 640 || with_tokens * k.n_kv_heads < 2 * kSms);
+            const bool cut = split && (joined ? len > 128 : len > 384 && (len > 640 || with_tokens * k.n_kv_heads < 2 * kSms));
             p.splits = cut ? 2 : 1;
             if (cut) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
             return p;
@@ -85,7 +86,7 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
         // that make up much of their cache); long units are cut where a few rounds of whole ones would leave CTAs idle.
         const int64_t units = (n_tokens / (p.tq * p.nt) + with_tokens) * k.n_kv_heads;
         p.splits = 1;
-        if (split && (p.nt == 1 ? len > 1280 : units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
+        if (split && (p.nt == 1 ? len > (joined ? 128 : 1280) : units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
         else if (split && p.nt == 2 && units > p.grid) p.splits = 3;
         if (p.splits == 2) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         if (p.splits == 3) p.bytes = sizeof(int4);
@@ -99,12 +100,13 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
     if (split) {
         const int64_t units = (int64_t)p.tiles * k.n_kv_heads;
         int64_t s = (12 * kSms + units - 1) / units;  // four rounds of three CTAs per SM: the last one costs little
+        const int64_t least = joined ? kPartSlots : 256;  // slots that a CTA has at least
         if (s > (len + least - 1) / least) s = (len + least - 1) / least;
         if (s > 64) s = 64;
         // Few rows: short units that fill the SMs by themselves are not worth joining (one token, 8 KV heads, cut / whole: 37 sequences of up
         // to 577 slots 25.8 / 24.3 us, with 128-element rows 42.5 / 39.8, 16 of them 31.6 / 42.1; 64 sequences 37.4 / 32.0, of up to 1153
         // slots 60 / 58, with 128-element rows 103 / 112).
-        if (p.bm < 64 && len <= 768 && units >= 2 * kSms) s = 1;
+        if (!joined && p.bm < 64 && len <= 768 && units >= 2 * kSms) s = 1;
         p.splits = s < 1 ? 1 : (int)s;
     }
     p.bytes = p.splits > 1 ? (size_t)p.splits * n_tokens * k.n_kv_heads * group * (d + 2) * sizeof(float) : 0;
@@ -114,7 +116,7 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
 // Workspace of a call and of every smaller one: the largest need over the launch shapes that attn_plan may choose for at most these
 // sequences, tokens, tokens of a chunk (0: n_tokens) and entries (0: what the table holds).  A call's own need goes up and down with its
 // sizes (fewer units are cut into more parts), and a program has one workspace for all of its calls.
-inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, int64_t least = 256) {
+inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n_tokens, int max_chunk, int max_len, bool joined = false) {
     const int64_t chunk = max_chunk > 0 ? max_chunk : n_tokens;
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
@@ -127,13 +129,13 @@ inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n
         auto take = [&](size_t n) { most = n > most ? n : most; };
         // few rows: each chunk length is a launch shape; where any length up to len is cut, one near len is
         for (int64_t c = 1; c <= chunk && c * group <= few; ++c) {
-            AttnPlan p = attn_plan(one, group, 1, (int)c, len > 640 ? 641 : (int)len, true);
+            AttnPlan p = attn_plan(one, group, 1, (int)c, len > 640 ? 641 : (int)len, true, joined);
             take(p.bytes);
         }
         // one row tile (of two CTAs per SM at most), then two: their rows are bounded by the 128 of a tile
         const int64_t t1 = chunk < 128 / group ? chunk : 128 / group;
         const size_t part = (size_t)(d + 2) * sizeof(float), rows = (size_t)(t1 * group + 7) / 8 * 8, rows2 = (size_t)(128 / group * group + 7) / 8 * 8;
-        if (chunk * group > few && len > 1280) take(2 * kSms * (sizeof(int4) + 2 * rows * part));
+        if (chunk * group > few && len > (joined ? 128 : 1280)) take(2 * kSms * (sizeof(int4) + 2 * rows * part));
         if (chunk * group > 128 || (d == 128 && chunk * group > 32 && len >= 2048))
             take(len >= 2048 ? kSms * (sizeof(int4) + 4 * rows2 * part) : sizeof(int4));
         return most;
@@ -142,6 +144,7 @@ inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n
     // two splits or more only where there are fewer than 12 kSms units
     const int bm = chunk * group <= 8 ? 8 : chunk * group <= 16 ? 16 : 64;
     const int64_t spread = 12ll * kSms * (bm / group) / k.n_kv_heads, n = n_tokens < spread ? n_tokens : spread;
+    const int64_t least = joined ? kPartSlots : 256;
     int64_t s = (len + least - 1) / least;
     s = s > 64 ? 64 : s;
     if (s < 2) return 0;

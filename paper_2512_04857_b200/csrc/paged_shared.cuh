@@ -61,15 +61,15 @@ static __global__ void __launch_bounds__(kSharedPrepThreads) shared_prep_kernel(
         for (int s = s1 + tid; s < S; s += kSharedPrepThreads) a.start[s] = 0;
 }
 
-// What one of the two passes left: rows of whole units in row_o, row_ml ([n_tokens][hq][d]; parts of them behind one another where parts > 1); of the
-// units that range boundaries cut the parts, as join_parts_kernel finds them.
+// What one of the two passes left: rows of whole units in row_o, row_ml ([n_tokens][hq][d]; parts of them behind one another where parts > 1); of the units
+// that range boundaries cut the parts of every CTA, as join_parts_kernel finds them, and in row_ref which CTAs'.
 struct SharedPass {
     const float* row_o;
     const float* row_ml;
-    const int4* records;  // null: nothing is cut
+    const int2* row_ref;  // null: nothing is cut
     const float* part_o;
     const float* part_ml;
-    int parts, ranges, nt, tq, rows_cap;
+    int parts, range_rows;  // rows that a range leaves
 };
 
 struct SharedJoinArgs {
@@ -83,59 +83,63 @@ struct SharedJoinArgs {
 
 constexpr int kSharedJoinThreads = 256;
 
-// A row per warp, the slots in common first.  Bound by latency: a few MB at most.
+// A row has 1, 2, 4 or 8 warps, as many as the grid has for it, and each of them every so many-th part.  Bound by latency: a few MB at most.
 template <typename T, int D>
 __global__ void __launch_bounds__(kSharedJoinThreads) shared_join_kernel(const __grid_constant__ SharedJoinArgs a) {
-    constexpr int LPR = D / 4, HALVES = 32 / LPR;
-    extern __shared__ int4 rec[];  // of both passes
+    constexpr int LPR = D / 4, HALVES = 32 / LPR, WARPS = kSharedJoinThreads / 32;
+    __shared__ PartSum sums[WARPS][LPR];
     grid_dep_wait();
-    for (int i = threadIdx.x; i < a.pass[0].ranges + a.pass[1].ranges; i += kSharedJoinThreads)
-        rec[i] = i < a.pass[0].ranges ? a.pass[0].records[i] : a.pass[1].records[i - a.pass[0].ranges];
-    const int lane = threadIdx.x & 31, e = (lane % LPR) * 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = (lane % LPR) * 4;
     const long long n_rows = (long long)a.kv.n_tokens * a.hq;
     const int first = a.kv.cu ? a.kv.cu[0] : 0, end = a.kv.cu ? a.kv.cu[a.kv.n_seqs] : a.kv.n_tokens;  // (tokens of no sequence are left as they were)
     const int g0 = a.cu[0], g1 = a.cu[a.n_groups];
-    __syncthreads();
-    for (long long row = (long long)blockIdx.x * (kSharedJoinThreads / 32) + (threadIdx.x >> 5); row < n_rows; row += (long long)gridDim.x * (kSharedJoinThreads / 32)) {
-        const int t = (int)(row / a.hq), h = (int)(row - (long long)t * a.hq), kvh = h / a.group;
-        if (t < first || t >= end) continue;
+    int split = WARPS;  // warps of a row
+    while (split > 1 && n_rows * split > (long long)gridDim.x * WARPS) split >>= 1;
+    const int at_once = WARPS / split, part0 = (warp % split) * HALVES + lane / LPR, step = split * HALVES;
+    for (long long row0 = (long long)blockIdx.x * at_once; row0 < n_rows; row0 += (long long)gridDim.x * at_once) {  // (the same trips for all warps)
+        const long long row = row0 + warp / split;
+        const int t = (int)(row / a.hq), h = (int)(row - (long long)t * a.hq);
+        const bool mine = row < n_rows && t >= first && t < end;
         PartSum sum;
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
+        for (int w = 0; w < 2; ++w) {  // the slots in common first
             const SharedPass& p = a.pass[w];
-            if (w == 0 && (t < g0 || t >= g1)) continue;  // a sequence of no group
-            const int4* r = rec + (w ? a.pass[0].ranges : 0);
-            int range = -1;  // the range that the row's unit begins in, if it is cut
-            for (int c = lane; c < p.ranges; c += 32) {
-                const int4 u = r[c];
-                if (u.z == kvh && t >= u.x && t < u.x + u.y) range = c;
-            }
-            range = __reduce_max_sync(0xffffffffu, range);
-            if (range >= 0) {
-                const int4 u = r[range];
-                const int tu = t - u.x, tile = p.nt == 2 && tu >= p.tq ? 1 : 0, last = min(u.w, p.ranges - 1);
-                const int tile_row = (tu - tile * p.tq) * a.group + h - kvh * a.group;
-#pragma unroll 8
-                for (int c = range + lane / LPR; c <= last; c += HALVES) {
-                    const size_t at = ((size_t)(c * 2 + (c == range ? 1 : 0)) * p.nt + tile) * p.rows_cap + tile_row;
+            if (!mine || (w == 0 && (t < g0 || t >= g1))) continue;  // (a sequence of no group)
+            const int2 ref = p.row_ref ? p.row_ref[row] : make_int2(-1, 0);
+            if (ref.x >= 0) {
+                const int range = ref.x & 0xffff, last = ref.x >> 16;
+#pragma unroll 4
+                for (int c = range + part0; c <= last; c += step) {
+                    const size_t at = (size_t)(c * 2 + (c == range ? 1 : 0)) * p.range_rows + ref.y;
                     sum.add(*reinterpret_cast<const float2*>(p.part_ml + at * 2), *reinterpret_cast<const float4*>(p.part_o + at * D + e), a.scale_log2);
                 }
             } else {
-#pragma unroll 8
-                for (int s = lane / LPR; s < p.parts; s += HALVES) {
+#pragma unroll 4
+                for (int s = part0; s < p.parts; s += step) {
                     const long long at = s * n_rows + row;
                     sum.add(*reinterpret_cast<const float2*>(p.row_ml + at * 2), *reinterpret_cast<const float4*>(p.row_o + at * D + e), a.scale_log2);
                 }
             }
         }
         if (HALVES == 2) sum.add_lane(16, a.scale_log2);
-        if (lane >= LPR) continue;
-        const float inv = sum.L > 0.f ? 1.0f / sum.L : sum.L;  // nothing seen: 0; NaN stays NaN
-        char* dst = a.out.p + ((long long)t * a.out.token_stride + (long long)h * a.out.head_stride + e) * (long long)sizeof(T);
-        if (sizeof(T) == 4)
-            *reinterpret_cast<float4*>(dst) = make_float4(sum.o.x * inv, sum.o.y * inv, sum.o.z * inv, sum.o.w * inv);
-        else
-            *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(sum.o.x * inv, sum.o.y * inv), pack_bf16(sum.o.z * inv, sum.o.w * inv));
+        if (split > 1) {
+            if (lane < LPR) sums[warp][lane] = sum;
+            __syncthreads();
+            if (warp % split == 0 && lane < LPR)
+                for (int w = 1; w < split; ++w) {
+                    const PartSum& s = sums[warp + w][lane];
+                    sum.add(make_float2(s.M, s.L), s.o, a.scale_log2);
+                }
+        }
+        if (mine && warp % split == 0 && lane < LPR) {
+            const float inv = sum.L > 0.f ? 1.0f / sum.L : sum.L;  // nothing seen: 0; NaN stays NaN
+            char* dst = a.out.p + ((long long)t * a.out.token_stride + (long long)h * a.out.head_stride + e) * (long long)sizeof(T);
+            if (sizeof(T) == 4)
+                *reinterpret_cast<float4*>(dst) = make_float4(sum.o.x * inv, sum.o.y * inv, sum.o.z * inv, sum.o.w * inv);
+            else
+                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(sum.o.x * inv, sum.o.y * inv), pack_bf16(sum.o.z * inv, sum.o.w * inv));
+        }
+        if (split > 1) __syncthreads();
     }
 }
 

@@ -15,9 +15,6 @@ using namespace lar;
 // share a read).
 constexpr int kSharedRows = 128;
 
-// fp32: slots in common that a CTA has at least (16 tokens of 4 heads a group, 2 groups, 4 KV heads, up to 4160 slots in common: 54 us with 256).
-constexpr int64_t kSharedLeast = 64;
-
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct SharedPlan {
@@ -45,8 +42,8 @@ SharedPlan shared_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int
     p.apart = chunk * group <= kSharedRows && n_tokens * group <= (int64_t)k.n_seqs * kSharedRows;
     if (!p.apart) return p;
     const int64_t per_group = (n_tokens + n_groups - 1) / n_groups;
-    p.pass[0] = attn_plan(groups_of(k, n_groups), group, n_tokens, (int)per_group, max_shared > 0 && max_shared < cap ? max_shared : (int)cap, true, kSharedLeast);
-    p.pass[1] = attn_plan(k, group, n_tokens, (int)chunk, (int)own_len(cap, max_len, max_shared), true);
+    p.pass[0] = attn_plan(groups_of(k, n_groups), group, n_tokens, (int)per_group, max_shared > 0 && max_shared < cap ? max_shared : (int)cap, true, true);
+    p.pass[1] = attn_plan(k, group, n_tokens, (int)chunk, (int)own_len(cap, max_len, max_shared), true, true);
     if (k.dtype == LAR_BF16)
         for (AttnPlan& w : p.pass)
             if (w.splits == 3) {  // (whole units round-robin: the counter of units on demand is cleared by a copy between the kernels)
@@ -56,7 +53,7 @@ SharedPlan shared_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int
     p.ints = up256(((size_t)n_groups * 3 + 1 + k.n_seqs) * sizeof(int));
     const size_t row = (size_t)hq * (d + 2) * sizeof(float);
     if (k.dtype == LAR_BF16) {
-        p.rows = up256((size_t)n_tokens * row);
+        p.rows = up256((size_t)n_tokens * (row + hq * sizeof(int2)));
         p.ws0 = up256(p.pass[0].bytes);
         p.ws1 = up256(p.pass[1].bytes);
         p.bytes = p.ints + 2 * p.rows + p.ws0 + p.ws1;
@@ -88,9 +85,9 @@ size_t lar_paged_attn_shared_workspace_bytes(const lar_paged_kv_t* kv, int n_q_h
     // Apart: no more rows than the sequences have of the longest chunks that are taken apart; a pass is a call of its own with any lengths up to the bounds
     const int64_t most = (int64_t)kv->n_seqs * kSharedRows / group, n = n_tokens < most ? n_tokens : most;
     if (n < 1) return whole;
-    const size_t row = (size_t)n_q_heads * (d + 2) * sizeof(float), ints = up256(((size_t)n_groups * 3 + 1 + kv->n_seqs) * sizeof(int));
-    const size_t a = attn_workspace_bound(groups_of(*kv, n_groups), group, n, (int)n, max_shared, kSharedLeast);
-    const size_t b = attn_workspace_bound(*kv, group, n, (int)(chunk < n ? chunk : n), max_len);
+    const size_t row = (size_t)n_q_heads * ((d + 2) * sizeof(float) + (kv->dtype == LAR_BF16 ? sizeof(int2) : 0)), ints = up256(((size_t)n_groups * 3 + 1 + kv->n_seqs) * sizeof(int));
+    const size_t a = attn_workspace_bound(groups_of(*kv, n_groups), group, n, (int)n, max_shared, true);
+    const size_t b = attn_workspace_bound(*kv, group, n, (int)(chunk < n ? chunk : n), max_len, true);
     // (fp32: one part at least; the bounds hold from two parts on)
     const size_t rows = (size_t)n * row;
     const size_t apart = kv->dtype == LAR_BF16 ? ints + 2 * up256(rows) + up256(a) + up256(b) : ints + up256(a > rows ? a : rows) + up256(b > rows ? b : rows);
@@ -167,19 +164,17 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
         if (kv->dtype == LAR_BF16) {
             b.row_o = reinterpret_cast<float*>(at);
             b.row_ml = b.row_o + (size_t)n_tokens * n_q_heads * d;
+            b.row_ref = reinterpret_cast<int2*>(b.row_ml + (size_t)n_tokens * n_q_heads * 2);
             at += p.rows;
             b.part_o = reinterpret_cast<float*>(at);
             left.row_o = b.row_o;
             left.row_ml = b.row_ml;
             left.parts = 1;
-            left.nt = plan.nt == 2 ? 2 : 1;
-            left.tq = plan.tq;
-            left.rows_cap = plan.rows_cap;
+            left.range_rows = (plan.nt == 2 ? 2 : 1) * plan.rows_cap;
             if (plan.splits == 2) {  // as launch_tc lays it out
-                left.ranges = plan.grid;
-                left.records = reinterpret_cast<const int4*>(at);
-                left.part_ml = reinterpret_cast<const float*>(left.records + plan.grid);
-                left.part_o = left.part_ml + (size_t)plan.grid * 2 * left.nt * plan.rows_cap * 2;
+                left.row_ref = b.row_ref;
+                left.part_ml = reinterpret_cast<const float*>(reinterpret_cast<int4*>(at) + plan.grid);
+                left.part_o = left.part_ml + (size_t)plan.grid * 2 * left.range_rows * 2;
             }
             st = launch_bf16<true>(w == 0 ? kg : *kv, b, plan, s);
         } else {
@@ -193,12 +188,11 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
         at += w == 0 ? p.ws0 : p.ws1;
         if (st != LAR_OK) return st;
     }
-    const int64_t warps = n_tokens * n_q_heads, ctas = (warps + kSharedJoinThreads / 32 - 1) / (kSharedJoinThreads / 32);
+    const int64_t ctas = n_tokens * n_q_heads;
     cudaLaunchConfig_t lc;
     memset(&lc, 0, sizeof(lc));
-    lc.gridDim = dim3((unsigned)(ctas < 8 * kSms ? ctas : 8 * kSms), 1, 1);
+    lc.gridDim = dim3((unsigned)(ctas < 6 * kSms ? ctas : 6 * kSms), 1, 1);
     lc.blockDim = dim3(kSharedJoinThreads, 1, 1);
-    lc.dynamicSmemBytes = (size_t)(j.pass[0].ranges + j.pass[1].ranges) * sizeof(int4);
     lc.stream = s;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
