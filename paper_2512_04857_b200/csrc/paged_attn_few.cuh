@@ -80,8 +80,8 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
         *abort_flag = 0;
         mbar_fence_init_smem();
     }
-    if (PART) {  // (own slots: behind the kernel that makes start; slots in common: beside the one of the own slots, see the end)
-        if (!a.kv.row_of) grid_dep_wait();
+    if (PART) {  // (slots in common: behind the kernel that makes the groups; own slots: beside this one, see the end)
+        if (a.kv.row_of) grid_dep_wait();
         grid_dep_launch();
     }
     if (!PART && ta.split) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
     }
     __syncthreads();
     if (tid == 0 && *abort_flag) paged_report(a.kv, kStWaitLimit);
-    if (PART && a.kv.row_of) grid_dep_wait();  // (who waits for this kernel's end has waited for the other's)
+    if (PART && !a.kv.row_of) grid_dep_wait();  // (who waits for this kernel's end has waited for the other's)
 }
 
 }  // namespace lar

@@ -386,8 +386,8 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
         if (tid == 0) out[0] = 0;
         __syncthreads();
     };
-    if (PART) {  // (own slots: behind the kernel that makes start; slots in common: beside the one of the own slots, see the end)
-        if (!a.kv.row_of) grid_dep_wait();
+    if (PART) {  // (slots in common: behind the kernel that makes the groups; own slots: beside this one, see the end)
+        if (a.kv.row_of) grid_dep_wait();
         grid_dep_launch();
     }
     if (!PART && ta.split) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the joining kernel waits for this one's end)
@@ -874,7 +874,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
     tc_fence_after();
     if (warp == S::SM_WARPS) tc_dealloc(tmem, S::TMEM_COLS);
     if (tid == 0 && *abort_flag) paged_report(a.kv, kStWaitLimit);
-    if (PART && a.kv.row_of) grid_dep_wait();  // (who waits for this kernel's end has waited for the other's)
+    if (PART && !a.kv.row_of) grid_dep_wait();  // (who waits for this kernel's end has waited for the other's)
 }
 
 // Adds up the parts of the units that range boundaries cut, in the order of the CTAs that left them.

@@ -85,7 +85,7 @@ constexpr int kSharedJoinThreads = 256;
 
 // A row has 1, 2, 4 or 8 warps, as many as the grid has for it, and each of them every so many-th part.  Bound by latency: a few MB at most.
 template <typename T, int D>
-__global__ void __launch_bounds__(kSharedJoinThreads) shared_join_kernel(const __grid_constant__ SharedJoinArgs a) {
+__global__ void __launch_bounds__(kSharedJoinThreads, 4) shared_join_kernel(const __grid_constant__ SharedJoinArgs a) {
     constexpr int LPR = D / 4, HALVES = 32 / LPR, WARPS = kSharedJoinThreads / 32;
     __shared__ PartSum sums[WARPS][LPR];
     grid_dep_wait();

@@ -50,6 +50,23 @@ SharedPlan shared_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int
                 w.splits = 1;
                 w.bytes = 0;
             }
+    if (k.dtype == LAR_BF16 && p.pass[0].nt == 2) {
+        // Two row tiles have an SM to themselves: the passes run side by side, each on a share of the SMs as its work is (else one behind the other, the second's CTAs
+        // taking the place of the first's): microseconds of an SM for a slot of a unit, where two row tiles keep
+        // the tensor cores busy (2 us for 128 slots) or a slot's bytes pass (44 GB/s), and as many slots more as taking up a unit costs (TcWork).  Own
+        // lengths are taken as half of what they may be, few rows' bytes pass faster.  (64 images of one prompt, 8192 slots in common: 45 us, 51 one behind the other.)
+        auto work = [&](const AttnPlan& w, double units, double slots) {
+            const double cost = w.nt == 2 ? 256 : w.nt == 1 ? (d == 64 ? 192 : 128) : (d == 64 ? 256 : 128);
+            return units * k.n_kv_heads * (slots + cost) * (w.nt == 2 ? 2.0 / 128 : 4.0 * d / 44e3);
+        };
+        auto tiles = [](int64_t tokens, const AttnPlan& w) { return (tokens + w.tq * (w.nt == 2 ? 2 : 1) - 1) / (w.tq * (w.nt == 2 ? 2 : 1)); };
+        const double work0 = (p.pass[1].nt == 0 ? 1.5 : 1.0) * work(p.pass[0], (double)n_groups * tiles(per_group, p.pass[0]), (double)(max_shared > 0 && max_shared < cap ? max_shared : cap));
+        const double work1 = work(p.pass[1], (double)(n_tokens < k.n_seqs ? n_tokens : k.n_seqs) * tiles(chunk, p.pass[1]), own_len(cap, max_len, max_shared) / 2.0);
+        int share = (int)(kSms * work0 / (work0 + work1) + 0.5);
+        share = share < 8 ? 8 : share > kSms - 8 ? kSms - 8 : share;
+        p.pass[0].grid = p.pass[0].grid / kSms * share;
+        p.pass[1].grid = p.pass[1].grid / kSms * (kSms - share);
+    }
     p.ints = up256(((size_t)n_groups * 3 + 1 + k.n_seqs) * sizeof(int));
     const size_t row = (size_t)hq * (d + 2) * sizeof(float);
     if (k.dtype == LAR_BF16) {
@@ -142,8 +159,7 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
     j.group = group;
     j.scale_log2 = a.scale_log2;
     const lar_paged_kv_t kg = groups_of(*kv, n_groups);
-    // The own slots first: as their CTAs end, those of the slots in common take their place.
-    for (int w = 1; w >= 0; --w) {
+    for (int w = 0; w < 2; ++w) {
         const AttnPlan& plan = p.pass[w];
         SharedPass& left = j.pass[w];
         PagedAttnArgs b = a;
@@ -191,7 +207,7 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
     const int64_t ctas = n_tokens * n_q_heads;
     cudaLaunchConfig_t lc;
     memset(&lc, 0, sizeof(lc));
-    lc.gridDim = dim3((unsigned)(ctas < 6 * kSms ? ctas : 6 * kSms), 1, 1);
+    lc.gridDim = dim3((unsigned)(ctas < 4 * kSms ? ctas : 4 * kSms), 1, 1);
     lc.blockDim = dim3(kSharedJoinThreads, 1, 1);
     lc.stream = s;
     cudaLaunchAttribute attr;
