@@ -1,5 +1,6 @@
-// Attention over an 8-bit paged cache (paged_q8.cuh) for at most 16 (token, head of the group) rows of a KV head per unit: single tokens and
-// short candidate chunks.  Bound by the cache's bytes; one step below, by what turns codes into operands.
+// Attention over an 8-bit paged cache (paged_q8.cuh) from its codes, at most 16 (token, head of the group) rows of a KV head per unit: single tokens and
+// short candidate chunks, and whatever has fp32 rows.  Single tokens are bound by the cache's bytes (3 x 1 token over 23398 to 65537 slots, 8 KV heads
+// of 128: 313 MB in 65 us), short units by the chain of a tile, more rows by the warps that the registers leave room for.
 //
 // The layout of work is that of paged_attn_few.cuh: every consumer warp takes a tile of 32 slots through S^T = K q^T and O^T += V^T P^T with
 // mma.sync (the slots as the rows of the product), a producer warp keeps a ring of K/V tiles full, an epilogue warp merges the warps'
@@ -22,7 +23,7 @@
 
 namespace lar {
 
-constexpr int kQ8Rows = 16;  // rows of a unit up to which the kernel below is taken
+constexpr int kQ8Rows = 16;  // rows of a unit at most
 
 // A step of a CTA's work, worked out by the producer: some slot tiles of one unit.
 struct alignas(16) Q8Seg {
@@ -632,11 +633,11 @@ struct Q8UnpackArgs {
 
 constexpr int kQ8UnpackSlots = 32;
 
-// Live entries of every sequence as dense pages of 128 rows, for the kernels of longer chunks (each element is read by many row tiles there: turned once, not once for
+// Live entries of every sequence as dense pages of 128 bf16 rows (exact), for the kernels of longer chunks of bf16 rows (each element is read by many row tiles there: turned once, not once for
 // each).  A CTA has 32 slots of K or V; slots outside [start, len) are left alone: whoever reads the pages masks them.
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kQ8ReadThreads) q8_unpack_kernel(const __grid_constant__ Q8UnpackArgs a) {
-    constexpr int IPR = D / 16, E = Elt<T>::kPerChunk, BATCH = 4;
+    constexpr int IPR = D / 16, E = 8, BATCH = 4;
     const int tid = threadIdx.x, s = blockIdx.y, is_v = blockIdx.z, first = blockIdx.x * kQ8UnpackSlots;
     if (tid == 0 && is_v == 0 && (first & 127) == 0) a.table[s * a.cols + (first >> 7)] = s * a.cols + (first >> 7);
     const int len = min(live_len(a.kv, s, 0, false), a.cols * 128), lo = a.start ? max(a.start[s], 0) : 0;
@@ -645,7 +646,7 @@ __global__ void __launch_bounds__(kQ8ReadThreads) q8_unpack_kernel(const __grid_
     const int c = tid & (IPR - 1), heads = a.kv.n_kv_heads, n_items = (j1 - j0) * heads * IPR;
     const char* pool = is_v ? a.kv.v_pool : a.kv.k_pool;
     const unsigned char* scale_pool = is_v ? a.q8.v_scale : a.q8.k_scale;
-    T* out = reinterpret_cast<T*>(a.out[is_v]) + (long long)s * a.cols * 128 * heads * D;
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out[is_v]) + (long long)s * a.cols * 128 * heads * D;
     for (int base = 0; base < n_items; base += kQ8ReadThreads * BATCH) {
         uint4 codes[BATCH];
         int byte[BATCH];
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(kQ8ReadThreads) q8_unpack_kernel(const __grid_
         for (int b = 0; b < BATCH; ++b) {
             const int r = (base + b * kQ8ReadThreads + tid) / IPR, jl = r / heads;
             if (j0 + jl >= j1) continue;
-            T* dst = out + ((long long)j0 * heads + r) * D + c * 16;
+            __nv_bfloat16* dst = out + ((long long)j0 * heads + r) * D + c * 16;
             const float scale = q8_scale(byte[b]);
             float x[16];
             q8_values4(codes[b].x, scale, x);
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(kQ8ReadThreads) q8_unpack_kernel(const __grid_
                 float part[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) part[e] = x[i + e];
-                *reinterpret_cast<uint4*>(dst + i) = PackRow<T>::pack(part);
+                *reinterpret_cast<uint4*>(dst + i) = PackRow<__nv_bfloat16>::pack(part);
             }
         }
     }

@@ -29,7 +29,7 @@ size_t few_smem(int d, int nr, int n_seqs) {
     return nr == 1 ? Q8Shape<T, 128, 1>::bytes(n_seqs) : Q8Shape<T, 128, 2>::bytes(n_seqs);
 }
 
-constexpr size_t kUnpackBytes = 256u << 20;  // unpacked rows at a time
+constexpr size_t kUnpackBytes = (size_t)1 << 30;  // unpacked rows at a time
 
 size_t round_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
@@ -39,11 +39,12 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
     const int64_t chunk = max_chunk > 0 ? max_chunk : (n_tokens + k.n_seqs - 1) / k.n_seqs;
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
-    const int64_t with_tokens = n_tokens < k.n_seqs ? n_tokens : k.n_seqs;
-    const int d = k.head_dim, elt = elt_of(rows_dtype);
-    p.few = chunk * group <= kQ8Rows;
+    const int d = k.head_dim;
+    // From the codes: fp32 rows, and up to 32 rows of bf16 (12 sequences of 2080 to 4160 slots, 8 KV heads of 128, codes / unpacked: 32 bf16 rows 64 / 88 us, 64
+    // 108 / 90; 500 slots, 32 rows 23 / 28; fp32, 64 rows 158 / 336, 2000 rows 4.3 / 5.2 ms, 8320 rows 7.4 / 7.2, over 500 slots 0.71 / 0.65).
+    p.few = rows_dtype == LAR_FP32 || chunk * group <= 32;
     if (p.few) {
-        p.tq = (int)chunk;
+        p.tq = (int)(chunk < kQ8Rows / group ? chunk : kQ8Rows / group);
         p.rows_cap = p.tq * group;
         p.nr = p.rows_cap > 8 ? 2 : 1;
         p.smem = rows_dtype == LAR_BF16 ? few_smem<__nv_bfloat16>(d, p.nr, k.n_seqs) : few_smem<float>(d, p.nr, k.n_seqs);
@@ -52,12 +53,13 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
         // Units of few slots, or short ones in some number, stay whole: joining costs a launch (one token, 8 KV heads of 128, cut / whole: up to 300 slots 4
         // sequences 10.3 / 9.5 us, 64 20.5 / 17.3; up to 577: 4 sequences 10.3 / 12.3, 16 13.6 / 13.0, 64 27.4 / 24.7; up to 1153: 64 of unlike
         // length 25.4 / 28.7, with 20 heads 46.6 / 57.9).
-        p.split = split && len > 384 && (len > 640 || with_tokens * k.n_kv_heads < kSms / 2);
+        const int64_t seqs = n_tokens < k.n_seqs ? n_tokens : k.n_seqs, tiles = (n_tokens + p.tq - 1) / p.tq, units = (tiles > seqs ? tiles : seqs) * k.n_kv_heads;
+        p.split = split && len > 384 && (len > 640 || units < kSms / 2);
         if (p.split) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         return p;
     }
     p.cols = (int)((len + 127) / 128);
-    const size_t page = (size_t)128 * k.n_kv_heads * d * elt, seq = 2 * page * p.cols;
+    const size_t page = (size_t)128 * k.n_kv_heads * d * 2, seq = 2 * page * p.cols;
     const size_t fit = seq > kUnpackBytes ? 1 : kUnpackBytes / seq;
     p.batch = fit < (size_t)k.n_seqs ? (int)fit : k.n_seqs;
     p.table_bytes = round_up((size_t)p.batch * p.cols * sizeof(int), 256);
@@ -67,10 +69,10 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
 }
 
 // The unpacked pages of a batch of sequences as a cache of their own.
-lar_paged_kv_t unpacked(const lar_paged_kv_t& k, int rows_dtype, const Q8Plan& p, int n_seqs, void* workspace) {
+lar_paged_kv_t unpacked(const lar_paged_kv_t& k, const Q8Plan& p, int n_seqs, void* workspace) {
     lar_paged_kv_t u = k;
     char* at = static_cast<char*>(workspace);
-    u.dtype = rows_dtype;
+    u.dtype = LAR_BF16;
     u.n_seqs = n_seqs;
     u.page_tokens = 128;
     u.n_pages = n_seqs * p.cols;
@@ -170,14 +172,14 @@ size_t lar_paged_q8_attn_workspace_bytes(const lar_paged_q8_t* cache, int rows_d
         const size_t n = q8_plan(one, rows_dtype, group, 1, (int)c, len > 640 ? 641 : (int)len, true).bytes;
         most = n > most ? n : most;
     }
-    if (chunk * group > kQ8Rows) {
+    if (rows_dtype == LAR_BF16 && chunk * group > 32) {
         // unpacked rows: at most what is unpacked at a time, or one sequence where that is more; a table of as many pages (at most one for every
         // 16 KB, the smallest page); and the workspace of the attention over them
-        const size_t page = (size_t)128 * k.n_kv_heads * k.head_dim * elt_of(rows_dtype), cols = (size_t)((len + 127) / 128);
+        const size_t page = (size_t)128 * k.n_kv_heads * k.head_dim * 2, cols = (size_t)((len + 127) / 128);
         const size_t seq = 2 * page * cols, all = seq * k.n_seqs, dense = seq > kUnpackBytes ? seq : all < kUnpackBytes ? all : kUnpackBytes;
         const size_t table = round_up(dense / (2 * page) * sizeof(int), 256);
         const Q8Plan p = q8_plan(k, rows_dtype, group, n_tokens, (int)chunk, (int)len, true);
-        lar_paged_kv_t u = unpacked(k, rows_dtype, p, k.n_seqs, reinterpret_cast<void*>(256));
+        lar_paged_kv_t u = unpacked(k, p, k.n_seqs, reinterpret_cast<void*>(256));
         const size_t n = table + dense + lar_paged_attn_workspace_bytes(&u, n_q_heads, n_tokens, (int)(chunk > INT32_MAX ? INT32_MAX : chunk), (int)len);
         most = n > most ? n : most;
     }
@@ -218,7 +220,7 @@ lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, cons
     }
     for (int s0 = 0; s0 < k.n_seqs; s0 += p.batch) {
         const int n = k.n_seqs - s0 < p.batch ? k.n_seqs - s0 : p.batch;
-        lar_paged_kv_t u = unpacked(k, rows_dtype, p, n, workspace);
+        lar_paged_kv_t u = unpacked(k, p, n, workspace);
         u.lens = k.lens + s0 * k.lens_stride;
         Q8UnpackArgs w;
         w.kv = a.kv;
@@ -231,8 +233,7 @@ lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, cons
         w.out[1] = static_cast<char*>(u.v_pool);
         w.table = const_cast<int*>(u.page_table);
         w.cols = p.cols;
-        void (*fn)(const Q8UnpackArgs) = rows_dtype == LAR_BF16 ? (d == 64 ? q8_unpack_kernel<__nv_bfloat16, 64> : q8_unpack_kernel<__nv_bfloat16, 128>)
-                                                                : (d == 64 ? q8_unpack_kernel<float, 64> : q8_unpack_kernel<float, 128>);
+        void (*fn)(const Q8UnpackArgs) = d == 64 ? q8_unpack_kernel<64> : q8_unpack_kernel<128>;
         fn<<<dim3((unsigned)(p.cols * (128 / kQ8UnpackSlots)), (unsigned)n, 2), kQ8ReadThreads, 0, s>>>(w);
         LAR_CUDA(cudaGetLastError());
         lar_rows_t qr = {q->data, a.q.token_stride, a.q.head_stride}, orow = {out->data, a.out.token_stride, a.out.head_stride};
