@@ -104,7 +104,7 @@ size_t lar_paged_attn_shared_workspace_bytes(const lar_paged_kv_t* kv, int n_q_h
     if (n < 1) return whole;
     const size_t row = (size_t)n_q_heads * ((d + 2) * sizeof(float) + (kv->dtype == LAR_BF16 ? sizeof(int2) : 0)), ints = up256(((size_t)n_groups * 3 + 1 + kv->n_seqs) * sizeof(int));
     const size_t a = attn_workspace_bound(groups_of(*kv, n_groups), group, n, (int)n, max_shared, true);
-    const size_t b = attn_workspace_bound(*kv, group, n, (int)(chunk < n ? chunk : n), max_len, true);
+    const size_t b = attn_workspace_bound(*kv, group, n, (int)(chunk < kSharedRows / group ? chunk : kSharedRows / group), max_len, true);
     // (fp32: one part at least; the bounds hold from two parts on)
     const size_t rows = (size_t)n * row;
     const size_t apart = kv->dtype == LAR_BF16 ? ints + 2 * up256(rows) + up256(a) + up256(b) : ints + up256(a > rows ? a : rows) + up256(b > rows ? b : rows);
