@@ -108,7 +108,7 @@ bool append_args(NormRopeArgs& a, int rows_dtype, int n_kv_heads, int d, const l
 namespace lar {
 
 bool q8_view(const lar_paged_q8_t* c, int64_t n_tokens, const int32_t* cu, PagedView& v, Q8View& q) {
-    if (!c || c->struct_size != sizeof(lar_paged_q8_t) || !paged_view(&c->kv, n_tokens, cu, v, true)) return false;
+    if (!c || c->struct_size != sizeof(lar_paged_q8_t) || c->reserved || !paged_view(&c->kv, n_tokens, cu, v, true)) return false;
     if (c->kv.k_pool == c->kv.v_pool || c->k_scale == c->v_scale) return false;
     if (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)) return false;
     const int64_t strides[2] = {c->scale_page_stride, c->scale_head_stride};

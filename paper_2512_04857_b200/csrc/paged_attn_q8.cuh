@@ -181,26 +181,25 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
         if (tid == 0) pre[0] = 0;
         __syncthreads();
     }
-    Work work;
-    work.info = info;
-    work.pre = work.items = pre;
-    work.n_seqs = a.kv.n_seqs;
-    work.tq = a.tq;
-    work.causal = a.causal;
-    work.x = blockIdx.x;
-    work.step = gridDim.x;
-    work.end = ta.split ? 0 : pre[a.kv.n_seqs];
-    work.first_cut = 0;
-    work.y = work.y_end = 0;
-    const int total = ta.split ? pre[a.kv.n_seqs] : 0;
-    const int n_ranges = min((total + ta.min_items - 1) / ta.min_items, (int)gridDim.x);
-    if ((int)blockIdx.x < n_ranges) {
-        work.y = (int)((long long)total * blockIdx.x / n_ranges);
-        work.y_end = (int)((long long)total * (blockIdx.x + 1) / n_ranges);
-    }
-
     if (warp == 0) {
         // ------------------------------------------------------------------ producer: a lane for every page (or part of one) of a tile
+        Work work;
+        work.info = info;
+        work.pre = work.items = pre;
+        work.n_seqs = a.kv.n_seqs;
+        work.tq = a.tq;
+        work.causal = a.causal;
+        work.x = blockIdx.x;
+        work.step = gridDim.x;
+        work.end = ta.split ? 0 : pre[a.kv.n_seqs];
+        work.first_cut = 0;
+        work.y = work.y_end = 0;
+        const int total = ta.split ? pre[a.kv.n_seqs] : 0;
+        const int n_ranges = min((total + ta.min_items - 1) / ta.min_items, (int)gridDim.x);
+        if ((int)blockIdx.x < n_ranges) {
+            work.y = (int)((long long)total * blockIdx.x / n_ranges);
+            work.y_end = (int)((long long)total * (blockIdx.x + 1) / n_ranges);
+        }
         int issued = 0, segs = 0;
         RingPos kv;
         bool ok = true;

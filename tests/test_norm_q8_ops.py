@@ -25,12 +25,12 @@ def _r(data=4096, token_stride=128, head_stride=64):
     return lar.lar_rows_t(data, token_stride, head_stride)
 
 
-def _q8(k_scale=4096, v_scale=8192, sp=64, sh=32, struct_size=C.sizeof(lar.lar_paged_q8_t), **kw):
+def _q8(k_scale=4096, v_scale=8192, sp=64, sh=32, struct_size=C.sizeof(lar.lar_paged_q8_t), reserved=0, **kw):
     kv = dict(struct_size=C.sizeof(lar.lar_paged_kv_t), dtype=lar.LAR_E4M3, n_seqs=2, n_kv_heads=2, head_dim=64, page_tokens=32, n_pages=8,
               table_cols=4, page_stride=2 * 32 * 64, row_stride=2 * 64, head_stride=64, k_pool=4096, v_pool=8192, page_table=256,
               table_seq_stride=4, table_head_stride=0, lens=512, lens_stride=1, status=None)
     kv.update(kw)
-    return lar.lar_paged_q8_t(struct_size, 0, lar.lar_paged_kv_t(**kv), k_scale, v_scale, sp, sh)
+    return lar.lar_paged_q8_t(struct_size, reserved, lar.lar_paged_kv_t(**kv), k_scale, v_scale, sp, sh)
 
 
 BAD_NORMS = [dict(struct_size=8), dict(kind=2), dict(kind=-1), dict(weight_dtype=2), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
@@ -66,7 +66,7 @@ def test_norm_rope_refusals():
 
 
 @pytest.mark.parametrize("bad", [
-    dict(struct_size=8), dict(dtype=0), dict(dtype=1), dict(dtype=3), dict(n_seqs=0), dict(head_dim=96), dict(page_tokens=48), dict(row_stride=72),
+    dict(struct_size=8), dict(reserved=1), dict(dtype=0), dict(dtype=1), dict(dtype=3), dict(n_seqs=0), dict(head_dim=96), dict(page_tokens=48), dict(row_stride=72),
     dict(row_stride=48), dict(page_stride=2 * 32 * 64 + 8), dict(head_stride=0), dict(k_pool=4104), dict(v_pool=None), dict(lens=None),
     dict(k_scale=None), dict(v_scale=None), dict(k_scale=4104), dict(v_scale=8196), dict(sp=40), dict(sp=16), dict(sp=-64), dict(sh=0), dict(sh=16),
     dict(sh=40), dict(sh=-32), dict(head_stride=0, table_head_stride=8, sh=32),
