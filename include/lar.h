@@ -461,7 +461,8 @@ lar_status_t lar_append_kv_norm_rope(lar_cache_t* c, int layer, const lar_head_n
 
 /* A paged cache in 8 bits: kv as above with dtype LAR_E4M3 (pools of one-byte codes; strides in elements are bytes, multiples of 16), and a byte b
  * for every row: the byte of row r of page p and head h is scale[p * scale_page_stride + h * scale_head_stride + r] (16-byte aligned, strides
- * multiples of 16; heads with pages of their own have scale_head_stride = 0).  An element is  e4m3(code) * 2^(b - 127);  a row is stored
+ * multiples of 16; heads with pages of their own have scale_head_stride = 0).  The pools of K and V are different and lie within 2^40 bytes of each other
+ * (of one GPU's memory that is so), and so do the bytes.  An element is  e4m3(code) * 2^(b - 127);  a row is stored
  * with the smallest power 2^(b - 127), at least 2^-117, for which none of its elements exceeds 448 times it, codes rounded to nearest even (an element
  * below 2^-15 of the row's largest to a multiple of 2^-18 of it); a row of zeros has b = 127.  A row with an element that is not
  * finite is stored as b = 255 and reads as NaN. */
@@ -502,7 +503,8 @@ size_t lar_paged_q8_attn_workspace_bytes(const lar_paged_q8_t* cache, int rows_d
 
 /* lar_paged_attn (bf16 and fp32 caches, no kv_start) for sequences that have their first slots in common: many images of one prompt.  Group g is the sequences
  * cu_groups[g] .. cu_groups[g + 1] - 1 (device, int32, [n_groups + 1], ascending), and their first shared_lens[g] slots (device, int32, [n_groups]) hold the
- * same keys and values: the same pages in every table, or copies; those of the group's first sequence are read, once for all of its tokens.
+ * same keys and values: the same pages in every table, or copies; those of the group's first sequence that has tokens are read, once for all tokens of
+ * the group.
  * Every sequence of a group that has tokens holds the slots in common before its chunk; of a length that says more, only what the shortest of the group's caches
  * held before its chunk is taken as common.  Sequences of no group share nothing.  shared_lens need not be multiples of page_tokens.
  * The result is that of lar_paged_attn up to rounding.  max_shared bounds shared_lens (0: not known) and chooses the launch shape only.  Chunks of more than

@@ -27,7 +27,7 @@ constexpr int kSharedPrepThreads = 128;
 
 // The groups as sequences, a CTA each.
 static __global__ void __launch_bounds__(kSharedPrepThreads) shared_prep_kernel(const __grid_constant__ SharedPrepArgs a) {
-    __shared__ int least[kSharedPrepThreads / 32];
+    __shared__ int least[kSharedPrepThreads / 32], firsts[kSharedPrepThreads / 32];
     grid_dep_launch();
     const int tid = threadIdx.x, g = blockIdx.x, S = a.kv.n_seqs;
     const int s0 = min(max(a.groups[g], 0), S), s1 = min(max(a.groups[g + 1], s0), S);
@@ -36,22 +36,32 @@ static __global__ void __launch_bounds__(kSharedPrepThreads) shared_prep_kernel(
         chunk_of(a.kv, min(s, S - 1), t0, t1);
         return s < S ? t0 : t1;
     };
-    int L = INT_MAX;
+    int L = INT_MAX, first = INT_MAX;  // first: the first sequence with tokens; one without (an image that is done) may have given up its pages
     for (int s = s0 + tid; s < s1; s += kSharedPrepThreads) {
         int t0, t1;
         chunk_of(a.kv, s, t0, t1);
-        if (t1 > t0) L = min(L, max(live_len(a.kv, s, 0, false) - (t1 - t0), 0));
+        if (t1 > t0) {
+            L = min(L, max(live_len(a.kv, s, 0, false) - (t1 - t0), 0));
+            first = min(first, s);
+        }
     }
     L = __reduce_min_sync(0xffffffffu, L);
-    if ((tid & 31) == 0) least[tid >> 5] = L;
+    first = __reduce_min_sync(0xffffffffu, first);
+    if ((tid & 31) == 0) {
+        least[tid >> 5] = L;
+        firsts[tid >> 5] = first;
+    }
     __syncthreads();
-    for (int w = 0; w < kSharedPrepThreads / 32; ++w) L = min(L, least[w]);
+    for (int w = 0; w < kSharedPrepThreads / 32; ++w) {
+        L = min(L, least[w]);
+        first = min(first, firsts[w]);
+    }
     L = L == INT_MAX ? 0 : min(L, max(a.shared[g], 0));  // (no tokens: nothing to do)
     for (int s = s0 + tid; s < s1; s += kSharedPrepThreads) a.start[s] = L;
     if (tid == 0) {
         a.cu[g] = token_of(s0);
         a.len[g] = L;
-        a.row_of[g] = min(s0, S - 1);
+        a.row_of[g] = min(first, S - 1);
         if (g == a.n_groups - 1) a.cu[g + 1] = token_of(s1);
     }
     // sequences of no group have all slots for themselves

@@ -560,7 +560,6 @@ class PagedKV:
               hq, n, _ints(cu_tokens, self.n_seqs + 1, dev, "attn: cu_tokens"), _ints(kv_start, self.n_seqs, dev, "attn: kv_start"),
               int(causal), softmax_scale, max_chunk, max_len, ws_at, ws)
 
-
     def attn_shared_workspace(self, n_q_heads, n_tokens, n_groups, max_chunk=0, max_len=0, max_shared=0):
         """A workspace tensor for attn_shared calls of these sizes and all smaller ones (None where none is used)."""
         import torch

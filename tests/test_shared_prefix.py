@@ -208,6 +208,20 @@ def test_shared_attention_in_a_graph_of_a_growing_cache(dtype, n):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hints", [True, False])
+def test_shared_attention_of_groups_whose_first_sequences_are_done(dtype, hints):
+    """Sequences without tokens, whose pages and lengths are gone, in every place of a group."""
+    n, lens, groups, said = [0, 0, 1, 2, 0, 1, 0, 0, 3, 0], [0, 0, 300, 290, 0, 310, 0, 0, 205, 0], [(0, 5), (5, 7), (7, 10)], [270, 300, 200]
+    c = _case(dtype, 64, 2, 16, "nhd", n, lens, [(2, 4)], [270])
+    for s, m in enumerate(n):
+        if m == 0:
+            c.kv._keep[2][s] = -1
+    for causal in (True, False):
+        _check(c, 4, groups, said, causal, hints=hints)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_shared_attention_reports_bad_pages(dtype):
     c = _case(dtype, 64, 1, 16, "nhd", [1, 1], [100, 90], [(0, 2)], [80])
     c.kv._keep[2][0, 2] = -1                                                 # read for both sequences: zeros
