@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(FewShape<D, NR>::THREADS, FewShape<D, NR>::PER
             chunk_of(a.kv, s, v.t0, t1);
             v.n = t1 - v.t0;
             v.len = live_len(a.kv, s, v.n, blockIdx.x == 0 && !(PART && a.kv.row_of));
-            v.lo = a.start ? max(a.start[s], 0) : 0;
+            v.lo = a.start ? max(__ldcg(a.start + s), 0) : 0;  // (from L2: with PART written by a kernel before the last)
             info[s] = v;
             sum += (v.n + a.tq - 1) / a.tq * a.kv.n_kv_heads * (ta.split ? Work::items_of_unit(v) : 1);
             pre[s + 1] = sum;
