@@ -26,7 +26,7 @@ struct PagedAttnArgs {
     float* part_o;     // partial results of units whose slots are spread over several CTAs
     float* part_ml;
     int n_splits;
-    int parts;         // fp32: rows are left as parts (split, or joined with another call's)
+    int parts;         // fp32: 1: rows are left as parts (split); 2: as one of two passes that are joined
     float* row_o;      // kernels with PART: (O, m, l) of every (token, head) instead of its output row
     float* row_ml;
     int2* row_ref;     // where a row's unit is cut: first range + 65536 * last, place among a range's rows; else -1 (row_o, row_ml hold the row)

@@ -25,6 +25,18 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// A pass over slots in common or over sequences' own (parts = 2) is launched before its predecessor's end: the first waits at its start for the kernel that
+// makes the groups; of the second, which runs beside the first, one CTA waits at its end, so that who waits for this kernel's end has waited for
+// both.
+__device__ __forceinline__ void pass_begin(const PagedAttnArgs& a) {
+    if (a.parts != 2) return;
+    if (a.kv.row_of) grid_dep_wait();
+    grid_dep_launch();
+}
+__device__ __forceinline__ void pass_end(const PagedAttnArgs& a) {
+    if (a.parts == 2 && !a.kv.row_of && blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1) grid_dep_wait();
+}
+
 // The unit of a CTA: blockIdx.x counts the row tiles of all sequences, blockIdx.y the KV heads, blockIdx.z the splits.
 struct Fp32Unit {
     int seq, head, tok0, n_tok, rows;  // tokens of the tile, (token, head of the group) rows
@@ -66,7 +78,7 @@ struct Fp32Unit {
         n_tok = min(a.tq, t1 - tok0);
         rows = n_tok * a.group;
         slot0 = len - (t1 - tok0);
-        lo = a.start ? max(a.start[seq], 0) : 0;
+        lo = a.start ? max(__ldcg(a.start + seq), 0) : 0;  // (from L2: a pass's are written by a kernel before the last)
         hi = a.causal ? min(len, slot0 + n_tok) : len;
         const int first = lo / kFp32Keys, end = hi > lo ? (hi + kFp32Keys - 1) / kFp32Keys : first;
         const int per = (end - first + a.n_splits - 1) / a.n_splits;
@@ -227,7 +239,11 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
     float* vs = ks + kFp32Keys * RS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, qrow = lane >> 2;
     Fp32Unit u;
-    if (!u.find(a)) return;
+    pass_begin(a);
+    if (!u.find(a)) {
+        pass_end(a);
+        return;
+    }
     u.fetch_q<D>(a, qs, RS, S::BM);
     const int row_w = FEW ? 0 : warp * 16, slot_w = FEW ? warp * 16 : 0;  // the warp's first row, first slot of a step
     const int row0 = row_w + qrow;  // this thread's rows: row0, row0 + 8
@@ -372,6 +388,7 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
         }
         __syncthreads();
         u.merge_warps<D, S::WARPS, S::BM, PS>(a, ks);
+        pass_end(a);
         return;
     }
 #pragma unroll
@@ -384,6 +401,7 @@ __global__ void __launch_bounds__(Tf32Shape<D, FEW>::THREADS, Tf32Shape<D, FEW>:
         for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(o[n][2 * r] * inv, o[n][2 * r + 1] * inv);
         if (a.parts && quad == 0) *reinterpret_cast<float2*>(a.part_ml + u.part_row(a, row) * 2) = make_float2(m[r], l[r]);
     }
+    pass_end(a);
 }
 
 // At most 8 rows of a KV head (a decode step).  The slots are the 16 rows of a product and the query rows its 8 columns (S^T = K q^T,
@@ -411,7 +429,11 @@ __global__ void __launch_bounds__(kFp32Threads, Tf32DecodeShape<D>::PER_SM) page
     float* vs = ks + kFp32Keys * RS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, qrow = lane >> 2;
     Fp32Unit u;
-    if (!u.find(a)) return;
+    pass_begin(a);
+    if (!u.find(a)) {
+        pass_end(a);
+        return;
+    }
     const int slot_w = warp * 16;  // the warp's first slot of a step
     const int last[2] = {u.last_slot(a, 2 * quad), u.last_slot(a, 2 * quad + 1)};
     float m[2], l[2], o[OT][4];
@@ -558,6 +580,7 @@ __global__ void __launch_bounds__(kFp32Threads, Tf32DecodeShape<D>::PER_SM) page
     }
     __syncthreads();
     u.merge_warps<D, S::WARPS, S::ROWS, PS>(a, ks);
+    pass_end(a);
 }
 
 // Joins the splits of every row, in the order of the splits: one warp per (token, head).

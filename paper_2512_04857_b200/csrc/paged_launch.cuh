@@ -162,8 +162,18 @@ lar_status_t launch_fp32(const PagedAttnArgs& a, const AttnPlan& p, cudaStream_t
                      : p.bm == 16 ? Tf32Shape<D, true>::SMEM
                                   : Tf32DecodeShape<D>::SMEM;
     LAR_CUDA(cudaFuncSetAttribute((const void*)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    fn<<<dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits), kFp32Threads, smem, s>>>(a);
-    LAR_CUDA(cudaGetLastError());
+    cudaLaunchConfig_t lc;
+    memset(&lc, 0, sizeof(lc));
+    lc.gridDim = dim3((unsigned)p.tiles, (unsigned)a.kv.n_kv_heads, (unsigned)p.splits);
+    lc.blockDim = dim3(kFp32Threads, 1, 1);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = &at;
+    lc.numAttrs = a.parts == 2 ? 1 : 0;  // (waits by itself)
+    LAR_CUDA(cudaLaunchKernelEx(&lc, fn, a));
     if (p.splits > 1 && join) {
         const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.n_kv_heads * a.group;
         combine_splits_kernel<D><<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);

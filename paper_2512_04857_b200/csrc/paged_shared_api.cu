@@ -148,7 +148,7 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
 
     a.group = group;
     a.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d)) * 1.4426950408889634f;
-    a.parts = 1;
+    a.parts = 2;
     SharedJoinArgs j;
     memset(&j, 0, sizeof(j));
     j.kv = a.kv;
@@ -214,7 +214,7 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = &attr;
-    lc.numAttrs = kv->dtype == LAR_BF16 ? 1 : 0;
+    lc.numAttrs = 1;
     void (*fn)(const SharedJoinArgs) = kv->dtype == LAR_BF16 ? (d == 64 ? shared_join_kernel<__nv_bfloat16, 64> : shared_join_kernel<__nv_bfloat16, 128>)
                                                              : (d == 64 ? shared_join_kernel<float, 64> : shared_join_kernel<float, 128>);
     LAR_CUDA(cudaLaunchKernelEx(&lc, fn, (const SharedJoinArgs)j));
