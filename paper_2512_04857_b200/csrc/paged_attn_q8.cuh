@@ -42,10 +42,12 @@ struct Q8Shape {
     static constexpr int TILE_BYTES = KT * D, STAGE_BYTES = 2 * TILE_BYTES, SCALE_BYTES = 2 * KT;
     static constexpr int SCALE_PITCH = KT / 16 * 128;  // of a stage: a copy's destination is 128-byte aligned, and a page has 16 slots at least
     static constexpr int W = 4, THREADS = (W + 2) * 32;  // producer, consumers, epilogue
-    static constexpr int NS = KT == 64 ? 4 : 8;  // stages: a multiple of W, a stage is always read by the same consumer
+    static constexpr int NS = W;  // stages: a multiple of W, a stage is always read by the same consumer
     static constexpr int PER_SM = D == 64 && NR == 1 ? 3 : 2;  // (64 x 577 slots, 20 heads of 64, 1 to 8 tokens: 27 us with three CTAs, 31 with two)
     static constexpr int ROWS = 8 * NR;
-    static constexpr int QS = 4;                  // units that the producer is ahead by at most
+    // Units that the producer is ahead by at most.  (Two where rows are many, which lets two CTAs share an SM with 128 elements: 16 x 4288 slots, 16 rows 38.6 instead of 43.8
+    // us, 32 rows 57 instead of 70; fp32 with 4 stages instead of 8, 51 instead of 55.)
+    static constexpr int QS = NR == 2 ? 2 : 4;
     static constexpr int Q_SLOT = ROWS * D * (int)sizeof(T);
     static constexpr int PS = D + 4;              // floats of a partial row: O, m, l, padding
     static constexpr int PBUFS = NR == 1 ? 2 : 1;

@@ -29,6 +29,7 @@ size_t few_smem(int d, int nr, int n_seqs) {
     return nr == 1 ? Q8Shape<T, 128, 1>::bytes(n_seqs) : Q8Shape<T, 128, 2>::bytes(n_seqs);
 }
 
+constexpr int kCodesRows = 64;  // bf16 rows of a KV head that are computed from the codes
 constexpr size_t kUnpackBytes = (size_t)1 << 30;  // unpacked rows at a time
 
 size_t round_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
@@ -40,9 +41,10 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
     const int d = k.head_dim;
-    // From the codes: fp32 rows, and up to 32 rows of bf16 (12 sequences of 2080 to 4160 slots, 8 KV heads of 128, codes / unpacked: 32 bf16 rows 64 / 88 us, 64
-    // 108 / 90; 500 slots, 32 rows 23 / 28; fp32, 64 rows 158 / 336, 2000 rows 4.3 / 5.2 ms, 8320 rows 7.4 / 7.2, over 500 slots 0.71 / 0.65).
-    p.few = rows_dtype == LAR_FP32 || chunk * group <= 32;
+    // From the codes: fp32 rows, and up to 64 rows of bf16 (16 sequences of up to 4288 slots, 8 KV heads of 128, codes / unpacked: 48 bf16 rows 77 / 112 us,
+    // 64 96 / 111, 96 130 / 112; elements of 64, 64 rows 60 / 62, 96 80 / 65; up to 600 slots, 64 rows 30 / 36, 96 39 / 36; 4 sequences 32 / 42,
+    // 41 / 45.  fp32, 12 sequences of 2080 to 4160 slots: 64 rows 158 / 336, 2000 rows 4.3 / 5.2 ms, 8320 rows 7.4 / 7.2, over 500 slots 0.71 / 0.65).
+    p.few = rows_dtype == LAR_FP32 || chunk * group <= kCodesRows;
     if (p.few) {
         p.tq = (int)(chunk < kQ8Rows / group ? chunk : kQ8Rows / group);
         p.rows_cap = p.tq * group;
@@ -172,7 +174,7 @@ size_t lar_paged_q8_attn_workspace_bytes(const lar_paged_q8_t* cache, int rows_d
         const size_t n = q8_plan(one, rows_dtype, group, 1, (int)c, len > 640 ? 641 : (int)len, true).bytes;
         most = n > most ? n : most;
     }
-    if (rows_dtype == LAR_BF16 && chunk * group > 32) {
+    if (rows_dtype == LAR_BF16 && chunk * group > kCodesRows) {
         // unpacked rows: at most what is unpacked at a time, or one sequence where that is more; a table of as many pages (at most one for every
         // 16 KB, the smallest page); and the workspace of the attention over them
         const size_t page = (size_t)128 * k.n_kv_heads * k.head_dim * 2, cols = (size_t)((len + 127) / 128);

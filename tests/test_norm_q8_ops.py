@@ -370,9 +370,9 @@ def _check_attention(c, hq, dtype, causal, start, workspace, seed, hints=True, q
     buf = torch.full((q.shape[0], hq + 1, d), 5.0, dtype=dtype, device=DEV)     # out is a view with a gap behind each token
     out = buf[:, :hq]
     mc, ml = hints if isinstance(hints, tuple) else (max(c.n), max(c.lens)) if hints else (0, 0)
-    # The bound of the chunks decides which kernels a call takes: above 32 bf16 rows per KV head those of bf16 caches, which round a weight to bf16
+    # The bound of the chunks decides which kernels a call takes: above 64 bf16 rows per KV head those of bf16 caches, which round a weight to bf16
     # (2^-8 of it, and the sum over the weights' magnitudes 2^-8 of mag), the others to fp16 (2^-11; two of them for fp32 rows).
-    few = dtype == F32 or (mc or -(-q.shape[0] // len(c.n))) * group <= 32
+    few = dtype == F32 or (mc or -(-q.shape[0] // len(c.n))) * group <= 64
     ws = c.kv.attn_workspace(hq, q.shape[0], mc, ml, dtype=dtype) if workspace or not few else None
     if ws is not None:
         ws.fill_(255)
