@@ -113,7 +113,7 @@ struct NormRope {
     static constexpr int NP = E;                 // pieces of four parameters that a thread has: weights and biases in turn
 
     struct Shared {
-        float cs[kNormTokens][D];  // cosines, sines
+        float cs[kNormTokens][D];  // cosines, sines: a thread's four side by side with its neighbours'
         int slot_of[kNormTokens], seq_of[kNormTokens];
         float4 params[kNormThreads * NP];  // [head][piece][thread of the row]
     };
@@ -183,13 +183,13 @@ struct NormRope {
         const float4* params = sh.params + (group - sub * na.heads[KIND]) * NP * IPR + c;
         // sines, cosines and slots of the CTA's tokens
         if (turn) {
-            const int i = tid & (HP - 1);
+            const int i = tid & (HP - 1), at = ((i % E / 4) * IPR + i / E) * 4 + i % 4;
             const double f = a.f.turns[i];
             const int* p = a.pos + a.f.axis[i] * a.pos_axis_stride + t0;
             for (int l = tid / HP; l < t1 - t0; l += blockDim.x / HP) {
                 const float2 v = cos_sin_of(f, p[l]);
-                sh.cs[l][i] = v.x;
-                sh.cs[l][HP + i] = v.y;
+                sh.cs[l][at] = v.x;
+                sh.cs[l][HP + at] = v.y;
             }
         }
         if (DEST)
@@ -245,10 +245,10 @@ struct NormRope {
             const int l = min(t - t0, kNormTokens - 1);
             if (turn) {
                 const uint64_t minus = pack_f32x2(-1.f, -1.f);
-                const float* cosv = &sh.cs[l][c * E];
+                const float* cosv = &sh.cs[l][c * 4];
 #pragma unroll
                 for (int i = 0; i < E / 2; i += 2) {
-                    const float4 u = *reinterpret_cast<const float4*>(cosv + 2 * i), v = *reinterpret_cast<const float4*>(cosv + HP + 2 * i);
+                    const float4 u = *reinterpret_cast<const float4*>(cosv + i * 2 * IPR), v = *reinterpret_cast<const float4*>(cosv + HP + i * 2 * IPR);
                     const uint64_t co[2] = {pack_f32x2(u.x, u.y), pack_f32x2(u.z, u.w)}, si[2] = {pack_f32x2(v.x, v.y), pack_f32x2(v.z, v.w)};
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
