@@ -41,8 +41,9 @@ struct PartSum {
 // CTAs of a range's unit: few enough rows each that warps share them.
 inline unsigned join_ctas(int unit_rows) { return unit_rows <= 2 ? 1u : unit_rows <= 64 ? (unsigned)(unit_rows + 1) / 2 : 32u; }
 
-// A launch of (ranges, join_ctas) CTAs; rows of output type T; NT, rows_cap and records as the kernel before left them (TcArgs).
-template <typename T, int D, int NT>
+// A launch of (ranges, join_ctas) CTAs; rows of output type T; rows_cap and records as the kernel before left them (TcArgs).
+// 3 us behind the attention of one token over 16 x 4288 slots.
+template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(const __grid_constant__ TcArgs ta) {
     constexpr int LPR = D / 4, HALVES = 32 / LPR;  // lanes of a row of a part, parts that a warp reads at a time
     __shared__ PartSum sums[kJoinWarps][LPR];
@@ -59,10 +60,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_parts_kernel(const __grid_c
         const int unit_row = row0 + mine;
         PartSum sum;
         if (unit_row < end) {
-            const int t = unit_row / a.group, tile = NT == 2 && t >= a.tq ? 1 : 0, tile_row = unit_row - tile * a.tq * a.group;
 #pragma unroll 8
             for (int c = first + part0; c <= last; c += split * HALVES) {
-                const size_t at = ((size_t)(c * 2 + (c == first ? 1 : 0)) * NT + tile) * ta.rows_cap + tile_row;
+                const size_t at = (size_t)(c * 2 + (c == first ? 1 : 0)) * ta.rows_cap + unit_row;
                 sum.add(*reinterpret_cast<const float2*>(a.part_ml + at * 2), *reinterpret_cast<const float4*>(a.part_o + at * D + e), a.scale_log2);
             }
         }

@@ -1,8 +1,10 @@
 // Attention over an 8-bit paged cache (paged_q8.cuh) from its codes, at most 16 (token, head of the group) rows of a KV head per unit: single tokens and
 // short candidate chunks, and whatever has fp32 rows.  Single tokens are bound by the cache's bytes (3 x 1 token over 23398 to 65537 slots, 8 KV heads
-// of 128: 313 MB in 65 us), short units by the chain of a tile, more rows by the warps that the registers leave room for.
+// of 128: 313 MB in 65 us; 16 x 129 to 4288 slots: 78 MB in 24 us, of which 9.6 are launch, lengths, page table and first tile, and 3 the join), short units by
+// the chain of a tile, more rows by the warps that the registers leave room for (64 x 1 to 577 slots, 20 heads of 64, up to 16 fp32 rows: 40 us, tensor pipe
+// 20 % busy, 11 warps on an SM).
 //
-// The layout of work is that of paged_attn_few.cuh: every consumer warp takes a tile of 32 slots through S^T = K q^T and O^T += V^T P^T with
+// The layout of work is that of paged_attn_few.cuh: every consumer warp takes a tile of 64 slots (32 where registers are short) through S^T = K q^T and O^T += V^T P^T with
 // mma.sync (the slots as the rows of the product), a producer warp keeps a ring of K/V tiles full, an epilogue warp merges the warps'
 // partial results.  What 8 bits change:
 //   * Codes go to fp16, which holds every e4m3 number: one conversion for two of them, no scale applied.  A row's scale is a power of two that belongs to a

@@ -142,7 +142,7 @@ lar_status_t launch_few(const lar_paged_q8_t& c, const PagedAttnArgs& a, const Q
         at.val.programmaticStreamSerializationAllowed = 1;
         lc.attrs = &at;
         lc.numAttrs = 1;
-        LAR_CUDA(cudaLaunchKernelEx(&lc, join_parts_kernel<T, D, 1>, (const TcArgs)t));
+        LAR_CUDA(cudaLaunchKernelEx(&lc, join_parts_kernel<T, D>, (const TcArgs)t));
     }
     return LAR_OK;
 }
