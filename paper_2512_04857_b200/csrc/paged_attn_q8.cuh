@@ -1,7 +1,7 @@
 // Attention over an 8-bit paged cache (paged_q8.cuh) from its codes, at most 16 (token, head of the group) rows of a KV head per unit: single tokens and
 // short candidate chunks, and whatever has fp32 rows.  Single tokens are bound by the cache's bytes (3 x 1 token over 23398 to 65537 slots, 8 KV heads
 // of 128: 313 MB in 65 us; 16 x 129 to 4288 slots: 78 MB in 24 us, of which 9.6 are launch, lengths, page table and first tile, and 3 the join), short units by
-// the chain of a tile, more rows by the warps that the registers leave room for (64 x 1 to 577 slots, 20 heads of 64, up to 16 fp32 rows: 40 us, tensor pipe
+// the chain of a tile, more rows by the warps that the registers leave room for (64 x 1 to 577 slots, 20 heads of 64, up to 16 fp32 rows: 37.5 us, tensor pipe
 // 20 % busy, 11 warps on an SM).
 //
 // The layout of work is that of paged_attn_few.cuh: every consumer warp takes a tile of 64 slots (32 where registers are short) through S^T = K q^T and O^T += V^T P^T with
@@ -38,13 +38,15 @@ template <typename T, int D, int NR>
 struct Q8Shape {
     static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
     // Slots of a tile (64 instead of 32, one token over 16 x 4288 slots: 25 instead of 27 us, 3 x 65537 slots 68 instead of 75; 16 rows of 64 fp32
-    // elements 40 instead of 44; of 128, where the registers do not hold it, 66 instead of 57).
-    static constexpr int KT = TERMS == 2 && NR == 2 && D == 128 ? 32 : 64;
+    // elements 40 instead of 44).  With 16 rows of 128 elements tiles of 32 and two of them for each consumer (38.6 -> 33.6 us, 64 rows 96 -> 87; fp32 66 -> 57).
+    static constexpr int KT = NR == 2 && D == 128 ? 32 : 64;
     static constexpr int MT = KT / 16, KS = D / 16;
     static constexpr int TILE_BYTES = KT * D, STAGE_BYTES = 2 * TILE_BYTES, SCALE_BYTES = 2 * KT;
     static constexpr int SCALE_PITCH = KT / 16 * 128;  // of a stage: a copy's destination is 128-byte aligned, and a page has 16 slots at least
     static constexpr int W = 4, THREADS = (W + 2) * 32;  // producer, consumers, epilogue
-    static constexpr int NS = W;  // stages: a multiple of W, a stage is always read by the same consumer
+    // Stages: a multiple of W, a stage is always read by the same consumer.  Two for each where two CTAs still fit (16 rows of 64 elements over 16 x 4288 slots 30.1 -> 27.5 us
+    // in fp32, 26.6 -> 25.4 in bf16): with one, a consumer that is done waits for the next tile.  One where rows are few: bandwidth then comes from many CTAs.
+    static constexpr int NS = (D == 64 && NR == 2) || (TERMS == 1 && KT == 32) ? 8 : 4;
     static constexpr int PER_SM = D == 64 && NR == 1 ? 3 : 2;  // (64 x 577 slots, 20 heads of 64, 1 to 8 tokens: 27 us with three CTAs, 31 with two)
     static constexpr int ROWS = 8 * NR;
     // Units that the producer is ahead by at most.  (Two where rows are many, which lets two CTAs share an SM with 128 elements: 16 x 4288 slots, 16 rows 38.6 instead of 43.8

@@ -41,9 +41,9 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
     const int d = k.head_dim;
-    // From the codes: fp32 rows, and up to 64 rows of bf16 (16 sequences of up to 4288 slots, 8 KV heads of 128, codes / unpacked: 48 bf16 rows 77 / 112 us,
-    // 64 96 / 111, 96 130 / 112; elements of 64, 64 rows 60 / 62, 96 80 / 65; up to 600 slots, 64 rows 30 / 36, 96 39 / 36; 4 sequences 32 / 42,
-    // 41 / 45.  fp32, 12 sequences of 2080 to 4160 slots: 64 rows 158 / 336, 2000 rows 4.3 / 5.2 ms, 8320 rows 7.4 / 7.2, over 500 slots 0.71 / 0.65).
+    // From the codes: fp32 rows, and up to 64 rows of bf16 (16 sequences of up to 4288 slots, 8 KV heads of 128, codes / unpacked: 48 bf16 rows 69 / 112 us,
+    // 64 87 / 111, 96 about 120 / 112; elements of 64, 64 rows 59 / 62, 96 80 / 65; up to 600 slots, 64 rows 28 / 36; 4 sequences 27 / 42.  fp32, 12 sequences of
+    // 2080 to 4160 slots: 64 rows 126 / 336, 2000 rows 3.0 / 5.2 ms, up to 8320 rows 5.2 / 7.2).
     p.few = rows_dtype == LAR_FP32 || chunk * group <= kCodesRows;
     if (p.few) {
         p.tq = (int)(chunk < kQ8Rows / group ? chunk : kQ8Rows / group);
