@@ -134,7 +134,7 @@ class Cache8:
 
 
 def attention_tolerance(dtype, ref, mag, big, d, longest, vmax):
-    """As R.attention_tolerance; rows of at most 16 per KV head take weights in fp16 (2^-11 of each; fp32 rows two of them: 2^-22), which below
+    """As R.attention_tolerance; what is computed from the codes takes weights in fp16 (2^-11 of each; fp32 rows two of them: 2^-22), which below
     2^-28 of the largest is off by 2^-39 of it; q in two fp16 numbers is off by 2^-22.  Longer chunks are the kernels of bf16 and fp32 caches."""
     rel = 2 * (big * (d * 2.0 ** -24 + 2.0 ** -21) + longest * 2.0 ** -24 + 2.0 ** -20)[..., None]
     tol = mag * rel + longest * 2.0 ** -39 * 2 * vmax + 1e-30
