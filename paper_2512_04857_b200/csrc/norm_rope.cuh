@@ -19,11 +19,6 @@
 
 namespace lar {
 
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ float sum_of(uint64_t v) {
     float a, b;
     unpack_f32x2(v, a, b);

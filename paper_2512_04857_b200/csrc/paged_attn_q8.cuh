@@ -12,7 +12,8 @@
 //   * The elements of a row may be contracted in any order, so a thread takes the four neighbouring codes that ldmatrix gives it as elements 2t,
 //     2t + 1, 2t + 8, 2t + 9 of the product, and q's fragments are loaded to match.  V^T comes from ldmatrix.trans on pairs of codes: rows g and g + 8 of a
 //     product are elements 2g and 2g + 1.
-//   * q is scaled by a power of two to 2^8 .. 2^9 per row (exact in fp16 down to 2^-22 of the row's largest element, off by 2^-33 of it below).  fp32
+//   * q is scaled by a power of two to 2^8 .. 2^9 per row (exact in fp16 down to 2^-22 of the row's largest element, off by 2^-33 of it below); the logits are
+//     multiplied by it again, so that they are finite where fp32 holds them, whatever q and K are.  fp32
 //     rows take two fp16 numbers for q and for the weights (22 bits), and sums of a tile are added to the accumulator with rounding.
 //   * A weight is p_j 2^(v_j), v_j the exponent of the slot's values.  fp16 has 5 bits of exponent, so each row keeps a reference vr of its own, the
 //     largest (logit - m) log2(e) scale + v_j so far: weights are at most 2^14, and what fp16 cannot hold is below 2^-38 of the row's largest weight.
@@ -26,6 +27,7 @@
 namespace lar {
 
 constexpr int kQ8Rows = 16;  // rows of a unit at most
+constexpr int kQ8WideByte = 229;  // a slot's power beyond 2^102
 
 // A step of a CTA's work, worked out by the producer: some slot tiles of one unit.
 struct alignas(16) Q8Seg {
@@ -295,7 +297,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
             if (n < 0) break;
             // per row of this thread (8 r + 2 quad + e): largest logit, sum, reference of the weights, accumulator (element 16 k + 2 qrow: e, + 1: 2 + e)
             float m[NR][2], l[NR][2], vr[NR][2], o[NR][KS][4];
-            float qs_row[NR][2], sc[NR][2];  // power of two that q was divided by, softmax scale of the divided logits
+            float qs_row[NR][2];  // power of two that q was divided by
             int last[NR][2];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
@@ -304,7 +306,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     const int row = 8 * r + 2 * quad + e;
                     m[r][e] = vr[r][e] = -INFINITY;
                     l[r][e] = 0.f;
-                    qs_row[r][e] = sc[r][e] = 0.f;
+                    qs_row[r][e] = 0.f;
                     last[r][e] = row >= g.n_tok * G ? -1 : a.causal ? min(g.slot0 + (int)(row * by_group >> 16), g.len - 1) : g.len - 1;
                 }
 #pragma unroll
@@ -344,10 +346,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        qs_row[r][e] = __shfl_sync(0xffffffffu, back, (2 * quad + e) * 4);
-                        sc[r][e] = fmaxf(a.scale_log2 * qs_row[r][e], 1.17549435e-38f);  // (-inf times it is -inf)
-                    }
+                    for (int e = 0; e < 2; ++e) qs_row[r][e] = __shfl_sync(0xffffffffu, back, (2 * quad + e) * 4);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty(qs));
@@ -369,12 +368,14 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     }
                     // scales of this thread's slots 16 mt + qrow + 8 h
                     float kf[MT][2], ve[MT][2];
+                    int k_most = 0;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at];
-                            kf[mt][h] = q8_scale(gscales[at + ks_at]);
+                            const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at], kb = gscales[at + ks_at];
+                            kf[mt][h] = q8_scale(kb);
+                            k_most = max(k_most, kb);
                             ve[mt][h] = vb == kQ8NaN ? INFINITY : (float)(vb - 127);
                         }
                     // S^T[slot][row]
@@ -400,12 +401,32 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                                 for (int r = 0; r < NR; ++r) mma_f16(s[mt][r], x[2], x[3], y[2], y[3], qf[u][r][k + 1][0], qf[u][r][k + 1][1]);
                         }
+                    // The products (2^25 at most) times the slot's power; the row's comes with the subtraction below.  Where a slot's power is above 2^102, both at
+                    // once and the slot's in two parts, the second one last, so that nothing on the way is beyond fp32 that the logit is not.
+                    const bool wide = __any_sync(0xffffffffu, k_most > kQ8WideByte);
+                    if (wide) {
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                        for (int r = 0; r < NR; ++r)
+                            for (int h = 0; h < 2; ++h) {
+                                const bool two = kf[mt][h] > 0x1p102f;
+                                const float first = two ? kf[mt][h] * 0x1p-64f : kf[mt][h], second = two ? 0x1p64f : 1.f;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[mt][r][e] *= kf[mt][e >> 1];
+                                for (int r = 0; r < NR; ++r)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        float& x = s[mt][r][2 * h + e];
+                                        x = x * first * qs_row[r][e] * second;
+                                    }
+                            }
+                    } else {
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) s[mt][r][e] *= kf[mt][e >> 1];
+                    }
                     if (base_slot < g.lo || base_slot + KT - 1 > min_last) {
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
@@ -440,7 +461,8 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     for (int r = 0; r < NR; ++r)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float mn = fmaxf(m[r][e], mx[r][e]), ref = softmax_ref(mn), shift = (m[r][e] - ref) * sc[r][e];
+                            const float f = wide ? 1.f : qs_row[r][e], mn = fmaxf(m[r][e], mx[r][e] * f);
+                            const float ref = mn == INFINITY ? NAN : softmax_ref(mn), shift = (m[r][e] - ref) * a.scale_log2;  // (beyond fp32: NaN)
                             m[r][e] = mn;
                             vr[r][e] += shift;
                             float sum = 0.f, most = -INFINITY;
@@ -449,7 +471,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                                 for (int h = 0; h < 2; ++h) {
                                     float& x = s[mt][r][2 * h + e];
-                                    x = (x - ref) * sc[r][e];
+                                    x = fmaf(x, f, -ref) * a.scale_log2;
                                     sum += ex2_approx(x);
                                     x += ve[mt][h];
                                     most = fmaxf(most, x);
@@ -559,7 +581,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                     for (int k = 0; k < KS; ++k) *reinterpret_cast<float2*>(p + 16 * k + 2 * qrow) = make_float2(o[r][k][e] * f, o[r][k][2 + e] * f);
                     if (qrow == 0) {
-                        p[D] = m[r][e] == -INFINITY ? -INFINITY : m[r][e] * qs_row[r][e];
+                        p[D] = m[r][e];
                         p[D + 1] = l[r][e];
                     }
                 }

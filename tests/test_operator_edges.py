@@ -1,0 +1,60 @@
+"""Head norms, 8-bit caches and slots in common where numbers, lengths and addresses come to their ends, against plain 64-bit forms."""
+import pytest
+import torch
+
+import _q8_reference as Q
+from _q8_reference import Cache8
+from paper_2512_04857_b200 import lar
+from test_norm_q8_ops import _check_attention, _close, _randn
+
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _store(c, which, s, rows):
+    """rows [hkv, n, d] into the slots of sequence s from 0 on, as the cache holds them."""
+    codes, byte = Q.quantise(rows)
+    c.put(s, which, 0, codes, byte)
+    c.vals[which][s] = Q.values(codes, byte)
+
+
+# ------------------------------------------------------------------------------------------------- logits of all sizes
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 3, 40])
+@pytest.mark.parametrize("a,b", [(0, 0), (0, 114), (0, 118), (8, 110), (-60, 118), (-100, 112), (-118, 117), (-124, 118), (60, -60), (100, -110), (119, -117), (115, -20)])
+def test_8bit_attention_of_queries_and_keys_of_any_size(dtype, d, n, a, b):
+    """q of 2^a and keys of up to 2^(b + 8), whose logits 2^(a + b) (257 + i) are exact in fp32: the softmax is that of i, whatever a and b are.  Some slots'
+    keys are as large as keys can be where q is zero: their logits are 0, as those of a row of zeros are."""
+    L = 300
+    c = Cache8(d, 1, 32, "nhd", [n], [L])
+    c.fill(1)
+    i = torch.arange(L) % 13
+    keys = torch.zeros(1, L, d, dtype=torch.float64)
+    keys[0, :, 0], keys[0, :, 1] = 2.0 ** (b + 8), (i + 1) * 2.0 ** b
+    keys[0, ::50] = 0
+    keys[0, 7::50] = 0
+    keys[0, 7::50, 5] = 2.0 ** 127
+    _store(c, 0, 0, keys.float())
+    assert torch.equal(c.vals[0][0], keys)
+    q = torch.zeros(n, 2, d, dtype=torch.float64)
+    q[:, :, :2] = 2.0 ** a
+    q = q.to(dtype)
+    out = torch.empty(n, 2, d, dtype=dtype, device=DEV)
+    c.kv.attn(q.to(DEV), out, softmax_scale=2.0 ** -(a + b), max_chunk=n, max_len=L, workspace=c.kv.attn_workspace(2, n, n, L, dtype=dtype))
+    x = keys[0, :, :2].sum(-1) * 2.0 ** -b
+    for t in range(n):
+        p = torch.softmax(x[:L - n + t + 1], 0)
+        V = c.vals[1][0][0, :L - n + t + 1]
+        ref, mag = p @ V, p @ V.abs()
+        # A logit times the scale: 12 below the largest at most where the weight counts, off by three roundings (2^-22 of 18, in powers of two); exponential
+        # 2^-21, sums of 300 terms: below 2^-15 of mag, in numerator and denominator.  Weights of bf16 rows: rounded to fp16 or bf16 (2^-8).
+        tol = mag * 2.0 ** -14
+        if dtype == BF:
+            tol = tol + mag * (2.0 ** -8 if 2 * n > 64 else 2.0 ** -11)
+            tol = tol + (ref.abs() + tol) * 2.0 ** -8
+        else:
+            tol = tol + ref.abs() * 2.0 ** -24
+        _close(out[t], ref.expand(2, d), tol.expand(2, d), f"token {t}")
