@@ -210,10 +210,14 @@ struct NormRope {
                 float ss, up = 1.f;
                 auto sums = [&]() {
                     if (layer) {
-                        uint64_t y = x[0];
+                        uint64_t y[E / 2];  // (pairs of pairs: the sum of equal elements is exact, and so is their mean)
 #pragma unroll
-                        for (int i = 1; i < E; ++i) y = add_f32x2(y, x[i]);
-                        const float mean = row_sum(sum_of(y)) * (-1.0f / D);
+                        for (int i = 0; i < E / 2; ++i) y[i] = add_f32x2(x[i], x[E / 2 + i]);
+#pragma unroll
+                        for (int n = E / 4; n > 0; n >>= 1)
+#pragma unroll
+                            for (int i = 0; i < n; ++i) y[i] = add_f32x2(y[i], y[n + i]);
+                        const float mean = row_sum(sum_of(y[0])) * (-1.0f / D);
                         const uint64_t m2 = pack_f32x2(mean, mean);
 #pragma unroll
                         for (int i = 0; i < E; ++i) x[i] = add_f32x2(x[i], m2);
@@ -225,12 +229,13 @@ struct NormRope {
                 };
                 sums();
                 if (__any_sync(0xffffffffu, !(ss <= 3.4e38f))) {
-                    // squares (or the sum) beyond fp32: once more from the row times 2^-80, beside which eps is nothing
+                    // squares (or the sum) beyond fp32: once more from the row times 2^-80.  What is left after the mean is then 2^96 of the row's units and more, beside which
+                    // eps is nothing, or nothing at all
                     if (!(ss <= 3.4e38f)) up = 0x1p-80f;
                     unpack(lo, hi, up, x);
                     sums();
                 }
-                const float f = rsqrtf(fmaf(ss, 1.0f / D, h.eps * up * up));
+                const float f = rsqrtf(max_nan(fmaf(ss, 1.0f / D, h.eps * up * up), 0x1p-126f));
                 const uint64_t f2 = pack_f32x2(f, f);
 #pragma unroll
                 for (int i = 0; i < E; i += 2) {

@@ -58,3 +58,29 @@ def test_8bit_attention_of_queries_and_keys_of_any_size(dtype, d, n, a, b):
         else:
             tol = tol + ref.abs() * 2.0 ** -24
         _close(out[t], ref.expand(2, d), tol.expand(2, d), f"token {t}")
+
+
+# ---------------------------------------------------------------------------------------------------- constant rows
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_layer_norm_of_large_rows_of_one_value(dtype, d):
+    """A row of equal elements has nothing left after its mean: what comes out is the bias, also where the row's sum lies beyond fp32.  Rows of +x and -x in
+    turn come out as +-1 times the weight and the bias."""
+    sizes = [0.0, 1.0, 3333.333, -0.7e-3, -2.0 ** 40, 2.0 ** 100, 2.0 ** 119, 2.0 ** 121, -2.0 ** 122, 1.9e36, 2.0 ** 126, 2.0 ** 127, -2.0 ** 127, 3.3e38]
+    x = torch.tensor(sizes)[None, :, None].expand(2, -1, d).clone()
+    x[1, :, ::2] *= -1
+    x = x.to(dtype)
+    w, b = _randn((d,), F32, 1, 0.3) + 1, _randn((d,), F32, 2)
+    out = torch.empty(2, len(sizes), d, dtype=dtype, device=DEV)
+    norm = lar.HeadNorm("layer", w.to(DEV), b.to(DEV))
+    lar.norm_rope_rotate(None, None, x.to(DEV), out, q_norm=norm)
+    assert torch.equal(out[0].cpu(), b.to(dtype).expand(len(sizes), d))
+    _close(out[1], Q.norm(x[1:], "layer", w, b, 1e-6)[0], Q.rounded(Q.norm(x[1:], "layer", w, b, 1e-6), Q.norm_tolerance(x[1:], "layer", w, b, 1e-6), dtype)[0])
+    # the same rows as keys on the way into an 8-bit cache
+    S = len(sizes)
+    c = Cache8(d, S, 16, "nhd", [2], [2])
+    c.kv.append_norm_rope(x.to(DEV), x.to(DEV), k_norm=norm)
+    codes, byte = c.get(0, 0, 0, 1)
+    want = Q.quantise(b.expand(S, 1, d))
+    assert torch.equal(codes.view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(byte, want[1])
