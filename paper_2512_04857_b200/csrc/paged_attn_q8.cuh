@@ -16,7 +16,8 @@
 //     multiplied by it again, so that they are finite where fp32 holds them, whatever q and K are.  fp32
 //     rows take two fp16 numbers for q and for the weights (22 bits), and sums of a tile are added to the accumulator with rounding.
 //   * A weight is p_j 2^(v_j), v_j the exponent of the slot's values.  fp16 has 5 bits of exponent, so each row keeps a reference vr of its own, the
-//     largest (logit - m) log2(e) scale + v_j so far: weights are at most 2^14, and what fp16 cannot hold is below 2^-38 of the row's largest weight.
+//     largest (logit - m) log2(e) scale + v_j so far: weights are at most 2^14, and what fp16 cannot hold is below 2^-38 of the row's largest weight.  A row
+//     of zeros, whose byte says nothing about it, has no weight.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -368,15 +369,15 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     }
                     // scales of this thread's slots 16 mt + qrow + 8 h
                     float kf[MT][2], ve[MT][2];
-                    int k_most = 0;
+                    bool rare = false;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at], kb = gscales[at + ks_at];
                             kf[mt][h] = q8_scale(kb);
-                            k_most = max(k_most, kb);
                             ve[mt][h] = vb == kQ8NaN ? INFINITY : (float)(vb - 127);
+                            rare |= kb > kQ8WideByte || vb == 127;
                         }
                     // S^T[slot][row]
                     float s[MT][NR][4];
@@ -401,10 +402,28 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                                 for (int r = 0; r < NR; ++r) mma_f16(s[mt][r], x[2], x[3], y[2], y[3], qf[u][r][k + 1][0], qf[u][r][k + 1][1]);
                         }
-                    // The products (2^25 at most) times the slot's power; the row's comes with the subtraction below.  Where a slot's power is above 2^102, both at
+                    rare = __any_sync(0xffffffffu, rare);
+                    if (rare) {
+                        // a row of zeros has a byte of 127: its weight is none, and must not be what the others' are measured by
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                uint32_t any = 0;  // a quarter of the row's codes
+#pragma unroll
+                                for (int c = 0; c < D / 64; ++c) {
+                                    uint32_t x[4];
+                                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(tile + v_at + block(mt) * D + off(qrow + 8 * h, quad * (D / 64) + c)));
+                                    any |= (x[0] | x[1] | x[2] | x[3]) & 0x7f7f7f7fu;
+                                }
+                                any |= __shfl_xor_sync(0xffffffffu, any, 1);
+                                any |= __shfl_xor_sync(0xffffffffu, any, 2);
+                                if (any == 0 && ve[mt][h] == 0.f) ve[mt][h] = -INFINITY;
+                            }
+                    }
+                    // The products (2^25 at most) times the slot's power; the row's comes with the subtraction below.  Where a slot's power may be above 2^102, both at
                     // once and the slot's in two parts, the second one last, so that nothing on the way is beyond fp32 that the logit is not.
-                    const bool wide = __any_sync(0xffffffffu, k_most > kQ8WideByte);
-                    if (wide) {
+                    if (rare) {
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -461,7 +480,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     for (int r = 0; r < NR; ++r)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float f = wide ? 1.f : qs_row[r][e], mn = fmaxf(m[r][e], mx[r][e] * f);
+                            const float f = rare ? 1.f : qs_row[r][e], mn = fmaxf(m[r][e], mx[r][e] * f);
                             const float ref = mn == INFINITY ? NAN : softmax_ref(mn), shift = (m[r][e] - ref) * a.scale_log2;  // (beyond fp32: NaN)
                             m[r][e] = mn;
                             vr[r][e] += shift;

@@ -84,3 +84,23 @@ def test_layer_norm_of_large_rows_of_one_value(dtype, d):
     codes, byte = c.get(0, 0, 0, 1)
     want = Q.quantise(b.expand(S, 1, d))
     assert torch.equal(codes.view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(byte, want[1])
+
+
+# ------------------------------------------------------------------------------------------------- values of all sizes
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,hkv,hq", [(64, 2, 4), (128, 1, 8)])
+@pytest.mark.parametrize("n,lens", [([1], [300]), ([3, 1], [700, 90]), ([40, 9], [400, 1200])])
+@pytest.mark.parametrize("power", [-10, -30, -45, -70])
+def test_8bit_attention_of_small_values_beside_rows_of_zeros(dtype, d, hkv, hq, n, lens, power):
+    """A row of zeros adds nothing, whatever its byte (127) says: small values beside it keep all their bits."""
+    c = Cache8(d, hkv, 32, "nhd", n, lens, seed=1)
+    c.fill(2)
+    g = torch.Generator().manual_seed(3)
+    for s, L in enumerate(lens):
+        v = torch.randn(hkv, L, d, generator=g) * 2.0 ** power
+        v[:, ::5] = 0
+        v[:, 3:90] = 0                                           # whole tiles of them
+        _store(c, 1, s, v)
+    for causal in (True, False):
+        _check_attention(c, hq, dtype, causal, None, True, 4)
