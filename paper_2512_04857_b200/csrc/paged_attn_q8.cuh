@@ -596,9 +596,9 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                     for (int w = 4; w <= 16; w <<= 1) l[r][e] += __shfl_xor_sync(0xffffffffu, l[r][e], w);
                     float* p = part + (8 * r + 2 * quad + e) * S::PS;
-                    const float f = ex2_approx(vr[r][e] - 14.f);  // (nothing seen: 0)
+                    const float f = ex2_approx(vr[r][e]);  // (nothing seen: 0; with the 2^-14 in it the smallest would be zero too)
 #pragma unroll
-                    for (int k = 0; k < KS; ++k) *reinterpret_cast<float2*>(p + 16 * k + 2 * qrow) = make_float2(o[r][k][e] * f, o[r][k][2 + e] * f);
+                    for (int k = 0; k < KS; ++k) *reinterpret_cast<float2*>(p + 16 * k + 2 * qrow) = make_float2(o[r][k][e] * 0x1p-14f * f, o[r][k][2 + e] * 0x1p-14f * f);
                     if (qrow == 0) {
                         p[D] = m[r][e];
                         p[D + 1] = l[r][e];

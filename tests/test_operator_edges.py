@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import _paged_reference as R
 import _q8_reference as Q
 from _q8_reference import Cache8
 from paper_2512_04857_b200 import lar
@@ -104,3 +105,25 @@ def test_8bit_attention_of_small_values_beside_rows_of_zeros(dtype, d, hkv, hq, 
         _store(c, 1, s, v)
     for causal in (True, False):
         _check_attention(c, hq, dtype, causal, None, True, 4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 5, 50])
+def test_8bit_attention_of_the_smallest_values(dtype, d, n):
+    """Values of 2^-98 to 2^-114: the result is as small, but far from what fp32 cannot hold."""
+    L = 200
+    for power in (-98, -104, -108, -114):
+        c = Cache8(d, 1, 16, "nhd", [n], [L])
+        c.fill(1)
+        g = torch.Generator().manual_seed(3)
+        _store(c, 1, 0, torch.randn(1, L, d, generator=g).clamp(-4, 4) * 2.0 ** power)
+        q = _randn((n, 2, d), dtype, 5)
+        out = torch.empty(n, 2, d, dtype=dtype, device=DEV)
+        c.kv.attn(q.to(DEV), out, max_chunk=n, max_len=L, workspace=c.kv.attn_workspace(2, n, n, L, dtype=dtype))
+        up = 2.0 ** -power
+        big_v = c.vals[1][0] * up
+        ref, mag, big = R.attention(q, c.rows(0), lambda s, h, j0, j1: big_v[h, j0:j1], [n], [L], None, True, 2, d ** -0.5)
+        tol = torch.maximum(Q.attention_tolerance(dtype, ref, mag, big, d, L, 4.0), R.attention_tolerance(dtype, ref, mag, big, d, L) if 2 * n > 64 else torch.zeros(()))
+        _close(out.double() * up, ref, tol + 2.0 ** -149 * up * 2 * L, f"2^{power}")
