@@ -13,6 +13,7 @@
 #pragma once
 #include "join_parts.cuh"
 #include "paged_attn.cuh"
+#include "part_range.h"
 
 namespace lar {
 
@@ -83,7 +84,7 @@ struct SharedPass {
     const int2* row_ref;  // null: nothing is cut
     const float* part_o;
     const float* part_ml;
-    int parts, range_rows;  // rows that a range leaves
+    int parts, ranges, range_rows;  // ranges that units are cut into, rows that one leaves
 };
 
 struct SharedJoinArgs {
@@ -120,11 +121,11 @@ __global__ void __launch_bounds__(kSharedJoinThreads, 4) shared_join_kernel(cons
             const SharedPass& p = a.pass[w];
             if (!mine || (w == 0 && (t < g0 || t >= g1))) continue;  // (a sequence of no group)
             const int2 ref = p.row_ref ? p.row_ref[row] : make_int2(-1, 0);
-            if (ref.x >= 0) {
-                const int range = ref.x & 0xffff, last = ref.x >> 16;
+            const PartRange r = part_range(ref.x, ref.y, p.ranges, p.range_rows);
+            if (r.first >= 0) {
 #pragma unroll 4
-                for (int c = range + part0; c <= last; c += step) {
-                    const size_t at = (size_t)(c * 2 + (c == range ? 1 : 0)) * p.range_rows + ref.y;
+                for (int c = r.first + part0; c <= r.last; c += step) {
+                    const size_t at = (size_t)(c * 2 + (c == r.first ? 1 : 0)) * p.range_rows + r.row;
                     sum.add(*reinterpret_cast<const float2*>(p.part_ml + at * 2), *reinterpret_cast<const float4*>(p.part_o + at * D + e), a.scale_log2);
                 }
             } else {

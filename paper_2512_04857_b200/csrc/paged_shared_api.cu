@@ -186,6 +186,7 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
             left.row_o = b.row_o;
             left.row_ml = b.row_ml;
             left.parts = 1;
+            left.ranges = plan.grid;
             left.range_rows = (plan.nt == 2 ? 2 : 1) * plan.rows_cap;
             if (plan.splits == 2) {  // as launch_tc lays it out
                 left.row_ref = b.row_ref;

@@ -1,4 +1,9 @@
 """Head norms, 8-bit caches and slots in common where numbers, lengths and addresses come to their ends, against plain 64-bit forms."""
+import ctypes as C
+import os
+import random
+import subprocess
+
 import pytest
 import torch
 
@@ -127,3 +132,30 @@ def test_8bit_attention_of_the_smallest_values(dtype, d, n):
         ref, mag, big = R.attention(q, c.rows(0), lambda s, h, j0, j1: big_v[h, j0:j1], [n], [L], None, True, 2, d ** -0.5)
         tol = torch.maximum(Q.attention_tolerance(dtype, ref, mag, big, d, L, 4.0), R.attention_tolerance(dtype, ref, mag, big, d, L) if 2 * n > 64 else torch.zeros(()))
         _close(out.double() * up, ref, tol + 2.0 ** -149 * up * 2 * L, f"2^{power}")
+
+
+# ------------------------------------------------------------------------------------- what a pass that gave up leaves
+def test_parts_of_a_row_lie_inside_the_workspace(tmp_path):
+    """The join of slots in common reads a row's parts where the row's pass says; a pass whose wait ran out leaves whatever the workspace held.  For any words there the ranges
+    and the row stay inside what the pass has, and what a pass does write is taken as it is."""
+    src = tmp_path / "t.cpp"
+    src.write_text('''#include "part_range.h"
+        extern "C" void f(int x, int y, int ranges, int rows, int* out) {
+            lar::PartRange p = lar::part_range(x, y, ranges, rows);
+            out[0] = p.first; out[1] = p.last; out[2] = p.row;
+        }''')
+    so = tmp_path / "t.so"
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", "-I", os.path.join(os.path.dirname(lar.LIB_PATH), "csrc"), "-o", str(so), str(src)], check=True)
+    f, out, rng = C.CDLL(str(so)).f, (C.c_int * 3)(), random.Random(1)
+    word = lambda: rng.choice([0, -1, 255, 2 ** 31 - 1, -2 ** 31, rng.getrandbits(32) - 2 ** 31, rng.getrandbits(24), rng.getrandbits(9)])
+    for _ in range(20000):
+        ranges, rows = rng.choice([1, 8, 148, 296, 444]), rng.choice([1, 8, 64, 256])
+        x, y = word(), word()
+        f(x, y, ranges, rows, out)
+        if x < 0:
+            assert out[0] == -1
+            continue
+        assert 0 <= out[0] < ranges and out[1] < ranges and 0 <= out[2] < rows
+        a, b, r = rng.randrange(ranges), rng.randrange(ranges), rng.randrange(rows)
+        f(a + 65536 * b, r, ranges, rows, out)
+        assert list(out) == [a, b, r]
