@@ -680,12 +680,16 @@ struct Q8UnpackArgs {
 constexpr int kQ8UnpackSlots = 32;
 
 // Live entries of every sequence as dense pages of 128 bf16 rows (exact), for the kernels of longer chunks of bf16 rows (each element is read by many row tiles there: turned once, not once for
-// each).  A CTA has 32 slots of K or V; slots outside [start, len) are left alone: whoever reads the pages masks them.
+// each).  A CTA has 32 slots of K or V; slots outside [start, len) are left alone: whoever reads the pages masks them.  So are sequences without tokens: nobody reads theirs,
+// and their own pages may be gone.
 template <int D>
 __global__ void __launch_bounds__(kQ8ReadThreads) q8_unpack_kernel(const __grid_constant__ Q8UnpackArgs a) {
     constexpr int IPR = D / 16, E = 8, BATCH = 4;
     const int tid = threadIdx.x, s = blockIdx.y, is_v = blockIdx.z, first = blockIdx.x * kQ8UnpackSlots;
     if (tid == 0 && is_v == 0 && (first & 127) == 0) a.table[s * a.cols + (first >> 7)] = s * a.cols + (first >> 7);
+    int t0, t1;
+    chunk_of(a.kv, s, t0, t1);
+    if (t0 == t1) return;
     const int len = min(live_len(a.kv, s, 0, false), a.cols * 128), lo = a.start ? max(a.start[s], 0) : 0;
     const int j0 = max(first, lo), j1 = min(first + kQ8UnpackSlots, len);
     if (j0 >= j1) return;

@@ -228,6 +228,7 @@ lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, cons
         w.kv = a.kv;
         w.kv.table += s0 * k.table_seq_stride;
         w.kv.lens = u.lens;
+        if (cu_tokens) w.kv.cu = cu_tokens + s0;
         w.kv.n_seqs = n;
         w.q8 = q8;
         w.start = kv_start ? kv_start + s0 : nullptr;

@@ -159,3 +159,21 @@ def test_parts_of_a_row_lie_inside_the_workspace(tmp_path):
         a, b, r = rng.randrange(ranges), rng.randrange(ranges), rng.randrange(rows)
         f(a + 65536 * b, r, ranges, rows, out)
         assert list(out) == [a, b, r]
+
+
+# ------------------------------------------------------------------------------------------------- idle sequences
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,lens", [([0, 1, 0, 1], [90, 70, 0, 300]), ([0, 6, 1, 0], [700, 70, 130, 40]), ([0, 150, 0, 1, 0], [500, 300, 0, 200, 260]),
+                                    ([70, 0, 33], [2500, 90, 2100])])
+def test_8bit_attention_beside_sequences_without_tokens(dtype, n, lens):
+    """Sequences without tokens may have given up their pages, whatever their lengths still say: nothing of them is looked at and nothing recorded."""
+    for layout, d, hkv, hq in (("nhd", 128, 2, 4), ("heads", 64, 2, 2)):
+        c = Cache8(d, hkv, 32, layout, n, lens, seed=4)
+        c.fill(5)
+        for s, m in enumerate(n):
+            if m == 0:
+                c.table_dev[s] = -1
+        for causal in (True, False):
+            for hints in (True, False):
+                _check_attention(c, hq, dtype, causal, None, True, 6, hints=hints)
