@@ -111,6 +111,12 @@ bool q8_view(const lar_paged_q8_t* c, int64_t n_tokens, const int32_t* cu, Paged
     if (!c || c->struct_size != sizeof(lar_paged_q8_t) || c->reserved || !paged_view(&c->kv, n_tokens, cu, v, true)) return false;
     if (c->kv.k_pool == c->kv.v_pool || c->k_scale == c->v_scale) return false;
     if (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)) return false;
+    // the attention's copies take K and V as one tensor with the distance as a stride, which a tensor map holds below 2^40 bytes
+    auto far = [](const void* x, const void* y) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+        return (p < q ? q - p : p - q) >= ((uintptr_t)1 << 40);
+    };
+    if (far(c->kv.k_pool, c->kv.v_pool) || far(c->k_scale, c->v_scale)) return false;
     const int64_t strides[2] = {c->scale_page_stride, c->scale_head_stride};
     for (int64_t s : strides)
         if (s < 0 || s > (1ll << 36) || s % 16) return false;

@@ -588,6 +588,7 @@ class PagedKV8(PagedKV):
 
     k_pool, v_pool    float8_e4m3fn or uint8, shaped and strided as PagedKV's
     k_scale, v_scale  uint8 [pages, heads, page_tokens], the bytes of a page's slots side by side; strides multiples of 16
+                      (the two pools less than 2^40 bytes apart, and the two scales: one allocation for both is)
     page_table, lens, status as PagedKV's
 
     The rows that go in and come out (k, v, q, out) are bf16 or fp32, whichever the call's tensors are.

@@ -11,10 +11,11 @@ import _paged_reference as R
 import _q8_reference as Q
 from _q8_reference import Cache8
 from paper_2512_04857_b200 import lar
-from test_norm_q8_ops import _check_attention, _close, _randn
+from test_norm_q8_ops import _check_attention, _close, _q8, _r, _randn
 
 DEV = "cuda:0"
 BF, F32 = torch.bfloat16, torch.float32
+INVALID = lar.LAR_ERR_INVALID_ARG
 dev = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
 
 
@@ -177,3 +178,23 @@ def test_8bit_attention_beside_sequences_without_tokens(dtype, n, lens):
         for causal in (True, False):
             for hints in (True, False):
                 _check_attention(c, hq, dtype, causal, None, True, 6, hints=hints)
+
+
+# ------------------------------------------------------------------------------------------------ addresses, refusals
+def test_pools_too_far_apart_are_refused_by_every_call():
+    """K and V are one tensor to the copies, the distance of their pools one of its strides: below 2^40 bytes, and that of the scales too."""
+    L, rows = lar.lib(), _r()
+    for far, near in ((1 << 40, (1 << 40) - 16), ((1 << 46) + 4096, 1 << 20)):
+        for where in ("pool", "scale"):
+            for first, second in ((4096, 4096 + far), (4096 + far, 4096)):
+                c = _q8(k_pool=first, v_pool=second) if where == "pool" else _q8(k_scale=first, v_scale=second)
+                assert L.lar_paged_q8_append(c, 0, None, None, None, None, 0, rows, rows, None, None, 0, 6, None, None) == INVALID
+                assert L.lar_paged_q8_append(c, 0, None, None, None, None, 0, rows, rows, None, None, 0, 0, None, None) == INVALID
+                assert L.lar_paged_q8_read(c, 0, rows, rows, 0, None, None) == INVALID
+                for n in (0, 6, 200):
+                    assert L.lar_paged_q8_attn(c, 0, rows, rows, 2, n, None, None, 1, 0.0, 0, 0, None, 0, None) == INVALID
+                assert L.lar_paged_q8_attn_workspace_bytes(c, 0, 2, 200, 100, 0) == 0
+            ok = _q8(k_pool=4096, v_pool=4096 + near) if where == "pool" else _q8(k_scale=4096 + near, v_scale=4096)
+            assert L.lar_paged_q8_read(ok, 0, rows, rows, 0, None, None) == lar.LAR_OK
+            assert L.lar_paged_q8_attn(ok, 0, rows, rows, 2, 0, None, None, 1, 0.0, 0, 0, None, 0, None) == lar.LAR_OK
+            assert L.lar_paged_q8_attn_workspace_bytes(ok, 0, 2, 200, 100, 0) > 0
