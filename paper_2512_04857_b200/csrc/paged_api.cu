@@ -91,6 +91,13 @@ bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, Pa
     return true;
 }
 
+lar_status_t paged_attn_fits(const lar_paged_kv_t& kv, int group, int64_t n_tokens, int max_chunk, int max_len, bool workspace, size_t workspace_bytes) {
+    if (kv.dtype == LAR_BF16 && kv.n_seqs > kTcMaxSeqs) return LAR_ERR_CAPACITY;
+    const AttnPlan p = attn_plan(kv, group, n_tokens, max_chunk, max_len, workspace);
+    if (p.bytes > workspace_bytes) return LAR_ERR_NOMEM;
+    return kv.dtype == LAR_BF16 && !countable(kv, p, n_tokens) ? LAR_ERR_CAPACITY : LAR_OK;
+}
+
 // Launch shape of the rotary kernels: token blocks x slices of a token's rows.
 dim3 rope_grid(RopeRowsArgs& a) {
     a.n_rows = a.heads[0] + a.heads[1] + a.heads[2];
@@ -238,11 +245,10 @@ lar_status_t lar_paged_attn(const lar_paged_kv_t* kv, const lar_rows_t* q, const
     if (n_tokens == 0) return LAR_OK;
     const int elt = elt_of(kv->dtype), d = kv->head_dim;
     if (!rows_view(q, n_tokens, n_q_heads, d, elt, false, a.q) || !rows_view(out, n_tokens, n_q_heads, d, elt, true, a.out)) return LAR_ERR_INVALID_ARG;
-    if (kv->dtype == LAR_BF16 && kv->n_seqs > lar::kTcMaxSeqs) return LAR_ERR_CAPACITY;
-    const AttnPlan p = attn_plan(*kv, group, n_tokens, max_chunk, max_len, workspace != nullptr);
     if (workspace && !aligned(workspace, 16)) return LAR_ERR_INVALID_ARG;
-    if (p.bytes > workspace_bytes) return LAR_ERR_NOMEM;
-    if (kv->dtype == LAR_BF16 && !countable(*kv, p, n_tokens)) return LAR_ERR_CAPACITY;
+    const lar_status_t fits = lar::paged_attn_fits(*kv, group, n_tokens, max_chunk, max_len, workspace != nullptr, workspace_bytes);
+    if (fits != LAR_OK) return fits;
+    const AttnPlan p = attn_plan(*kv, group, n_tokens, max_chunk, max_len, workspace != nullptr);
     a.start = kv_start;
     a.group = group;
     a.causal = causal != 0;

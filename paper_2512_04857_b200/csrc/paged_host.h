@@ -19,6 +19,8 @@ inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_
 bool rope_freqs(const lar_rope_t* r, int inverse, RopeFreqs& f);
 bool rows_view(const lar_rows_t* r, int64_t tokens, int heads, int d, int elt, bool output, RowsView& v);
 bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, PagedView& v, bool q8 = false);
+// What lar_paged_attn with these (checked) arguments would be refused for: LAR_ERR_CAPACITY, LAR_ERR_NOMEM, or LAR_OK.
+lar_status_t paged_attn_fits(const lar_paged_kv_t& kv, int group, int64_t n_tokens, int max_chunk, int max_len, bool workspace, size_t workspace_bytes);
 struct Q8View;
 bool q8_view(const lar_paged_q8_t* c, int64_t n_tokens, const int32_t* cu, PagedView& v, Q8View& q);
 dim3 rope_grid(RopeRowsArgs& a);

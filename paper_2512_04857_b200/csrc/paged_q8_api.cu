@@ -220,6 +220,12 @@ lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, cons
         a.part_o = static_cast<float*>(workspace);
         return rows_dtype == LAR_BF16 ? launch_few_of<__nv_bfloat16>(*cache, a, p, s) : launch_few_of<float>(*cache, a, p, s);
     }
+    // Everything that may be refused is, before the first launch: a full batch, and the last one where it is smaller.
+    for (int n : {p.batch, k.n_seqs % p.batch}) {
+        if (n == 0) continue;
+        const lar_status_t st = paged_attn_fits(unpacked(k, p, n, workspace), group, cu_tokens ? n_tokens : (int64_t)n * a.kv.chunk, max_chunk, max_len, true, workspace_bytes - p.bytes);
+        if (st != LAR_OK) return st;
+    }
     for (int s0 = 0; s0 < k.n_seqs; s0 += p.batch) {
         const int n = k.n_seqs - s0 < p.batch ? k.n_seqs - s0 : p.batch;
         lar_paged_kv_t u = unpacked(k, p, n, workspace);

@@ -198,3 +198,18 @@ def test_pools_too_far_apart_are_refused_by_every_call():
             assert L.lar_paged_q8_read(ok, 0, rows, rows, 0, None, None) == lar.LAR_OK
             assert L.lar_paged_q8_attn(ok, 0, rows, rows, 2, 0, None, None, 1, 0.0, 0, 0, None, 0, None) == lar.LAR_OK
             assert L.lar_paged_q8_attn_workspace_bytes(ok, 0, 2, 200, 100, 0) > 0
+
+
+def test_a_long_8bit_call_is_refused_before_anything_is_launched():
+    """A workspace that holds the unpacked rows but not what the attention over them wants, and caches whose tiles that attention cannot count: refused by the checks, not behind the
+    first kernels (without a GPU a launch would fail in another way)."""
+    L = lar.lib()
+    c, n = _q8(n_seqs=2, n_pages=4096, table_cols=200, table_seq_stride=200), 400     # 2 x 6400 slots, 2 heads of 64
+    need = L.lar_paged_q8_attn_workspace_bytes(c, 0, 2, n, 200, 0)
+    slots = 200 * 32
+    unpacked = 2 * 2 * slots * 2 * 64 * 2 + -(-2 * slots // 128 * 4 // 256) * 256       # K and V of both sequences as bf16 rows, their page table
+    assert unpacked + 4096 < need
+    call = lambda c, n, nb: L.lar_paged_q8_attn(c, 0, _r(), _r(1 << 20), 2, n, None, None, 1, 0.0, 200, 0, 4096, nb, None)
+    assert call(c, n, unpacked - 1) == lar.LAR_ERR_NOMEM and call(c, n, unpacked) == lar.LAR_ERR_NOMEM
+    huge = _q8(n_seqs=8, n_pages=1 << 24, table_cols=1 << 23, page_tokens=128, sp=256, sh=128, page_stride=2 * 128 * 64)
+    assert call(huge, 8 * 20000, 1 << 62) == lar.LAR_ERR_CAPACITY
