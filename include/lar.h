@@ -463,8 +463,8 @@ lar_status_t lar_append_kv_norm_rope(lar_cache_t* c, int layer, const lar_head_n
  * for every row: the byte of row r of page p and head h is scale[p * scale_page_stride + h * scale_head_stride + r] (16-byte aligned, strides
  * multiples of 16; heads with pages of their own have scale_head_stride = 0).  The pools of K and V are different and lie less than 2^40 bytes apart, and so do
  * k_scale and v_scale: allocate them together (memory of different allocators of one GPU may lie farther apart; such a cache is refused).  An element is  e4m3(code) * 2^(b - 127);  a row is stored
- * with the smallest power 2^(b - 127), at least 2^-117, for which none of its elements exceeds 448 times it, codes rounded to nearest even (an element
- * below 2^-15 of the row's largest to a multiple of 2^-18 of it); a row of zeros has b = 127.  A row with an element that is not
+ * with the smallest power 2^(b - 127), at least 2^-117, for which none of its elements exceeds 448 times it, codes rounded to nearest even: 4 significant
+ * bits down to 2^-6 times that power (2^-13.8 to 2^-14.8 of the row's largest element), below it multiples of 2^-9 times the power (2^-16.8 to 2^-17.8 of it); a row of zeros has b = 127.  A row with an element that is not
  * finite is stored as b = 255 and reads as NaN. */
 #define LAR_E4M3 2
 typedef struct lar_paged_q8 {

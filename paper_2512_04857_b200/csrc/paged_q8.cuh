@@ -2,7 +2,7 @@
 //
 // A row x of head_dim elements is held as e4m3 codes c and one byte b:  x = c 2^(b - 127),  b - 127 = k the smallest power for which no
 // element exceeds 448 2^k (448 is e4m3's largest number), at least -117.  A power of two costs no accuracy (the codes have an exponent of
-// their own: 4 significant bits down to 2^-15 of the row's largest element, absolute steps of 2^-18 of it below), needs no
+// their own: 4 significant bits down to 2^(k - 6), which is 2^-13.8 to 2^-14.8 of the row's largest element, absolute steps of 2^(k - 9) below), needs no
 // division, and makes every value exact in bf16 and fp32, so that reading back loses nothing.  A row with an element that is not finite has
 // b = 255 and codes of zero: it reads as NaN (0 times infinity), all of it.
 #pragma once

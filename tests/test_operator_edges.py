@@ -135,6 +135,31 @@ def test_8bit_attention_of_the_smallest_values(dtype, d, n):
         _close(out.double() * up, ref, tol + 2.0 ** -149 * up * 2 * L, f"2^{power}")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_8bit_rows_are_as_near_as_the_format_says(dtype):
+    """Rows whose largest element is anything from just above 224 to 448 times the power, the others down to 2^-12 of the power: off by half a step, 2^-4 of an element or 2^-10 of the
+    power (for the first of these rows 2^-17.8 of the largest element)."""
+    g = torch.Generator().manual_seed(1)
+    tops = [225.0, 226.0, 256.0, 300.0, 446.0, 448.0]
+    rows = torch.exp2(torch.rand(len(tops) * 40, 64, generator=g) * 14 - 12) * torch.where(torch.rand(len(tops) * 40, 64, generator=g) < 0.5, -1.0, 1.0)
+    rows[:, 0] = torch.tensor(tops).repeat(40)
+    rows[:, 1] = 2.0 ** -9 * 1.5 - 2.0 ** -16                      # just below the middle of two steps
+    x = (rows * torch.exp2(torch.arange(len(rows)) % 50 - 25.0)[:, None]).to(dtype)[:, None]
+    n = len(x)
+    c = Cache8(64, 1, 16, "nhd", [n], [n])
+    c.kv.append_rope(x.to(DEV), x.to(DEV))
+    ko, vo = torch.empty_like(x, device=DEV), torch.empty_like(x, device=DEV)
+    c.kv.read(ko, vo)
+    assert torch.equal(ko, vo)
+    power = torch.exp2(c.get(0, 0, 0, n)[1][0].double() - 127)[:, None]
+    x, diff = x[:, 0].double(), (ko[:, 0].cpu().double() - x[:, 0].double()).abs()
+    largest = x.abs().amax(1, keepdim=True)
+    assert (largest > 224 * power).all() and (largest <= 448 * power).all()
+    assert (diff <= torch.maximum(x.abs() * 2.0 ** -4, power * 2.0 ** -10)).all()
+    assert (diff <= torch.maximum(x.abs() * 2.0 ** -4, largest * 2.0 ** -17.8)).all() and (diff > torch.maximum(x.abs() * 2.0 ** -4, largest * 2.0 ** -18)).any()
+
+
 # ------------------------------------------------------------------------------------- what a pass that gave up leaves
 def test_parts_of_a_row_lie_inside_the_workspace(tmp_path):
     """The join of slots in common reads a row's parts where the row's pass says; a pass whose wait ran out leaves whatever the workspace held.  For any words there the ranges
