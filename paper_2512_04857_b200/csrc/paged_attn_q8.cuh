@@ -53,14 +53,16 @@ struct Q8Shape {
     static constexpr int PER_SM = D == 64 && NR == 1 ? 3 : 2;  // (64 x 577 slots, 20 heads of 64, 1 to 8 tokens: 27 us with three CTAs, 31 with two)
     static constexpr int ROWS = 8 * NR;
     // Units that the producer is ahead by at most.  (Two where rows are many, which lets two CTAs share an SM with 128 elements: 16 x 4288 slots, 16 rows 38.6 instead of 43.8
-    // us, 32 rows 57 instead of 70; fp32 with 4 stages instead of 8, 51 instead of 55.)
-    static constexpr int QS = NR == 2 ? 2 : 4;
+    // us, 32 rows 57 instead of 70; fp32 with 4 stages instead of 8, 51 instead of 55.  So with 8 rows of 128: four steps and two buffers of parts leave fp32 rows one CTA, and
+    // bf16 rows from 192 sequences on, as the lengths take shared memory too: one fp32 row over 16 x 4288 slots 30.2 -> 23.7 us, 3 x 65537 81 -> 56, bf16 256 x 1153 102 -> 70, 1024 x
+    // 577 251 -> 153; bf16 over few sequences is the same either way.)
+    static constexpr int QS = NR == 2 || D == 128 ? 2 : 4;
     static constexpr int Q_SLOT = ROWS * D * (int)sizeof(T);
     static constexpr int PS = D + 4;              // floats of a partial row: O, m, l, padding
-    static constexpr int PBUFS = NR == 1 ? 2 : 1;
+    static constexpr int PBUFS = NR == 1 && D == 64 ? 2 : 1;
     static constexpr int PBUF_FLOATS = W * ROWS * PS;
     static constexpr int FIXED = 1024 + NS * (STAGE_BYTES + SCALE_PITCH) + QS * (Q_SLOT + (int)sizeof(Q8Seg)) + PBUFS * PBUF_FLOATS * 4 + 32 * 8;
-    static __host__ __device__ int bytes(int n_seqs) { return FIXED + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
+    static __host__ __device__ constexpr int bytes(int n_seqs) { return FIXED + n_seqs * 16 + 2 * (n_seqs + 1) * 4 + 16 * 4; }
 };
 
 struct Q8Maps {
@@ -120,6 +122,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
     using S = Q8Shape<T, D, NR>;
     using Work = TcWork<1, S::KT, D>;
     constexpr int KT = S::KT, W = S::W, NS = S::NS, TERMS = S::TERMS, KS = S::KS, MT = S::MT;
+    static_assert(S::PER_SM * (S::bytes(128) + 1024) <= 233472, "shared memory of an SM");
     const PagedAttnArgs& a = ta.a;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
