@@ -28,7 +28,6 @@
 namespace lar {
 
 constexpr int kQ8Rows = 16;  // rows of a unit at most
-constexpr int kQ8WideByte = 229;  // a slot's power beyond 2^102
 
 // A step of a CTA's work, worked out by the producer: some slot tiles of one unit.
 struct alignas(16) Q8Seg {
@@ -290,6 +289,9 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
         const uint32_t box_bytes = ta.box_rows * D, k_at = maps.v_first ? box_bytes : 0, v_at = maps.v_first ? 0 : box_bytes;
         const int ks_at = maps.v_scale_first ? ta.box_rows : 0, vs_at = maps.v_scale_first ? 0 : ta.box_rows;
         const int box_mask = ta.box_rows - 1, box_shift = __ffs(ta.box_rows) - 1;
+        // Four of a tile's bytes, of K or of V, for each lane: rare are powers of K from 2^97 on (a byte whose three highest bits are set), and V's byte of a row of zeros
+        const int rare_slot = lane % (KT / 4) * 4, rare_v = lane / (KT / 4) & 1;
+        const int rare_at = (rare_slot >> box_shift) * 128 + (rare_slot & box_mask) + (rare_v ? vs_at : ks_at);
         auto block = [&](int mt) { return (uint32_t)((16 * mt & ~box_mask) * 2 + (16 * mt & box_mask)); };  // rows before the block
         // byte offset of 16-byte chunk c of row r of a block (128- or 64-byte swizzle)
         auto off = [](int r, int c) { return (uint32_t)(D == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); };
@@ -372,7 +374,6 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     }
                     // scales of this thread's slots 16 mt + qrow + 8 h
                     float kf[MT][2], ve[MT][2];
-                    bool rare = false;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -380,7 +381,6 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                             const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at], kb = gscales[at + ks_at];
                             kf[mt][h] = q8_scale(kb);
                             ve[mt][h] = vb == kQ8NaN ? INFINITY : (float)(vb - 127);
-                            rare |= kb > kQ8WideByte || vb == 127;
                         }
                     // S^T[slot][row]
                     float s[MT][NR][4];
@@ -405,7 +405,9 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                                 for (int r = 0; r < NR; ++r) mma_f16(s[mt][r], x[2], x[3], y[2], y[3], qf[u][r][k + 1][0], qf[u][r][k + 1][1]);
                         }
-                    rare = __any_sync(0xffffffffu, rare);
+                    const uint32_t bytes = *reinterpret_cast<const uint32_t*>(gscales + st * S::SCALE_PITCH + rare_at);
+                    const uint32_t not127 = bytes ^ 0x7f7f7f7fu;
+                    const bool rare = __any_sync(0xffffffffu, ((rare_v ? (not127 - 0x01010101u) & ~not127 : bytes & bytes << 1 & bytes << 2) & 0x80808080u) != 0);
                     if (rare) {
                         // a row of zeros has a byte of 127: its weight is none, and must not be what the others' are measured by
 #pragma unroll
@@ -423,10 +425,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                                 any |= __shfl_xor_sync(0xffffffffu, any, 2);
                                 if (any == 0 && ve[mt][h] == 0.f) ve[mt][h] = -INFINITY;
                             }
-                    }
-                    // The products (2^25 at most) times the slot's power; the row's comes with the subtraction below.  Where a slot's power may be above 2^102, both at
-                    // once and the slot's in two parts, the second one last, so that nothing on the way is beyond fp32 that the logit is not.
-                    if (rare) {
+                        // logits: a power above 2^102 in two parts, the second one behind the row's, so that nothing on the way is beyond fp32 that the logit is not
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -441,7 +440,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                                         x = x * first * qs_row[r][e] * second;
                                     }
                             }
-                    } else {
+                    } else {  // the products (2^25 at most) times the slot's power; the row's comes with the subtraction below
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
