@@ -42,6 +42,7 @@ namespace lar {
 
 constexpr int kTcMaxSeqs = 1024;  // sequences of a call (their lengths are kept in shared memory)
 constexpr int kTcMaxStages = 4;
+constexpr int kCutTiles = 8, kCutTilesJoined = 4;  // slot tiles that idle CTAs have to gain for units to be cut: a join of its own, or one that follows anyway
 
 template <int D, int NT>
 struct TcShape {
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(TcShape<D, NT>::THREADS, NT == 2 ? 1 : 2) page
             scan(sum, items);
             total = items[a.kv.n_seqs];
             // a last round that fills most of the CTAs, or whose idle ones would wait for a few slot tiles only, stays whole
-            if ((long long)total * (gridDim.x - left) >= 8ll * left * gridDim.x) work.end = work.first_cut = first;
+            if ((long long)total * (gridDim.x - left) >= (long long)(PART ? kCutTilesJoined : kCutTiles) * left * gridDim.x) work.end = work.first_cut = first;
             else total = 0;
         } else {
             total = items[a.kv.n_seqs];

@@ -14,6 +14,9 @@ namespace lar {
 
 // Where rows are joined with others anyway: slot tiles that a range has at least (bf16), slots that a CTA has (fp32).
 constexpr int kPartItems = 3, kPartSlots = 64;
+// Slots above which units of two row tiles that leave CTAs idle may be cut there (2 KV heads, 64 rows of 4 heads of 128, whole / cut: 512 slots 24.0 / 23.0 us, 768 27.4 / 24.4,
+// 1024 30.3 / 24.0, 1536 37 / 23; 8 KV heads 23.8 / 24.4, 26.9 / 24.7, 30.1 / 24.2, 36 / 25.6).
+constexpr int kJoinedLen = 640;
 
 struct AttnPlan {
     int tq;        // tokens of a row tile
@@ -83,10 +86,10 @@ inline AttnPlan attn_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, 
         // One row tile: cut above 1280 slots (8 tokens of 64-element rows, 8 KV heads, cut / whole: 37 sequences of up to 577 slots 22 / 14 us,
         // up to 1153 28 / 20, up to 2000 36 / 31, of unlike length 29 / 30, up to 4100 43 / 54; 16 sequences 18 / 14, 22 / 20, 25 / 29,
         // 34 / 52 at the same lengths).  Two: whole units on demand where there are many, or where their lengths differ much (chunks
-        // that make up much of their cache); long units are cut where a few rounds of whole ones would leave CTAs idle.
+        // that make up much of their cache); long units are cut where a few rounds of whole ones would leave CTAs idle (joined: shorter ones too).
         const int64_t units = (n_tokens / (p.tq * p.nt) + with_tokens) * k.n_kv_heads;
         p.splits = 1;
-        if (split && (p.nt == 1 ? len > (joined ? 128 : 1280) : units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
+        if (split && (p.nt == 1 ? len > (joined ? 128 : 1280) : joined && units <= p.grid ? len > kJoinedLen : units < 4 * p.grid && len >= 2048 && (2 * chunk < len || units <= p.grid))) p.splits = 2;
         else if (split && p.nt == 2 && units > p.grid) p.splits = 3;
         if (p.splits == 2) p.bytes = (size_t)p.grid * (sizeof(int4) + 2 * p.nt * (size_t)p.rows_cap * (d + 2) * sizeof(float));
         if (p.splits == 3) p.bytes = sizeof(int4);
@@ -137,7 +140,7 @@ inline size_t attn_workspace_bound(const lar_paged_kv_t& k, int group, int64_t n
         const size_t part = (size_t)(d + 2) * sizeof(float), rows = (size_t)(t1 * group + 7) / 8 * 8, rows2 = (size_t)(128 / group * group + 7) / 8 * 8;
         if (chunk * group > few && len > (joined ? 128 : 1280)) take(2 * kSms * (sizeof(int4) + 2 * rows * part));
         if (chunk * group > 128 || (d == 128 && chunk * group > 32 && len >= 2048))
-            take(len >= 2048 ? kSms * (sizeof(int4) + 4 * rows2 * part) : sizeof(int4));
+            take(len > (joined ? kJoinedLen : 2047) ? kSms * (sizeof(int4) + 4 * rows2 * part) : sizeof(int4));
         return most;
     }
     // fp32: s splits of n tokens, s <= 12 kSms / units + 1 with at least n / tq * KV heads units, so that s n <= 12 kSms tq / KV heads + n; and

@@ -64,6 +64,13 @@ SharedPlan shared_plan(const lar_paged_kv_t& k, int group, int64_t n_tokens, int
         const double work1 = work(p.pass[1], (double)(n_tokens < k.n_seqs ? n_tokens : k.n_seqs) * tiles(chunk, p.pass[1]), own_len(cap, max_len, max_shared) / 2.0);
         int share = (int)(kSms * work0 / (work0 + work1) + 0.5);
         share = share < 8 ? 8 : share > kSms - 8 ? kSms - 8 : share;
+        // Units that the kernel would leave whole are not looked at for cutting (3 us).
+        const int64_t units = (n_tokens / (2 * p.pass[0].tq) + (n_tokens < n_groups ? n_tokens : n_groups)) * k.n_kv_heads;
+        const int64_t common = max_shared > 0 && max_shared < cap ? max_shared : cap;
+        if (p.pass[0].splits == 2 && common < 2048 && (units >= share || (common / 128 + 2) * (share - units) < kCutTilesJoined * share)) {
+            p.pass[0].splits = 1;
+            p.pass[0].bytes = 0;
+        }
         p.pass[0].grid = p.pass[0].grid / kSms * share;
         p.pass[1].grid = p.pass[1].grid / kSms * (kSms - share);
     }

@@ -9,6 +9,7 @@ import torch
 
 import _paged_reference as R
 import _q8_reference as Q
+import test_shared_prefix
 from _q8_reference import Cache8
 from paper_2512_04857_b200 import lar
 from test_norm_q8_ops import _check_attention, _close, _q8, _r, _randn
@@ -158,6 +159,15 @@ def test_8bit_rows_are_as_near_as_the_format_says(dtype):
     assert (largest > 224 * power).all() and (largest <= 448 * power).all()
     assert (diff <= torch.maximum(x.abs() * 2.0 ** -4, power * 2.0 ** -10)).all()
     assert (diff <= torch.maximum(x.abs() * 2.0 ** -4, largest * 2.0 ** -17.8)).all() and (diff > torch.maximum(x.abs() * 2.0 ** -4, largest * 2.0 ** -18)).any()
+
+
+# ---------------------------------------------------------------------------------------- slots in common, row tiles
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,hkv,hq", [(128, 2, 8), (64, 1, 8)])
+@pytest.mark.parametrize("seqs,tokens,common,own", [(90, 1, 700, 20), (100, 1, 1100, 64), (60, 3, 1536, 200), (400, 1, 1990, 30)])
+def test_shared_attention_of_row_tiles_that_leave_sms_idle(d, hkv, hq, seqs, tokens, common, own):
+    """More than 128 rows per KV head and group over fewer than 2048 slots in common: few units, which are cut as a join follows anyway."""
+    test_shared_prefix.test_shared_attention_of_many_sequences(BF, d, hkv, hq, seqs, tokens, common, own)
 
 
 # ------------------------------------------------------------------------------------- what a pass that gave up leaves
