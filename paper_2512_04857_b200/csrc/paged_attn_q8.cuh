@@ -12,8 +12,9 @@
 //   * The elements of a row may be contracted in any order, so a thread takes the four neighbouring codes that ldmatrix gives it as elements 2t,
 //     2t + 1, 2t + 8, 2t + 9 of the product, and q's fragments are loaded to match.  V^T comes from ldmatrix.trans on pairs of codes: rows g and g + 8 of a
 //     product are elements 2g and 2g + 1.
-//   * q is scaled by a power of two to 2^8 .. 2^9 per row (exact in fp16 down to 2^-22 of the row's largest element, off by 2^-33 of it below); the logits are
-//     multiplied by it again, so that they are finite where fp32 holds them, whatever q and K are.  fp32
+//   * q is scaled by a power of two to 2^4 .. 2^5 per row (bf16 exact in fp16 down to 2^-21 of the row's largest element, off by 2^-29 of it below), and K's powers by 2^-14,
+//     so that the product of the two is at most 2^127; what both leave out of the logit comes back with the subtraction of the largest one.  So nothing on the way is beyond fp32
+//     that the logit is not.  (Rows of q from 2^118 on are scaled to 2^14 at most, as the power that comes back ends at 2^127.)  fp32
 //     rows take two fp16 numbers for q and for the weights (22 bits), and sums of a tile are added to the accumulator with rounding.
 //   * A weight is p_j 2^(v_j), v_j the exponent of the slot's values.  fp16 has 5 bits of exponent, so each row keeps a reference vr of its own, the
 //     largest (logit - m) log2(e) scale + v_j so far: weights are at most 2^14, and what fp16 cannot hold is below 2^-38 of the row's largest weight.  A row
@@ -289,9 +290,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
         const uint32_t box_bytes = ta.box_rows * D, k_at = maps.v_first ? box_bytes : 0, v_at = maps.v_first ? 0 : box_bytes;
         const int ks_at = maps.v_scale_first ? ta.box_rows : 0, vs_at = maps.v_scale_first ? 0 : ta.box_rows;
         const int box_mask = ta.box_rows - 1, box_shift = __ffs(ta.box_rows) - 1;
-        // Four of a tile's bytes, of K or of V, for each lane: rare are powers of K from 2^97 on (a byte whose three highest bits are set), and V's byte of a row of zeros
-        const int rare_slot = lane % (KT / 4) * 4, rare_v = lane / (KT / 4) & 1;
-        const int rare_at = (rare_slot >> box_shift) * 128 + (rare_slot & box_mask) + (rare_v ? vs_at : ks_at);
+        const int zero_slot = lane % (KT / 4) * 4, zero_at = (zero_slot >> box_shift) * 128 + (zero_slot & box_mask) + vs_at;  // four of V's bytes for each lane
         auto block = [&](int mt) { return (uint32_t)((16 * mt & ~box_mask) * 2 + (16 * mt & box_mask)); };  // rows before the block
         // byte offset of 16-byte chunk c of row r of a block (128- or 64-byte swizzle)
         auto off = [](int r, int c) { return (uint32_t)(D == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); };
@@ -303,7 +302,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
             if (n < 0) break;
             // per row of this thread (8 r + 2 quad + e): largest logit, sum, reference of the weights, accumulator (element 16 k + 2 qrow: e, + 1: 2 + e)
             float m[NR][2], l[NR][2], vr[NR][2], o[NR][KS][4];
-            float qs_row[NR][2];  // power of two that q was divided by
+            float qs_row[NR][2];  // logit of a product of scaled q and K
             int last[NR][2];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
@@ -338,8 +337,8 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
                     big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
                     const int ex = big == 0 ? 135 : max((int)(big >> 23), 9);
-                    const float inv = __uint_as_float((unsigned)(262 - ex) << 23);          // 2^(8 - (ex - 127))
-                    const float back = __uint_as_float((unsigned)(ex - 8) << 23);
+                    const float inv = __uint_as_float((unsigned)max(258 - ex, 14) << 23);    // 2^(4 - (ex - 127))
+                    const float back = __uint_as_float((unsigned)min(ex + 10, 254) << 23);   // 2^14 / inv
 #pragma unroll
                     for (int k = 0; k < KS; ++k) {
                         x[k].x *= inv; x[k].y *= inv; x[k].z *= inv; x[k].w *= inv;
@@ -372,16 +371,6 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                         }
                         __syncwarp();
                     }
-                    // scales of this thread's slots 16 mt + qrow + 8 h
-                    float kf[MT][2], ve[MT][2];
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at], kb = gscales[at + ks_at];
-                            kf[mt][h] = q8_scale(kb);
-                            ve[mt][h] = vb == kQ8NaN ? INFINITY : (float)(vb - 127);
-                        }
                     // S^T[slot][row]
                     float s[MT][NR][4];
 #pragma unroll
@@ -405,10 +394,18 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
 #pragma unroll
                                 for (int r = 0; r < NR; ++r) mma_f16(s[mt][r], x[2], x[3], y[2], y[3], qf[u][r][k + 1][0], qf[u][r][k + 1][1]);
                         }
-                    const uint32_t bytes = *reinterpret_cast<const uint32_t*>(gscales + st * S::SCALE_PITCH + rare_at);
-                    const uint32_t not127 = bytes ^ 0x7f7f7f7fu;
-                    const bool rare = __any_sync(0xffffffffu, ((rare_v ? (not127 - 0x01010101u) & ~not127 : bytes & bytes << 1 & bytes << 2) & 0x80808080u) != 0);
-                    if (rare) {
+                    // scales of this thread's slots 16 mt + qrow + 8 h
+                    float kf[MT][2], ve[MT][2];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int at = st * S::SCALE_PITCH + (16 * mt >> box_shift) * 128 + (16 * mt & box_mask) + qrow + 8 * h, vb = gscales[at + vs_at], kb = gscales[at + ks_at];
+                            kf[mt][h] = q8_scale(kb) * 0x1p-14f;
+                            ve[mt][h] = vb == kQ8NaN ? INFINITY : (float)(vb - 127);
+                        }
+                    const uint32_t not127 = *reinterpret_cast<const uint32_t*>(gscales + st * S::SCALE_PITCH + zero_at) ^ 0x7f7f7f7fu;
+                    if (__any_sync(0xffffffffu, ((not127 - 0x01010101u) & ~not127 & 0x80808080u) != 0)) {
                         // a row of zeros has a byte of 127: its weight is none, and must not be what the others' are measured by
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
@@ -425,29 +422,13 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                                 any |= __shfl_xor_sync(0xffffffffu, any, 2);
                                 if (any == 0 && ve[mt][h] == 0.f) ve[mt][h] = -INFINITY;
                             }
-                        // logits: a power above 2^102 in two parts, the second one behind the row's, so that nothing on the way is beyond fp32 that the logit is not
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const bool two = kf[mt][h] > 0x1p102f;
-                                const float first = two ? kf[mt][h] * 0x1p-64f : kf[mt][h], second = two ? 0x1p64f : 1.f;
-#pragma unroll
-                                for (int r = 0; r < NR; ++r)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        float& x = s[mt][r][2 * h + e];
-                                        x = x * first * qs_row[r][e] * second;
-                                    }
-                            }
-                    } else {  // the products (2^25 at most) times the slot's power; the row's comes with the subtraction below
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int r = 0; r < NR; ++r)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) s[mt][r][e] *= kf[mt][e >> 1];
                     }
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int r = 0; r < NR; ++r)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[mt][r][e] *= kf[mt][e >> 1];
                     if (base_slot < g.lo || base_slot + KT - 1 > min_last) {
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
@@ -482,7 +463,7 @@ paged_attn_q8_kernel(const __grid_constant__ TcArgs ta, const __grid_constant__ 
                     for (int r = 0; r < NR; ++r)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float f = rare ? 1.f : qs_row[r][e], mn = fmaxf(m[r][e], mx[r][e] * f);
+                            const float f = qs_row[r][e], mn = fmaxf(m[r][e], mx[r][e] * f);
                             const float ref = mn == INFINITY ? NAN : softmax_ref(mn), shift = (m[r][e] - ref) * a.scale_log2;  // (beyond fp32: NaN)
                             m[r][e] = mn;
                             vr[r][e] += shift;
