@@ -98,6 +98,13 @@ lar_status_t paged_attn_fits(const lar_paged_kv_t& kv, int group, int64_t n_toke
     return kv.dtype == LAR_BF16 && !countable(kv, p, n_tokens) ? LAR_ERR_CAPACITY : LAR_OK;
 }
 
+}  // namespace lar
+
+namespace {
+
+using namespace lar;
+
+// ------------------------------------------------------------------------------------------ rotary rows
 // Launch shape of the rotary kernels: token blocks x slices of a token's rows.
 dim3 rope_grid(RopeRowsArgs& a) {
     a.n_rows = a.heads[0] + a.heads[1] + a.heads[2];
@@ -115,13 +122,6 @@ dim3 rope_grid(RopeRowsArgs& a) {
     return dim3((unsigned)token_blocks, (unsigned)slices);
 }
 
-}  // namespace lar
-
-namespace {
-
-using namespace lar;
-
-// ------------------------------------------------------------------------------------------ rotary rows
 using RopeFn = void (*)(const lar::RopeRowsArgs);
 template <typename T, int D, bool PAGED>
 RopeFn rope_fn_pairs(bool inter) { return inter ? lar::rope_rows_kernel<T, D, true, PAGED> : lar::rope_rows_kernel<T, D, false, PAGED>; }

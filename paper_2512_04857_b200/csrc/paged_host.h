@@ -23,7 +23,6 @@ bool paged_view(const lar_paged_kv_t* k, int64_t n_tokens, const int32_t* cu, Pa
 lar_status_t paged_attn_fits(const lar_paged_kv_t& kv, int group, int64_t n_tokens, int max_chunk, int max_len, bool workspace, size_t workspace_bytes);
 struct Q8View;
 bool q8_view(const lar_paged_q8_t* c, int64_t n_tokens, const int32_t* cu, PagedView& v, Q8View& q);
-dim3 rope_grid(RopeRowsArgs& a);
 
 // Bookkeeping of the library's own cache that an append advances along with the rows (empty caches only: the prefill).
 struct OwnCache {

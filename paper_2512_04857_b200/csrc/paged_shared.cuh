@@ -91,7 +91,7 @@ struct SharedJoinArgs {
     PagedView kv;
     RowsView out;
     const int* cu;        // [n_groups + 1] tokens of the groups
-    int n_groups, hq, group;
+    int n_groups, hq;
     float scale_log2;
     SharedPass pass[2];   // slots in common, own slots
 };

@@ -163,7 +163,6 @@ lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q
     j.cu = pr.cu;
     j.n_groups = n_groups;
     j.hq = n_q_heads;
-    j.group = group;
     j.scale_log2 = a.scale_log2;
     const lar_paged_kv_t kg = groups_of(*kv, n_groups);
     for (int w = 0; w < 2; ++w) {
