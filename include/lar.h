@@ -490,10 +490,11 @@ lar_status_t lar_paged_q8_read(const lar_paged_q8_t* cache, int rows_dtype, cons
 
 /* lar_paged_attn over an 8-bit cache, q and out of rows_dtype.  fp32 rows, and bf16 rows of chunks of at most 64 rows per KV head (max_chunk times the heads of
  * a group), are computed from the codes, the weights in fp16 (two of them with fp32 rows).  For longer chunks of bf16 rows the live entries are first read
- * into the workspace as bf16 rows (exact), as many sequences at a time as 1 GB holds (at least one), and lar_paged_attn's kernels run over those: such
+ * into the workspace as bf16 rows (exact; sequences without tokens are left out), as many sequences at a time as 1 GB holds (at least one), and lar_paged_attn's
+ * kernels run over those, which round the weights to bf16: such
  * a call needs its workspace (LAR_ERR_NOMEM with NULL), and max_len (0: what the table holds) has to bound its caches' entries: of a longer one the first max_len
  * entries (rounded up to 128) are taken, and status bit 64 is recorded.  LAR_ERR_CAPACITY: more than 1024 sequences, and as lar_paged_attn.  The waits of
- * every kernel are bounded, also with fp32 rows: status bit 4. */
+ * every kernel are bounded, also with fp32 rows: status bit 4.  A logit beyond fp32 makes its row NaN. */
 lar_status_t lar_paged_q8_attn(const lar_paged_q8_t* cache, int rows_dtype, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads,
                                int64_t n_tokens, const int32_t* cu_tokens, const int32_t* kv_start, int causal, float softmax_scale,
                                int max_chunk, int max_len, void* workspace, size_t workspace_bytes, void* stream);
@@ -507,7 +508,8 @@ size_t lar_paged_q8_attn_workspace_bytes(const lar_paged_q8_t* cache, int rows_d
  * the group.
  * Every sequence of a group that has tokens holds the slots in common before its chunk; of a length that says more, only what the shortest of the group's caches
  * held before its chunk is taken as common.  Sequences of no group share nothing.  shared_lens need not be multiples of page_tokens.
- * The result is that of lar_paged_attn up to rounding.  max_shared bounds shared_lens (0: not known) and chooses the launch shape only.  Chunks of more than
+ * The result is that of lar_paged_attn up to rounding.  It costs four launches, some 10 us more than lar_paged_attn, before it saves anything: with no more than a few hundred slots in
+ * common, or a group for each sequence, lar_paged_attn is the faster call.  max_shared bounds shared_lens (0: not known) and chooses the launch shape only.  Chunks of more than
  * 128 rows per KV head, and calls with workspace NULL, go through lar_paged_attn: a read of a slot serves that many rows there already.
  * workspace: lar_paged_attn_shared_workspace_bytes of these arguments or larger ones; as lar_paged_attn otherwise. */
 lar_status_t lar_paged_attn_shared(const lar_paged_kv_t* kv, const lar_rows_t* q, const lar_rows_t* out, int n_q_heads, int64_t n_tokens,

@@ -7,7 +7,7 @@
 // Bound: HBM bytes (each row once in, once out), as long as an element costs few instructions.  So a CTA has rows of one kind (q, k or v: what depends on the
 // kind is the same for all its threads) and a thread stays with one head, of which it has 16 bytes of each half of a row (or 32 bytes side by side
 // where pairs interleave), and goes through tokens: its pointers are in registers from the start, and weights, biases, sines, cosines and slots of the
-// CTA in shared memory behind one barrier (weights in registers leave room for half the warps: 275 us where this takes 230, 5.9 TB/s, on 66560 tokens of 40 bf16 rows of 128, layer norm), in the
+// CTA in shared memory behind one barrier (weights in registers leave room for half the warps: 275 us where this takes 230, 5.9 TB/s, on 66560 tokens of 40 bf16 rows of 128, layer norm, in a graph; calls one by one take 244 to 256), in the
 // order in which threads read them (sines and cosines in their own order cost bank conflicts: 247 us).  The D / 16 (bf16) or D / 8 (fp32) threads of a row are
 // neighbours in a warp: the row's sums are a few shuffles, taken with the row in registers, the mean first and the squares of what is left after it, not the difference of two large sums.  fp32
 // arithmetic goes two elements to an instruction.  While a token is worked on the next one is on the way.  16 tokens take 3.6 us, a launch; 24 prompts of up to 2048

@@ -1,8 +1,8 @@
 // Attention over an 8-bit paged cache (paged_q8.cuh) from its codes, at most 16 (token, head of the group) rows of a KV head per unit: single tokens and
 // short candidate chunks, and whatever has fp32 rows.  Single tokens are bound by the cache's bytes (3 x 1 token over 23398 to 65537 slots, 8 KV heads
-// of 128: 313 MB in 65 us; 16 x 129 to 4288 slots: 78 MB in 24 us, of which 9.6 are launch, lengths, page table and first tile, and 3 the join), short units by
-// the chain of a tile, more rows by the warps that the registers leave room for (64 x 1 to 577 slots, 20 heads of 64, up to 16 fp32 rows: 37.5 us, tensor pipe
-// 20 % busy, 11 warps on an SM).
+// of 128: 313 MB in 65 us; 16 x 129 to 4288 slots: 78 MB in 25 us, of which 9.6 are launch, lengths, page table and first tile, and 3 the join), short units by
+// the chain of a tile, more rows by the warps that the registers leave room for (64 x 1 to 577 slots, 20 heads of 64, up to 16 fp32 rows: 38 us, tensor pipe
+// 21 % busy, 11 warps on an SM).
 //
 // The layout of work is that of paged_attn_few.cuh: every consumer warp takes a tile of 64 slots (32 where registers are short) through S^T = K q^T and O^T += V^T P^T with
 // mma.sync (the slots as the rows of the product), a producer warp keeps a ring of K/V tiles full, an epilogue warp merges the warps'
@@ -42,6 +42,7 @@ struct Q8Shape {
     static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
     // Slots of a tile (64 instead of 32, one token over 16 x 4288 slots: 25 instead of 27 us, 3 x 65537 slots 68 instead of 75; 16 rows of 64 fp32
     // elements 40 instead of 44).  With 16 rows of 128 elements tiles of 32 and two of them for each consumer (38.6 -> 33.6 us, 64 rows 96 -> 87; fp32 66 -> 57).
+    // (These and the figures below were taken before logits of any size and rows of zeros were looked after, which costs 1 to 4 %.)
     static constexpr int KT = NR == 2 && D == 128 ? 32 : 64;
     static constexpr int MT = KT / 16, KS = D / 16;
     static constexpr int TILE_BYTES = KT * D, STAGE_BYTES = 2 * TILE_BYTES, SCALE_BYTES = 2 * KT;

@@ -41,9 +41,10 @@ Q8Plan q8_plan(const lar_paged_kv_t& k, int rows_dtype, int group, int64_t n_tok
     const int64_t cap = (int64_t)k.table_cols * k.page_tokens;
     const int64_t len = max_len > 0 && max_len < cap ? max_len : cap;
     const int d = k.head_dim;
-    // From the codes: fp32 rows, and up to 64 rows of bf16 (16 sequences of up to 4288 slots, 8 KV heads of 128, codes / unpacked: 48 bf16 rows 69 / 112 us,
-    // 64 87 / 111, 96 about 120 / 112; elements of 64, 64 rows 59 / 62, 96 80 / 65; up to 600 slots, 64 rows 28 / 36; 4 sequences 27 / 42.  fp32, 12 sequences of
-    // 2080 to 4160 slots: 64 rows 126 / 336, 2000 rows 3.0 / 5.2 ms, up to 8320 rows 5.2 / 7.2).
+    // From the codes: fp32 rows, and up to 64 rows of bf16 (16 sequences of up to 4288 slots, 8 KV heads of 128, codes / unpacked: 48 bf16 rows 71 / 112 us,
+    // 64 92 / 111, 96 about 125 / 110; elements of 64, 64 rows 59 / 62, 96 80 / 65; up to 600 slots, 64 rows 28 / 36; 4 sequences 27 / 42.  fp32, 12 sequences of
+    // 2080 to 4160 slots: 64 rows 132 / 336, 2000 rows 3.1 / 5.2 ms, up to 8320 rows 5.4 / 7.2.
+    // A bf16 cache takes 46, 62 and 62 us with 32, 64 and 96 rows of 128: from 32 rows on it is the faster one.)
     p.few = rows_dtype == LAR_FP32 || chunk * group <= kCodesRows;
     if (p.few) {
         p.tq = (int)(chunk < kQ8Rows / group ? chunk : kQ8Rows / group);
