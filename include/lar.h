@@ -489,7 +489,8 @@ lar_status_t lar_paged_q8_read(const lar_paged_q8_t* cache, int rows_dtype, cons
                                const int32_t* cu_rows, void* stream);
 
 /* lar_paged_attn over an 8-bit cache, q and out of rows_dtype.  fp32 rows, and bf16 rows of chunks of at most 64 rows per KV head (max_chunk times the heads of
- * a group), are computed from the codes, the weights in fp16 (two of them with fp32 rows).  For longer chunks of bf16 rows the live entries are first read
+ * a group), are computed from the codes, the weights in fp16 (two of them with fp32 rows).  A weight carries the power of its slot's values there: what is below 2^-38 of a
+ * row's largest (a slot whose values are that much smaller than another's, or weigh that much less) is left out.  For longer chunks of bf16 rows the live entries are first read
  * into the workspace as bf16 rows (exact; sequences without tokens are left out), as many sequences at a time as 1 GB holds (at least one), and lar_paged_attn's
  * kernels run over those, which round the weights to bf16: such
  * a call needs its workspace (LAR_ERR_NOMEM with NULL), and max_len (0: what the table holds) has to bound its caches' entries: of a longer one the first max_len
